@@ -43,6 +43,7 @@
 #ifndef HB_H
 #define HB_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -439,6 +440,108 @@ int hb_hogbatch_run_epoch(hb_sched *s, hb_model *gpu, int32_t gpu_worker, int32_
                           const int32_t *host_y, float *host_model, float lr_per_example, int32_t cpu_threads,
                           double beta, int32_t merge_every, float merge_weight, double *gpu_updates,
                           double *cpu_updates, hb_epoch_stats *stats);
+
+/*
+ * ---- Operators on device tensors ------------------------------------------------------------
+ *
+ * For callers whose network, or the part of it that is not a handle's, lives elsewhere: matrices of
+ * HB_TENSOR_F32 or HB_TENSOR_BF16 elements in device memory, row-major, `ld` elements from row to row (ld >= the row's length; any
+ * base address that is aligned to the elements, any ld).  The calls only enqueue kernels on
+ * hip_stream (a hipStream_t, NULL = the default stream): nothing is allocated, copied, cleared or synchronised, so they may be
+ * captured.  Everything has to be on the device that is current at the call, the stream too: pointers that are not in
+ * its memory are HB_ERR_INVALID, as is a stream of another device.  Inputs are only read, and only in stream order.
+ */
+enum { HB_TENSOR_F32 = 0, HB_TENSOR_BF16 = 1 };
+
+/*
+ * Dropout.  out = x / (1 - p') where an element is kept, else +0 (whatever x holds there), for a rows x cols
+ * matrix; an element is kept with probability 1 - p', p' = floor(65536 p + 1/2) / 65536, 0 <= p, p' < 1.  Nothing of the mask is
+ * stored: it is a function of (seed, offset, row, column) alone, not of the type, the pitches or the pointers, so the same call on
+ * the gradient of out gives the gradient of x.  The generator is Philox4x32-10 (Salmon et al., SC 2011) with the
+ * key (low, high half of seed) and the counter (column / 8, row, low, high half of offset); of its four
+ * words, the element in column c takes half c % 8, low halves first, and is kept if that is at least 65536 p'.
+ * Another offset (or seed) is another mask.  d_out may be d_x with ldo = ldx; otherwise they must not overlap.
+ * bf16: the product is rounded once.  rows, cols, ldx, ldo < 2^31; rows or cols 0: nothing to do.
+ */
+int hb_dropout_async(const void *d_x, int64_t ldx, void *d_out, int64_t ldo, int tensor, int64_t rows, int64_t cols, float p,
+                     uint64_t seed, uint64_t offset, void *hip_stream);
+
+/*
+ * Log-probabilities of chosen classes.  d_Z holds B rows of K logits (`tensor` elements, ldz apart), d_y the class of each row.
+ *     logp_i = z_i[y_i] - lse_i,   lse_i = log of the sum over k of exp(z_i[k])
+ * A logit of -inf is a class that is not allowed.  A row whose class is outside [0, K) has no choice (padding, a prompt):
+ * logp = lse = 0, and its logits are not looked at.  A row whose logits are all -inf has logp = lse = -inf.  Beyond that,
+ * NaN and infinities go through the formulas.  d_lse may be NULL.
+ * d_ws: hb_choice_workspace_bytes(B, 0) bytes on the device, 16-byte aligned, for the work of this call alone (calls whose
+ * execution may overlap need one each; so do captured graphs that may run at the same time).
+ * 0 <= B <= 2^22, 1 <= K <= 2^24, ldz < 2^31.
+ */
+int hb_logprob_async(const void *d_Z, int64_t ldz, int tensor, const int32_t *d_y, int64_t B, int32_t K, float *d_logp,
+                     float *d_lse, void *d_ws, size_t ws_bytes, void *hip_stream);
+/*
+ * Its gradient: dZ_i[k] = g_i ([k = y_i] - exp(z_i[k] - lse_i)), with d_logp and d_lse as hb_logprob_async left them for the
+ * same d_Z and d_y, and d_g the gradient of each log-probability.  Rows without a choice, without an
+ * allowed class, or with g_i = 0 get zeros, whatever their logits hold.  d_dZ has the type of d_Z; it may be d_Z
+ * itself with lddz = ldz, otherwise they must not overlap.
+ */
+int hb_logprob_grad_async(const void *d_Z, int64_t ldz, int tensor, const int32_t *d_y, int64_t B, int32_t K, const float *d_logp,
+                          const float *d_lse, const float *d_g, void *d_dZ, int64_t lddz, void *hip_stream);
+
+/*
+ * The clipped policy loss with a KL term to a reference, and its gradient in the logits, in one call.  A row is one
+ * sampled action or token: class y_i, log-probability old_i when it was sampled, advantage A_i, weight w_i.  With lp_i as
+ * logp_i above, r_i = exp(lp_i - old_i) and d_i = ref_i - lp_i:
+ *     loss = sum over the rows of w_i (pg_i + kl_coef kl_i)
+ *     pg_i = -min(r_i A_i, clip(r_i, 1 - clip_low, 1 + clip_high) A_i)      (0 where A_i = 0)
+ *     kl_i = exp(d_i) - d_i - 1
+ *     dZ_i[k] = w_i g_i ([k = y_i] - softmax(z_i)[k]),   g_i = -[not cut] r_i A_i + kl_coef (1 - exp(d_i))
+ *     cut: A_i > 0 and r_i > 1 + clip_high, or A_i < 0 and r_i < 1 - clip_low
+ * Rows take no part if their class is outside [0, K), their weight is 0 or their logits are all -inf: what else
+ * they hold is not looked at, their gradient is 0.  All pointers are DEVICE pointers to B floats.
+ * d_stats (4 floats): loss, sum of w pg, sum of w kl, sum of w [cut].  d_logp (may be NULL): B floats, lp_i (rows
+ * without a choice or weight 0).  d_dZ: as for hb_logprob_grad_async; NULL: the loss only.
+ * d_ws: hb_choice_workspace_bytes(B, 0) bytes, as above.  B = 0 gives stats of 0.  Sums are made in a
+ * fixed order: the same call gives the same bits.
+ */
+typedef struct hb_policy {
+    const float *d_old_logp;
+    const float *d_ref_logp;  /* NULL: no KL term (kl_coef has to be 0 then) */
+    const float *d_adv;
+    const float *d_weight;    /* NULL: 1 / B each */
+    float clip_low;           /* 0 .. 1 */
+    float clip_high;          /* >= 0 */
+    float kl_coef;            /* >= 0 */
+} hb_policy;
+int hb_policy_loss_async(const void *d_Z, int64_t ldz, int tensor, const int32_t *d_y, int64_t B, int32_t K,
+                         const hb_policy *policy, float *d_stats, float *d_logp, void *d_dZ, int64_t lddz, void *d_ws,
+                         size_t ws_bytes, void *hip_stream);
+
+/*
+ * The preference loss over paired log ratios, and its gradient in the logits, in one call.  The rows form 2 `pairs` sequences,
+ * one behind the other: sequence q has the rows d_seq[q] .. d_seq[q + 1] - 1 (d_seq: 2 pairs + 1 int32 on the
+ * device, non-decreasing, within [0, B]; a sequence may be empty); sequence 2n was preferred over 2n + 1.
+ * With s_q = the sum of logp over the rows of sequence q that have a choice and h_n = (s_2n - ref_2n) - (s_2n+1 - ref_2n+1):
+ *     loss = mean over the pairs of -(1 - smoothing) log sigma(beta h_n) - smoothing log sigma(-beta h_n)
+ * and dZ is its gradient.  Rows without a choice or without an allowed class add nothing and get zeros.  Rows in front
+ * of the first and behind the last sequence are neither read nor written.  Offsets out of range are cut to it;
+ * decreasing ones make a sequence empty, and the results of its neighbours mean nothing then.
+ * d_stats (4 floats): loss, share of the pairs with h_n > 0, mean of beta (s_2n - ref_2n), mean of beta
+ * (s_2n+1 - ref_2n+1).  d_seq_logp (may be NULL): 2 pairs floats, s_q.  d_dZ: as for hb_logprob_grad_async; NULL: the loss
+ * only.  d_ws: hb_choice_workspace_bytes(B, pairs) bytes, as above.  The same call gives the same bits.
+ */
+typedef struct hb_preference {
+    const int32_t *d_seq;
+    const float *d_ref_logp;  /* 2 pairs floats, the reference's s_q; NULL: all 0 */
+    int32_t pairs;            /* 1 .. 2^22 */
+    float beta;               /* > 0 */
+    float smoothing;          /* 0 .. 0.5 */
+} hb_preference;
+int hb_preference_loss_async(const void *d_Z, int64_t ldz, int tensor, const int32_t *d_y, int64_t B, int32_t K,
+                             const hb_preference *preference, float *d_stats, float *d_seq_logp, void *d_dZ, int64_t lddz,
+                             void *d_ws, size_t ws_bytes, void *hip_stream);
+
+/* Bytes of workspace for the calls above (pairs: 0 but for the preference loss); 0 for arguments that they refuse. */
+size_t hb_choice_workspace_bytes(int64_t B, int32_t pairs);
 
 #ifdef __cplusplus
 }

@@ -10,6 +10,7 @@ _LIB_PATH = os.path.join(_HERE, "libhb.so")
 HB_ACT_SIGMOID, HB_ACT_RELU = 0, 1
 HB_LOSS_SOFTMAX_CE, HB_LOSS_LOGISTIC = 0, 1
 HB_F32, HB_BF16_F32MASTER = 0, 1
+HB_TENSOR_F32, HB_TENSOR_BF16 = 0, 1
 HB_OK, HB_ERR_INVALID, HB_ERR_ALLOC, HB_ERR_DEVICE, HB_ERR_UNSUPPORTED, HB_ERR_STATE = 0, -1, -2, -3, -4, -5
 
 # name -> (restype, argtypes); every symbol include/hb.h declares
@@ -78,6 +79,29 @@ SIGNATURES["hb_cpu_worker_run_epoch"] = (_int, [_vp, _i32, _i32p, _i32, _int, _i
 
 SIGNATURES["hb_hogbatch_run_epoch"] = (_int, [_vp, _vp, _i32, _i32, _vp, _vp, _vp, _f32, _i32, _f64, _i32, _f32, _f64p,
                                               _f64p, _vp])
+
+
+
+class Policy(ctypes.Structure):
+    """Mirror of hb_policy."""
+    _fields_ = [("d_old_logp", _vp), ("d_ref_logp", _vp), ("d_adv", _vp), ("d_weight", _vp), ("clip_low", _f32),
+                ("clip_high", _f32), ("kl_coef", _f32)]
+
+
+class Preference(ctypes.Structure):
+    """Mirror of hb_preference."""
+    _fields_ = [("d_seq", _vp), ("d_ref_logp", _vp), ("pairs", _i32), ("beta", _f32), ("smoothing", _f32)]
+
+
+_u64, _sz = ctypes.c_uint64, ctypes.c_size_t
+SIGNATURES["hb_dropout_async"] = (_int, [_vp, _i64, _vp, _i64, _int, _i64, _i64, _f32, _u64, _u64, _vp])
+SIGNATURES["hb_choice_workspace_bytes"] = (_sz, [_i64, _i32])
+SIGNATURES["hb_logprob_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _vp, _vp, _vp, _sz, _vp])
+SIGNATURES["hb_logprob_grad_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _i64, _vp])
+SIGNATURES["hb_policy_loss_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, ctypes.POINTER(Policy), _vp, _vp, _vp, _i64,
+                                             _vp, _sz, _vp])
+SIGNATURES["hb_preference_loss_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, ctypes.POINTER(Preference), _vp, _vp, _vp,
+                                                 _i64, _vp, _sz, _vp])
 
 _lib = None
 
@@ -333,3 +357,114 @@ def cpu_worker_run_epoch(sched, worker, layer_dims, activation, loss, host_X, ho
                                          int(threads), float(beta), ctypes.byref(u), ctypes.byref(nb),
                                          ctypes.byref(ls)))
     return u.value, nb.value, ls.value
+
+
+# ---- operators on device tensors: torch tensors in, nothing returned, everything enqueued on `stream`
+
+_TENSOR = {"torch.float32": HB_TENSOR_F32, "torch.bfloat16": HB_TENSOR_BF16}
+
+
+def _invalid(message):
+    raise HbError(HB_ERR_INVALID, message)
+
+
+def _matrix(t, name, like=None):
+    """(address, pitch, HB_TENSOR_*) of a torch matrix with elements of a row next to each other."""
+    kind = _TENSOR.get(str(t.dtype))
+    if kind is None:
+        _invalid(f"{name} has type {t.dtype}: float32 or bfloat16 is needed")
+    if t.dim() != 2:
+        _invalid(f"{name} has {t.dim()} dimensions: a matrix is needed")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+        _invalid(f"{name} is {tuple(t.shape)} {t.dtype}: {tuple(like.shape)} {like.dtype} is needed")
+    rows, cols = t.shape
+    step, along = t.stride()
+    if cols > 1 and along != 1:
+        _invalid(f"{name}: the elements of a row must be next to each other")
+    if rows > 1 and step < cols:
+        _invalid(f"{name}: its rows overlap")
+    return t.data_ptr(), (step if rows > 1 else max(cols, 1)), kind
+
+
+def _vector(t, name, n, dtype="torch.float32"):
+    """Address of n elements one behind the other, or None."""
+    if t is None:
+        return None
+    if str(t.dtype) != dtype or t.numel() != n or not t.is_contiguous():
+        _invalid(f"{name} is {tuple(t.shape)} {t.dtype}: {n} elements of {dtype}, one behind the other, are needed")
+    return t.data_ptr()
+
+
+def _workspace(ws):
+    if ws is None:
+        _invalid("ws is needed: a tensor of choice_workspace_bytes() bytes")
+    if not ws.is_contiguous():
+        _invalid("ws must be contiguous")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def choice_workspace_bytes(B, pairs=0) -> int:
+    """hb_choice_workspace_bytes: what `ws` of logprob, policy_loss and preference_loss has to hold."""
+    return int(lib().hb_choice_workspace_bytes(int(B), int(pairs)))
+
+
+def dropout(x, out, p, seed, offset=0, stream=None):
+    """hb_dropout_async on matrices x and out (out may be x).  The gradient of x is the same call on the gradient of out."""
+    px, ldx, kind = _matrix(x, "x")
+    po, ldo, _ = _matrix(out, "out", x)
+    _check(lib().hb_dropout_async(px, ldx, po, ldo, kind, x.shape[0], x.shape[1], p, seed, offset, stream if stream else None))
+
+
+def logprob(Z, y, logp, lse=None, ws=None, stream=None):
+    """hb_logprob_async: log-probabilities of the classes y (int32) in rows of logits Z."""
+    pz, ldz, kind = _matrix(Z, "Z")
+    B, K = Z.shape
+    pw, nw = _workspace(ws)
+    _check(lib().hb_logprob_async(pz, ldz, kind, _vector(y, "y", B, "torch.int32"), B, K, _vector(logp, "logp", B),
+                                  _vector(lse, "lse", B), pw, nw, stream if stream else None))
+
+
+def logprob_grad(Z, y, logp, lse, g, dZ, stream=None):
+    """hb_logprob_grad_async: dZ = g d logp / d Z (dZ may be Z)."""
+    pz, ldz, kind = _matrix(Z, "Z")
+    pd, ldd, _ = _matrix(dZ, "dZ", Z)
+    B, K = Z.shape
+    _check(lib().hb_logprob_grad_async(pz, ldz, kind, _vector(y, "y", B, "torch.int32"), B, K, _vector(logp, "logp", B),
+                                       _vector(lse, "lse", B), _vector(g, "g", B), pd, ldd, stream if stream else None))
+
+
+def _policy(B, old, adv, ref, weight, clip, kl_coef):
+    return Policy(_vector(old, "old", B), _vector(ref, "ref", B), _vector(adv, "adv", B), _vector(weight, "weight", B),
+                  clip[0], clip[1], kl_coef)
+
+
+def policy_loss(Z, y, old, adv, stats, dZ=None, ref=None, weight=None, clip=(0.2, 0.2), kl_coef=0.0, logp=None, ws=None,
+                stream=None):
+    """hb_policy_loss_async: stats (4 floats: loss, policy part, KL, cut share) and dZ (may be Z; None: the loss only)."""
+    pz, ldz, kind = _matrix(Z, "Z")
+    pd, ldd, _ = (None, ldz, 0) if dZ is None else _matrix(dZ, "dZ", Z)
+    B, K = Z.shape
+    pw, nw = _workspace(ws)
+    args = _policy(B, old, adv, ref, weight, clip, kl_coef)
+    _check(lib().hb_policy_loss_async(pz, ldz, kind, _vector(y, "y", B, "torch.int32"), B, K, ctypes.byref(args),
+                                      _vector(stats, "stats", 4), _vector(logp, "logp", B), pd, ldd, pw, nw,
+                                      stream if stream else None))
+
+
+def _preference(seq, ref, beta, smoothing):
+    n = seq.numel() - 1
+    if n < 2 or n % 2:
+        _invalid(f"seq has {n + 1} offsets: 2 pairs + 1 are needed")
+    return Preference(_vector(seq, "seq", n + 1, "torch.int32"), _vector(ref, "ref", n), n // 2, beta, smoothing), n
+
+
+def preference_loss(Z, y, seq, stats, dZ=None, ref=None, beta=0.1, smoothing=0.0, seq_logp=None, ws=None, stream=None):
+    """hb_preference_loss_async: stats (4 floats: loss, accuracy, mean rewards) and dZ (may be Z; None: the loss only)."""
+    pz, ldz, kind = _matrix(Z, "Z")
+    pd, ldd, _ = (None, ldz, 0) if dZ is None else _matrix(dZ, "dZ", Z)
+    B, K = Z.shape
+    pw, nw = _workspace(ws)
+    args, n = _preference(seq, ref, beta, smoothing)
+    _check(lib().hb_preference_loss_async(pz, ldz, kind, _vector(y, "y", B, "torch.int32"), B, K, ctypes.byref(args),
+                                          _vector(stats, "stats", 4), _vector(seq_logp, "seq_logp", n), pd, ldd, pw, nw,
+                                          stream if stream else None))

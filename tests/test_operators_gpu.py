@@ -1,0 +1,602 @@
+"""The operators on device tensors (dropout, log-probabilities of chosen classes, policy and preference loss) against their
+definitions in 64 bits.
+
+Tolerances, with u = 2^-24 (half a step of fp32) and T the largest |z_k - max z| among classes that matter:
+  an exponential is off by (T + 4) u relative (argument rounded twice, function, product), a term of weight below 2^-24 / K
+  does not matter, so T <= 17 + log K counts; a sum of n terms in chains of c and a tree adds (c + 16) u.
+  eps_s = (T + 4 + c + 16) u bounds the relative error of o and s, hence the absolute error of lp and lse, to
+  which the rounding of the result adds u |lp|.  A chain is at most K / 64 + 64 long.
+  p = exp(z - lse) is off by eps_s + (T' + |lse| + 4) u where T' = |z - lse| (and vanishes with it: 1e-30 absolute).
+  What follows from lp (a ratio r = exp(lp - old)) is off by the absolute error of lp relative.
+A bf16 result adds its rounding, 2^-8 relative (2^-133 absolute near zero).
+"""
+import numpy as np
+import pytest
+import torch
+
+import operators_ref as ref
+import paper_2004_08771_amd as hb
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def eps_s(K):
+    return (17 + np.log(K) + 4 + K / 64 + 64 + 16) * U
+
+
+def lp_tol(lp, K):
+    return eps_s(K) + U * np.abs(np.where(np.isfinite(lp), lp, 0.0))
+
+
+def check(got, want, tol, what):
+    got = host(got) if torch.is_tensor(got) else np.asarray(got, np.float64)
+    tol = np.broadcast_to(np.asarray(tol, np.float64), want.shape)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    inf = np.isinf(want)
+    assert np.array_equal(np.isinf(got), inf) and np.array_equal(got[inf], want[inf]), what
+    fine = np.isfinite(want)
+    off = np.abs(got[fine] - want[fine]) - tol[fine]
+    assert not (off > 0).any(), f"{what}: {int((off > 0).sum())} of {off.size} off, the worst by {off.max():.3g} more than allowed"
+
+
+def grad_tol(want, Z, y, part, lp, lse, p, g, g_off, K, dtype):
+    """Of dz = g ([k = y] - p): g off by g_off, p relative, a bf16 result rounded."""
+    far = np.abs(np.where(np.isfinite(Z), Z, 0.0) - np.where(np.isfinite(lse), lse, 0.0)[:, None])
+    rel = eps_s(K) + (far + np.abs(np.where(np.isfinite(lse), lse, 0.0))[:, None] + 8) * U
+    unit = ref.grad_ref(part, p, y, np.ones(len(y)))
+    tol = np.abs(g)[:, None] * rel * np.abs(unit) + g_off[:, None] * np.abs(unit) + 4 * U * np.abs(want) + 1e-30
+    return tol + (2.0 ** -8 * np.abs(want) + 2.0 ** -133 if dtype == "bf16" else 0.0)
+
+
+def matrix(a, dtype, ld=None, base=0):
+    """A device copy of a host matrix with pitch ld, `base` elements into its allocation; everything else holds NaN."""
+    rows, cols = a.shape
+    ld = cols if ld is None else ld
+    flat = torch.full((base + max(rows, 1) * ld + 9,), float("nan"), dtype=TYPES[dtype], device="cuda")
+    m = flat[base:base + rows * ld].view(rows, ld)[:, :cols]
+    m.copy_(torch.as_tensor(a))
+    return m, flat
+
+
+def outside_is_nan(flat, m):
+    mask = torch.ones_like(flat, dtype=torch.bool)
+    n = (m.data_ptr() - flat.data_ptr()) // flat.element_size()
+    mask[n:n + m.shape[0] * m.stride(0)].view(m.shape[0], m.stride(0))[:, :m.shape[1]] = False
+    return bool(torch.isnan(flat[mask]).all())
+
+
+def vec(a, dtype=torch.float32):
+    return torch.as_tensor(np.asarray(a)).to(dtype).cuda()
+
+
+def ws(B, pairs=0):
+    return torch.full((hb.choice_workspace_bytes(B, pairs),), 0xFF, dtype=torch.uint8, device="cuda")
+
+
+def logits(B, K, rng, dtype, masked=True, scale=2.0):
+    """Logits as stored, and classes: disallowed ones at -inf and at the lowest value, rows without a choice, a row where
+    nothing is allowed, rows with one class far above, NaN where there is no choice."""
+    z = (scale * rng.standard_normal((B, K))).astype(np.float32)
+    y = rng.integers(0, K, B).astype(np.int32)
+    if masked and K > 2:
+        off = rng.random((B, K)) < 0.15
+        off[np.arange(B), y] = False
+        z[off] = -np.inf
+        low = (rng.random((B, K)) < 0.05) & ~off
+        low[np.arange(B), y] = False
+        z[low] = torch.finfo(TYPES[dtype]).min
+    if masked:
+        for i in range(B):
+            kind = i % 11
+            if kind == 3:
+                y[i] = [-1, K, -2 ** 31, 2 ** 31 - 1][(i // 11) % 4]
+                z[i, rng.integers(0, K)] = np.nan
+            elif kind == 5:
+                z[i] = -np.inf
+            elif kind == 7:
+                z[i, y[i]] = 40.0      # all but certain
+            elif kind == 9:
+                z[i, (y[i] + 1) % K] = 60.0  # all but impossible
+    z = torch.as_tensor(z).to(TYPES[dtype]).double().numpy()
+    return z, y
+
+
+# ---------------------------------------------------------------- dropout
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,ldx,ldo,base", [
+    (1, 1, 1, 1, 0), (1, 7, 7, 7, 0), (3, 8, 8, 8, 0), (61, 983, 983, 983, 0), (5, 983, 1001, 990, 3), (1000, 3, 3, 5, 1),
+    (17, 64, 64, 64, 0), (33, 1000, 1000, 1024, 0), (2, 100003, 100003, 100003, 0), (257, 512, 520, 512, 4), (70000, 2, 2, 2, 0),
+])
+def test_dropout(rows, cols, ldx, ldo, base, dtype):
+    rng = np.random.default_rng(rows * 1000 + cols)
+    x, flat_x = matrix(rng.standard_normal((rows, cols)), dtype, ldx, base)
+    out, flat_o = matrix(np.zeros((rows, cols)), dtype, ldo, base)
+    hx = host(x)
+    for p, seed, offset in [(0.1, 1, 0), (0.5, 2 ** 63 + 12345, 2 ** 40 + 7), (0.0, 5, 5), (0.9999, 3, 2 ** 64 - 1)]:
+        hb.dropout(x, out, p, seed, offset)
+        keep, scale = ref.dropout_keep(rows, cols, p, seed, offset)
+        # the factor rounded, the product rounded; bf16: once more
+        check(out, np.where(keep, hx * scale, 0.0), np.abs(hx) * scale * (2 * U + (2.0 ** -8 if dtype == "bf16" else 0)), f"p {p}")
+        got = host(out)
+        assert not got[~keep].any() and not np.signbit(got[~keep]).any()
+        assert outside_is_nan(flat_o, out)
+    assert np.array_equal(host(x), hx) and outside_is_nan(flat_x, x)
+
+
+def test_dropout_in_place_and_as_its_own_gradient():
+    """The same call on the gradient: <dropout(x), v> = <x, dropout(v)>, by element; differences of it are exact (it is linear)."""
+    rng = np.random.default_rng(5)
+    x, _ = matrix(rng.standard_normal((77, 333)), "f32", 341, 2)
+    want = torch.empty_like(x)
+    hb.dropout(x, want, 0.3, 99, 4)
+    v = torch.ones_like(want)
+    dx = torch.empty_like(v)
+    hb.dropout(v, dx, 0.3, 99, 4)
+    assert torch.equal(want, x * dx)
+    h = torch.empty_like(want)
+    hb.dropout(x + 1024.0, h, 0.3, 99, 4)   # (f(x + 1024) - f(x)) / 1024 = the gradient, rounding aside
+    assert ((h - want) / 1024 - dx).abs().max() <= 4 * 1030 * 2.0 ** -23 / 1024 * 2
+    hb.dropout(x, x, 0.3, 99, 4)
+    assert torch.equal(x, want)
+
+
+def test_dropout_drops_what_is_not_finite_and_is_even():
+    x = torch.full((4096, 1024), float("inf"), device="cuda")
+    x[::2] = float("nan")
+    out = torch.empty_like(x)
+    hb.dropout(x, out, 0.25, 11, 1)
+    dropped = out == 0
+    # share of 2^22 independent trials: 0.25 within 6 standard deviations of 2.1e-4
+    assert abs(float(dropped.double().mean()) - 0.25) < 6 * 2.12e-4
+    assert bool(torch.isnan(out[::2][~dropped[::2]]).all()) and bool(torch.isinf(out[1::2][~dropped[1::2]]).all())
+    other = torch.empty_like(x)
+    hb.dropout(x, other, 0.25, 11, 2)
+    both = float((dropped & (other == 0)).double().mean())
+    assert abs(both - 0.0625) < 6 * 1.19e-4     # another offset, another mask
+
+
+def test_dropout_past_32_bits():
+    """Three rows 2^30 + 8 elements apart, and one row of 2^31 - 1 elements: its end against the definition."""
+    ld = (1 << 30) + 8
+    base = torch.zeros(2 * ld + 16, dtype=torch.bfloat16, device="cuda")
+    x = base.as_strided((3, 16), (ld, 1))
+    x.copy_(torch.arange(1, 49).view(3, 16))
+    out = torch.zeros(3, 16, dtype=torch.bfloat16, device="cuda")
+    hb.dropout(x, out, 0.5, 77, 0)
+    keep, _ = ref.dropout_keep(3, 16, 0.5, 77, 0)
+    assert torch.equal(out.cpu(), torch.as_tensor(keep * np.arange(1, 49).reshape(3, 16) * 2.0).bfloat16())
+    del base, x
+    n = (1 << 31) - 1
+    x = torch.ones(1, n, dtype=torch.bfloat16, device="cuda")
+    hb.dropout(x, x, 0.5, 78, 9)
+    groups = np.arange((n - 100) // 8, (n + 7) // 8, dtype=np.uint64)
+    ctr = np.stack([groups, 0 * groups, 0 * groups + np.uint64(9), 0 * groups], -1)
+    w = ref.philox(ctr, (78, 0))
+    bits = np.stack([w & np.uint64(0xFFFF), w >> np.uint64(16)], -1).reshape(-1)
+    start = 8 * int(groups[0])
+    assert np.array_equal(host(x[0, start:]) != 0, bits[:n - start] >= 32768)
+
+
+def test_dropout_of_more_groups_than_a_launch_takes():
+    """2^31 and more groups of eight go out in several launches: the last rows against the definition."""
+    cols, rows = 9, (1 << 30) + 3          # two groups a row: 2^31 + 6 groups, 19 GB
+    x = torch.ones(rows, cols, dtype=torch.bfloat16, device="cuda")
+    hb.dropout(x, x, 0.5, 3, 1)
+    tail = np.arange(rows - 64, rows, dtype=np.uint64)
+    for g in range(2):
+        ctr = np.stack([0 * tail + np.uint64(g), tail, 0 * tail + np.uint64(1), 0 * tail], -1)
+        w = ref.philox(ctr, (3, 0))
+        bits = np.stack([w & np.uint64(0xFFFF), w >> np.uint64(16)], -1).reshape(64, 8)[:, :min(8, cols - 8 * g)]
+        assert np.array_equal(host(x[rows - 64:, 8 * g:8 * g + 8]) != 0, bits >= 32768)
+
+
+# ---------------------------------------------------------------- log-probabilities
+SHAPES = [(1, 1), (1, 2), (5, 1), (64, 7), (300, 2), (33, 16), (129, 17), (40, 63), (41, 64), (23, 65), (70, 100), (26, 255), (22, 513), (31, 983),
+          (12, 2049), (23, 4100), (11, 8200), (5, 16385), (3, 33000), (2, 70001), (1, 140001), (600, 40), (300, 1000)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,K", SHAPES)
+def test_logprob_and_its_gradient(B, K, dtype):
+    rng = np.random.default_rng(B * 7 + K)
+    z, y = logits(B, K, rng, dtype)
+    part, lp, lse, p = ref.rows_ref(z, y)
+    g = rng.standard_normal(B).astype(np.float32)
+    g[1::13] = 0.0
+    part_g = part & (g != 0)
+    want = ref.grad_ref(part_g, p, y, g.astype(np.float64))
+    for ld, ldd, base in [(K, K, 0), (K + 5, K + 11, 3)]:
+        Z, flat_z = matrix(z, dtype, ld, base)
+        dZ, flat_d = matrix(np.full((B, K), 7.0), dtype, ldd, base + 2)
+        dy = vec(y, torch.int32)
+        a, b = torch.full((B,), 7.0, device="cuda"), torch.full((B,), 7.0, device="cuda")
+        hb.logprob(Z, dy, a, b, ws=ws(B))
+        check(a, lp, lp_tol(lp, K), "logp")
+        check(b, lse, lp_tol(lse, K), "lse")
+        only = torch.full((B,), 7.0, device="cuda")
+        hb.logprob(Z, dy, only, ws=ws(B))
+        assert np.array_equal(host(only), host(a))
+        hb.logprob_grad(Z, dy, a, b, vec(g), dZ)
+        tol = grad_tol(want, z, y, part_g, lp, lse, p, g.astype(np.float64), np.zeros(B), K, dtype)
+        # lse is rounded between the two calls
+        tol = tol + np.abs(g)[:, None] * ref.grad_ref(part_g, p, y, -np.ones(B)).clip(min=0) * lp_tol(lse, K)[:, None]
+        check(dZ, want, tol, "dZ")
+        assert outside_is_nan(flat_d, dZ)
+        hb.logprob_grad(Z, dy, a, b, vec(g), Z)            # in place
+        assert np.array_equal(host(Z), host(dZ)) and outside_is_nan(flat_z, Z)
+
+
+def test_logprob_of_certain_choices_keeps_its_digits():
+    """1 - p of a choice with p = 1 - 2e-8 and the like: relative to what is left, not to one."""
+    z = np.array([[20.0, 2.0, 1.0], [40.0, 0.0, -3.0], [88.0, -10.0, 0.0]])
+    y = np.zeros(3, np.int32)
+    Z, _ = matrix(z, "f32")
+    a, b = torch.zeros(3, device="cuda"), torch.zeros(3, device="cuda")
+    hb.logprob(Z, vec(y, torch.int32), a, b, ws=ws(3))
+    part, lp, lse, p = ref.rows_ref(z, y)
+    rel = (100 + 8) * U                     # exponents of up to 98: the exponential's relative error
+    check(a, lp, rel * np.abs(lp), "logp")
+    dZ = torch.zeros_like(Z)
+    hb.logprob_grad(Z, vec(y, torch.int32), a, b, torch.ones(3, device="cuda"), dZ)
+    want = ref.grad_ref(part, p, y, np.ones(3))
+    # exp(-88) = 6.05e-39 and exp(-98) are below the smallest normal value, 2^-126 = 1.18e-38: the hardware's exponential gives
+    # 0 there, an absolute error of less than 2^-126 (the third row: 6.05e-39 < 2^-126)
+    check(dZ, want, (3 * 100 + 16) * U * np.abs(want) + 2.0 ** -126, "dZ")
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("K", [7, 100, 5000, 70001])
+def test_logprob_of_rows_that_are_not_finite(K, bad):
+    rng = np.random.default_rng(K)
+    z, y = logits(6, K, rng, "f32", masked=False)
+    z[1, (y[1] + 3) % K] = bad      # another class
+    z[3, y[3]] = bad                # the chosen one
+    z[4, :] = -np.inf
+    z[4, (y[4] + 1) % K] = bad
+    Z, _ = matrix(z, "f32")
+    a, b = torch.zeros(6, device="cuda"), torch.zeros(6, device="cuda")
+    hb.logprob(Z, vec(y, torch.int32), a, b, ws=ws(6))
+    a, b = host(a), host(b)
+    assert np.isnan(a[[1, 3, 4]]).all() and np.isnan(b[[1, 3, 4]]).all()
+    _, lp, lse, _ = ref.rows_ref(z[[0, 2, 5]], y[[0, 2, 5]])
+    check(a[[0, 2, 5]], lp, lp_tol(lp, K), "logp")
+    check(b[[0, 2, 5]], lse, lp_tol(lse, K), "lse")
+
+
+def test_logprob_past_32_bits():
+    ld = (1 << 30) + 24
+    base = torch.zeros(2 * ld + 1001, dtype=torch.bfloat16, device="cuda")
+    Z = base.as_strided((3, 1001), (ld, 1))
+    rng = np.random.default_rng(1)
+    Z.copy_(torch.as_tensor(rng.standard_normal((3, 1001))))
+    z, y = host(Z), np.array([1000, 0, 7], np.int32)
+    a, b = torch.zeros(3, device="cuda"), torch.zeros(3, device="cuda")
+    hb.logprob(Z, vec(y, torch.int32), a, b, ws=ws(3))
+    part, lp, lse, p = ref.rows_ref(z, y)
+    check(a, lp, lp_tol(lp, 1001), "logp")
+    g = np.ones(3)
+    hb.logprob_grad(Z, vec(y, torch.int32), a, b, vec(g), Z)
+    want = ref.grad_ref(part, p, y, g)
+    check(Z, want, grad_tol(want, z, y, part, lp, lse, p, g, lp_tol(lse, 1001), 1001, "bf16"), "dZ")
+
+
+# ---------------------------------------------------------------- policy loss
+def policy_inputs(B, K, rng, dtype, masked=True):
+    """Log-ratios 1e-2 and more away from the borders of the clip (log 0.8 = -0.223, log 1.28 = 0.247)."""
+    z, y = logits(B, K, rng, dtype, masked)
+    _, lp, _, _ = ref.rows_ref(z, y)
+    lp = np.where(np.isfinite(lp), lp, 0.0)
+    away = rng.choice([-0.7, -0.3, -0.1, 0.0, 0.1, 0.35, 0.7], B) + rng.uniform(-0.03, 0.03, B)
+    old = (lp - away).astype(np.float32)
+    adv = rng.standard_normal(B).astype(np.float32)
+    adv[2::7] = 0.0
+    refs = (lp + 0.5 * rng.standard_normal(B)).astype(np.float32)
+    w = rng.uniform(0.5, 1.5, B).astype(np.float32) / B
+    w[4::9] = 0.0
+    return z, y, old, adv, refs, w
+
+
+def policy_tols(z, y, old, adv, refs, w, clip, kl, stats, lp, want, g, K, dtype):
+    e = lp_tol(lp, K) + 4 * U
+    part, lp2, lse, p = ref.rows_ref(z, y, w)
+    weight = np.full(len(y), 1.0 / len(y)) if w is None else np.abs(w.astype(np.float64))
+    r = np.exp(np.where(part, lp - old, 0.0))
+    d = np.where(part, refs.astype(np.float64) - lp, 0.0) if refs is not None else np.zeros(len(y))
+    e = np.where(part, e, 0.0)
+    g_off = weight * (r * np.abs(adv) + kl * np.exp(d)) * e * 2
+    pg = weight * r * np.abs(adv) * e * 2
+    k3 = weight * np.abs(np.expm1(d)) * e * 2
+    s_tol = np.array([(pg + kl * k3).sum(), pg.sum(), k3.sum(), 0.0]) + 4 * U * np.abs(stats)
+    s_tol[3] += U
+    return s_tol, grad_tol(want, z, y, part, lp, lse, p, g, g_off, K, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,K", SHAPES + [(2000, 7), (1100, 130)])
+def test_policy_loss_and_its_gradient(B, K, dtype):
+    rng = np.random.default_rng(B + 31 * K)
+    z, y, old, adv, refs, w = policy_inputs(B, K, rng, dtype)
+    clip = (0.2, 0.28)
+    for use_ref, use_w, kl, ld, base in [(True, True, 0.04, K, 0), (False, False, 0.0, K + 3, 1), (True, True, 0.0, K + 8, 0)]:
+        rr, ww = (refs if use_ref else None), (w if use_w else None)
+        stats, lp, want, g = ref.policy_ref(z, y, old, adv, rr, ww, clip, kl)
+        Z, flat_z = matrix(z, dtype, ld, base)
+        dZ, flat_d = matrix(np.full((B, K), 7.0), dtype, ld + base, base)
+        st, a = torch.full((4,), 7.0, device="cuda"), torch.full((B,), 7.0, device="cuda")
+        args = dict(ref=None if rr is None else vec(rr), weight=None if ww is None else vec(ww), clip=clip, kl_coef=kl, ws=ws(B))
+        head = (Z, vec(y, torch.int32), vec(old), vec(adv))
+        hb.policy_loss(*head, st, dZ=dZ, logp=a, **args)
+        s_tol, d_tol = policy_tols(z, y, old, adv, rr, ww, clip, kl, stats, lp, want, g, K, dtype)
+        check(a, lp, lp_tol(lp, K), "logp")
+        check(st, stats, s_tol, "stats")
+        check(dZ, want, d_tol, "dZ")
+        assert outside_is_nan(flat_d, dZ)
+        st2 = torch.full((4,), 7.0, device="cuda")          # the loss alone
+        hb.policy_loss(*head, st2, **args)
+        check(st2, stats, s_tol, "stats of the loss alone")
+        again, st3 = torch.full_like(dZ, 7.0), torch.full((4,), 7.0, device="cuda")
+        hb.policy_loss(*head, st3, dZ=again, **args)        # the same bits
+        assert torch.equal(st3, st) and np.array_equal(host(again), host(dZ))
+        hb.policy_loss(*head, st3, dZ=Z, **args)            # in place
+        assert np.array_equal(host(Z), host(dZ)) and torch.equal(st3, st) and outside_is_nan(flat_z, Z)
+
+
+@pytest.mark.parametrize("B,K", [(9, 5), (4, 700), (3, 9000)])
+def test_policy_gradient_against_differences(B, K):
+    """(L(z + h v) - L(z - h v)) / 2h of the kernel's own loss against <dz, v>: the quotient's truncation is that of the
+    definition in 64 bits, its rounding the losses' tolerance over h."""
+    rng = np.random.default_rng(B * K)
+    z, y, old, adv, refs, w = policy_inputs(B, K, rng, "f32", masked=False)
+    v, h, clip, kl = rng.standard_normal((B, K)), 2.0 ** -7, (0.2, 0.28), 0.04
+    v /= np.sqrt(K)
+    L, tol = [], 0.0
+    L64 = []
+    for s in (1, -1):
+        zs = np.float32(z + s * h * v)
+        st = torch.zeros(4, device="cuda")
+        hb.policy_loss(matrix(zs, "f32")[0], vec(y, torch.int32), vec(old), vec(adv), st, ref=vec(refs), weight=vec(w), clip=clip,
+                       kl_coef=kl, ws=ws(B))
+        stats, lp, want, g = ref.policy_ref(zs, y, old, adv, refs, w, clip, kl)
+        tol += policy_tols(zs, y, old, adv, refs, w, clip, kl, stats, lp, want, g, K, "f32")[0][0]
+        L.append(float(st[0]))
+        L64.append(stats[0])
+    Z, dZ, st = matrix(z, "f32")[0], torch.zeros(B, K, device="cuda"), torch.zeros(4, device="cuda")
+    hb.policy_loss(Z, vec(y, torch.int32), vec(old), vec(adv), st, dZ=dZ, ref=vec(refs), weight=vec(w), clip=clip, kl_coef=kl, ws=ws(B))
+    stats, lp, want, g = ref.policy_ref(z, y, old, adv, refs, w, clip, kl)
+    truncation = abs((L64[0] - L64[1]) / (2 * h) - (want * v).sum())
+    d_tol = (policy_tols(z, y, old, adv, refs, w, clip, kl, stats, lp, want, g, K, "f32")[1] * np.abs(v)).sum()
+    assert abs((L[0] - L[1]) / (2 * h) - (host(dZ) * v).sum()) <= truncation + tol / (2 * h) + d_tol
+    assert truncation < 0.1 * abs((want * v).sum()) + 1e-3       # the check says something
+
+
+def test_policy_without_rows_and_with_nothing_that_takes_part():
+    st = torch.full((4,), 7.0, device="cuda")
+    e = torch.zeros(0, device="cuda")
+    hb.policy_loss(torch.zeros(0, 5, device="cuda"), e.int(), e, e, st, dZ=torch.zeros(0, 5, device="cuda"), ws=ws(0))
+    assert not host(st).any()
+    n = torch.full((3, 1000), float("nan"), device="cuda")
+    d = torch.full((3, 1000), 7.0, device="cuda")
+    row = torch.full((3,), float("nan"), device="cuda")
+    st.fill_(7.0)
+    hb.policy_loss(n, torch.zeros(3, dtype=torch.int32, device="cuda"), row, row, st, dZ=d, ref=row,
+                   weight=torch.zeros(3, device="cuda"), kl_coef=1.0, ws=ws(3))
+    assert not host(st).any() and not host(d).any()
+
+
+def test_policy_ratios_that_overflow():
+    """An advantage of 0 takes no ratio; a large ratio against a positive one is cut; both finite."""
+    z = np.zeros((3, 4))
+    st, d = torch.zeros(4, device="cuda"), torch.zeros(3, 4, device="cuda")
+    old = np.array([-1e4, -1e4, 0.0], np.float32)
+    adv = np.array([0.0, 2.0, 1.0], np.float32)
+    hb.policy_loss(matrix(z, "f32")[0], torch.zeros(3, dtype=torch.int32, device="cuda"), vec(old), vec(adv), st, dZ=d, ws=ws(3))
+    stats = np.array([(-1.2 * 2.0 - 0.25) / 3, (-1.2 * 2.0 - 0.25) / 3, 0.0, 1 / 3])
+    check(st, stats, 1e-6, "stats")
+    got = host(d)
+    assert not got[:2].any()
+    check(got[2], -0.25 / 3 * np.array([0.75, -0.25, -0.25, -0.25]), 1e-7, "dZ")
+
+
+# ---------------------------------------------------------------- preference loss
+def preference_case(B, K, pairs, rng, dtype, masked=True):
+    z, y = logits(B, K, rng, dtype, masked)
+    lo, hi = (0, B) if B < 5 else (1, B - 2)
+    cuts = np.sort(rng.integers(lo, hi + 1, 2 * pairs - 1))
+    seq = np.concatenate([[lo], cuts, [hi]]).astype(np.int32)
+    _, lp, _, _ = ref.rows_ref(z, y)
+    s = np.array([np.where(np.isfinite(lp), lp, 0)[seq[q]:seq[q + 1]].sum() for q in range(2 * pairs)])
+    refs = (s + 3 * rng.standard_normal(2 * pairs)).astype(np.float32)
+    return z, y, seq, refs
+
+
+def preference_tols(z, y, seq, refs, beta, eps, stats, s, want, g, K, dtype):
+    part, lp, lse, p = ref.rows_ref(z, y)
+    e = np.where(part, lp_tol(lp, K), 0.0)
+    pairs = len(seq) // 2
+    se = np.array([e[seq[q]:seq[q + 1]].sum() for q in range(2 * pairs)])
+    s_tol = se + U * np.abs(s)
+    he = se[0::2] + se[1::2]
+    st = np.array([beta * he.mean(), 0.0, beta * se[0::2].mean(), beta * se[1::2].mean()]) + 4 * U * np.abs(stats) + 4 * U
+    g_off = np.zeros(len(y))
+    for q in range(2 * pairs):   # the slope changes by at most beta / pairs * beta / 4 a unit of h
+        g_off[seq[q]:seq[q + 1]] = beta / pairs * beta / 4 * he[q // 2] + 4 * U * beta / pairs
+    tol = grad_tol(np.where(np.isnan(want), 0, want), z, y, part, lp, lse, p, g, g_off, K, dtype)
+    return s_tol, st, tol
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,K,pairs", [(1, 3, 1), (2, 7, 1), (40, 7, 3), (167, 983, 4), (64, 64, 40), (90, 2050, 2), (9, 33000, 2),
+                                       (5, 70001, 1), (700, 20, 1), (2500, 5, 7)])
+def test_preference_loss_and_its_gradient(B, K, pairs, dtype):
+    rng = np.random.default_rng(B + K * 3 + pairs)
+    z, y, seq, refs = preference_case(B, K, pairs, rng, dtype)
+    for use_ref, beta, eps, ld, base in [(True, 0.1, 0.05, K, 0), (False, 0.01, 0.0, K + 5, 3), (True, 0.5, 0.5, K + 8, 0)]:
+        rr = refs if use_ref else None
+        stats, s, want, g = ref.preference_ref(z, y, seq, rr, beta, eps)
+        Z, flat_z = matrix(z, dtype, ld, base)
+        dZ, flat_d = matrix(np.full((B, K), np.nan), dtype, ld + base, base)
+        st, sl = torch.full((4,), 7.0, device="cuda"), torch.full((2 * pairs,), 7.0, device="cuda")
+        args = dict(ref=None if rr is None else vec(rr), beta=beta, smoothing=eps, ws=ws(B, pairs))
+        head = (Z, vec(y, torch.int32), vec(seq, torch.int32))
+        hb.preference_loss(*head, st, dZ=dZ, seq_logp=sl, **args)
+        s_tol, st_tol, d_tol = preference_tols(z, y, seq, rr, beta, eps, stats, s, want, g, K, dtype)
+        check(sl, s, s_tol, "seq_logp")
+        check(st, stats, st_tol, "stats")
+        check(dZ, want, d_tol, "dZ")        # NaN where nothing is written
+        assert outside_is_nan(flat_d, dZ)
+        again, st2 = torch.full_like(dZ, float("nan")), torch.zeros(4, device="cuda")
+        hb.preference_loss(*head, st2, **args)
+        check(st2, stats, st_tol, "stats of the loss alone")
+        hb.preference_loss(*head, st2, dZ=again, **args)
+        assert torch.equal(st2, st) and np.array_equal(host(again), host(dZ), equal_nan=True)
+        keep = host(Z)
+        hb.preference_loss(*head, st2, dZ=Z, **args)
+        inside = slice(seq[0], seq[-1])
+        got = host(Z)
+        assert np.array_equal(got[inside], host(dZ)[inside]) and outside_is_nan(flat_z, Z)
+        assert np.array_equal(got[:seq[0]], keep[:seq[0]], equal_nan=True) and np.array_equal(got[seq[-1]:], keep[seq[-1]:], equal_nan=True)
+
+
+def test_preference_gradient_against_differences():
+    rng = np.random.default_rng(17)
+    B, K, pairs, beta, eps, h = 14, 300, 2, 0.3, 0.1, 2.0 ** -6
+    z, y, seq, refs = preference_case(B, K, pairs, rng, "f32", masked=False)
+    v = rng.standard_normal((B, K)) / np.sqrt(K)
+    L, L64, tol = [], [], 0.0
+    for s in (1, -1):
+        zs = np.float32(z + s * h * v)
+        st = torch.zeros(4, device="cuda")
+        hb.preference_loss(matrix(zs, "f32")[0], vec(y, torch.int32), vec(seq, torch.int32), st, ref=vec(refs), beta=beta,
+                           smoothing=eps, ws=ws(B, pairs))
+        stats, sl, want, g = ref.preference_ref(zs, y, seq, refs, beta, eps)
+        tol += preference_tols(zs, y, seq, refs, beta, eps, stats, sl, want, g, K, "f32")[1][0]
+        L.append(float(st[0]))
+        L64.append(stats[0])
+    stats, sl, want, g = ref.preference_ref(z, y, seq, refs, beta, eps)
+    dZ, st = torch.zeros(B, K, device="cuda"), torch.zeros(4, device="cuda")
+    hb.preference_loss(matrix(z, "f32")[0], vec(y, torch.int32), vec(seq, torch.int32), st, dZ=dZ, ref=vec(refs), beta=beta,
+                       smoothing=eps, ws=ws(B, pairs))
+    along = (np.nan_to_num(want) * v).sum()
+    truncation = abs((L64[0] - L64[1]) / (2 * h) - along)
+    d_tol = (preference_tols(z, y, seq, refs, beta, eps, stats, sl, want, g, K, "f32")[2] * np.abs(v)).sum()
+    assert abs((L[0] - L[1]) / (2 * h) - (host(dZ) * v).sum()) <= truncation + tol / (2 * h) + d_tol
+    assert truncation < 0.1 * abs(along) + 1e-3
+
+
+def test_preference_offsets_out_of_range_write_nothing_outside():
+    """Offsets beyond the rows are cut to them, decreasing ones make a sequence empty: no access outside, whatever they say."""
+    rng = np.random.default_rng(3)
+    B, K = 12, 100
+    z, y = logits(B, K, rng, "f32", masked=False)
+    for seq, same in [([-5, 4, 99], [0, 4, 12]), ([0, 12, 12], None), ([12, 12, 12], None), ([50, 60, 70], [12, 12, 12])]:
+        out = []
+        for q in (seq, same or seq):
+            dZ, flat = matrix(np.full((B, K), np.nan), "f32", K + 1, 2)
+            st, sl = torch.zeros(4, device="cuda"), torch.zeros(2, device="cuda")
+            hb.preference_loss(matrix(z, "f32")[0], vec(y, torch.int32), vec(q, torch.int32), st, dZ=dZ, seq_logp=sl, ws=ws(B, 1))
+            assert outside_is_nan(flat, dZ)
+            out.append((host(st), host(sl), host(dZ)))
+        for a, b in zip(*out):
+            assert np.array_equal(a, b, equal_nan=True)
+    dZ, flat = matrix(np.full((B, K), np.nan), "f32", K + 1, 2)
+    st = torch.zeros(4, device="cuda")
+    hb.preference_loss(matrix(z, "f32")[0], vec(y, torch.int32), vec([9, 3, 2 ** 31 - 1, -2 ** 31, 5], torch.int32), st, dZ=dZ, ws=ws(B, 2))
+    torch.cuda.synchronize()
+    assert outside_is_nan(flat, dZ)
+
+
+# ---------------------------------------------------------------- how they are called
+def test_refusals_that_need_a_device():
+    Z = torch.zeros(4, 8)
+    y, r = torch.zeros(4, dtype=torch.int32), torch.zeros(4)
+    for call in (lambda: hb.dropout(Z, torch.zeros(4, 8).cuda(), 0.5, 1), lambda: hb.dropout(Z.cuda(), Z, 0.5, 1),
+                 lambda: hb.logprob(Z, y.cuda(), r.cuda(), r.cuda(), ws=ws(4)),
+                 lambda: hb.logprob(Z.cuda(), y, r.cuda(), r.cuda(), ws=ws(4)),
+                 lambda: hb.logprob(Z.cuda(), y.cuda(), r.cuda(), r, ws=ws(4)),
+                 lambda: hb.policy_loss(Z.cuda(), y.cuda(), r.cuda(), r.cuda(), r.cuda(), weight=r, ws=ws(4)),
+                 lambda: hb.policy_loss(Z.cuda(), y.cuda(), r.cuda(), r.cuda(), r.cuda(), ws=torch.zeros(1 << 17, dtype=torch.uint8)),
+                 lambda: hb.preference_loss(Z.cuda(), y.cuda(), torch.tensor([0, 1, 2], dtype=torch.int32), r.cuda(), ws=ws(4, 1)),
+                 lambda: hb.logprob_grad(Z.cuda(), y.cuda(), r.cuda(), r.cuda(), r, Z.cuda())):
+        with pytest.raises(hb.HbError) as e:
+            call()
+        assert e.value.code == hb.HB_ERR_INVALID and "device pointer" in str(e.value)
+
+
+@pytest.mark.parametrize("B,K", [(40, 7), (300, 1500), (3, 60000), (20, 20000)])
+def test_captured_and_replayed_beside_eager_work(B, K):
+    """One graph with all of them, replayed five times with other inputs, eager calls and synchronisations between."""
+    rng = np.random.default_rng(B)
+    pairs = 2
+    st = torch.cuda.Stream()
+    z, y, old, adv, refs, w = policy_inputs(B, K, rng, "f32")
+    _, _, seq, _ = preference_case(B, K, pairs, rng, "f32")
+    Z, dy, dold, dadv, dref, dw, dseq = (matrix(z, "f32")[0], vec(y, torch.int32), vec(old), vec(adv), vec(refs), vec(w),
+                                         vec(seq, torch.int32))
+
+    def buffers():
+        return dict(x=torch.zeros(B, K, device="cuda"), d1=torch.zeros(B, K, device="cuda"), d2=torch.zeros(B, K, device="cuda"),
+                    d3=torch.zeros(B, K, device="cuda"), s1=torch.zeros(4, device="cuda"), s2=torch.zeros(4, device="cuda"),
+                    lp=torch.zeros(B, device="cuda"), lse=torch.zeros(B, device="cuda"))
+
+    def calls(o, work, stream):
+        hb.dropout(Z, o["x"], 0.2, 5, 6, stream=stream)
+        hb.policy_loss(o["x"], dy, dold, dadv, o["s1"], dZ=o["d1"], ref=dref, weight=dw, kl_coef=0.1, ws=work, stream=stream)
+        hb.preference_loss(Z, dy, dseq, o["s2"], dZ=o["d2"], ws=work, stream=stream)
+        hb.logprob(Z, dy, o["lp"], o["lse"], ws=work, stream=stream)
+        hb.logprob_grad(Z, dy, o["lp"], o["lse"], dadv, o["d3"], stream=stream)
+
+    captured, eager = buffers(), buffers()
+    work_c, work_e = ws(B, pairs), ws(B, pairs)
+    torch.cuda.synchronize()
+    calls(captured, work_c, st.cuda_stream)
+    st.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        calls(captured, work_c, st.cuda_stream)
+    for k in range(5):
+        Z.copy_(torch.as_tensor(logits(B, K, rng, "f32")[0]))
+        for t in captured.values():
+            t.fill_(7.0)
+        work_c.fill_(k)
+        torch.cuda.synchronize()
+        calls(eager, work_e, None)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for name in captured:
+            rows = slice(seq[0], seq[-1]) if name == "d2" else slice(None)
+            assert np.array_equal(host(captured[name])[rows], host(eager[name])[rows], equal_nan=True), (k, name)
+
+
+def test_two_streams_at_once():
+    """Calls on two streams with a workspace each, their inputs made on those streams."""
+    rng = np.random.default_rng(8)
+    B, K = 400, 3000
+    z, y, old, adv, refs, w = policy_inputs(B, K, rng, "f32")
+    want = []
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    parts = []
+    torch.cuda.synchronize()
+    for i, s in enumerate(streams):
+        with torch.cuda.stream(s):
+            Z = torch.as_tensor(z * (1 + i)).float().cuda(non_blocking=True)
+            args = [vec(y, torch.int32), vec(old), vec(adv)]
+            o = (torch.zeros(4, device="cuda"), torch.empty(B, K, device="cuda"), ws(B))
+            parts.append((Z, args, o))
+    for _ in range(4):
+        for s, (Z, args, o) in zip(streams, parts):
+            hb.policy_loss(Z, *args, o[0], dZ=o[1], ws=o[2], stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for Z, args, o in parts:
+        a, b = torch.zeros(4, device="cuda"), torch.empty(B, K, device="cuda")
+        hb.policy_loss(Z, *args, a, dZ=b, ws=ws(B))
+        torch.cuda.synchronize()
+        assert torch.equal(a, o[0]) and np.array_equal(host(b), host(o[1]))
