@@ -12,11 +12,12 @@ namespace hb {
 namespace {
 
 constexpr int NT = 256;
-constexpr int MAX_SUM_BLOCKS = 1024;  // blocks that leave partial sums of a loss, at most
+constexpr int MAX_SUM_BLOCKS = 1024;  // blocks of merge_kernel, at most
+constexpr int SUM_SLICES = 256;       // more than 16 partial sums for each of these are added up in two steps
 constexpr int MAX_CHUNKED = 2048;     // (row, chunk) pairs of the calls that split their rows, at most
 
 // ---------------------------------------------------------------- rows in memory
-// A 16-byte piece of a row, as it is stored: four values, or eight of two bytes.
+// 16 bytes of a row, as they are stored: four values, or eight of two bytes.
 template <typename T>
 struct Piece {
     static constexpr int V = 16 / sizeof(T);
@@ -26,19 +27,21 @@ struct Piece {
         if (sizeof(T) == 4) return __uint_as_float(w[e]);
         return __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
     }
-    __device__ __forceinline__ void set(int e, T v)
-    {
-        if constexpr (sizeof(T) == 4) {
-            w[e] = __float_as_uint(v);
-        } else {
-            const unsigned h = __builtin_bit_cast(unsigned short, v);
-            w[e >> 1] = (e & 1) ? (w[e >> 1] & 0xffffu) | h << 16 : (w[e >> 1] & 0xffff0000u) | h;
-        }
-    }
-    __device__ __forceinline__ void set_none()
+    __device__ __forceinline__ void set_none()  // -inf
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    }
+    // without element `at` of it, where `own`
+    __device__ __forceinline__ void drop(int at, bool own)
+    {
+        const unsigned half = sizeof(T) == 4 ? 0xffffffffu : (at & 1) ? 0xffff0000u : 0xffffu;
+        const int word = sizeof(T) == 4 ? at : at >> 1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned m = own && i == word ? half : 0u;
+            w[i] = (m & (sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u)) | (~m & w[i]);
+        }
     }
     // Between two passes over pieces in registers: what the first has made of them (eight floats of four words) is made
     // again in the second, not kept.
@@ -47,68 +50,83 @@ struct Piece {
 #pragma unroll
         for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));
     }
-    // without element y of the row, where the piece begins with element j0
-    __device__ __forceinline__ void drop(int j0, int y)
-    {
-        if ((unsigned)(y - j0) < (unsigned)V) {
-            const int at = y - j0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (sizeof(T) == 4) {
-                    w[i] = i == at ? 0xff800000u : w[i];
-                } else {
-                    const unsigned low = (w[i] & 0xffff0000u) | 0xff80u, high = (w[i] & 0xffffu) | 0xff800000u;
-                    w[i] = 2 * i == at ? low : 2 * i + 1 == at ? high : w[i];
-                }
-            }
-        }
-    }
 };
 
-// The pieces of a row begin at 16-byte boundaries in memory: piece p has the elements p * V - lead .. + V, the first and
-// the last may be cut by the row's ends.
+// A row is whole pieces that begin at 16-byte boundaries in memory, and an edge of fewer than V single elements at either
+// end.  Piece p has the elements first(p) .. + V.
 template <typename T>
 struct Row {
     static constexpr int V = Piece<T>::V;
+    static constexpr int EDGE = 2 * V;  // places: V for either end
     const T *z;
-    int K, lead, pieces;
+    int K, head, pieces;
     __device__ __forceinline__ Row(const void *Z, long long ld, long long row, int K_)
         : z(static_cast<const T *>(Z) + row * ld), K(K_)
     {
-        lead = (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
-        pieces = (K + lead + V - 1) / V;
+        const int past = (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
+        head = past ? min(V - past, K) : 0;
+        pieces = (K - head) / V;
     }
-    __device__ __forceinline__ int first(int piece) const { return piece * V - lead; }
-    // what is outside of the row reads as -inf
-    __device__ __forceinline__ Piece<T> load(int j0) const
+    __device__ __forceinline__ int first(int piece) const { return head + piece * V; }
+    __device__ __forceinline__ Piece<T> load(int piece) const
     {
         Piece<T> t;
-        if (j0 >= 0 && j0 + V <= K) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(z + j0);
-            t.w[0] = u.x, t.w[1] = u.y, t.w[2] = u.z, t.w[3] = u.w;
-        } else {
-            t.set_none();
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                if (j0 + e >= 0 && j0 + e < K) t.set(e, z[j0 + e]);
-        }
+        const uint4 u = *reinterpret_cast<const uint4 *>(z + first(piece));
+        t.w[0] = u.x, t.w[1] = u.y, t.w[2] = u.z, t.w[3] = u.w;
         return t;
     }
+    // The pieces as a buffer, for wavefronts that have one row (z the same in all lanes): what is behind the last reads as 0
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const
+    {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(z + head), (short)0, pieces * 16, 0x00027000);
+    }
+    __device__ __forceinline__ static Piece<T> load(__amdgpu_buffer_rsrc_t rs, int lane_piece, int first_piece)
+    {
+        typedef unsigned v4u __attribute__((ext_vector_type(4)));
+        const v4u u = __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * lane_piece, 16 * first_piece, 0);
+        Piece<T> t;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t.w[i] = u[i];
+        return t;
+    }
+    // the element in place i of the edges, -1 if there is none
+    __device__ __forceinline__ int edge(int i) const
+    {
+        const int tail = first(pieces);
+        const int j = i < V ? i : tail + i - V;
+        return i < V ? (j < head ? j : -1) : (j < K && i < EDGE ? j : -1);
+    }
+    __device__ __forceinline__ float at(int j) const { return j >= 0 ? (float)z[j] : -INFINITY; }
 };
 
-// V elements of a row of dZ from j0 on, those in [0, K)
+// V elements of a row of dZ
 template <typename T, int V>
-__device__ __forceinline__ void store(T *dz, int j0, int K, const float *x)
+__device__ __forceinline__ void store(T *dz, const float *x)
 {
-    if (j0 >= 0 && j0 + V <= K) {
-        T t[V];
+    T t[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) t[e] = T(x[e]);
-        __builtin_memcpy(dz + j0, t, sizeof(t));
+    for (int e = 0; e < V; ++e) t[e] = T(x[e]);
+    __builtin_memcpy(dz, t, sizeof(t));
+}
+
+// ... through a buffer
+template <typename T, int V>
+__device__ __forceinline__ void store_buffer(__amdgpu_buffer_rsrc_t rs, int lane_piece, int first_piece, const float *x)
+{
+    constexpr int B = V * sizeof(T);
+    T t[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) t[e] = T(x[e]);
+    if constexpr (B == 16) {
+        typedef unsigned v4u __attribute__((ext_vector_type(4)));
+        v4u u;
+        __builtin_memcpy(&u, t, 16);
+        __builtin_amdgcn_raw_buffer_store_b128(u, rs, B * lane_piece, B * first_piece, 0);
     } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            if (j0 + e >= 0 && j0 + e < K) dz[j0 + e] = T(x[e]);
+        typedef unsigned v2u __attribute__((ext_vector_type(2)));
+        v2u u;
+        __builtin_memcpy(&u, t, 8);
+        __builtin_amdgcn_raw_buffer_store_b64(u, rs, B * lane_piece, B * first_piece, 0);
     }
 }
 
@@ -124,23 +142,37 @@ __device__ __forceinline__ bool has_choice(const ChoiceRows &r, long long row)
     return y >= 0 && y < r.K && (r.weight == nullptr || r.weight[row] != 0.f);
 }
 
-// exp(t).  Of log2 e = 1.4426950 + 1.9e-8 the second part matters in sums: without it every term is too small by 1.3e-8 |t|
-// relative, all in one direction, which the log-probabilities of a sequence add up.
-__device__ __forceinline__ float exp_for_sum(float t)
-{
-    return __builtin_amdgcn_exp2f(__builtin_fmaf(t, 0x1.715476p+0f, t * 0x1.4ae0cp-26f));
-}
+// Exponentials are powers of two of z * LOG2E - top * LOG2E: one fused multiply-add and one v_exp_f32.  LOG2E is log2 e to 24
+// bits, so what is added up is the softmax of logits that are 1.3e-8 smaller; log-probabilities are made of z_y * LOG2E
+// and that sum in the same way, which leaves an error of 1.3e-8 (E z - z_y) in them, of both signs (with the exact factor
+// outside it would be 1.3e-8 times the entropy, always of one sign, which the tokens of a sequence add up).
+constexpr float LOG2E = 0x1.715476p+0f;
+constexpr double LN2 = 0.693147180559945309;
+__device__ __forceinline__ float exp2_of(float u) { return __builtin_amdgcn_exp2f(u); }
 
-// log(s) for a positive s, in two parts whose sum is off by less than 2^-23: of s = 2^k f, f in [1/2, 1), the first is k times the
-// leading bits of log 2 (exact), the second, at most 1, the rest.
+// The exponent u = z * factor - shift under a maximum (0 where that is -inf).  From 2^100 on top * LOG2E could leave the range,
+// but logits differ from it by 0 or by 2^76 and more: any power of two as the factor tells these apart, exactly.
+struct Under {
+    float shift, factor;
+    bool far;
+    __device__ __forceinline__ explicit Under(float top)
+    {
+        const float ref = top == -INFINITY ? 0.f : top;
+        far = fabsf(ref) >= 0x1p100f;
+        factor = far ? 0x1p-40f : LOG2E;
+        shift = ref * factor;
+    }
+    __device__ __forceinline__ Under(float shift_, float factor_) : shift(shift_), factor(factor_), far(false) {}
+    __device__ __forceinline__ float exp(float z) const { return exp2_of(__builtin_fmaf(z, factor, -shift)); }
+};
+
+// log2(s) for a positive s, in two parts: an integer, and at most 1 with an error of 2^-24
 struct TwoLog {
     float hi, lo;
 };
-__device__ __forceinline__ TwoLog two_log(float s)
+__device__ __forceinline__ TwoLog two_log2(float s)
 {
-    const int k = __builtin_amdgcn_frexp_expf(s);
-    const float f = __builtin_amdgcn_frexp_mantf(s);
-    return {(float)k * 0.693359375f, __builtin_fmaf((float)k, -2.12194440e-4f, __logf(f))};
+    return {(float)__builtin_amdgcn_frexp_expf(s), __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(s))};
 }
 
 // exp(d) - 1 - d, to a few roundings where d is small, too: d^2 times a series
@@ -163,34 +195,42 @@ __device__ __forceinline__ float kl_of(float d, float em /* exp(d) - 1 */)
 // part: the row takes part.  One without a choice has lp = lse = 0, one whose logits are all -inf has -inf.
 struct RowTerms {
     bool part;
-    float top;               // the maximum, 0 where that is -inf
+    Under under;             // of the maximum
     float inv_sum, others;   // 1 / s, 1 - p_y
     double lp, lse;          // log-probability, log of the sum of exponentials: off by 1e-7 beside what s is
 };
 
-// zy: the chosen logit; top: the maximum; o: the sum over the others of exp(z - top) (z itself where top = -inf).
+// zy: the chosen logit; top: the maximum; o: the sum over the others under it.
 // 64-bit additions, but no function of 64 bits: those would take more registers than the rows do.
 __device__ __forceinline__ RowTerms finish_row(float zy, float top, float o)
 {
-    RowTerms t = {false, 0.f, 0.f, 0.f, 0.0, 0.0};
+    RowTerms t = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
     if (top == -INFINITY && o == 0.f && zy == zy) {  // NaN in o or zy: no maximum either, but a row that takes part
         t.lp = t.lse = -INFINITY;
         return t;
     }
     t.part = true;
-    t.top = top == -INFINITY ? 0.f : top;
-    const float e = exp_for_sum(zy - t.top), s = o + e;
-    const TwoLog l = two_log(s);
+    t.under = Under(top);
+    const float e = t.under.exp(zy), s = (o == INFINITY ? NAN : o) + e;  // infinite: a logit that no maximum has seen
+    const TwoLog l = two_log2(s);
     t.inv_sum = 1.f / s;
     t.others = o * t.inv_sum;
-    t.lse = (double)t.top + (double)l.hi + (double)l.lo;
-    t.lp = o < e ? -(double)log1pf(o / e) : (double)zy - t.lse;
+    const double log2_s = (double)l.hi + (double)l.lo;
+    if (t.under.far) {
+        t.lse = (double)top + LN2 * log2_s;
+        t.lp = (double)zy - t.lse;
+    } else {
+        const double lse2 = (double)t.under.shift + log2_s;
+        t.lse = LN2 * lse2;
+        t.lp = LN2 * ((double)zy * (double)LOG2E - lse2);
+    }
+    if (o < e) t.lp = -(double)log1pf(o / e);
     return t;
 }
 
-// The gradient of a row: dz_k = scale * exp(z_k - base) for k != y and `chosen` for k = y; all zero where both are
+// The gradient of a row: dz_k = scale * 2^(z_k * factor - shift) for k != y and `chosen` for k = y; all zero where both are
 struct RowCoef {
-    float base, scale, chosen, pad;
+    float shift, factor, scale, chosen;
 };
 
 struct Four {
@@ -216,7 +256,7 @@ struct RowHead {
     int kind;
     float *logp, *lse;  // LOGPROB: results (lse may be null).  POLICY: in p
     double *row_lp;     // TERMS: 0 where a row takes no part
-    RowCoef *coef;      // TERMS: {top, 1 / s, 1 - p_y}.  POLICY: null, or the gradient's coefficients
+    RowCoef *coef;      // TERMS: {shift, factor, 1 / s, 1 - p_y}.  POLICY: null, or the gradient's coefficients
     PolicyTerms p;
 };
 
@@ -234,7 +274,7 @@ __device__ __forceinline__ RowCoef head_row(const RowHead &h, const ChoiceRows &
     if (h.kind == HEAD_TERMS) {
         if (write) {
             h.row_lp[row] = t.part ? t.lp : 0.0;
-            if (h.coef) h.coef[row] = RowCoef{t.top, t.inv_sum, t.others, 0.f};
+            if (h.coef) h.coef[row] = RowCoef{t.under.shift, t.under.factor, t.inv_sum, t.others};
         }
         return c;
     }
@@ -261,7 +301,8 @@ __device__ __forceinline__ RowCoef head_row(const RowHead &h, const ChoiceRows &
             sums = add_four(sums, Four{{p.kl_coef != 0.f ? pgw + (double)p.kl_coef * klw : pgw, pgw, klw, cut ? (double)w : 0.0}});
         }
         g *= w;
-        c.base = t.top;
+        c.shift = t.under.shift;
+        c.factor = t.under.factor;
         c.scale = -g * t.inv_sum;
         c.chosen = g * t.others;
     }
@@ -306,6 +347,17 @@ __global__ __launch_bounds__(NT) void sum_four_kernel(SumFour f)
     sum_four(f, red);
 }
 
+// One of SUM_SLICES neighbouring parts of the sums a block
+__global__ __launch_bounds__(NT) void sum_slices_kernel(const Four *partial, int n, Four *out)
+{
+    __shared__ Four red[NT / 64];
+    const int per = (n + SUM_SLICES - 1) / SUM_SLICES, end = min(n, ((int)blockIdx.x + 1) * per);
+    Four s = {};
+    for (int i = (int)blockIdx.x * per + threadIdx.x; i < end; i += NT) s = add_four(s, partial[i]);
+    s = sum_block(s, red);
+    if (threadIdx.x == 0) out[blockIdx.x] = s;
+}
+
 // ---------------------------------------------------------------- whole rows in registers
 struct RowsArgs {
     ChoiceRows r;
@@ -315,100 +367,169 @@ struct RowsArgs {
     float *stats;   // ... the statistics themselves
 };
 
-// G lanes have a row between them, N pieces each: it is read once, whole, for the maximum, the sum and the gradient.
-template <typename T, typename TO, int G, int N>
-__global__ __launch_bounds__(G > NT ? G : NT) void rows_kernel(RowsArgs a)
+constexpr int row_threads(int g) { return g > 64 ? g : NT; }
+// wavefronts a SIMD that the registers have to leave room for
+constexpr int row_waves(int n) { return n <= 4 ? 6 : n <= 8 ? 5 : n <= 16 ? 4 : 3; }
+
+// A row of dZ and its padding
+template <int G, typename TO>
+__device__ __forceinline__ void zero_row(TO *dz, const RowsArgs &a, int g)
 {
-    constexpr int V = Piece<T>::V, THREADS = G > NT ? G : NT, WAVES = THREADS / 64, ROWS = THREADS / G;
+    const int n = max(a.r.K, a.d.pad);
+    for (int j = g; j < n; j += G) dz[j] = TO(0.f);
+}
+
+// The maximum over the G lanes of a row; red: a wavefront each
+template <int G, int WAVES>
+__device__ __forceinline__ float max_of_row(float top, float *red)
+{
+#pragma unroll
+    for (int o = (G < 64 ? G : 64) / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if (G > 64) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+        __syncthreads();
+        top = red[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, red[w]);
+    }
+    return top;
+}
+
+// G lanes have a row between them, N pieces each and what there is at its ends: it is read once, whole, for the maximum,
+// the sum and the gradient.
+template <typename T, typename TO, int G, int N>
+__device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long row, int g, float *red_top, float *red_sum,
+                                                 RowCoef *red_coef, Four &sums)
+{
+    constexpr int V = Piece<T>::V, WAVES = row_threads(G) / 64;
+    constexpr int E = G < Row<T>::EDGE ? Row<T>::EDGE / G : 1;
+    const Row<T> z(a.r.Z, a.r.ldz, row, a.r.K);
+    const int y = a.r.y[row];
+    // the choice: its place in the pieces (if it is in one), the lane that has it, and which piece of that lane's it is
+    const int ay = y - z.head, py = ay / V, iy = py / G;
+    const bool own = ay >= 0 && py < z.pieces && py % G == g;
+    TO *dz = static_cast<TO *>(a.d.dZ) + row * a.d.ld;
+    if (!has_choice(a.r, row)) {
+        const RowTerms t = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
+        if (g == 0) head_row(a.h, a.r, row, t, true, sums);
+        if (a.d.dZ) zero_row<G>(dz, a, g);
+        return;
+    }
+    Piece<T> x[N];
+    float edge[E];
+    const float zy = logit(a.r, row, y);
+    const int most = a.r.K / V;  // pieces of any row; one less is in all of them
+    if constexpr (G >= 64) {
+        const __amdgpu_buffer_rsrc_t rs = z.buffer();
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i * G < most) x[i] = Row<T>::load(rs, g, i * G);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if ((i + 1) * G < most) x[i] = z.load(i * G + g);
+            else if (i * G + g < z.pieces) x[i] = z.load(i * G + g);
+        }
+    }
+    float top = zy;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const int j = z.edge(i * G + g);
+        edge[i] = j == y ? -INFINITY : z.at(j);
+        top = fmaxf(top, edge[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i * G >= most) continue;
+        if (i == iy) x[i].drop(ay % V, own);
+        if ((i + 1) * G >= most && i * G + g >= z.pieces) x[i].set_none();
+#pragma unroll
+        for (int e = 0; e < V; ++e) top = fmaxf(top, x[i].get(e));
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    top = max_of_row<G, WAVES>(top, red_top);
+    float others = 0.f;
+    {
+        const Under under(top);
+        float o4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < E; ++i) o4[i & 3] += under.exp(edge[i]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i * G >= most) continue;
+            x[i].forget();
+            float t[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) t[e] = under.exp(x[i].get(e));
+#pragma unroll
+            for (int e = 0; e < V; ++e) o4[e & 3] += t[e];
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        others = (o4[0] + o4[1]) + (o4[2] + o4[3]);
+    }
+#pragma unroll
+    for (int o = (G < 64 ? G : 64) / 2; o > 0; o >>= 1) others += __shfl_xor(others, o, 64);
+    RowCoef c;
+    if (G <= 64) {
+        c = head_row(a.h, a.r, row, finish_row(zy, top, others), g == 0, sums);
+    } else {
+        if ((threadIdx.x & 63) == 0) red_sum[threadIdx.x >> 6] = others;
+        __syncthreads();
+        if (threadIdx.x < 64) {
+            others = red_sum[0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) others += red_sum[w];
+            c = head_row(a.h, a.r, row, finish_row(zy, top, others), g == 0, sums);
+            if (threadIdx.x == 0) *red_coef = c;
+        }
+        __syncthreads();
+        c = *red_coef;
+    }
+    if (!a.d.dZ) return;
+    if (c.scale == 0.f && c.chosen == 0.f) {
+        zero_row<G>(dz, a, g);
+        return;
+    }
+    const Under under(c.shift, c.factor);
+    TO *to = dz + z.head;
+    // whole wavefronts that store at 16-byte boundaries: through a buffer, which leaves out what is behind the row
+    const bool through = G >= 64 && (reinterpret_cast<uintptr_t>(to) & (V * sizeof(TO) - 1)) == 0;
+    const __amdgpu_buffer_rsrc_t rs =
+        __builtin_amdgcn_make_buffer_rsrc(to, (short)0, z.pieces * V * (int)sizeof(TO), 0x00027000);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i * G >= most) continue;
+        x[i].forget();
+        float out[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = c.scale * under.exp(x[i].get(e));
+        if (through) store_buffer<TO, V>(rs, g, i * G, out);
+        else if (i * G + g < z.pieces) store<TO, V>(to + (i * G + g) * V, out);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (own) dz[y] = TO(c.chosen);  // over what this lane has just stored there
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const int j = z.edge(i * G + g);
+        if (j >= 0) dz[j] = TO(j == y ? c.chosen : c.scale * under.exp(edge[i]));
+    }
+    for (int j = a.r.K + g; j < a.d.pad; j += G) dz[j] = TO(0.f);
+}
+
+template <typename T, typename TO, int G, int N>
+__global__ __launch_bounds__(row_threads(G), row_waves(N)) void rows_kernel(RowsArgs a)
+{
+    constexpr int THREADS = row_threads(G), WAVES = THREADS / 64, ROWS = THREADS / G;
     __shared__ float red_top[WAVES], red_sum[WAVES];
     __shared__ RowCoef red_coef;
     __shared__ Four red_four[WAVES];
-    const int g = threadIdx.x % G;
+    const int g = threadIdx.x % G, sub = G >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / G) : threadIdx.x / G;
+    const long long row = (long long)blockIdx.x * ROWS + sub;
+    // (a loop over rows would keep registers for the row before)
     Four sums = {};
-    for (long long row = (long long)blockIdx.x * ROWS + threadIdx.x / G; row < a.r.B; row += (long long)gridDim.x * ROWS) {
-        const Row<T> z(a.r.Z, a.r.ldz, row, a.r.K);
-        const int y = a.r.y[row];
-        const bool choice = has_choice(a.r, row);
-        Piece<T> x[N];
-        RowCoef c = {0.f, 0.f, 0.f, 0.f};
-        RowTerms t = {false, 0.f, 0.f, 0.f, 0.0, 0.0};
-        if (choice) {
-            const float zy = logit(a.r, row, y);
-#pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = z.load(z.first(i * G + g));
-            float top = zy;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                x[i].drop(z.first(i * G + g), y);
-#pragma unroll
-                for (int e = 0; e < V; ++e) top = fmaxf(top, x[i].get(e));
-            }
-#pragma unroll
-            for (int o = (G < 64 ? G : 64) / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-            if (G > 64) {
-                if ((threadIdx.x & 63) == 0) red_top[threadIdx.x >> 6] = top;
-                __syncthreads();
-                top = red_top[0];
-#pragma unroll
-                for (int w = 1; w < WAVES; ++w) top = fmaxf(top, red_top[w]);
-            }
-            const float ref = top == -INFINITY ? 0.f : top;
-            float o4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                x[i].forget();
-#pragma unroll
-                for (int e = 0; e < V; ++e) o4[e & 3] += exp_for_sum(x[i].get(e) - ref);
-            }
-            float others = (o4[0] + o4[1]) + (o4[2] + o4[3]);
-#pragma unroll
-            for (int o = (G < 64 ? G : 64) / 2; o > 0; o >>= 1) others += __shfl_xor(others, o, 64);
-            if (G <= 64) {
-                t = finish_row(zy, top, others);
-                c = head_row(a.h, a.r, row, t, g == 0, sums);
-            } else {
-                if ((threadIdx.x & 63) == 0) red_sum[threadIdx.x >> 6] = others;
-                __syncthreads();
-                if (threadIdx.x < 64) {
-                    others = red_sum[0];
-#pragma unroll
-                    for (int w = 1; w < WAVES; ++w) others += red_sum[w];
-                    t = finish_row(zy, top, others);
-                    c = head_row(a.h, a.r, row, t, g == 0, sums);
-                    if (threadIdx.x == 0) red_coef = c;
-                }
-                __syncthreads();
-                c = red_coef;
-            }
-        } else if (g == 0) {
-            head_row(a.h, a.r, row, t, true, sums);
-        }
-        if (a.d.dZ) {
-            TO *dz = static_cast<TO *>(a.d.dZ) + row * a.d.ld;
-            const bool none = c.scale == 0.f && c.chosen == 0.f;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int j0 = z.first(i * G + g);
-                if (j0 >= a.r.K) break;
-                float out[V];
-                if (none) {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) out[e] = 0.f;
-                } else {
-                    x[i].forget();
-#pragma unroll
-                    for (int e = 0; e < V; ++e) out[e] = c.scale * __expf(x[i].get(e) - c.base);
-                    if ((unsigned)(y - j0) < (unsigned)V)
-#pragma unroll
-                        for (int e = 0; e < V; ++e) out[e] = e == y - j0 ? c.chosen : out[e];
-                }
-                store<TO, V>(dz, j0, a.r.K, out);
-            }
-            for (int j = a.r.K + g; j < a.d.pad; j += G) dz[j] = TO(0.f);
-        }
-    }
+    if (row < a.r.B) row_in_registers<T, TO, G, N>(a, row, g, red_top, red_sum, &red_coef, sums);
     if (a.h.kind == HEAD_POLICY) {
-        sums = sum_block(sums, red_four);
+        if (G <= 64) sums = sum_block(sums, red_four);  // else the first thread's
         if (a.stats) store_stats(a.stats, sums);
         else if (threadIdx.x == 0) a.sums[blockIdx.x] = sums;
     }
@@ -420,48 +541,67 @@ struct TopSum {
     float top, sum;
 };
 
-__device__ __forceinline__ float under(float x, float top) { return exp_for_sum(x - (top == -INFINITY ? 0.f : top)); }
+// What a sum under `from` is multiplied with to be one under `to` >= from: the difference of their shifts, as rounded
+__device__ __forceinline__ float rescale(float from, float to)
+{
+    if (from == to || from == -INFINITY) return 1.f;
+    const Under f(from), t(to);
+    return f.far == t.far ? exp2_of(f.shift - t.shift) : 0.f;
+}
 
 __device__ __forceinline__ TopSum join(TopSum a, TopSum b)
 {
     const float top = fmaxf(a.top, b.top);
-    return {top, a.sum * under(a.top, top) + b.sum * under(b.top, top)};
+    return {top, a.sum * rescale(a.top, top) + b.sum * rescale(b.top, top)};
 }
 
-// Without the chosen class.
+// A block a chunk, without the chosen class; the first chunk has the edges.  A row of one chunk is finished here.
 template <typename T>
-__global__ __launch_bounds__(NT) void row_sums_kernel(ChoiceRows r, int chunks, int pieces_per_chunk, TopSum *partial)
+__global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, int pieces_per_chunk, TopSum *partial)
 {
     constexpr int V = Piece<T>::V, U = 4;
     __shared__ TopSum red[NT / 64];
+    const ChoiceRows &r = a.r;
     const long long row = blockIdx.x / chunks;
     const int c = blockIdx.x % chunks;
-    if (!has_choice(r, row)) return;
+    if (!has_choice(r, row)) {
+        const RowTerms none = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
+        Four sums = {};
+        if (chunks == 1 && a.h.kind != HEAD_POLICY && threadIdx.x == 0) head_row(a.h, r, row, none, true, sums);
+        return;
+    }
     const Row<T> z(r.Z, r.ldz, row, r.K);
     const int y = r.y[row], end = min(z.pieces, (c + 1) * pieces_per_chunk);
     TopSum t = {-INFINITY, 0.f};
+    if (c == 0) {
+        const int j = z.edge(threadIdx.x);
+        const float v = j == y ? -INFINITY : z.at(j);
+        t.top = v == v ? v : -INFINITY;
+        t.sum = Under(t.top).exp(v);
+    }
     for (int p = c * pieces_per_chunk + (int)threadIdx.x; p < end; p += U * NT) {
         Piece<T> x[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (p + u * NT < end) x[u] = z.load(z.first(p + u * NT));
+            if (p + u * NT < end) x[u] = z.load(p + u * NT);
             else x[u].set_none();
         }
         float top = t.top;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            x[u].drop(z.first(p + u * NT), y);
+            x[u].drop(y - z.first(p + u * NT), (unsigned)(y - z.first(p + u * NT)) < (unsigned)V);
 #pragma unroll
             for (int e = 0; e < V; ++e) top = fmaxf(top, x[u].get(e));
         }
-        const float ref = top == -INFINITY ? 0.f : top;
+        t.sum *= rescale(t.top, top);
+        t.top = top;
+        const Under at(top);
         float o = 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int e = 0; e < V; ++e) o += exp_for_sum(x[u].get(e) - ref);
-        t.sum = t.sum * under(t.top, top) + o;
-        t.top = top;
+            for (int e = 0; e < V; ++e) o += at.exp(x[u].get(e));
+        t.sum += o;
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) t = join(t, TopSum{__shfl_xor(t.top, o, 64), __shfl_xor(t.sum, o, 64)});
@@ -469,7 +609,13 @@ __global__ __launch_bounds__(NT) void row_sums_kernel(ChoiceRows r, int chunks, 
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int w = 1; w < NT / 64; ++w) t = join(t, red[w]);
-        partial[blockIdx.x] = t;
+        if (chunks == 1 && a.h.kind != HEAD_POLICY) {  // (its sums are added up over the rows)
+            const float zy = logit(r, row, y), top = fmaxf(t.top, zy);
+            Four sums = {};
+            head_row(a.h, r, row, finish_row(zy, top, t.sum * rescale(t.top, top)), true, sums);
+        } else {
+            partial[blockIdx.x] = t;
+        }
     }
 }
 
@@ -479,14 +625,14 @@ __global__ __launch_bounds__(NT) void merge_kernel(RowsArgs a, int chunks, const
     __shared__ Four red[NT / 64];
     Four sums = {};
     for (long long row = (long long)blockIdx.x * NT + threadIdx.x; row < a.r.B; row += (long long)gridDim.x * NT) {
-        RowTerms t = {false, 0.f, 0.f, 0.f, 0.0, 0.0};
+        RowTerms t = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
         if (has_choice(a.r, row)) {
             const TopSum *part = partial + row * chunks;
             const float zy = logit(a.r, row, a.r.y[row]);
             float top = zy;
             for (int c = 0; c < chunks; ++c) top = fmaxf(top, part[c].top);
             float o = 0.f;
-            for (int c = 0; c < chunks; ++c) o += part[c].sum * under(part[c].top, top);
+            for (int c = 0; c < chunks; ++c) o += part[c].sum * rescale(part[c].top, top);
             t = finish_row(zy, top, o);
         }
         head_row(a.h, a.r, row, t, true, sums);
@@ -516,7 +662,9 @@ __device__ __forceinline__ RowCoef coef_of(const GradArgs &a, long long row)
     RowCoef c = {0.f, 0.f, 0.f, 0.f};
     const float lse = a.lse[row], g = a.g[row];
     if (!has_choice(a.r, row) || lse == -INFINITY || g == 0.f) return c;
-    c.base = lse;
+    const Under under(lse);
+    c.shift = under.shift;
+    c.factor = under.factor;
     c.scale = -g;
     c.chosen = -g * expm1f(a.logp[row]);
     return c;
@@ -551,27 +699,41 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradArgs a)
     const RowCoef k = coef_of(a, row);
     const int y = a.r.y[row], end = G == NT ? min(z.pieces, (c + 1) * a.pieces_per_chunk) : z.pieces;
     const bool none = k.scale == 0.f && k.chosen == 0.f;
+    const Under under(k.shift, k.factor);
     for (int p = c * a.pieces_per_chunk + g; p < end; p += U * G) {
         Piece<T> x[U];
         if (!none)
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (p + u * G < end) x[u] = z.load(z.first(p + u * G));
+                if (p + u * G < end) x[u] = z.load(p + u * G);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (p + u * G >= end) break;
             const int j0 = z.first(p + u * G);
             float out[V];
+            if (none) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) out[e] = none ? 0.f : k.scale * __expf(x[u].get(e) - k.base);
-            if ((unsigned)(y - j0) < (unsigned)V)
+                for (int e = 0; e < V; ++e) out[e] = 0.f;
+            } else {
 #pragma unroll
-                for (int e = 0; e < V; ++e) out[e] = e == y - j0 ? k.chosen : out[e];
-            store<TO, V>(dz, j0, a.r.K, out);
+                for (int e = 0; e < V; ++e) out[e] = k.scale * under.exp(x[u].get(e));
+                if ((unsigned)(y - j0) < (unsigned)V)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) out[e] = e == y - j0 ? k.chosen : out[e];
+            }
+            store<TO, V>(dz + j0, out);
         }
     }
-    if (c == a.chunks - 1)
+    if (c == a.chunks - 1) {
+        constexpr int E = G < Row<T>::EDGE ? Row<T>::EDGE / G : 1;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const int j = z.edge(i * G + g);
+            if (j < 0) continue;
+            dz[j] = TO(none ? 0.f : j == y ? k.chosen : k.scale * under.exp(z.at(j)));
+        }
         for (int j = a.r.K + g; j < a.d.pad; j += G) dz[j] = TO(0.f);
+    }
 }
 
 // ---------------------------------------------------------------- pairs of sequences
@@ -619,7 +781,7 @@ __global__ __launch_bounds__(NT) void preference_kernel(PreferenceTerms p, long 
 
 // ---------------------------------------------------------------- launches
 struct Workspace {
-    Four *sums;
+    Four *sums;      // all of it for a call that leaves a sum a block of rows and nothing else
     RowCoef *coef;
     double *row_lp;
     TopSum *partial;
@@ -637,11 +799,7 @@ struct Workspace {
 };
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
-int most_pieces(const ChoiceRows &r)  // of a row at any alignment
-{
-    const int V = r.tensor == TENSOR_BF16 ? 8 : 4;
-    return (r.K + V - 1 + V - 1) / V;
-}
+int most_pieces(const ChoiceRows &r) { return r.K / (r.tensor == TENSOR_BF16 ? 8 : 4); }  // of a row, wherever it begins
 
 struct Split {
     int chunks, pieces_per_chunk;
@@ -649,13 +807,18 @@ struct Split {
 
 constexpr int ROW_PIECES = 20 * 1024;  // the longest row that rows_kernel has a form for
 
-// Rows go through registers unless they are too long for a workgroup, or too few to fill the device.
-bool rows_in_registers(const ChoiceRows &r) { return most_pieces(r) <= ROW_PIECES; }
+// A pass that makes a gradient keeps the rows in registers, unless they are too long for a workgroup or too few to fill the device.
+// One that only reads them does so where several rows share a wavefront.
+bool rows_in_registers(const ChoiceRows &r, bool grad)
+{
+    const int n = most_pieces(r);
+    return n <= (grad ? ROW_PIECES : 512);
+}
 
 Split split_for(const ChoiceRows &r)
 {
     const int pieces = most_pieces(r);
-    int chunks = ceil_div(pieces, 4 * NT);
+    int chunks = pieces > 0 ? ceil_div(pieces, 4 * NT) : 1;
     const long long room = r.B < MAX_CHUNKED ? MAX_CHUNKED / (r.B > 0 ? r.B : 1) : 1;
     if (chunks > room) chunks = (int)room;
     return {chunks, ceil_div(pieces, chunks)};
@@ -664,27 +827,28 @@ Split split_for(const ChoiceRows &r)
 template <typename T, typename TO, int G, int N>
 hipError_t rows_form(RowsArgs a, int *blocks_out, hipStream_t stream, const LaunchEvents &ev)
 {
-    constexpr int ROWS = G > NT ? 1 : NT / G;
-    int blocks = ceil_div(a.r.B, ROWS);
-    if (a.h.kind == HEAD_POLICY && blocks > MAX_SUM_BLOCKS) blocks = MAX_SUM_BLOCKS;
+    int blocks = ceil_div(a.r.B, row_threads(G) / G);
     if (blocks > 1) a.stats = nullptr;
     *blocks_out = blocks;
-    return launch_kernel(rows_kernel<T, TO, G, N>, dim3((unsigned)blocks), dim3(G > NT ? G : NT), stream, ev, a);
+    return launch_kernel(rows_kernel<T, TO, G, N>, dim3((unsigned)blocks), dim3(row_threads(G)), stream, ev, a);
 }
 
 template <typename T, typename TO>
 hipError_t rows_of_type(const RowsArgs &a, int *blocks, hipStream_t s, const LaunchEvents &ev)
 {
     const int n = most_pieces(a.r);
-    if (n <= 8) return rows_form<T, TO, 8, 1>(a, blocks, s, ev);
-    if (n <= 32) return rows_form<T, TO, 16, 2>(a, blocks, s, ev);
-    if (n <= 128) return rows_form<T, TO, 64, 2>(a, blocks, s, ev);
-    if (n <= 256) return rows_form<T, TO, 64, 4>(a, blocks, s, ev);
-    if (n <= 512) return rows_form<T, TO, 64, 8>(a, blocks, s, ev);
-    if (n <= 1024) return rows_form<T, TO, 256, 4>(a, blocks, s, ev);
-    if (n <= 2048) return rows_form<T, TO, 256, 8>(a, blocks, s, ev);
-    if (n <= 4096) return rows_form<T, TO, 512, 8>(a, blocks, s, ev);
-    if (n <= 8192) return rows_form<T, TO, 1024, 8>(a, blocks, s, ev);
+    if (n <= 4) return rows_form<T, TO, 4, 1>(a, blocks, s, ev);
+    if (n <= 16) return rows_form<T, TO, 4, 4>(a, blocks, s, ev);
+    if (n <= 32) return rows_form<T, TO, 4, 8>(a, blocks, s, ev);
+    if (n <= 64) return rows_form<T, TO, 4, 16>(a, blocks, s, ev);
+    if (n <= 128) return rows_form<T, TO, 8, 16>(a, blocks, s, ev);
+    if (n <= 256) return rows_form<T, TO, 16, 16>(a, blocks, s, ev);
+    if (n <= 512) return rows_form<T, TO, 32, 16>(a, blocks, s, ev);
+    if (n <= 1024) return rows_form<T, TO, 64, 16>(a, blocks, s, ev);
+    if (n <= 2048) return rows_form<T, TO, 128, 16>(a, blocks, s, ev);
+    if (n <= 4096) return rows_form<T, TO, 256, 16>(a, blocks, s, ev);
+    if (n <= 6656) return rows_form<T, TO, 512, 13>(a, blocks, s, ev);
+    if (n <= 8192) return rows_form<T, TO, 512, 16>(a, blocks, s, ev);
     if (n <= 12288) return rows_form<T, TO, 1024, 12>(a, blocks, s, ev);
     if (n <= 16384) return rows_form<T, TO, 1024, 16>(a, blocks, s, ev);
     return rows_form<T, TO, 1024, 20>(a, blocks, s, ev);
@@ -702,9 +866,9 @@ hipError_t chunked_rows(RowsArgs a, const Split &s, TopSum *partial, int *blocks
 {
     const dim3 grid((unsigned)(a.r.B * s.chunks)), block(NT);
     const hipError_t e = a.r.tensor == TENSOR_BF16
-                             ? launch_kernel(row_sums_kernel<__bf16>, grid, block, stream, ev, a.r, s.chunks, s.pieces_per_chunk, partial)
-                             : launch_kernel(row_sums_kernel<float>, grid, block, stream, ev, a.r, s.chunks, s.pieces_per_chunk, partial);
-    if (e != hipSuccess) return e;
+                             ? launch_kernel(row_sums_kernel<__bf16>, grid, block, stream, ev, a, s.chunks, s.pieces_per_chunk, partial)
+                             : launch_kernel(row_sums_kernel<float>, grid, block, stream, ev, a, s.chunks, s.pieces_per_chunk, partial);
+    if (e != hipSuccess || (s.chunks == 1 && a.h.kind != HEAD_POLICY)) return e;
     *blocks = ceil_div(a.r.B, NT);
     if (*blocks > MAX_SUM_BLOCKS) *blocks = MAX_SUM_BLOCKS;
     if (*blocks > 1) a.stats = nullptr;
@@ -732,8 +896,16 @@ hipError_t logit_grad(const GradArgs &a, hipStream_t stream, const LaunchEvents 
     return a.d.tensor == TENSOR_BF16 ? grad_of_type<float, __bf16>(a, stream, ev) : grad_of_type<float, float>(a, stream, ev);
 }
 
-hipError_t add_sums(const SumFour &f, hipStream_t stream)
+// more: room for SUM_SLICES
+hipError_t add_sums(SumFour f, Four *more, hipStream_t stream)
 {
+    if (f.n > 16 * SUM_SLICES) {
+        const hipError_t e =
+            launch_kernel(sum_slices_kernel, dim3(SUM_SLICES), dim3(NT), stream, LaunchEvents(), f.partial, f.n, more);
+        if (e != hipSuccess) return e;
+        f.partial = more;
+        f.n = SUM_SLICES;
+    }
     return launch_kernel(sum_four_kernel, dim3(1), dim3(NT), stream, LaunchEvents(), f);
 }
 
@@ -741,6 +913,8 @@ hipError_t add_sums(const SumFour &f, hipStream_t stream)
 
 size_t choice_workspace(long long B, int pairs)
 {
+    static_assert(sizeof(RowCoef) + sizeof(double) + sizeof(TopSum) == sizeof(Four) && MAX_SUM_BLOCKS >= SUM_SLICES,
+                  "a sum for each row, and SUM_SLICES more");
     return sizeof(Four) * (size_t)(pairs > MAX_SUM_BLOCKS ? pairs : MAX_SUM_BLOCKS) + (sizeof(RowCoef) + sizeof(double)) * (size_t)B +
            sizeof(TopSum) * (size_t)(B > MAX_CHUNKED ? B : MAX_CHUNKED);
 }
@@ -754,7 +928,7 @@ hipError_t launch_logprob(const ChoiceRows &r, float *logp, float *lse, void *ws
     a.h.logp = logp;
     a.h.lse = lse;
     int blocks = 0;
-    if (rows_in_registers(r)) return rows(a, &blocks, stream, ev);
+    if (rows_in_registers(r, false)) return rows(a, &blocks, stream, ev);
     return chunked_rows(a, split_for(r), Workspace(ws, r.B, 0).partial, &blocks, stream, ev);
 }
 
@@ -776,23 +950,24 @@ hipError_t launch_policy(const ChoiceRows &r, const PolicyTerms &t, const Choice
 {
     const Workspace w(ws, r.B, 0);
     SumFour fin = {w.sums, 0, t.stats};
-    if (r.B == 0) return add_sums(fin, stream);
+    Four *const more = w.sums + r.B;  // (rows_kernel leaves a sum a row at most, in all of the workspace)
+    if (r.B == 0) return add_sums(fin, more, stream);
     RowsArgs a = {};
     a.r = r;
     a.h.kind = HEAD_POLICY;
     a.h.p = t;
     a.sums = w.sums;
     a.stats = t.stats;
-    if (rows_in_registers(r)) {
+    if (rows_in_registers(r, d.dZ != nullptr)) {
         a.d = d;
         const hipError_t e = rows(a, &fin.n, stream, ev);
-        return e != hipSuccess || fin.n == 1 ? e : add_sums(fin, stream);
+        return e != hipSuccess || fin.n == 1 ? e : add_sums(fin, more, stream);
     }
     a.h.coef = d.dZ ? w.coef : nullptr;
     const hipError_t e = chunked_rows(a, split_for(r), w.partial, &fin.n, stream, ev);
     if (e != hipSuccess) return e;
     if (fin.n == 1) fin.n = 0;
-    if (!d.dZ) return fin.n ? add_sums(fin, stream) : hipSuccess;
+    if (!d.dZ) return fin.n ? add_sums(fin, nullptr, stream) : hipSuccess;
     GradArgs g = {};
     g.r = r;
     g.d = d;
@@ -812,12 +987,13 @@ hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, cons
     a.h.coef = d.dZ ? w.coef : nullptr;
     int blocks = 0;
     hipError_t e = hipSuccess;
-    if (r.B > 0) e = rows_in_registers(r) ? rows(a, &blocks, stream, ev) : chunked_rows(a, split_for(r), w.partial, &blocks, stream, ev);
+    if (r.B > 0) e = rows_in_registers(r, false) ? rows(a, &blocks, stream, ev) : chunked_rows(a, split_for(r), w.partial, &blocks, stream, ev);
     if (e == hipSuccess)
         e = launch_kernel(preference_kernel, dim3((unsigned)t.pairs), dim3(NT), stream, LaunchEvents(), t, r.B,
                           (const double *)w.row_lp, d.dZ ? w.coef : nullptr, w.sums);
     const SumFour fin = {w.sums, t.pairs, t.stats};
-    if (e != hipSuccess || !d.dZ || r.B == 0) return e != hipSuccess ? e : add_sums(fin, stream);
+    if (e != hipSuccess) return e;
+    if (!d.dZ || r.B == 0) return launch_kernel(sum_four_kernel, dim3(1), dim3(NT), stream, LaunchEvents(), fin);
     GradArgs g = {};
     g.r = r;
     g.d = d;
