@@ -48,6 +48,7 @@ struct ChoiceGrad {
     long long ld;
     int tensor;
     int pad;
+    bool past;             // set by the launchers: stored past the caches
 };
 struct PolicyTerms {
     const float *old_logp, *ref_logp, *adv;  // B entries; ref_logp may be null
