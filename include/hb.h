@@ -203,6 +203,42 @@ int hb_batch_loss_csr_async(hb_model *m, const int32_t *d_row_ptr, const int32_t
                             float *d_loss);
 
 /*
+ * Dropout of the hidden activations, in every later call of this handle that makes a gradient (steps and gradients of any loss,
+ * dense or CSR, also those of the worker loops); losses, evaluations and log-probabilities take the network as it is.  Each
+ * such call n (next_call, next_call + 1, ...; below 2^59) multiplies the activations of hidden layer l, as layer l + 1 and its weight
+ * gradient read them, and the gradient on its way back through them with the mask that hb_dropout_async has for (seed, offset
+ * 32 n + l) and a B x d_l matrix, so a call can be made again, here or elsewhere.  p as there; 0 switches it off.
+ * bf16 mode: what a layer keeps is rounded once more.  A replay of a captured step repeats the masks of the captured call.
+ * The first call with p > 0 allocates one more buffer for each hidden layer.  hb_model_get_activations gives the activations before
+ * dropout.  The network then runs layer by layer (not in the kernels of whole small networks or fused output layers).
+ */
+int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call);
+
+/*
+ * Learning from rewards and comparisons instead of labels: the network is a policy over d_L classes, X the states of B rows
+ * and y the class chosen in each (outside [0, d_L): no choice, padding).  The losses, their arguments (DEVICE pointers)
+ * and what they return are those of hb_logprob_async, hb_policy_loss_async and hb_preference_loss_async below, on the last
+ * layer's logits; rows outside of all sequences have no gradient.  Dense models with HB_LOSS_SOFTMAX_CE; pairs <= max_B.
+ *   hb_batch_logprob_async    forward pass; the log-probabilities of the chosen classes (d_lse may be NULL)
+ *   hb_policy_step_async      one step W <- W - lr dloss/dW of the policy loss
+ *   hb_policy_grad_async      its gradient instead (d_grad_flat: P floats, flat layout); the replica is left untouched
+ *   hb_preference_step_async, hb_preference_grad_async   the same of the preference loss
+ * Nothing is synchronised; the calls enqueue kernels only and may be captured once one ordinary call of them has been made (the
+ * first allocates the handle's workspace for them).
+ */
+struct hb_policy;
+struct hb_preference;
+int hb_batch_logprob_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, float *d_logp, float *d_lse);
+int hb_policy_step_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, float lr, const struct hb_policy *policy,
+                         float *d_stats, float *d_logp);
+int hb_policy_grad_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, const struct hb_policy *policy,
+                         float *d_grad_flat, float *d_stats, float *d_logp);
+int hb_preference_step_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, float lr,
+                             const struct hb_preference *preference, float *d_stats, float *d_seq_logp);
+int hb_preference_grad_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, const struct hb_preference *preference,
+                             float *d_grad_flat, float *d_stats, float *d_seq_logp);
+
+/*
  * Replica <-> global model exchange (Section 6.2: the replica is a deep copy of the
  * global model, pushed back to it after the update; a stale replica's contribution can be
  * damped).  With H = host_model (HOST pointer, P floats, flat layout; pinned memory makes
@@ -234,7 +270,7 @@ enum {
     HB_K_UPDATE = 4,     /* W <- W - lr * sum of partials, all tensors      (Eq. (3)) */
     HB_K_SPMM_FWD = 5,   /* CSR first layer, forward */
     HB_K_SPARSE_DW = 6,  /* CSR first layer, gradient + update of the touched columns */
-    HB_K_OTHER = 7,      /* helpers, numbered in `layer`; 6: a network that fits a workgroup, whole (M = rows) */
+    HB_K_OTHER = 7,      /* helpers, numbered in `layer`; 6: a network that fits a workgroup, whole (M = rows); 7: dropout */
     HB_K_OUT_LAYER = 8,  /* narrow output layer: forward + loss + delta + its gradients, fused */
     HB_K_BWD_PAIR = 9    /* two backward products in one launch, flops / bytes cover both.  fp32: backward-data and
                             weight gradient of `layer`, M, N, K those of the backward-data product.  bf16: the

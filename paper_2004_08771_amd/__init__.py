@@ -10,5 +10,5 @@ from .binding import (  # noqa: F401
     HB_ERR_INVALID, HB_ERR_STATE, HB_ERR_UNSUPPORTED, HB_F32, HB_LOSS_LOGISTIC,
     HB_LOSS_SOFTMAX_CE, HB_OK, HB_TENSOR_BF16, HB_TENSOR_F32, HbError, Model, Sched, batch_loss_static,
     choice_workspace_bytes, cpu_worker_run_epoch, dropout, hogbatch_run_epoch, lib, lib_path, logprob, logprob_grad,
-    policy_loss, preference_loss,
+    policy_args, policy_loss, preference_args, preference_loss,
 )

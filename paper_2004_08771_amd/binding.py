@@ -94,13 +94,20 @@ class Preference(ctypes.Structure):
 
 
 _u64, _sz = ctypes.c_uint64, ctypes.c_size_t
+_polp, _prfp = ctypes.POINTER(Policy), ctypes.POINTER(Preference)
+SIGNATURES["hb_model_set_dropout"] = (_int, [_vp, _f32, _u64, _u64])
+SIGNATURES["hb_batch_logprob_async"] = (_int, [_vp, _vp, _vp, _i64, _vp, _vp])
+SIGNATURES["hb_policy_step_async"] = (_int, [_vp, _vp, _vp, _i64, _f32, _polp, _vp, _vp])
+SIGNATURES["hb_policy_grad_async"] = (_int, [_vp, _vp, _vp, _i64, _polp, _vp, _vp, _vp])
+SIGNATURES["hb_preference_step_async"] = (_int, [_vp, _vp, _vp, _i64, _f32, _prfp, _vp, _vp])
+SIGNATURES["hb_preference_grad_async"] = (_int, [_vp, _vp, _vp, _i64, _prfp, _vp, _vp, _vp])
 SIGNATURES["hb_dropout_async"] = (_int, [_vp, _i64, _vp, _i64, _int, _i64, _i64, _f32, _u64, _u64, _vp])
 SIGNATURES["hb_choice_workspace_bytes"] = (_sz, [_i64, _i32])
 SIGNATURES["hb_logprob_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _vp, _vp, _vp, _sz, _vp])
 SIGNATURES["hb_logprob_grad_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _i64, _vp])
-SIGNATURES["hb_policy_loss_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, ctypes.POINTER(Policy), _vp, _vp, _vp, _i64,
+SIGNATURES["hb_policy_loss_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _polp, _vp, _vp, _vp, _i64,
                                              _vp, _sz, _vp])
-SIGNATURES["hb_preference_loss_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, ctypes.POINTER(Preference), _vp, _vp, _vp,
+SIGNATURES["hb_preference_loss_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _prfp, _vp, _vp, _vp,
                                                  _i64, _vp, _sz, _vp])
 
 _lib = None
@@ -233,6 +240,30 @@ class Model:
     def batch_loss_csr_async(self, d_row_ptr, d_col_idx, d_vals, nnz, dy, B, d_loss=None):
         _check(lib().hb_batch_loss_csr_async(self._h, _ptr(d_row_ptr), _ptr(d_col_idx), _ptr(d_vals), int(nnz),
                                              _ptr(dy), int(B), _ptr(d_loss)))
+
+    def set_dropout(self, p, seed=0, next_call=0):
+        _check(lib().hb_model_set_dropout(self._h, float(p), int(seed), int(next_call)))
+
+    def batch_logprob_async(self, dX, dy, B, d_logp, d_lse=None):
+        _check(lib().hb_batch_logprob_async(self._h, _ptr(dX), _ptr(dy), int(B), _ptr(d_logp), _ptr(d_lse)))
+
+    def policy_step_async(self, dX, dy, B, lr, policy, d_stats, d_logp=None):
+        """policy: policy_args()."""
+        _check(lib().hb_policy_step_async(self._h, _ptr(dX), _ptr(dy), int(B), float(lr), ctypes.byref(policy), _ptr(d_stats),
+                                          _ptr(d_logp)))
+
+    def policy_grad_async(self, dX, dy, B, policy, d_grad_flat, d_stats, d_logp=None):
+        _check(lib().hb_policy_grad_async(self._h, _ptr(dX), _ptr(dy), int(B), ctypes.byref(policy), _ptr(d_grad_flat),
+                                          _ptr(d_stats), _ptr(d_logp)))
+
+    def preference_step_async(self, dX, dy, B, lr, preference, d_stats, d_seq_logp=None):
+        """preference: preference_args()."""
+        _check(lib().hb_preference_step_async(self._h, _ptr(dX), _ptr(dy), int(B), float(lr), ctypes.byref(preference),
+                                              _ptr(d_stats), _ptr(d_seq_logp)))
+
+    def preference_grad_async(self, dX, dy, B, preference, d_grad_flat, d_stats, d_seq_logp=None):
+        _check(lib().hb_preference_grad_async(self._h, _ptr(dX), _ptr(dy), int(B), ctypes.byref(preference), _ptr(d_grad_flat),
+                                              _ptr(d_stats), _ptr(d_seq_logp)))
 
     def model_merge(self, host_model, weight):
         _check(lib().hb_model_merge(self._h, _ptr(host_model), float(weight)))
@@ -433,7 +464,8 @@ def logprob_grad(Z, y, logp, lse, g, dZ, stream=None):
                                        _vector(lse, "lse", B), _vector(g, "g", B), pd, ldd, stream if stream else None))
 
 
-def _policy(B, old, adv, ref, weight, clip, kl_coef):
+def policy_args(B, old, adv, ref=None, weight=None, clip=(0.2, 0.2), kl_coef=0.0) -> Policy:
+    """hb_policy of vectors of B floats on the device, which have to live as long as what is enqueued with it."""
     return Policy(_vector(old, "old", B), _vector(ref, "ref", B), _vector(adv, "adv", B), _vector(weight, "weight", B),
                   clip[0], clip[1], kl_coef)
 
@@ -445,17 +477,18 @@ def policy_loss(Z, y, old, adv, stats, dZ=None, ref=None, weight=None, clip=(0.2
     pd, ldd, _ = (None, ldz, 0) if dZ is None else _matrix(dZ, "dZ", Z)
     B, K = Z.shape
     pw, nw = _workspace(ws)
-    args = _policy(B, old, adv, ref, weight, clip, kl_coef)
+    args = policy_args(B, old, adv, ref, weight, clip, kl_coef)
     _check(lib().hb_policy_loss_async(pz, ldz, kind, _vector(y, "y", B, "torch.int32"), B, K, ctypes.byref(args),
                                       _vector(stats, "stats", 4), _vector(logp, "logp", B), pd, ldd, pw, nw,
                                       stream if stream else None))
 
 
-def _preference(seq, ref, beta, smoothing):
+def preference_args(seq, ref=None, beta=0.1, smoothing=0.0) -> Preference:
+    """hb_preference of 2 pairs + 1 offsets (int32) and 2 pairs floats on the device, which have to live as long."""
     n = seq.numel() - 1
     if n < 2 or n % 2:
         _invalid(f"seq has {n + 1} offsets: 2 pairs + 1 are needed")
-    return Preference(_vector(seq, "seq", n + 1, "torch.int32"), _vector(ref, "ref", n), n // 2, beta, smoothing), n
+    return Preference(_vector(seq, "seq", n + 1, "torch.int32"), _vector(ref, "ref", n), n // 2, beta, smoothing)
 
 
 def preference_loss(Z, y, seq, stats, dZ=None, ref=None, beta=0.1, smoothing=0.0, seq_logp=None, ws=None, stream=None):
@@ -464,7 +497,7 @@ def preference_loss(Z, y, seq, stats, dZ=None, ref=None, beta=0.1, smoothing=0.0
     pd, ldd, _ = (None, ldz, 0) if dZ is None else _matrix(dZ, "dZ", Z)
     B, K = Z.shape
     pw, nw = _workspace(ws)
-    args, n = _preference(seq, ref, beta, smoothing)
+    args = preference_args(seq, ref, beta, smoothing)
     _check(lib().hb_preference_loss_async(pz, ldz, kind, _vector(y, "y", B, "torch.int32"), B, K, ctypes.byref(args),
-                                          _vector(stats, "stats", 4), _vector(seq_logp, "seq_logp", n), pd, ldd, pw, nw,
+                                          _vector(stats, "stats", 4), _vector(seq_logp, "seq_logp", 2 * args.pairs), pd, ldd, pw, nw,
                                           stream if stream else None))

@@ -3,6 +3,7 @@
 // (Algorithm 1 / Algorithm 2 of the paper, worker side: "Gradient", then "Update model").
 #include "../../include/hb.h"
 #include "hb_internal.h"
+#include "operators.h"
 
 #include <cmath>
 #include <cstdarg>
@@ -162,6 +163,13 @@ struct hb_model {
     int b1_splits = 1;
     SmallNetLayer *d_net = nullptr;      // small networks (small_net_rows for some batch): what their kernel reads ...
     int *d_net_place = nullptr;          // ... and the place of every parameter in its LDS
+    // dropout of the hidden activations in calls that make a gradient (threshold 0: none): layer l of call n has the mask of
+    // offset 32 n + l; acts / act_bf keep the activations themselves, which their derivative is taken from
+    unsigned drop_threshold = 0;
+    uint64_t drop_seed = 0, drop_call = 0;
+    std::vector<void *> drop;            // [1..L-1] max_B x ld (fp32) or ld8 (bf16), allocated by the first hb_model_set_dropout
+    std::vector<int> gemm_splits;        // [1..L] fp32: slices that the general weight gradient may use
+    void *head_ws = nullptr;             // workspace of the policy and preference losses, allocated by the first call
     std::vector<void *> owned;           // every device allocation, for destroy
 
     // per-kernel profile (measurement only)
@@ -216,6 +224,8 @@ void release_device(hb_model *m)
     m->owned.clear();
     m->d_net = nullptr;
     m->d_net_place = nullptr;
+    m->drop.clear();
+    m->head_ws = nullptr;
     if (m->h_loss) (void)hipHostFree(m->h_loss);
     m->h_loss = nullptr;
 }
@@ -265,6 +275,48 @@ struct Input {
     const float *vals = nullptr;
     int64_t nnz = 0;
 };
+
+// A call whose loss is not the handle's own: one of the three
+struct Head {
+    const PolicyTerms *policy = nullptr;
+    const PreferenceTerms *preference = nullptr;
+    float *logp = nullptr, *lse = nullptr;  // log-probabilities only
+    const float *weight = nullptr;          // of the policy's rows
+};
+
+// The last layer's logits to a loss of `head`, and its delta
+int run_head(hb_model *m, const Head &head, const int32_t *y, int64_t B, void *delta, long long ldd, int delta_tensor, int pad)
+{
+    ChoiceRows r = {};
+    r.Z = m->acts[m->L];
+    r.ldz = m->ld[m->L];
+    r.tensor = TENSOR_F32;
+    r.y = y;
+    r.weight = head.weight;
+    r.B = B;
+    r.K = m->dims[m->L];
+    ChoiceGrad d = {};
+    d.dZ = delta;
+    d.ld = ldd;
+    d.tensor = delta_tensor;
+    d.pad = pad;
+    d.all_rows = true;
+    const LaunchEvents ev = prof_begin(m, HB_K_LOSS, 0, 0, 0, 0, 0.0, 4.0 * B * (r.K * (delta ? 2.0 : 1.0) + 1.0));
+    if (head.policy) HB_HIP(launch_policy(r, *head.policy, d, m->head_ws, m->stream, ev));
+    else if (head.preference) HB_HIP(launch_preference(r, *head.preference, d, m->head_ws, m->stream, ev));
+    else HB_HIP(launch_logprob(r, head.logp, head.lse, m->head_ws, m->stream, ev));
+    return HB_OK;
+}
+
+// Dropout of layer l's rows in the current call (in place for a delta)
+int run_dropout(hb_model *m, int l, const void *x, void *out, int ld, int64_t B)
+{
+    const int size = m->dtype == HB_BF16_F32MASTER ? 2 : 4;
+    HB_HIP(launch_dropout(m->dtype == HB_BF16_F32MASTER ? TENSOR_BF16 : TENSOR_F32, x, ld, out, ld, B, ld, m->drop_threshold,
+                          m->drop_seed, 32 * m->drop_call + (uint64_t)l, m->stream,
+                          prof_begin(m, HB_K_OTHER, 7, 0, 0, 0, 0.0, 2.0 * size * (double)B * m->dims[l])));
+    return HB_OK;
+}
 
 // W1t <-> the W_1 region of the flat buffer (sparse mode only)
 int sync_w1t_from_flat(hb_model *m)
@@ -379,20 +431,24 @@ int run_small_net(hb_model *m, const float *X, const int32_t *y, int64_t B, int 
 
 // Issues the kernels of one step.
 int run_step(hb_model *m, const Input &in, const int32_t *y, int64_t B, float lr, StepMode mode,
-             float *d_grad_flat, float *d_loss_user)
+             float *d_grad_flat, float *d_loss_user, const Head *head = nullptr)
 {
     const int L = m->L;
     const int Bi = (int)B;
     hipStream_t st = m->stream;
     const float *X = in.X;
-    if (m->d_net) {
+    const bool drop = m->drop_threshold > 0 && mode != MODE_LOSS;
+    const bool own_loss = head == nullptr && !drop;  // the kernels that have the loss or all layers in them
+    if (m->d_net && own_loss) {
         const int rows = small_net_rows(m->dims.data(), L, B);
         if (rows > 0) return run_small_net(m, X, y, B, rows, lr, mode, d_grad_flat, d_loss_user);
     }
 
     // narrow output layers (d_L <= 16) are handled by one fused kernel: forward, loss, D_L,
     // D_{L-1} and the dW_L / db_L partials from a single read of A_{L-1}
-    const bool fused_out = m->out_rows > 0 && aligned16(m->d_params + m->w_off[L]);
+    const bool fused_out = own_loss && m->out_rows > 0 && aligned16(m->d_params + m->w_off[L]);
+    // the input of layer l + 1: the activations of layer l, or what dropout leaves of them
+    auto input_of_next = [&](int l) { return drop ? static_cast<const float *>(m->drop[l]) : m->acts[l]; };
     const int L_gemm = fused_out ? L - 1 : L;
 
     // ---- sparse first layer: the batch's CSC arrays (needed by the weight gradient only) are
@@ -449,10 +505,14 @@ int run_step(hb_model *m, const Input &in, const int32_t *y, int64_t B, float lr
                                               8.0 * in.nnz + 4.0 * (B + 1.0) + 4.0 * touched_rows * m->dims[1] +
                                                   4.0 * B * (m->dims[1] + 1.0),
                                               gather)));
+            if (drop && L > 1) {
+                const int rc_d = run_dropout(m, 1, m->acts[1], m->drop[1], m->ld[1], B);
+                if (rc_d != HB_OK) return rc_d;
+            }
             continue;
         }
         GemmArgs g = {};
-        g.A = (l == 1) ? X : m->acts[l - 1];
+        g.A = (l == 1) ? X : input_of_next(l - 1);
         g.lda = (l == 1) ? m->dims[0] : m->ld[l - 1];
         g.B = m->d_params + m->w_off[l];
         g.ldb = m->dims[l - 1];
@@ -466,6 +526,10 @@ int run_step(hb_model *m, const Input &in, const int32_t *y, int64_t B, float lr
         HB_HIP(launch_gemm_f32(GEMM_FWD, g, 1, nullptr, st,
                                prof_begin(m, HB_K_FWD_GEMM, l, g.M, g.N, g.K, 2.0 * g.M * g.N * g.K,
                                           gemm_bytes(g.M, g.N, g.K, g.N))));
+        if (drop && l < L) {
+            const int rc_d = run_dropout(m, l, m->acts[l], m->drop[l], m->ld[l], B);
+            if (rc_d != HB_OK) return rc_d;
+        }
     }
 
     // the kernel that computes the loss leaves one partial sum per block; the update kernel
@@ -518,7 +582,10 @@ int run_step(hb_model *m, const Input &in, const int32_t *y, int64_t B, float lr
     la.ldd = m->ld[L];
     la.delta_bf16 = 0;
     la.block_partials = m->d_loss_partials;
-    if (!fused_out) {
+    if (head) {
+        const int rc_h = run_head(m, *head, y, B, la.delta, la.ldd, TENSOR_F32, 0);
+        if (rc_h != HB_OK || mode == MODE_LOSS) return rc_h;
+    } else if (!fused_out) {
         HB_HIP(launch_loss(la, st, prof_begin(m, HB_K_LOSS, 0, 0, 0, 0, 0.0,
                                               4.0 * B * (la.K * (la.delta ? 2.0 : 1.0) + 1.0))));
         fin.n = loss_grid_blocks(B, la.K);
@@ -572,7 +639,7 @@ int run_step(hb_model *m, const Input &in, const int32_t *y, int64_t B, float lr
         GemmArgs gdw = {};  // dW_l = D_l^T A_{l-1} (split-K partials), db_l = column sums of D_l
         gdw.A = delta_l;
         gdw.lda = m->ld[l];
-        gdw.B = (l == 1) ? X : m->acts[l - 1];
+        gdw.B = (l == 1) ? X : input_of_next(l - 1);
         gdw.ldb = (l == 1) ? m->dims[0] : m->ld[l - 1];
         gdw.C = m->partial_w[l];
         gdw.ldc = m->dims[l - 1];
@@ -587,7 +654,7 @@ int run_step(hb_model *m, const Input &in, const int32_t *y, int64_t B, float lr
         bool dw_done = false;
         if (l > 1 && dense_dw && gemm_f32_pair_ok(Bi, m->dims[l], m->dims[l - 1])) {
             HB_HIP(launch_gemm_f32_bwd_pair(
-                gda, gdw, m->cap_splits[l], &splits, st,
+                gda, gdw, m->gemm_splits[l], &splits, st,
                 prof_begin(m, HB_K_BWD_PAIR, l, gda.M, gda.N, gda.K,
                            2.0 * gda.M * gda.N * gda.K + 2.0 * gdw.M * gdw.N * gdw.K,
                            gemm_bytes(gda.M, gda.N, gda.K, (int64_t)gda.M * gda.N) +
@@ -598,6 +665,10 @@ int run_step(hb_model *m, const Input &in, const int32_t *y, int64_t B, float lr
                                    prof_begin(m, HB_K_DA_GEMM, l, gda.M, gda.N, gda.K,
                                               2.0 * gda.M * gda.N * gda.K,
                                               gemm_bytes(gda.M, gda.N, gda.K, (int64_t)gda.M * gda.N))));
+        }
+        if (drop && l > 1) {  // D_{l-1}, before the next layer reads it (what is left of layer l does not)
+            const int rc_d = run_dropout(m, l - 1, m->delta[l - 1], m->delta[l - 1], m->ld[l - 1], B);
+            if (rc_d != HB_OK) return rc_d;
         }
         if (l == 1 && m->sparse) {
             // db_1: column sums of delta_1; dW_1: column-segmented sums over the non-zeros,
@@ -659,7 +730,7 @@ int run_step(hb_model *m, const Input &in, const int32_t *y, int64_t B, float lr
             continue;
         }
         if (!dw_done)
-            HB_HIP(launch_gemm_f32(GEMM_DW, gdw, m->cap_splits[l], &splits, sw_stream,
+            HB_HIP(launch_gemm_f32(GEMM_DW, gdw, m->gemm_splits[l], &splits, sw_stream,
                                    prof_begin(m, HB_K_DW_GEMM, l, gdw.M, gdw.N, gdw.K,
                                               2.0 * gdw.M * gdw.N * gdw.K,
                                               gemm_bytes(gdw.M, gdw.N, gdw.K, gdw.M))));
@@ -684,6 +755,7 @@ int run_step(hb_model *m, const Input &in, const int32_t *y, int64_t B, float lr
     double upd_bytes = 0.0;  // read W, read one gradient, write W
     for (int i = 0; i < ua.n_seg; ++i) upd_bytes += 12.0 * (double)ua.seg[i].count;
     HB_HIP(launch_update(ua, st, prof_begin(m, HB_K_UPDATE, 0, 0, 0, 0, 2.0 * (double)m->P, upd_bytes)));
+    if (drop) ++m->drop_call;
     return HB_OK;
 }
 
@@ -698,13 +770,16 @@ int refresh_shadows(hb_model *m)
 
 // The step in bf16 mode.  X is dense B x d_0 bf16.
 int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float lr, StepMode mode,
-                  float *d_grad_flat, float *d_loss_user)
+                  float *d_grad_flat, float *d_loss_user, const Head *head = nullptr)
 {
     const int L = m->L;
     const int Bi = (int)B;
     const long long ldB = round_up(Bi, 8);
     hipStream_t st = m->stream;
     const bool back = (mode != MODE_LOSS);
+    const bool drop = m->drop_threshold > 0 && back;
+    // the input of layer l + 1: the activations of layer l, or what dropout leaves of them
+    auto input_of_next = [&](int l) -> const void * { return drop ? m->drop[l] : m->act_bf[l]; };
 
     // bmaj[l] (BF16_DW_*): the weight gradient of layer l reads the row-major D_l and A_{l-1}
     // themselves (batch-major operands); then neither D_l^T nor A_{l-1}^T is needed for it.  Transposed
@@ -715,7 +790,7 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
         for (int l = 1; l <= L; ++l)
             bmaj[l] = (char)gemm_bf16_dw_form(m->dims[l], m->dims[l - 1], Bi, m->ld8[l],
                                               (l == 1) ? (long long)m->dims[0] : (long long)m->ld8[l - 1],
-                                              m->delta_bf[l & 1], (l == 1) ? X : m->act_bf[l - 1]);
+                                              m->delta_bf[l & 1], (l == 1) ? X : input_of_next(l - 1));
     // D_l: while its weight gradient reads it, the backward-data product beside that reads D_{l-1} and writes D_{l-2}.  The third
     // buffer is that of the transposed copies of even layers, where none of those needs one.
     bool three = true;
@@ -727,7 +802,7 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
                                      prof_begin(m, HB_K_OTHER, 1, 0, 0, 0, 0.0, 4.0 * B * m->dims[0])));
     for (int l = 1; l <= L; ++l) {
         GemmBf16Args g = {};
-        g.A = (l == 1) ? X : m->act_bf[l - 1];
+        g.A = (l == 1) ? X : input_of_next(l - 1);
         g.lda = (l == 1) ? m->dims[0] : m->ld8[l - 1];
         g.B = m->shadow[l];
         g.ldb = m->ld8[l - 1];
@@ -742,7 +817,7 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
             g.C_bf16 = m->act_bf[l];
             g.ldcb = m->ld8[l];
             if (back) {
-                if (!bmaj[l + 1] || m->act == ACT_SIGMOID) {
+                if (!drop && (!bmaj[l + 1] || m->act == ACT_SIGMOID)) {
                     g.Ct_bf16 = m->act_t[l];
                     g.ldct = ldB;
                 }
@@ -759,6 +834,13 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
         HB_HIP(launch_gemm_bf16(GEMM_FWD, g, st,
                                 prof_begin(m, HB_K_FWD_GEMM, l, g.M, g.N, g.K, 2.0 * g.M * g.N * g.K,
                                            2.0 * ((double)g.M * g.K + (double)g.N * g.K + 2.0 * g.M * g.N))));
+        if (drop && l < L) {
+            const int rc_d = run_dropout(m, l, m->act_bf[l], m->drop[l], m->ld8[l], B);
+            if (rc_d != HB_OK) return rc_d;
+            if (!bmaj[l + 1])
+                HB_HIP(launch_transpose_bf16(m->drop[l], m->ld8[l], m->act_t[l], ldB, Bi, m->dims[l], st,
+                                             prof_begin(m, HB_K_OTHER, 1, 0, 0, 0, 0.0, 4.0 * B * m->dims[l])));
+        }
     }
 
     LossArgs la = {};
@@ -773,10 +855,16 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
     la.delta_bf16 = 1;
     la.zero_pad = 1;
     la.block_partials = m->d_loss_partials;
-    HB_HIP(launch_loss(la, st, prof_begin(m, HB_K_LOSS, 0, 0, 0, 0, 0.0, B * (4.0 * la.K + 2.0 * la.K + 4.0))));
-    LossFinalize fin = {m->d_loss_partials, loss_grid_blocks(B, la.K), B, m->d_loss, d_loss_user};
+    LossFinalize fin = {};
+    if (head) {
+        const int rc_h = run_head(m, *head, y, B, la.delta, la.ldd, TENSOR_BF16, la.ldd);
+        if (rc_h != HB_OK) return rc_h;
+    } else {
+        HB_HIP(launch_loss(la, st, prof_begin(m, HB_K_LOSS, 0, 0, 0, 0, 0.0, B * (4.0 * la.K + 2.0 * la.K + 4.0))));
+        fin = {m->d_loss_partials, loss_grid_blocks(B, la.K), B, m->d_loss, d_loss_user};
+    }
     // the mean: with the weight gradient of the output layer where its kernel can
-    if (!back || bmaj[L] != BF16_DW_BMAJ_MID) HB_HIP(launch_loss_finalize(fin, st));
+    if (!head && (!back || bmaj[L] != BF16_DW_BMAJ_MID)) HB_HIP(launch_loss_finalize(fin, st));
     if (!back) return HB_OK;
     if (!bmaj[L])
         HB_HIP(launch_transpose_bf16(delta(L), m->ld8[L], m->delta_t[L & 1], ldB, Bi, m->dims[L], st,
@@ -797,7 +885,7 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
         g.b_vec = 1;
         g.aux = m->act_bf[l - 1];
         g.ldaux = m->ld8[l - 1];
-        g.aux_t = m->act_t[l - 1];  // written by the forward pass of layer l-1
+        if (!drop) g.aux_t = m->act_t[l - 1];  // written by the forward pass of layer l-1
         g.ldauxt = ldB;
         if (m->act == ACT_RELU) {
             g.mask_in = m->relu_mask[l - 1];
@@ -806,6 +894,7 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
         g.act = m->act;
         g.C_bf16 = delta(l - 1);
         g.ldcb = m->ld8[l - 1];
+        if (drop) return g;  // its copy and its column sums are those of what dropout leaves
         if (!bmaj[l - 1]) {
             g.Ct_bf16 = m->delta_t[(l - 1) & 1];
             g.ldct = ldB;
@@ -823,7 +912,7 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
                 g.bias_out = grad_mode ? d_grad_flat + m->b_off[l] : m->d_params + m->b_off[l];
             g.A = delta(l);
             g.lda = m->ld8[l];
-            g.B = (l == 1) ? X : m->act_bf[l - 1];
+            g.B = (l == 1) ? X : input_of_next(l - 1);
             g.ldb = (l == 1) ? m->dims[0] : m->ld8[l - 1];
         } else {
             g.A = m->delta_t[l & 1];
@@ -858,13 +947,20 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
     auto dw_bytes = [&](const GemmBf16Args &g) {
         return 2.0 * ((double)g.M * g.K + (double)g.N * g.K) + (grad_mode ? 4.0 : 12.0) * g.M * g.N;
     };
-    const bool pairs_on = gemm_bf16_pairs_on();
+    const bool pairs_on = gemm_bf16_pairs_on() && !drop;  // dropout comes between the two
     std::vector<char> done_da((size_t)L + 2, 0), done_dw((size_t)L + 2, 0);
     for (int l = L; l >= 1; --l) {
         if (l > 1 && !done_da[l])
             HB_HIP(launch_gemm_bf16(GEMM_DA, da_args(l), st,
                                     prof_begin(m, HB_K_DA_GEMM, l, Bi, m->dims[l - 1], m->dims[l], da_flops(l), da_bytes(l)),
                                     &colsum_slices[l - 1]));
+        if (drop && l > 1) {
+            const int rc_d = run_dropout(m, l - 1, delta(l - 1), delta(l - 1), m->ld8[l - 1], B);
+            if (rc_d != HB_OK) return rc_d;
+            if (!bmaj[l - 1])
+                HB_HIP(launch_transpose_bf16(delta(l - 1), m->ld8[l - 1], m->delta_t[(l - 1) & 1], ldB, Bi, m->dims[l - 1], st,
+                                             prof_begin(m, HB_K_OTHER, 2, 0, 0, 0, 0.0, 4.0 * B * m->dims[l - 1])));
+        }
         if (done_dw[l]) continue;
         const GemmBf16Args g = dw_args(l);
         if (l > 1 && pairs_on) {  // with what comes next, which does not need it: D_{l-2}, or dW_1
@@ -932,10 +1028,11 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
                                       prof_begin(m, HB_K_UPDATE, l, 0, 0, 0, (double)B * m->dims[l],
                                                  2.0 * B * m->dims[l])));
     }
+    if (drop) ++m->drop_call;
     return HB_OK;
 }
 
-int validate_batch_call(hb_model *m, const void *a, const int32_t *dy, int64_t B, bool want_sparse)
+int validate_batch_call(hb_model *m, const void *a, const int32_t *dy, int64_t B, bool want_sparse, bool all_labels = true)
 {
     int rc = check_handle(m, true);
     if (rc != HB_OK) return rc;
@@ -951,7 +1048,7 @@ int validate_batch_call(hb_model *m, const void *a, const int32_t *dy, int64_t B
     // HB_CHECK_LABELS=1 (debug aid, costs a pass over y and a synchronisation per call): labels
     // outside their domain are an error instead of a silently wrong loss
     static const bool check_labels = getenv("HB_CHECK_LABELS") && atoi(getenv("HB_CHECK_LABELS")) != 0;
-    if (check_labels) {
+    if (check_labels && all_labels) {
         unsigned int *d_bad = reinterpret_cast<unsigned int *>(m->d_loss + 3);
         unsigned int bad = 0;
         HB_HIP(launch_fill_u32(d_bad, 1, 0u, m->stream));
@@ -1284,6 +1381,7 @@ int hb_mlp_configure(hb_model *m, int dtype, int64_t max_B, int sparse_first_lay
     m->partial_w.assign(L + 1, nullptr);
     m->partial_b.assign(L + 1, nullptr);
     m->cap_splits.assign(L + 1, 1);
+    m->gemm_splits.assign(L + 1, 1);
     for (int l = 0; l <= L; ++l) {
         m->ld[l] = round_up(m->dims[l], 4);
     }
@@ -1305,7 +1403,7 @@ int hb_mlp_configure(hb_model *m, int dtype, int64_t max_B, int sparse_first_lay
                 rc = dev_alloc(m, &m->partial_b[l], (size_t)m->cap_splits[l] * m->dims[l]);
                 continue;
             }
-            m->cap_splits[l] = gemm_f32_dw_splits(m->dims[l], m->dims[l - 1], (int)max_B, MAX_SPLITS);
+            m->gemm_splits[l] = m->cap_splits[l] = gemm_f32_dw_splits(m->dims[l], m->dims[l - 1], (int)max_B, MAX_SPLITS);
             if (l == L && L >= 2) {
                 m->out_rows = out_layer_rows(m->dims[L - 1], m->dims[L]);
                 if (m->out_rows > 0) {  // one partial per row block of the fused kernel
@@ -1706,6 +1804,128 @@ float hb_batch_grad_csr(hb_model *m, const int32_t *d_row_ptr, const int32_t *d_
     float out;
     if (fetch_loss(m, &out) != HB_OK) return std::numeric_limits<float>::quiet_NaN();
     return out;
+}
+
+int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call)
+{
+    int rc = check_handle(m, true);
+    if (rc != HB_OK) return rc;
+    unsigned threshold = 0;
+    rc = check_dropout_p(p, &threshold);
+    if (rc != HB_OK) return rc;
+    if (next_call >> 59) return fail(HB_ERR_INVALID, "next_call = %llu is not below 2^59", (unsigned long long)next_call);
+    if (threshold > 0 && m->drop.empty()) {
+        std::vector<void *> buffers((size_t)m->L + 1, nullptr);
+        for (int l = 1; l < m->L; ++l) {
+            if (m->dtype == HB_F32) {
+                float *b = nullptr;
+                rc = dev_alloc(m, &b, (size_t)m->max_B * m->ld[l]);
+                buffers[l] = b;
+            } else {
+                unsigned short *b = nullptr;
+                rc = dev_alloc(m, &b, (size_t)m->max_B * m->ld8[l]);
+                buffers[l] = b;
+            }
+            if (rc != HB_OK) return rc;  // what has been allocated goes with the handle
+        }
+        m->drop = buffers;
+    }
+    m->drop_threshold = threshold;
+    m->drop_seed = seed;
+    m->drop_call = next_call;
+    return HB_OK;
+}
+
+// What the calls with a loss of their own check, before their first device call but for the workspace of the handle's first one
+static int validate_head_call(hb_model *m, const void *dX, const int32_t *dy, int64_t B)
+{
+    int rc = validate_batch_call(m, dX, dy, B, false, false);
+    if (rc != HB_OK) return rc;
+    if (m->loss != HB_LOSS_SOFTMAX_CE) return fail(HB_ERR_INVALID, "this call needs a model with HB_LOSS_SOFTMAX_CE");
+    return HB_OK;
+}
+
+static int run_head_call(hb_model *m, const void *dX, const int32_t *dy, int64_t B, float lr, StepMode mode, float *d_grad_flat,
+                         const Head &head)
+{
+    if (!std::isfinite(lr)) return fail(HB_ERR_INVALID, "lr is not finite");
+    if (mode == MODE_GRAD && !d_grad_flat) return fail(HB_ERR_INVALID, "d_grad_flat is NULL");
+    if (!m->head_ws) {
+        unsigned char *ws = nullptr;
+        const int pairs = (int)(m->max_B < (1 << 22) ? m->max_B : (1 << 22));
+        const int rc = dev_alloc(m, &ws, choice_workspace(m->max_B, pairs));
+        if (rc != HB_OK) return rc;
+        m->head_ws = ws;
+    }
+    if (m->dtype == HB_BF16_F32MASTER) return run_step_bf16(m, dX, dy, B, lr, mode, d_grad_flat, nullptr, &head);
+    Input in;
+    in.X = static_cast<const float *>(dX);
+    return run_step(m, in, dy, B, lr, mode, d_grad_flat, nullptr, &head);
+}
+
+int hb_batch_logprob_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, float *d_logp, float *d_lse)
+{
+    const int rc = validate_head_call(m, dX, dy, B);
+    if (rc != HB_OK) return rc;
+    if (!d_logp) return fail(HB_ERR_INVALID, "d_logp is NULL");
+    Head head;
+    head.logp = d_logp;
+    head.lse = d_lse;
+    return run_head_call(m, dX, dy, B, 0.f, MODE_LOSS, nullptr, head);
+}
+
+static int policy_call(hb_model *m, const void *dX, const int32_t *dy, int64_t B, const hb_policy *policy, float lr, StepMode mode,
+                       float *d_grad_flat, float *d_stats, float *d_logp)
+{
+    int rc = validate_head_call(m, dX, dy, B);
+    if (rc == HB_OK) rc = check_policy(policy);
+    if (rc != HB_OK) return rc;
+    if (!policy->d_old_logp || !policy->d_adv) return fail(HB_ERR_INVALID, "d_old_logp or d_adv is NULL");
+    if (!d_stats) return fail(HB_ERR_INVALID, "d_stats is NULL");
+    const PolicyTerms t = policy_terms(policy, B, d_stats, d_logp);
+    Head head;
+    head.policy = &t;
+    head.weight = policy->d_weight;
+    return run_head_call(m, dX, dy, B, lr, mode, d_grad_flat, head);
+}
+
+int hb_policy_step_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, float lr, const hb_policy *policy,
+                         float *d_stats, float *d_logp)
+{
+    return policy_call(m, dX, dy, B, policy, lr, MODE_STEP, nullptr, d_stats, d_logp);
+}
+
+int hb_policy_grad_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, const hb_policy *policy, float *d_grad_flat,
+                         float *d_stats, float *d_logp)
+{
+    return policy_call(m, dX, dy, B, policy, 0.f, MODE_GRAD, d_grad_flat, d_stats, d_logp);
+}
+
+static int preference_call(hb_model *m, const void *dX, const int32_t *dy, int64_t B, const hb_preference *preference, float lr,
+                           StepMode mode, float *d_grad_flat, float *d_stats, float *d_seq_logp)
+{
+    int rc = validate_head_call(m, dX, dy, B);
+    if (rc == HB_OK) rc = check_preference(preference);
+    if (rc != HB_OK) return rc;
+    if (preference->pairs > m->max_B)
+        return fail(HB_ERR_INVALID, "pairs = %d is more than max_B = %lld", preference->pairs, (long long)m->max_B);
+    if (!d_stats) return fail(HB_ERR_INVALID, "d_stats is NULL");
+    const PreferenceTerms t = preference_terms(preference, d_stats, d_seq_logp);
+    Head head;
+    head.preference = &t;
+    return run_head_call(m, dX, dy, B, lr, mode, d_grad_flat, head);
+}
+
+int hb_preference_step_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, float lr, const hb_preference *preference,
+                             float *d_stats, float *d_seq_logp)
+{
+    return preference_call(m, dX, dy, B, preference, lr, MODE_STEP, nullptr, d_stats, d_seq_logp);
+}
+
+int hb_preference_grad_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, const hb_preference *preference,
+                             float *d_grad_flat, float *d_stats, float *d_seq_logp)
+{
+    return preference_call(m, dX, dy, B, preference, 0.f, MODE_GRAD, d_grad_flat, d_stats, d_seq_logp);
 }
 
 int hb_model_merge(hb_model *m, float *host_model, float weight)

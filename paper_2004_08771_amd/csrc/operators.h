@@ -48,6 +48,7 @@ struct ChoiceGrad {
     long long ld;
     int tensor;
     int pad;
+    bool all_rows;         // rows outside of all sequences are written, too: zeros
     bool past;             // set by the launchers: stored past the caches
 };
 struct PolicyTerms {
