@@ -392,23 +392,31 @@ def cpu_worker_run_epoch(sched, worker, layer_dims, activation, loss, host_X, ho
 
 # ---- operators on device tensors: torch tensors in, nothing returned, everything enqueued on `stream`
 
-_TENSOR = {"torch.float32": HB_TENSOR_F32, "torch.bfloat16": HB_TENSOR_BF16}
+_types = {}  # torch's types as objects -> HB_TENSOR_* or "int32"; they are known once a tensor has come
 
 
 def _invalid(message):
     raise HbError(HB_ERR_INVALID, message)
 
 
+def _type(t):
+    kind = _types.get(t.dtype)
+    if kind is None:
+        kind = {"torch.float32": HB_TENSOR_F32, "torch.bfloat16": HB_TENSOR_BF16, "torch.int32": "int32"}.get(str(t.dtype), "other")
+        _types[t.dtype] = kind
+    return kind
+
+
 def _matrix(t, name, like=None):
     """(address, pitch, HB_TENSOR_*) of a torch matrix with elements of a row next to each other."""
-    kind = _TENSOR.get(str(t.dtype))
-    if kind is None:
+    kind = _type(t)
+    if kind != HB_TENSOR_F32 and kind != HB_TENSOR_BF16:
         _invalid(f"{name} has type {t.dtype}: float32 or bfloat16 is needed")
     if t.dim() != 2:
         _invalid(f"{name} has {t.dim()} dimensions: a matrix is needed")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
-        _invalid(f"{name} is {tuple(t.shape)} {t.dtype}: {tuple(like.shape)} {like.dtype} is needed")
-    rows, cols = t.shape
+    rows, cols = shape = t.shape
+    if like is not None and (shape != like.shape or t.dtype != like.dtype):
+        _invalid(f"{name} is {tuple(shape)} {t.dtype}: {tuple(like.shape)} {like.dtype} is needed")
     step, along = t.stride()
     if cols > 1 and along != 1:
         _invalid(f"{name}: the elements of a row must be next to each other")
@@ -417,12 +425,13 @@ def _matrix(t, name, like=None):
     return t.data_ptr(), (step if rows > 1 else max(cols, 1)), kind
 
 
-def _vector(t, name, n, dtype="torch.float32"):
+def _vector(t, name, n, kind=HB_TENSOR_F32):
     """Address of n elements one behind the other, or None."""
     if t is None:
         return None
-    if str(t.dtype) != dtype or t.numel() != n or not t.is_contiguous():
-        _invalid(f"{name} is {tuple(t.shape)} {t.dtype}: {n} elements of {dtype}, one behind the other, are needed")
+    if (_types.get(t.dtype) != kind and _type(t) != kind) or t.numel() != n or not t.is_contiguous():
+        _invalid(f"{name} is {tuple(t.shape)} {t.dtype}: {n} elements of {'int32' if kind == 'int32' else 'float32'}, one behind the "
+                 "other, are needed")
     return t.data_ptr()
 
 
@@ -451,7 +460,7 @@ def logprob(Z, y, logp, lse=None, ws=None, stream=None):
     pz, ldz, kind = _matrix(Z, "Z")
     B, K = Z.shape
     pw, nw = _workspace(ws)
-    _check(lib().hb_logprob_async(pz, ldz, kind, _vector(y, "y", B, "torch.int32"), B, K, _vector(logp, "logp", B),
+    _check(lib().hb_logprob_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, _vector(logp, "logp", B),
                                   _vector(lse, "lse", B), pw, nw, stream if stream else None))
 
 
@@ -460,7 +469,7 @@ def logprob_grad(Z, y, logp, lse, g, dZ, stream=None):
     pz, ldz, kind = _matrix(Z, "Z")
     pd, ldd, _ = _matrix(dZ, "dZ", Z)
     B, K = Z.shape
-    _check(lib().hb_logprob_grad_async(pz, ldz, kind, _vector(y, "y", B, "torch.int32"), B, K, _vector(logp, "logp", B),
+    _check(lib().hb_logprob_grad_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, _vector(logp, "logp", B),
                                        _vector(lse, "lse", B), _vector(g, "g", B), pd, ldd, stream if stream else None))
 
 
@@ -478,7 +487,7 @@ def policy_loss(Z, y, old, adv, stats, dZ=None, ref=None, weight=None, clip=(0.2
     B, K = Z.shape
     pw, nw = _workspace(ws)
     args = policy_args(B, old, adv, ref, weight, clip, kl_coef)
-    _check(lib().hb_policy_loss_async(pz, ldz, kind, _vector(y, "y", B, "torch.int32"), B, K, ctypes.byref(args),
+    _check(lib().hb_policy_loss_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, ctypes.byref(args),
                                       _vector(stats, "stats", 4), _vector(logp, "logp", B), pd, ldd, pw, nw,
                                       stream if stream else None))
 
@@ -488,7 +497,7 @@ def preference_args(seq, ref=None, beta=0.1, smoothing=0.0) -> Preference:
     n = seq.numel() - 1
     if n < 2 or n % 2:
         _invalid(f"seq has {n + 1} offsets: 2 pairs + 1 are needed")
-    return Preference(_vector(seq, "seq", n + 1, "torch.int32"), _vector(ref, "ref", n), n // 2, beta, smoothing)
+    return Preference(_vector(seq, "seq", n + 1, "int32"), _vector(ref, "ref", n), n // 2, beta, smoothing)
 
 
 def preference_loss(Z, y, seq, stats, dZ=None, ref=None, beta=0.1, smoothing=0.0, seq_logp=None, ws=None, stream=None):
@@ -498,6 +507,6 @@ def preference_loss(Z, y, seq, stats, dZ=None, ref=None, beta=0.1, smoothing=0.0
     B, K = Z.shape
     pw, nw = _workspace(ws)
     args = preference_args(seq, ref, beta, smoothing)
-    _check(lib().hb_preference_loss_async(pz, ldz, kind, _vector(y, "y", B, "torch.int32"), B, K, ctypes.byref(args),
+    _check(lib().hb_preference_loss_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, ctypes.byref(args),
                                           _vector(stats, "stats", 4), _vector(seq_logp, "seq_logp", 2 * args.pairs), pd, ldd, pw, nw,
                                           stream if stream else None))

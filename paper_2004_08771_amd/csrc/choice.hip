@@ -13,7 +13,8 @@ namespace {
 
 constexpr int NT = 256;
 constexpr int MAX_SUM_BLOCKS = 1024;  // blocks of merge_kernel, at most
-constexpr int SUM_SLICES = 256;       // more than 16 partial sums for each of these are added up in two steps
+constexpr int SUM_THREADS = 1024;
+constexpr int SUM_SLICES = 256;       // more than 16 partial sums for each of SUM_THREADS are added up in two steps
 constexpr int MAX_CHUNKED = 2048;     // (row, chunk) pairs of the calls that split their rows, at most
 
 // ---------------------------------------------------------------- rows in memory
@@ -363,13 +364,14 @@ __device__ __forceinline__ void store_stats(float *stats, const Four &s)
 __device__ __forceinline__ void sum_four(const SumFour &f, Four *red)
 {
     Four s = {};
+#pragma unroll 8
     for (int i = threadIdx.x; i < f.n; i += blockDim.x) s = add_four(s, f.partial[i]);
     store_stats(f.stats, sum_block(s, red));
 }
 
-__global__ __launch_bounds__(NT) void sum_four_kernel(SumFour f)
+__global__ __launch_bounds__(SUM_THREADS) void sum_four_kernel(SumFour f)
 {
-    __shared__ Four red[NT / 64];
+    __shared__ Four red[SUM_THREADS / 64];
     sum_four(f, red);
 }
 
@@ -656,24 +658,27 @@ __global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, in
     }
 }
 
-// The rows' terms from their chunks, a thread a row.
+// The rows' terms from their chunks, G lanes a row.
+template <int G>
 __global__ __launch_bounds__(NT) void merge_kernel(RowsArgs a, int chunks, const TopSum *partial)
 {
     __shared__ Four red[NT / 64];
     Four sums = {};
-    for (long long row = (long long)blockIdx.x * NT + threadIdx.x; row < a.r.B; row += (long long)gridDim.x * NT) {
+    const int g = threadIdx.x % G;
+    const long long per_grid = (long long)gridDim.x * (NT / G);
+    for (long long row = (long long)blockIdx.x * (NT / G) + threadIdx.x / G; row < a.r.B; row += per_grid) {
         RowTerms t = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
         const RowInputs in(a.h, a.r, row);
         if (in.choice(a.r.K)) {
-            const TopSum *part = partial + row * chunks;
             const float zy = logit(a.r, row, in.y);
-            float top = zy;
-            for (int c = 0; c < chunks; ++c) top = fmaxf(top, part[c].top);
-            float o = 0.f;
-            for (int c = 0; c < chunks; ++c) o += part[c].sum * rescale(part[c].top, top);
-            t = finish_row(zy, top, o);
+            TopSum s = {-INFINITY, 0.f};
+            for (int c = g; c < chunks; c += G) s = join(s, partial[row * chunks + c]);
+#pragma unroll
+            for (int o = G / 2; o > 0; o >>= 1) s = join(s, TopSum{__shfl_xor(s.top, o, 64), __shfl_xor(s.sum, o, 64)});
+            const float top = fmaxf(s.top, zy);
+            t = finish_row(zy, top, s.sum * rescale(s.top, top));
         }
-        head_row(a.h, in, row, t, true, sums);
+        head_row(a.h, in, row, t, g == 0, sums);
     }
     if (a.h.kind == HEAD_POLICY) {
         sums = sum_block(sums, red);
@@ -925,10 +930,12 @@ hipError_t chunked_rows(RowsArgs a, const Split &s, TopSum *partial, int *blocks
                              ? launch_kernel(row_sums_kernel<__bf16>, grid, block, stream, ev, a, s.chunks, s.pieces_per_chunk, partial)
                              : launch_kernel(row_sums_kernel<float>, grid, block, stream, ev, a, s.chunks, s.pieces_per_chunk, partial);
     if (e != hipSuccess || (s.chunks == 1 && a.h.kind != HEAD_POLICY)) return e;
-    *blocks = ceil_div(a.r.B, NT);
+    *blocks = ceil_div(a.r.B, s.chunks == 1 ? NT : NT / 64);
     if (*blocks > MAX_SUM_BLOCKS) *blocks = MAX_SUM_BLOCKS;
     if (*blocks > 1) a.stats = nullptr;
-    return launch_kernel(merge_kernel, dim3((unsigned)*blocks), block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial);
+    const dim3 merge((unsigned)*blocks);
+    return s.chunks == 1 ? launch_kernel(merge_kernel<1>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial)
+                         : launch_kernel(merge_kernel<64>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial);
 }
 
 template <typename T, typename TO>
@@ -956,14 +963,14 @@ hipError_t logit_grad(GradArgs a, hipStream_t stream, const LaunchEvents &ev)
 // more: room for SUM_SLICES
 hipError_t add_sums(SumFour f, Four *more, hipStream_t stream)
 {
-    if (f.n > 16 * SUM_SLICES) {
+    if (f.n > 16 * SUM_THREADS) {
         const hipError_t e =
             launch_kernel(sum_slices_kernel, dim3(SUM_SLICES), dim3(NT), stream, LaunchEvents(), f.partial, f.n, more);
         if (e != hipSuccess) return e;
         f.partial = more;
         f.n = SUM_SLICES;
     }
-    return launch_kernel(sum_four_kernel, dim3(1), dim3(NT), stream, LaunchEvents(), f);
+    return launch_kernel(sum_four_kernel, dim3(1), dim3(f.n > NT ? SUM_THREADS : NT), stream, LaunchEvents(), f);
 }
 
 }  // namespace
@@ -1051,7 +1058,7 @@ hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, cons
                           (const double *)w.row_lp, d.dZ ? w.coef : nullptr, w.sums);
     const SumFour fin = {w.sums, t.pairs, t.stats};
     if (e != hipSuccess) return e;
-    if (!d.dZ || r.B == 0) return launch_kernel(sum_four_kernel, dim3(1), dim3(NT), stream, LaunchEvents(), fin);
+    if (!d.dZ || r.B == 0) return launch_kernel(sum_four_kernel, dim3(1), dim3(SUM_THREADS), stream, LaunchEvents(), fin);
     GradArgs g = {};
     g.r = r;
     g.d = d;
