@@ -858,12 +858,16 @@ struct Split {
 
 constexpr int ROW_PIECES = 20 * 1024;  // the longest row that rows_kernel has a form for
 
-// A pass that makes a gradient keeps the rows in registers, unless they are too long for a workgroup or too few to fill the device.
-// One that only reads them does so where several rows share a wavefront.
+// Rows go through registers, but for long ones that are few (a workgroup each leaves most of the device idle) or, where they are only
+// read, many (one workgroup of 1024 a compute unit waits between its rows), and those too long for a workgroup.
+// Measured on both sides of the lines, data from memory, us, registers against chunks (bf16): policy loss 4 x 32000 12.0 / 13.2,
+// 16 x 65000 15.1 / 15.9, 64 x 65000 18.1 / 19.8 (4 x 65000 14.6 / 13.2); 16 x 128000 22.7 / 17.6, 64 x 128000 25.9 / 23.5, 128 x 128000
+// 27.5 / 31.9, 256 x 128000 39.3 / 56.8; log-probabilities 64 x 65000 9.2 / 10.7, 1000 x 65000 33.2 / 35.8, 16 x 128000 12.1 / 9.8,
+// 1000 x 128000 74.9 / 57.7.
 bool rows_in_registers(const ChoiceRows &r, bool grad)
 {
     const int n = most_pieces(r);
-    return n <= (grad ? ROW_PIECES : 512);
+    return n <= 12288 || (grad && n <= ROW_PIECES && r.B > 64);
 }
 
 Split split_for(const ChoiceRows &r)
@@ -897,16 +901,21 @@ hipError_t rows_form(const RowsArgs &a, int *blocks, hipStream_t s, const Launch
 template <typename T, typename TO>
 hipError_t rows_of_type(const RowsArgs &a, int *blocks, hipStream_t s, const LaunchEvents &ev)
 {
+    // Four pieces a lane, in as many lanes as that takes, more pieces where a row would need more than 256 lanes.  Fewer lanes
+    // with more pieces make fewer wavefronts than it takes to wait for the memory, more lanes compute more of what is the same in all
+    // of them (policy loss, data from memory, kernel alone in us: 20000 x 983 fp32 64 lanes x 4 34.4, 16 x 16 48.0; 2047 x 983
+    // 10.7, 17.0, 256 x 1 9.2; 8192 x 983 19.6, 22.4, 24.6; 65536 x 100 fp32 8 x 4 20.1, 16 x 2 21.6, 32 x 1 33.0; 8192 x 4000
+    // bf16 128 x 4 26.9, 64 x 8 29.6, 256 x 2 29.7; 2048 x 32000 bf16 256 x 16 55.0, 512 x 8 55.4, 1024 x 4 57.7).
     const int n = most_pieces(a.r);
     if (n <= 4) return rows_form<T, TO, 4, 1>(a, blocks, s, ev);
     if (n <= 16) return rows_form<T, TO, 4, 4>(a, blocks, s, ev);
-    if (n <= 32) return rows_form<T, TO, 4, 8>(a, blocks, s, ev);
-    if (n <= 64) return rows_form<T, TO, 4, 16>(a, blocks, s, ev);
-    if (n <= 128) return rows_form<T, TO, 8, 16>(a, blocks, s, ev);
-    if (n <= 256) return rows_form<T, TO, 16, 16>(a, blocks, s, ev);
-    if (n <= 512) return rows_form<T, TO, 32, 16>(a, blocks, s, ev);
-    if (n <= 1024) return rows_form<T, TO, 64, 16>(a, blocks, s, ev);
-    if (n <= 2048) return rows_form<T, TO, 128, 16>(a, blocks, s, ev);
+    if (n <= 32) return rows_form<T, TO, 8, 4>(a, blocks, s, ev);
+    if (n <= 64) return rows_form<T, TO, 16, 4>(a, blocks, s, ev);
+    if (n <= 128) return rows_form<T, TO, 32, 4>(a, blocks, s, ev);
+    if (n <= 256) return rows_form<T, TO, 64, 4>(a, blocks, s, ev);
+    if (n <= 512) return rows_form<T, TO, 128, 4>(a, blocks, s, ev);
+    if (n <= 1024) return rows_form<T, TO, 256, 4>(a, blocks, s, ev);
+    if (n <= 2048) return rows_form<T, TO, 256, 8>(a, blocks, s, ev);
     if (n <= 4096) return rows_form<T, TO, 256, 16>(a, blocks, s, ev);
     if (n <= 6656) return rows_form<T, TO, 512, 13>(a, blocks, s, ev);
     if (n <= 8192) return rows_form<T, TO, 512, 16>(a, blocks, s, ev);
@@ -938,15 +947,25 @@ hipError_t chunked_rows(RowsArgs a, const Split &s, TopSum *partial, int *blocks
                          : launch_kernel(merge_kernel<64>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial);
 }
 
+// A row in G lanes
+template <typename T, typename TO, int G>
+hipError_t grad_form(const GradArgs &a, hipStream_t stream, const LaunchEvents &ev)
+{
+    const int blocks = ceil_div(a.r.B, NT / G) + (a.fin.n > 0 ? 1 : 0);
+    return launch_kernel(logit_grad_kernel<T, TO, G>, dim3((unsigned)blocks), dim3(NT), stream, ev, a);
+}
+
 template <typename T, typename TO>
 hipError_t grad_of_type(GradArgs a, hipStream_t stream, const LaunchEvents &ev)
 {
     const int n = most_pieces(a.r), fin = a.fin.n > 0 ? 1 : 0;
     a.chunks = 1;
     a.pieces_per_chunk = 0;
-    if (n <= 16) return launch_kernel(logit_grad_kernel<T, TO, 8>, dim3((unsigned)(ceil_div(a.r.B, NT / 8) + fin)), dim3(NT), stream, ev, a);
-    if (n <= 512)
-        return launch_kernel(logit_grad_kernel<T, TO, 64>, dim3((unsigned)(ceil_div(a.r.B, NT / 64) + fin)), dim3(NT), stream, ev, a);
+    if (n <= 4) return grad_form<T, TO, 4>(a, stream, ev);
+    if (n <= 32) return grad_form<T, TO, 8>(a, stream, ev);
+    if (n <= 64) return grad_form<T, TO, 16>(a, stream, ev);
+    if (n <= 128) return grad_form<T, TO, 32>(a, stream, ev);
+    if (n <= 512) return grad_form<T, TO, 64>(a, stream, ev);
     const Split s = split_for(a.r);
     a.chunks = s.chunks;
     a.pieces_per_chunk = s.pieces_per_chunk;
