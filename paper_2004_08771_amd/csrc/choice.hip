@@ -186,21 +186,44 @@ __device__ __forceinline__ TwoLog two_log2(float s)
     return {(float)__builtin_amdgcn_frexp_expf(s), __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(s))};
 }
 
-// exp(d) - 1 - d, to a few roundings where d is small, too: d^2 times a series
-__device__ __forceinline__ float kl_of(float d, float em /* exp(d) - 1 */)
+// exp(x), off by 2^-23 (1 + |x|) relative.  Of log2 e = LOG2E + 1.9e-8 both parts.
+__device__ __forceinline__ float exp_of(float x) { return exp2_of(__builtin_fmaf(x, LOG2E, x * 0x1.4ae0cp-26f)); }
+
+// log(1 + x) for x in [0, 1]: 2 atanh(x / (2 + x)), whose series in s = x / (2 + x) <= 1/3 is cut behind s^15 (s^16 / 17 < 2e-9)
+__device__ __forceinline__ float log1p_of(float x)
 {
-    if (fabsf(d) < 0.5f) {
-        float c = 1.f / 40320.f;
-        c = __builtin_fmaf(c, d, 1.f / 5040.f);
-        c = __builtin_fmaf(c, d, 1.f / 720.f);
-        c = __builtin_fmaf(c, d, 1.f / 120.f);
-        c = __builtin_fmaf(c, d, 1.f / 24.f);
-        c = __builtin_fmaf(c, d, 1.f / 6.f);
-        c = __builtin_fmaf(c, d, 0.5f);
-        return d * d * c;
-    }
-    return em == INFINITY ? INFINITY : em - d;
+    const float s = x * __builtin_amdgcn_rcpf(2.f + x), q = s * s;
+    float c = 1.f / 15.f;
+    c = __builtin_fmaf(c, q, 1.f / 13.f);
+    c = __builtin_fmaf(c, q, 1.f / 11.f);
+    c = __builtin_fmaf(c, q, 1.f / 9.f);
+    c = __builtin_fmaf(c, q, 1.f / 7.f);
+    c = __builtin_fmaf(c, q, 1.f / 5.f);
+    c = __builtin_fmaf(c, q, 1.f / 3.f);
+    return 2.f * __builtin_fmaf(s * q, c, s);
 }
+
+// exp(d) - 1 and exp(d) - 1 - d, to a few roundings where d is small, too: d^2 times a series there
+struct Expm1 {
+    float em, kl;
+    __device__ __forceinline__ explicit Expm1(float d)
+    {
+        if (fabsf(d) < 0.5f) {
+            float c = 1.f / 40320.f;
+            c = __builtin_fmaf(c, d, 1.f / 5040.f);
+            c = __builtin_fmaf(c, d, 1.f / 720.f);
+            c = __builtin_fmaf(c, d, 1.f / 120.f);
+            c = __builtin_fmaf(c, d, 1.f / 24.f);
+            c = __builtin_fmaf(c, d, 1.f / 6.f);
+            c = __builtin_fmaf(c, d, 0.5f);
+            kl = d * d * c;
+            em = d + kl;
+        } else {
+            em = exp_of(d) - 1.f;
+            kl = em == INFINITY ? INFINITY : em - d;
+        }
+    }
+};
 
 // ---------------------------------------------------------------- what a row comes down to
 // part: the row takes part.  One without a choice has lp = lse = 0, one whose logits are all -inf has -inf.
@@ -224,7 +247,7 @@ __device__ __forceinline__ RowTerms finish_row(float zy, float top, float o)
     t.under = Under(top);
     const float e = t.under.exp(zy), s = (o == INFINITY ? NAN : o) + e;  // infinite: a logit that no maximum has seen
     const TwoLog l = two_log2(s);
-    t.inv_sum = 1.f / s;
+    t.inv_sum = __builtin_amdgcn_rcpf(s);  // off by a rounding
     t.others = o * t.inv_sum;
     const double log2_s = (double)l.hi + (double)l.lo;
     if (t.under.far) {
@@ -235,7 +258,7 @@ __device__ __forceinline__ RowTerms finish_row(float zy, float top, float o)
         t.lse = LN2 * lse2;
         t.lp = LN2 * ((double)zy * (double)LOG2E - lse2);
     }
-    if (o < e) t.lp = -(double)log1pf(o / e);
+    if (o < e) t.lp = -(double)log1p_of(o * __builtin_amdgcn_rcpf(e));
     return t;
 }
 
@@ -311,16 +334,16 @@ __device__ __forceinline__ RowCoef head_row(const RowHead &h, const RowInputs &i
         float pg = 0.f, g = 0.f, kl = 0.f;
         bool cut = false;
         if (A != 0.f) {  // (NaN too); without an advantage the ratio does not matter, however large
-            const float ratio = expf((float)(t.lp - (double)in.old_logp));
+            const float ratio = exp_of((float)(t.lp - (double)in.old_logp));
             const float lo = 1.f - p.clip_low, hi = 1.f + p.clip_high;
             cut = (A > 0.f && ratio > hi) || (A < 0.f && ratio < lo);
             pg = cut ? -(A > 0.f ? hi : lo) * A : -ratio * A;
             g = cut ? 0.f : pg;
         }
         if (p.ref_logp) {
-            const float d = (float)((double)in.ref_logp - t.lp), em = expm1f(d);
-            kl = kl_of(d, em);
-            if (p.kl_coef != 0.f) g -= p.kl_coef * em;
+            const Expm1 d((float)((double)in.ref_logp - t.lp));
+            kl = d.kl;
+            if (p.kl_coef != 0.f) g -= p.kl_coef * d.em;
         }
         const float w = in.w;
         if (write) {
@@ -340,12 +363,14 @@ __device__ __forceinline__ RowCoef head_row(const RowHead &h, const RowInputs &i
     return c;
 }
 
-__device__ __forceinline__ Four sum_block(Four s, Four *red /* a wavefront each */)
+// Every G-th lane has something to add.  red: a wavefront each
+template <int G = 1>
+__device__ __forceinline__ Four sum_block(Four s, Four *red)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) s.v[i] += __shfl_xor(s.v[i], o, 64);
+        for (int o = 32; o >= G; o >>= 1) s.v[i] += __shfl_xor(s.v[i], o, 64);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
@@ -396,7 +421,7 @@ struct RowsArgs {
 };
 
 // wavefronts a SIMD that the registers have to leave room for
-constexpr int row_waves(int n) { return n <= 4 ? 6 : n <= 8 ? 5 : n <= 16 ? 4 : 3; }
+constexpr int row_waves(int g, int n) { return g == 1 || n > 4 ? (n > 8 ? 4 : 5) : 6; }
 
 // A row of dZ and its padding
 template <int G, typename TO>
@@ -430,6 +455,9 @@ __device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long ro
 {
     constexpr int V = Piece<T>::V;
     constexpr int E = G < Row<T>::EDGE ? Row<T>::EDGE / G : 1;
+    // The exponentials stay in registers, too, where they take the place of the logits or there is room for them; else they
+    // are made again for the gradient.
+    constexpr bool KEEP = sizeof(T) == 4 || N <= 4;
     const Row<T> z(a.r.Z, a.r.ldz, row, a.r.K);
     const RowInputs in(a.h, a.r, row);
     const int y = in.y;
@@ -459,6 +487,7 @@ __device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long ro
             else if (i * G + g < z.pieces) x[i] = z.load(i * G + g);
         }
     }
+    float v[KEEP ? N : 1][V];
     float top = zy;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -472,29 +501,33 @@ __device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long ro
         if (i == iy) x[i].drop(ay % V, own);
         if ((i + 1) * G >= most && i * G + g >= z.pieces) x[i].set_none();
 #pragma unroll
-        for (int e = 0; e < V; ++e) top = fmaxf(top, x[i].get(e));
+        for (int e = 0; e < V; ++e) {
+            const float t = x[i].get(e);
+            top = fmaxf(top, t);
+            if (KEEP) v[i][e] = t;
+        }
         __builtin_amdgcn_sched_barrier(0);
     }
     top = max_of_row<G, WAVES>(top, red_top);
-    float others = 0.f;
-    {
-        const Under under(top);
-        float o4[4] = {0.f, 0.f, 0.f, 0.f};
+    const Under under(top);
+    float o4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < E; ++i) o4[i & 3] += under.exp(edge[i]);
+    for (int i = 0; i < E; ++i) o4[i & 3] += edge[i] = under.exp(edge[i]);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if (i * G >= most) continue;
-            x[i].forget();
-            float t[V];
+    for (int i = 0; i < N; ++i) {
+        if (i * G >= most) continue;
+        if (!KEEP) x[i].forget();
+        float t[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) t[e] = under.exp(x[i].get(e));
+        for (int e = 0; e < V; ++e) t[e] = under.exp(KEEP ? v[i][e] : x[i].get(e));
 #pragma unroll
-            for (int e = 0; e < V; ++e) o4[e & 3] += t[e];
-            __builtin_amdgcn_sched_barrier(0);
+        for (int e = 0; e < V; ++e) {
+            o4[e & 3] += t[e];
+            if (KEEP) v[i][e] = t[e];
         }
-        others = (o4[0] + o4[1]) + (o4[2] + o4[3]);
+        __builtin_amdgcn_sched_barrier(0);
     }
+    float others = (o4[0] + o4[1]) + (o4[2] + o4[3]);
 #pragma unroll
     for (int o = (G < 64 ? G : 64) / 2; o > 0; o >>= 1) others += __shfl_xor(others, o, 64);
     RowCoef c;
@@ -518,7 +551,6 @@ __device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long ro
         zero_row<G>(dz, a, g);
         return;
     }
-    const Under under(c.shift, c.factor);
     TO *to = dz + z.head;
     // whole wavefronts that store at 16-byte boundaries: through a buffer, which leaves out what is behind the row
     const bool through = G >= 64 && (reinterpret_cast<uintptr_t>(to) & (V * sizeof(TO) - 1)) == 0;
@@ -527,10 +559,10 @@ __device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long ro
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         if (i * G >= most) continue;
-        x[i].forget();
+        if (!KEEP) x[i].forget();
         float out[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) out[e] = c.scale * under.exp(x[i].get(e));
+        for (int e = 0; e < V; ++e) out[e] = c.scale * (KEEP ? v[i][e] : under.exp(x[i].get(e)));
         if (through && a.d.past) store_buffer<TO, V, PAST>(rs, g, i * G, out);
         else if (through) store_buffer<TO, V, 0>(rs, g, i * G, out);
         else if (i * G + g < z.pieces) store<TO, V>(to + (i * G + g) * V, out, false);
@@ -540,13 +572,13 @@ __device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long ro
 #pragma unroll
     for (int i = 0; i < E; ++i) {
         const int j = z.edge(i * G + g);
-        if (j >= 0) dz[j] = TO(j == y ? c.chosen : c.scale * under.exp(edge[i]));
+        if (j >= 0) dz[j] = TO(j == y ? c.chosen : c.scale * edge[i]);
     }
     for (int j = a.r.K + g; j < a.d.pad; j += G) dz[j] = TO(0.f);
 }
 
 template <typename T, typename TO, int G, int N, int THREADS>
-__global__ __launch_bounds__(THREADS, row_waves(N)) void rows_kernel(RowsArgs a)
+__global__ __launch_bounds__(THREADS, row_waves(G, N)) void rows_kernel(RowsArgs a)
 {
     constexpr int WAVES = THREADS / 64, ROWS = THREADS / G;
     __shared__ float red_top[WAVES], red_sum[WAVES];
@@ -558,7 +590,7 @@ __global__ __launch_bounds__(THREADS, row_waves(N)) void rows_kernel(RowsArgs a)
     Four sums = {};
     if (row < a.r.B) row_in_registers<T, TO, G, N, WAVES>(a, row, g, red_top, red_sum, &red_coef, sums);
     if (a.h.kind == HEAD_POLICY) {
-        if (G <= 64) sums = sum_block(sums, red_four);  // else the first thread's
+        if constexpr (G <= 64) sums = sum_block<G>(sums, red_four);  // else the first thread's
         if (a.stats) store_stats(a.stats, sums);
         else if (threadIdx.x == 0) a.sums[blockIdx.x] = sums;
     }
@@ -905,9 +937,12 @@ hipError_t rows_of_type(const RowsArgs &a, int *blocks, hipStream_t s, const Lau
     // with more pieces make fewer wavefronts than it takes to wait for the memory, more lanes compute more of what is the same in all
     // of them (policy loss, data from memory, kernel alone in us: 20000 x 983 fp32 64 lanes x 4 34.4, 16 x 16 48.0; 2047 x 983
     // 10.7, 17.0, 256 x 1 9.2; 8192 x 983 19.6, 22.4, 24.6; 65536 x 100 fp32 8 x 4 20.1, 16 x 2 21.6, 32 x 1 33.0; 8192 x 4000
-    // bf16 128 x 4 26.9, 64 x 8 29.6, 256 x 2 29.7; 2048 x 32000 bf16 256 x 16 55.0, 512 x 8 55.4, 1024 x 4 57.7).
+    // bf16 128 x 4 26.9, 64 x 8 29.6, 256 x 2 29.7; 2048 x 32000 bf16 256 x 16 55.0, 512 x 8 55.4, 1024 x 4 57.7; the whole call:
+    // 65536 x 7 fp32 1 x 2 7.9, 2 x 1 10.5, 4 x 1 11.2).  Long rows in blocks that a compute unit has room for two of: 4000 x
+    // 83793 bf16 512 x 24 271, 1024 x 12 307.
     const int n = most_pieces(a.r);
-    if (n <= 4) return rows_form<T, TO, 4, 1>(a, blocks, s, ev);
+    if (n <= 2) return rows_form<T, TO, 1, 2>(a, blocks, s, ev);
+    if (n <= 4) return rows_form<T, TO, 2, 2>(a, blocks, s, ev);
     if (n <= 16) return rows_form<T, TO, 4, 4>(a, blocks, s, ev);
     if (n <= 32) return rows_form<T, TO, 8, 4>(a, blocks, s, ev);
     if (n <= 64) return rows_form<T, TO, 16, 4>(a, blocks, s, ev);
@@ -919,7 +954,7 @@ hipError_t rows_of_type(const RowsArgs &a, int *blocks, hipStream_t s, const Lau
     if (n <= 4096) return rows_form<T, TO, 256, 16>(a, blocks, s, ev);
     if (n <= 6656) return rows_form<T, TO, 512, 13>(a, blocks, s, ev);
     if (n <= 8192) return rows_form<T, TO, 512, 16>(a, blocks, s, ev);
-    if (n <= 12288) return rows_form<T, TO, 1024, 12>(a, blocks, s, ev);
+    if (n <= 12288) return rows_form<T, TO, 512, 24>(a, blocks, s, ev);
     if (n <= 16384) return rows_form<T, TO, 1024, 16>(a, blocks, s, ev);
     return rows_form<T, TO, 1024, 20>(a, blocks, s, ev);
 }
