@@ -534,8 +534,8 @@ int hb_logprob_grad_async(const void *d_Z, int64_t ldz, int tensor, const int32_
  *     cut: A_i > 0 and r_i > 1 + clip_high, or A_i < 0 and r_i < 1 - clip_low
  * Rows take no part if their class is outside [0, K), their weight is 0 or their logits are all -inf: what else
  * they hold is not looked at, their gradient is 0.  All pointers are DEVICE pointers to B floats.
- * d_stats (4 floats): loss, sum of w pg, sum of w kl, sum of w [cut].  d_logp (may be NULL): B floats, lp_i (rows
- * without a choice or weight 0).  d_dZ: as for hb_logprob_grad_async; NULL: the loss only.
+ * d_stats (4 floats): loss, sum of w pg, sum of w kl, sum of w [cut].  d_logp (may be NULL): B floats, lp_i (0 without
+ * a choice or with weight 0, -inf where all logits are).  d_dZ: as for hb_logprob_grad_async; NULL: the loss only.
  * d_ws: hb_choice_workspace_bytes(B, 0) bytes, as above.  B = 0 gives stats of 0.  Sums are made in a
  * fixed order: the same call gives the same bits.
  */

@@ -123,7 +123,7 @@ NETS = [
     ((54, 32, 7), SIG, F32, 64), ((54, 32, 7), RELU, F32, 1), ((54, 96, 7), SIG, F32, 1000), ((40, 72, 100), RELU, F32, 333),
     ((70, 65, 129, 67, 12), RELU, F32, 321), ((54, 512, 512, 7), SIG, F32, 2048), ((300, 257, 257, 983), SIG, F32, 130), ((33, 5), SIG, F32, 77),
     ((64, 128, 96, 40), SIG, BF16, 300), ((33, 70, 51, 9), SIG, BF16, 127), ((33, 70, 51, 9), RELU, BF16, 127), ((512, 768, 512, 200), RELU, BF16, 2048),
-    ((300, 1024, 1024, 33), SIG, BF16, 1001), ((64, 20, 24, 20, 16, 10), SIG, BF16, 65),
+    ((300, 1024, 1024, 33), SIG, BF16, 1001), ((128, 256, 1000), SIG, BF16, 200), ((64, 20, 24, 20, 16, 10), SIG, BF16, 65),
 ]
 
 

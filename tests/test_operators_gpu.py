@@ -199,7 +199,7 @@ def test_dropout_of_more_groups_than_a_launch_takes():
 
 # ---------------------------------------------------------------- log-probabilities
 SHAPES = [(1, 1), (1, 2), (5, 1), (64, 7), (300, 2), (33, 16), (129, 17), (40, 63), (41, 64), (23, 65), (70, 100), (26, 255), (22, 513), (31, 983),
-          (12, 2049), (23, 4100), (11, 8200), (5, 16385), (3, 33000), (2, 70001), (1, 140001), (600, 40), (300, 1000)]
+          (12, 2049), (12, 3001), (23, 4100), (11, 8200), (5, 16385), (3, 33000), (2, 70001), (1, 140001), (600, 40), (300, 1000), (100, 41), (3, 30000), (2, 99001)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -405,6 +405,96 @@ def test_policy_ratios_that_overflow():
     check(got[2], -0.25 / 3 * np.array([0.75, -0.25, -0.25, -0.25]), 1e-7, "dZ")
 
 
+# ---------------------------------------------------------------- large calls, against 64 bits on the device
+def rows_on_device(Z, y):
+    lsm = torch.log_softmax(Z.double(), 1)
+    part = (y >= 0) & (y < Z.shape[1])
+    at = y.clamp(0, Z.shape[1] - 1).long()[:, None]
+    return part, at, lsm, torch.where(part, lsm.gather(1, at)[:, 0], 0.0)
+
+
+def near_on_device(got, want, Z, g, K, dtype, what):
+    """grad_tol, with the largest |z - lse| of these inputs (normal logits of deviation 2: below 32) for all of them."""
+    rel = eps_s(K) + (32 + 32 + 8 + 8) * U + (2.0 ** -8 if dtype == "bf16" else 0.0)
+    off = (got.double() - want).abs() - rel * want.abs() - 4 * U * g.abs()[:, None] * (want != 0) / K - 1e-30
+    assert float(off.max()) <= 0, f"{what}: {float(off.max())}"
+
+
+@pytest.mark.parametrize("B,K,dtype", [
+    (17000, 2100, "f32"),     # 17000 blocks: their sums in two steps; a gradient past the caches
+    (17000, 4099, "bf16"),    # ... of odd rows
+    (1030, 50001, "f32"),     # long rows, many: whole rows by a block where they are only read
+    (1030, 82003, "f32"),     # too long for registers, one chunk a row
+    (70, 52000, "f32"), (66, 70003, "f32"), (70, 110001, "bf16"), (66, 150001, "bf16"),  # a row in 1024 lanes
+    (4, 300007, "bf16"), (1, 1 << 20, "f32"),
+])
+def test_large_calls(B, K, dtype):
+    g0 = torch.Generator(device="cuda").manual_seed(B + K)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g0)  # noqa: E731
+    Z = (2 * rnd(B, K)).to(TYPES[dtype])
+    y = torch.randint(0, K, (B,), device="cuda", generator=g0, dtype=torch.int32)
+    if B > 20:
+        y[::13] = -1
+    part, at, lsm, lp = rows_on_device(Z, y)
+    work = ws(B, 3)
+    a, b = torch.full((B,), 7.0, device="cuda"), torch.full((B,), 7.0, device="cuda")
+    hb.logprob(Z, y, a, b, ws=work)
+    lse = torch.where(part, Z[:, 0].double() - lsm[:, 0], 0.0)
+    assert float(((a - lp).abs() - eps_s(K) - 2 * U * lp.abs()).max()) <= 0
+    assert float(((b - lse).abs() - eps_s(K) - 2 * U * lse.abs()).max()) <= 0
+    unit = -lsm.exp_()
+    rest = -(unit.sum(1) - unit.gather(1, at)[:, 0])
+    unit.scatter_(1, at, rest[:, None])
+    unit *= part[:, None]
+    up = rnd(B)
+    dZ = torch.full_like(Z, 7.0)
+    hb.logprob_grad(Z, y, a, b, up, dZ)
+    near_on_device(dZ, unit * up.double()[:, None], Z, up, K, dtype, "logprob")
+    # policy: ratios away from the clip's borders
+    away = torch.tensor([-0.7, -0.1, 0.0, 0.1, 0.7], device="cuda")[torch.randint(0, 5, (B,), device="cuda", generator=g0)]
+    old, adv, refs = (lp - away).float(), rnd(B), (lp + 0.3 * rnd(B)).float()
+    w = (torch.rand(B, device="cuda", generator=g0) + 0.5) / B
+    r = torch.where(part, (lp - old.double()).exp(), 1.0)
+    A, d, wd = adv.double(), refs.double() - lp, w.double() * part
+    cut = ((A > 0) & (r > 1.2)) | ((A < 0) & (r < 0.8))
+    pg, kl = -torch.minimum(r * A, r.clamp(0.8, 1.2) * A), torch.expm1(d) - d
+    g = wd * (-(r * A) * ~cut + 0.05 * -torch.expm1(d))
+    stats = torch.stack([(wd * (pg + 0.05 * kl)).sum(), (wd * pg).sum(), (wd * kl).sum(), (wd * cut).sum()])
+    s_tol = float((wd * (r * A.abs() + 0.05 * d.exp())).sum()) * 4 * eps_s(K) + 8 * U * float(wd.sum()) + float((wd * d.exp()).sum()) * 4 * eps_s(K)
+    args = dict(ref=refs, weight=w, clip=(0.2, 0.2), kl_coef=0.05, ws=work)
+    st, st2 = torch.zeros(4, device="cuda"), torch.zeros(4, device="cuda")
+    dZ.fill_(7.0)
+    hb.policy_loss(Z, y, old, adv, st, dZ=dZ, **args)
+    hb.policy_loss(Z, y, old, adv, st2, **args)
+    assert float((st - stats).abs().max()) <= s_tol and float((st2 - stats).abs().max()) <= s_tol
+    g_off = wd * (r * A.abs() + 0.05 * d.exp()) * 4 * eps_s(K)
+    off = (dZ.double() - unit * g[:, None]).abs() - unit.abs() * g_off[:, None]
+    rel = eps_s(K) + 80 * U + (2.0 ** -8 if dtype == "bf16" else 0.0)
+    assert float((off - rel * (unit * g[:, None]).abs()).max()) <= 1e-30
+    # preference: three pairs over the rows but the first and the last
+    if B >= 66:
+        seq = torch.linspace(1, B - 1, 7, device="cuda").to(torch.int32)
+        cum = torch.cat([lp.new_zeros(1), lp.cumsum(0)])
+        sums = cum[seq[1:].long()] - cum[seq[:-1].long()]
+        rr = (sums + rnd(6)).float()
+        gain = (sums - rr.double()).view(3, 2)
+        h = gain[:, 0] - gain[:, 1]
+        slope = -0.1 / 3 * torch.sigmoid(-0.1 * h)
+        rows = torch.searchsorted(seq[1:].long(), torch.arange(B, device="cuda"), right=True).clamp(max=5)
+        g = torch.stack([slope, -slope], 1).view(-1)[rows]
+        sl = torch.zeros(6, device="cuda")
+        dZ.fill_(7.0)
+        hb.preference_loss(Z, y, seq, st, dZ=dZ, ref=rr, seq_logp=sl, ws=work)
+        many = B / 6
+        assert float(((sl - sums).abs() - many * eps_s(K) - 2 * U * sums.abs()).max()) <= 0
+        want = unit * g[:, None]
+        off = (dZ.double() - want).abs() - unit.abs() * (0.1 / 3 * 0.1 / 4 * 2 * many * eps_s(K)) - rel * want.abs()
+        assert float(off[1:B - 1].max()) <= 1e-30
+        assert bool((dZ[0] == 7.0).all()) and bool((dZ[B - 1] == 7.0).all())
+        hb.preference_loss(Z, y, seq, st2, ref=rr, ws=work)
+        assert torch.equal(st, st2)
+
+
 # ---------------------------------------------------------------- preference loss
 def preference_case(B, K, pairs, rng, dtype, masked=True):
     z, y = logits(B, K, rng, dtype, masked)
@@ -463,6 +553,18 @@ def test_preference_loss_and_its_gradient(B, K, pairs, dtype):
         got = host(Z)
         assert np.array_equal(got[inside], host(dZ)[inside]) and outside_is_nan(flat_z, Z)
         assert np.array_equal(got[:seq[0]], keep[:seq[0]], equal_nan=True) and np.array_equal(got[seq[-1]:], keep[seq[-1]:], equal_nan=True)
+
+
+def test_preference_rows_that_take_no_part_get_zeros_whatever_the_loss():
+    """A sequence of log-probability -inf: its loss is infinite or undefined, the gradients of padding are zeros all the same."""
+    z = np.zeros((6, 40))
+    z[1, 0] = z[3, 0] = -np.inf
+    y = np.array([-1, 0, 0, 0, 40, 5], np.int32)    # both sequences have an impossible choice, and padding
+    dZ, _ = matrix(np.full((6, 40), 7.0), "f32")
+    st = torch.zeros(4, device="cuda")
+    hb.preference_loss(matrix(z, "f32")[0], vec(y, torch.int32), vec([0, 3, 6], torch.int32), st, dZ=dZ, ws=ws(6, 1))
+    got = host(dZ)
+    assert not got[0].any() and not got[4].any() and np.isnan(host(st)[0])
 
 
 def test_preference_gradient_against_differences():
