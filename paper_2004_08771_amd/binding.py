@@ -407,22 +407,33 @@ def _type(t):
     return kind
 
 
-def _matrix(t, name, like=None):
-    """(address, pitch, HB_TENSOR_*) of a torch matrix with elements of a row next to each other."""
-    kind = _type(t)
+def _matrix(t, name):
+    """(address, pitch, HB_TENSOR_*, rows, columns) of a torch matrix with elements of a row next to each other."""
+    kind = _types.get(t.dtype)
+    if kind is None:
+        kind = _type(t)
     if kind != HB_TENSOR_F32 and kind != HB_TENSOR_BF16:
         _invalid(f"{name} has type {t.dtype}: float32 or bfloat16 is needed")
-    if t.dim() != 2:
-        _invalid(f"{name} has {t.dim()} dimensions: a matrix is needed")
-    rows, cols = shape = t.shape
-    if like is not None and (shape != like.shape or t.dtype != like.dtype):
-        _invalid(f"{name} is {tuple(shape)} {t.dtype}: {tuple(like.shape)} {like.dtype} is needed")
+    shape = t.shape
+    if len(shape) != 2:
+        _invalid(f"{name} has {len(shape)} dimensions: a matrix is needed")
+    rows, cols = shape
     step, along = t.stride()
-    if cols > 1 and along != 1:
+    if along != 1 and cols > 1:
         _invalid(f"{name}: the elements of a row must be next to each other")
-    if rows > 1 and step < cols:
+    if rows < 2:
+        step = cols if cols > 1 else 1
+    elif step < cols:
         _invalid(f"{name}: its rows overlap")
-    return t.data_ptr(), (step if rows > 1 else max(cols, 1)), kind
+    return t.data_ptr(), step, kind, rows, cols
+
+
+def _out_matrix(t, name, like):
+    """(address, pitch) of a matrix of the type and shape that _matrix gave for another."""
+    out = _matrix(t, name)
+    if out[2:] != like[2:]:
+        _invalid(f"{name} is {tuple(t.shape)} {t.dtype}: the input's shape and type are needed")
+    return out[0], out[1]
 
 
 def _vector(t, name, n, kind=HB_TENSOR_F32):
@@ -440,7 +451,13 @@ def _workspace(ws):
         _invalid("ws is needed: a tensor of choice_workspace_bytes() bytes")
     if not ws.is_contiguous():
         _invalid("ws must be contiguous")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.nbytes
+
+
+def _call(name, *args):
+    rc = getattr(_lib or lib(), name)(*args)
+    if rc != HB_OK:
+        _check(rc)
 
 
 def choice_workspace_bytes(B, pairs=0) -> int:
@@ -450,27 +467,25 @@ def choice_workspace_bytes(B, pairs=0) -> int:
 
 def dropout(x, out, p, seed, offset=0, stream=None):
     """hb_dropout_async on matrices x and out (out may be x).  The gradient of x is the same call on the gradient of out."""
-    px, ldx, kind = _matrix(x, "x")
-    po, ldo, _ = _matrix(out, "out", x)
-    _check(lib().hb_dropout_async(px, ldx, po, ldo, kind, x.shape[0], x.shape[1], p, seed, offset, stream if stream else None))
+    m = px, ldx, kind, rows, cols = _matrix(x, "x")
+    po, ldo = _out_matrix(out, "out", m)
+    _call("hb_dropout_async", px, ldx, po, ldo, kind, rows, cols, p, seed, offset, stream or None)
 
 
 def logprob(Z, y, logp, lse=None, ws=None, stream=None):
     """hb_logprob_async: log-probabilities of the classes y (int32) in rows of logits Z."""
-    pz, ldz, kind = _matrix(Z, "Z")
-    B, K = Z.shape
+    pz, ldz, kind, B, K = _matrix(Z, "Z")
     pw, nw = _workspace(ws)
-    _check(lib().hb_logprob_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, _vector(logp, "logp", B),
-                                  _vector(lse, "lse", B), pw, nw, stream if stream else None))
+    _call("hb_logprob_async", pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, _vector(logp, "logp", B), _vector(lse, "lse", B),
+          pw, nw, stream or None)
 
 
 def logprob_grad(Z, y, logp, lse, g, dZ, stream=None):
     """hb_logprob_grad_async: dZ = g d logp / d Z (dZ may be Z)."""
-    pz, ldz, kind = _matrix(Z, "Z")
-    pd, ldd, _ = _matrix(dZ, "dZ", Z)
-    B, K = Z.shape
-    _check(lib().hb_logprob_grad_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, _vector(logp, "logp", B),
-                                       _vector(lse, "lse", B), _vector(g, "g", B), pd, ldd, stream if stream else None))
+    m = pz, ldz, kind, B, K = _matrix(Z, "Z")
+    pd, ldd = _out_matrix(dZ, "dZ", m)
+    _call("hb_logprob_grad_async", pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, _vector(logp, "logp", B),
+          _vector(lse, "lse", B), _vector(g, "g", B), pd, ldd, stream or None)
 
 
 def policy_args(B, old, adv, ref=None, weight=None, clip=(0.2, 0.2), kl_coef=0.0) -> Policy:
@@ -482,14 +497,12 @@ def policy_args(B, old, adv, ref=None, weight=None, clip=(0.2, 0.2), kl_coef=0.0
 def policy_loss(Z, y, old, adv, stats, dZ=None, ref=None, weight=None, clip=(0.2, 0.2), kl_coef=0.0, logp=None, ws=None,
                 stream=None):
     """hb_policy_loss_async: stats (4 floats: loss, policy part, KL, cut share) and dZ (may be Z; None: the loss only)."""
-    pz, ldz, kind = _matrix(Z, "Z")
-    pd, ldd, _ = (None, ldz, 0) if dZ is None else _matrix(dZ, "dZ", Z)
-    B, K = Z.shape
+    m = pz, ldz, kind, B, K = _matrix(Z, "Z")
+    pd, ldd = (None, ldz) if dZ is None else _out_matrix(dZ, "dZ", m)
     pw, nw = _workspace(ws)
     args = policy_args(B, old, adv, ref, weight, clip, kl_coef)
-    _check(lib().hb_policy_loss_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, ctypes.byref(args),
-                                      _vector(stats, "stats", 4), _vector(logp, "logp", B), pd, ldd, pw, nw,
-                                      stream if stream else None))
+    _call("hb_policy_loss_async", pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, ctypes.byref(args), _vector(stats, "stats", 4),
+          _vector(logp, "logp", B), pd, ldd, pw, nw, stream or None)
 
 
 def preference_args(seq, ref=None, beta=0.1, smoothing=0.0) -> Preference:
@@ -502,11 +515,9 @@ def preference_args(seq, ref=None, beta=0.1, smoothing=0.0) -> Preference:
 
 def preference_loss(Z, y, seq, stats, dZ=None, ref=None, beta=0.1, smoothing=0.0, seq_logp=None, ws=None, stream=None):
     """hb_preference_loss_async: stats (4 floats: loss, accuracy, mean rewards) and dZ (may be Z; None: the loss only)."""
-    pz, ldz, kind = _matrix(Z, "Z")
-    pd, ldd, _ = (None, ldz, 0) if dZ is None else _matrix(dZ, "dZ", Z)
-    B, K = Z.shape
+    m = pz, ldz, kind, B, K = _matrix(Z, "Z")
+    pd, ldd = (None, ldz) if dZ is None else _out_matrix(dZ, "dZ", m)
     pw, nw = _workspace(ws)
     args = preference_args(seq, ref, beta, smoothing)
-    _check(lib().hb_preference_loss_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, ctypes.byref(args),
-                                          _vector(stats, "stats", 4), _vector(seq_logp, "seq_logp", 2 * args.pairs), pd, ldd, pw, nw,
-                                          stream if stream else None))
+    _call("hb_preference_loss_async", pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, ctypes.byref(args),
+          _vector(stats, "stats", 4), _vector(seq_logp, "seq_logp", 2 * args.pairs), pd, ldd, pw, nw, stream or None)
