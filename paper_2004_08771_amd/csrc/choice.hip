@@ -635,8 +635,9 @@ struct Count {
 };
 
 // A block a chunk, without the chosen class; the first chunk has the edges.  A row of one chunk is finished here.
+// chosen (may be null): the chosen logits, for a gradient that may be written over them.
 template <typename T>
-__global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, int pieces_per_chunk, TopSum *partial)
+__global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, int pieces_per_chunk, TopSum *partial, float *chosen)
 {
     constexpr int V = Piece<T>::V, U = 4;
     __shared__ TopSum red[NT / 64];
@@ -699,8 +700,19 @@ __global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, in
             head_row(a.h, in, row, finish_row(zy, top, t.sum * rescale(t.top, top)), true, sums);
         } else {
             partial[blockIdx.x] = t;
+            if (chosen && c == 0) chosen[row] = logit(r, row, y);
         }
     }
+}
+
+// The terms of a row from its chunks, in `lanes` neighbouring lanes (a power of two up to 64), of which this is number g.
+__device__ __forceinline__ RowTerms terms_of_chunks(const TopSum *partial, int chunks, float zy, int g, int lanes)
+{
+    TopSum s = {-INFINITY, 0.f};
+    for (int c = g; c < chunks; c += lanes) s = join(s, partial[c]);
+    for (int o = lanes / 2; o > 0; o >>= 1) s = join(s, TopSum{__shfl_xor(s.top, o, 64), __shfl_xor(s.sum, o, 64)});
+    const float top = fmaxf(s.top, zy);
+    return finish_row(zy, top, s.sum * rescale(s.top, top));
 }
 
 // The rows' terms from their chunks, G lanes a row.
@@ -714,15 +726,7 @@ __global__ __launch_bounds__(NT) void merge_kernel(RowsArgs a, int chunks, const
     for (long long row = (long long)blockIdx.x * (NT / G) + threadIdx.x / G; row < a.r.B; row += per_grid) {
         RowTerms t = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
         const RowInputs in(a.h, a.r, row);
-        if (in.choice(a.r.K)) {
-            const float zy = logit(a.r, row, in.y);
-            TopSum s = {-INFINITY, 0.f};
-            for (int c = g; c < chunks; c += G) s = join(s, partial[row * chunks + c]);
-#pragma unroll
-            for (int o = G / 2; o > 0; o >>= 1) s = join(s, TopSum{__shfl_xor(s.top, o, 64), __shfl_xor(s.sum, o, 64)});
-            const float top = fmaxf(s.top, zy);
-            t = finish_row(zy, top, s.sum * rescale(s.top, top));
-        }
+        if (in.choice(a.r.K)) t = terms_of_chunks(partial + row * chunks, chunks, logit(a.r, row, in.y), g, G);
         head_row(a.h, in, row, t, g == 0, sums);
     }
     if (a.h.kind == HEAD_POLICY) {
@@ -732,17 +736,169 @@ __global__ __launch_bounds__(NT) void merge_kernel(RowsArgs a, int chunks, const
     }
 }
 
+// ---------------------------------------------------------------- pairs of sequences
+__device__ __forceinline__ double softplus(double v) { return fmax(v, 0.0) + log1p(exp(-fabs(v))); }
+__device__ __forceinline__ double sigma(double v) { return v >= 0.0 ? 1.0 / (1.0 + exp(-v)) : exp(v) / (1.0 + exp(v)); }
+
+// The rows of pair n: at[0] .. at[1] - 1 were preferred over at[1] .. at[2] - 1
+struct PairRows {
+    long long at[3];
+    __device__ __forceinline__ PairRows(const PreferenceTerms &p, long long B, int n)
+    {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) at[i] = min(max((long long)p.seq[2 * n + i], i ? at[i - 1] : 0ll), B);
+    }
+};
+
+// s_0 and s_1: sums of log-probabilities over the sequences of pair n
+struct Pair {
+    double up, down;  // what they are above the reference's
+    __device__ __forceinline__ Pair(const PreferenceTerms &p, int n, double s0, double s1)
+        : up(s0 - (p.ref ? (double)p.ref[2 * n] : 0.0)), down(s1 - (p.ref ? (double)p.ref[2 * n + 1] : 0.0))
+    {
+    }
+    __device__ __forceinline__ Four stats(const PreferenceTerms &p) const
+    {
+        const double h = up - down, b = p.beta, eps = p.smoothing, mean = 1.0 / (double)p.pairs;
+        double loss = (1.0 - eps) * softplus(-b * h);
+        if (eps != 0.0) loss += eps * softplus(b * h);
+        return Four{{mean * loss, h > 0.0 ? mean : 0.0, mean * b * up, mean * b * down}};
+    }
+    // the loss' derivative in s_0; in s_1 its negative
+    __device__ __forceinline__ double slope(const PreferenceTerms &p) const
+    {
+        const double h = up - down, b = p.beta, eps = p.smoothing, mean = 1.0 / (double)p.pairs;
+        return b * mean * (eps * sigma(b * h) - (1.0 - eps) * sigma(-b * h));
+    }
+};
+
+__device__ __forceinline__ void store_sums(const PreferenceTerms &p, int n, double s0, double s1)
+{
+    if (!p.seq_logp) return;
+    p.seq_logp[2 * n] = (float)s0;
+    p.seq_logp[2 * n + 1] = (float)s1;
+}
+
+// From a row's terms to its coefficients, g = the loss' derivative in its log-probability
+__device__ __forceinline__ RowCoef slope_of_row(RowCoef c, float g)
+{
+    if (c.scale == 0.f && c.chosen == 0.f) return c;  // takes no part, whatever the slope
+    c.scale *= -g;
+    c.chosen *= g;
+    return c;
+}
+
+// One block per pair.
+__global__ __launch_bounds__(NT) void preference_kernel(PreferenceTerms p, long long B, const double *row_lp, RowCoef *coef,
+                                                        Four *sums)
+{
+    __shared__ Four red[NT / 64];
+    const int n = blockIdx.x;
+    const PairRows rows(p, B, n);
+    Four s = {};
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+        for (long long row = rows.at[q] + threadIdx.x; row < rows.at[q + 1]; row += NT) s.v[q] += row_lp[row];
+    s = sum_block(s, red);
+    const Pair pair(p, n, s.v[0], s.v[1]);
+    if (threadIdx.x == 0) {
+        sums[n] = pair.stats(p);
+        store_sums(p, n, s.v[0], s.v[1]);
+    }
+    if (!coef) return;
+    const double slope = pair.slope(p);
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+        for (long long row = rows.at[q] + threadIdx.x; row < rows.at[q + 1]; row += NT)
+            coef[row] = slope_of_row(coef[row], (float)(q ? -slope : slope));
+}
+
+// Sums over the sequences of a pair in `lanes` neighbouring lanes, of which this is number g
+__device__ __forceinline__ void sums_of_pair(const PairRows &rows, const double *row_lp, int g, int lanes, double (&s)[2])
+{
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        s[q] = 0.0;
+#pragma unroll 4
+        for (long long row = rows.at[q] + g; row < rows.at[q + 1]; row += lanes) s[q] += row_lp[row];
+    }
+    for (int o = lanes / 2; o > 0; o >>= 1) {
+        s[0] += __shfl_xor(s[0], o, 64);
+        s[1] += __shfl_xor(s[1], o, 64);
+    }
+}
+
 // ---------------------------------------------------------------- the gradient in the logits, from the rows' coefficients
-// Rows [*first_row, *end_row) only where there are bounds; the first block adds the sums up where there are any.
+// Rows [*first_row, *end_row) only where there are bounds.
+enum {
+    GRAD_ROWS,    // coefficients, or log-probabilities and what they are multiplied with
+    GRAD_CHUNKS,  // policy: what row_sums_kernel leaves
+    GRAD_PAIRS    // preference: the rows' terms
+};
 struct GradArgs {
     ChoiceRows r;
     ChoiceGrad d;
-    const RowCoef *coef;              // or
+    const RowCoef *coef;              // ROWS: or
     const float *logp, *lse, *g;      // ... of hb_logprob_grad
     const int32_t *first_row, *end_row;
     int chunks, pieces_per_chunk;     // G = NT
+    int first;                        // the first block does something else: it adds up the sums (ROWS), or makes them
     SumFour fin;
+    // CHUNKS: pieces are divided in row_sums_kernel as they are here
+    RowHead h;
+    const TopSum *partial;
+    const float *chosen;
+    // PAIRS
+    PreferenceTerms p;
+    const double *row_lp;
 };
+
+// What a call on few rows has its first block do instead of one more launch: the statistics and what else is returned
+constexpr int FEW = NT / 4;
+__device__ __forceinline__ void few_rows(const GradArgs &a, Four *red)
+{
+    int lanes = 64;
+    while (lanes * a.r.B > NT) lanes /= 2;
+    const int row = threadIdx.x / lanes, g = threadIdx.x % lanes;
+    Four sums = {};
+    if (row < a.r.B) {
+        RowTerms t = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
+        const RowInputs in(a.h, a.r, row);
+        if (in.choice(a.r.K)) t = terms_of_chunks(a.partial + row * a.chunks, a.chunks, a.chosen[row], g, lanes);
+        head_row(a.h, in, row, t, g == 0, sums);
+    }
+    store_stats(a.fin.stats, sum_block(sums, red));
+}
+__device__ __forceinline__ void few_pairs(const GradArgs &a, Four *red)
+{
+    int lanes = 64;
+    while (lanes * a.p.pairs > NT) lanes /= 2;
+    const int n = threadIdx.x / lanes, g = threadIdx.x % lanes;
+    Four sums = {};
+    if (n < a.p.pairs) {
+        double s[2];
+        sums_of_pair(PairRows(a.p, a.r.B, n), a.row_lp, g, lanes, s);
+        if (g == 0) {
+            sums = Pair(a.p, n, s[0], s[1]).stats(a.p);
+            store_sums(a.p, n, s[0], s[1]);
+        }
+    }
+    store_stats(a.fin.stats, sum_block(sums, red));
+}
+
+// The coefficients of a row of one of the pairs, in `lanes` neighbouring lanes.
+__device__ __forceinline__ RowCoef coef_in_pair(const GradArgs &a, long long row, int g, int lanes)
+{
+    int n = 0;  // pairs that end in front of it
+    for (int i = g; i < a.p.pairs; i += lanes) n += a.p.seq[2 * i + 2] <= row;
+    for (int o = lanes / 2; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+    n = min(n, a.p.pairs - 1);
+    const PairRows rows(a.p, a.r.B, n);
+    double s[2];
+    sums_of_pair(rows, a.row_lp, g, lanes, s);
+    const double slope = Pair(a.p, n, s[0], s[1]).slope(a.p);
+    return slope_of_row(a.coef[row], (float)(row < rows.at[1] ? slope : -slope));
+}
 
 __device__ __forceinline__ RowCoef coef_of(const GradArgs &a, long long row, int y)
 {
@@ -760,18 +916,19 @@ __device__ __forceinline__ RowCoef coef_of(const GradArgs &a, long long row, int
 
 // G lanes have a row, or a chunk of one, between them.  The last rows come first: they are what the pass over the logits
 // before this one has left in the caches.
-template <typename T, typename TO, int G>
+template <typename T, typename TO, int G, int FROM>
 __global__ __launch_bounds__(NT) void logit_grad_kernel(GradArgs a)
 {
-    constexpr int V = Piece<T>::V, U = 4;
+    constexpr int V = Piece<T>::V, U = 4, LANES = G < 64 ? G : 64;
     __shared__ Four red[NT / 64];
-    const int first = a.fin.n > 0;
-    if ((int)blockIdx.x < first) {
-        sum_four(a.fin, red);
+    if ((int)blockIdx.x < a.first) {
+        if (FROM == GRAD_CHUNKS) few_rows(a, red);
+        else if (FROM == GRAD_PAIRS) few_pairs(a, red);
+        else sum_four(a.fin, red);
         return;
     }
     const int g = threadIdx.x % G;
-    long long row = blockIdx.x - first;
+    long long row = blockIdx.x - a.first;
     int c = 0;
     if (G == NT) {
         c = (int)(row % a.chunks);
@@ -786,7 +943,15 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradArgs a)
     const Row<T> z(a.r.Z, a.r.ldz, row, a.r.K);
     TO *dz = static_cast<TO *>(a.d.dZ) + row * a.d.ld;
     const int y = a.r.y[row];
-    const RowCoef none_of = {0.f, 0.f, 0.f, 0.f}, k = outside ? none_of : coef_of(a, row, y);
+    RowCoef k = {0.f, 0.f, 0.f, 0.f};
+    if (FROM == GRAD_CHUNKS) {
+        const RowInputs in(a.h, a.r, row);
+        Four sums;
+        if (in.choice(a.r.K))
+            k = head_row(a.h, in, row, terms_of_chunks(a.partial + row * a.chunks, a.chunks, a.chosen[row], g % 64, 64), false, sums);
+    } else if (!outside) {
+        k = FROM == GRAD_PAIRS ? coef_in_pair(a, row, g % LANES, LANES) : coef_of(a, row, y);
+    }
     const int end = G == NT ? min(z.pieces, (c + 1) * a.pieces_per_chunk) : z.pieces;
     const bool none = k.scale == 0.f && k.chosen == 0.f;
     const Under under(k.shift, k.factor);
@@ -821,50 +986,6 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradArgs a)
         }
         for (int j = a.r.K + g; j < a.d.pad; j += G) dz[j] = TO(0.f);
     }
-}
-
-// ---------------------------------------------------------------- pairs of sequences
-__device__ __forceinline__ double softplus(double v) { return fmax(v, 0.0) + log1p(exp(-fabs(v))); }
-__device__ __forceinline__ double sigma(double v) { return v >= 0.0 ? 1.0 / (1.0 + exp(-v)) : exp(v) / (1.0 + exp(v)); }
-
-// One block per pair.
-__global__ __launch_bounds__(NT) void preference_kernel(PreferenceTerms p, long long B, const double *row_lp, RowCoef *coef,
-                                                        Four *sums)
-{
-    __shared__ Four red[NT / 64];
-    const int n = blockIdx.x;
-    long long at[3];
-#pragma unroll
-    for (int i = 0; i < 3; ++i) at[i] = min(max((long long)p.seq[2 * n + i], i ? at[i - 1] : 0ll), B);
-    Four s = {};
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-        for (long long row = at[q] + threadIdx.x; row < at[q + 1]; row += NT) s.v[q] += row_lp[row];
-    s = sum_block(s, red);
-    const double up = s.v[0] - (p.ref ? (double)p.ref[2 * n] : 0.0), down = s.v[1] - (p.ref ? (double)p.ref[2 * n + 1] : 0.0);
-    const double h = up - down, b = p.beta, eps = p.smoothing;
-    const double mean = 1.0 / (double)p.pairs;
-    if (threadIdx.x == 0) {
-        double loss = (1.0 - eps) * softplus(-b * h);
-        if (eps != 0.0) loss += eps * softplus(b * h);
-        sums[n] = Four{{mean * loss, h > 0.0 ? mean : 0.0, mean * b * up, mean * b * down}};
-        if (p.seq_logp) {
-            p.seq_logp[2 * n] = (float)s.v[0];
-            p.seq_logp[2 * n + 1] = (float)s.v[1];
-        }
-    }
-    if (!coef) return;
-    const double slope = b * mean * (eps * sigma(b * h) - (1.0 - eps) * sigma(-b * h));
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-        for (long long row = at[q] + threadIdx.x; row < at[q + 1]; row += NT) {
-            const float g = (float)(q ? -slope : slope);
-            RowCoef c = coef[row];
-            if (c.scale == 0.f && c.chosen == 0.f) continue;  // takes no part, whatever the slope
-            c.scale *= -g;
-            c.chosen *= g;
-            coef[row] = c;
-        }
 }
 
 // ---------------------------------------------------------------- launches
@@ -981,12 +1102,18 @@ hipError_t rows(const RowsArgs &a, int *blocks, hipStream_t stream, const Launch
 }
 
 // The heads of rows in chunks.  blocks: those that leave sums
-hipError_t chunked_rows(RowsArgs a, const Split &s, TopSum *partial, int *blocks, hipStream_t stream, const LaunchEvents &ev)
+hipError_t row_sums(const RowsArgs &a, const Split &s, TopSum *partial, float *chosen, hipStream_t stream, const LaunchEvents &ev)
 {
     const dim3 grid((unsigned)(a.r.B * s.chunks)), block(NT);
-    const hipError_t e = a.r.tensor == TENSOR_BF16
-                             ? launch_kernel(row_sums_kernel<__bf16>, grid, block, stream, ev, a, s.chunks, s.pieces_per_chunk, partial)
-                             : launch_kernel(row_sums_kernel<float>, grid, block, stream, ev, a, s.chunks, s.pieces_per_chunk, partial);
+    return a.r.tensor == TENSOR_BF16
+               ? launch_kernel(row_sums_kernel<__bf16>, grid, block, stream, ev, a, s.chunks, s.pieces_per_chunk, partial, chosen)
+               : launch_kernel(row_sums_kernel<float>, grid, block, stream, ev, a, s.chunks, s.pieces_per_chunk, partial, chosen);
+}
+
+hipError_t chunked_rows(RowsArgs a, const Split &s, TopSum *partial, int *blocks, hipStream_t stream, const LaunchEvents &ev)
+{
+    const dim3 block(NT);
+    const hipError_t e = row_sums(a, s, partial, nullptr, stream, ev);
     if (e != hipSuccess || (s.chunks == 1 && a.h.kind != HEAD_POLICY)) return e;
     *blocks = ceil_div(a.r.B, s.chunks == 1 ? NT : NT / 64);
     if (*blocks > MAX_SUM_BLOCKS) *blocks = MAX_SUM_BLOCKS;
@@ -997,35 +1124,58 @@ hipError_t chunked_rows(RowsArgs a, const Split &s, TopSum *partial, int *blocks
 }
 
 // A row in G lanes
-template <typename T, typename TO, int G>
+template <typename T, typename TO, int G, int FROM>
 hipError_t grad_form(const GradArgs &a, hipStream_t stream, const LaunchEvents &ev)
 {
-    const int blocks = ceil_div(a.r.B, NT / G) + (a.fin.n > 0 ? 1 : 0);
-    return launch_kernel(logit_grad_kernel<T, TO, G>, dim3((unsigned)blocks), dim3(NT), stream, ev, a);
+    const int blocks = ceil_div(a.r.B, NT / G) + a.first;
+    return launch_kernel(logit_grad_kernel<T, TO, G, FROM>, dim3((unsigned)blocks), dim3(NT), stream, ev, a);
 }
 
-template <typename T, typename TO>
+int grad_lanes(const ChoiceRows &r)
+{
+    const int n = most_pieces(r);
+    return n <= 4 ? 4 : n <= 32 ? 8 : n <= 64 ? 16 : n <= 128 ? 32 : n <= 512 ? 64 : NT;
+}
+
+template <typename T, typename TO, int FROM>
 hipError_t grad_of_type(GradArgs a, hipStream_t stream, const LaunchEvents &ev)
 {
-    const int n = most_pieces(a.r), fin = a.fin.n > 0 ? 1 : 0;
     a.chunks = 1;
     a.pieces_per_chunk = 0;
-    if (n <= 4) return grad_form<T, TO, 4>(a, stream, ev);
-    if (n <= 32) return grad_form<T, TO, 8>(a, stream, ev);
-    if (n <= 64) return grad_form<T, TO, 16>(a, stream, ev);
-    if (n <= 128) return grad_form<T, TO, 32>(a, stream, ev);
-    if (n <= 512) return grad_form<T, TO, 64>(a, stream, ev);
+    if constexpr (FROM != GRAD_CHUNKS) {
+        switch (grad_lanes(a.r)) {
+        case 4: return grad_form<T, TO, 4, FROM>(a, stream, ev);
+        case 8: return grad_form<T, TO, 8, FROM>(a, stream, ev);
+        case 16: return grad_form<T, TO, 16, FROM>(a, stream, ev);
+        case 32: return grad_form<T, TO, 32, FROM>(a, stream, ev);
+        case 64: return grad_form<T, TO, 64, FROM>(a, stream, ev);
+        }
+    }
     const Split s = split_for(a.r);
     a.chunks = s.chunks;
     a.pieces_per_chunk = s.pieces_per_chunk;
-    return launch_kernel(logit_grad_kernel<T, TO, NT>, dim3((unsigned)(a.r.B * s.chunks + fin)), dim3(NT), stream, ev, a);
+    return launch_kernel(logit_grad_kernel<T, TO, NT, FROM>, dim3((unsigned)(a.r.B * s.chunks + a.first)), dim3(NT), stream, ev, a);
 }
 
+template <int FROM>
 hipError_t logit_grad(GradArgs a, hipStream_t stream, const LaunchEvents &ev)
 {
     a.d.past = past_caches(a.r, a.d);
-    if (a.r.tensor == TENSOR_BF16) return grad_of_type<__bf16, __bf16>(a, stream, ev);
-    return a.d.tensor == TENSOR_BF16 ? grad_of_type<float, __bf16>(a, stream, ev) : grad_of_type<float, float>(a, stream, ev);
+    a.first = FROM != GRAD_ROWS || a.fin.n > 0;
+    if (a.r.tensor == TENSOR_BF16) return grad_of_type<__bf16, __bf16, FROM>(a, stream, ev);
+    return a.d.tensor == TENSOR_BF16 ? grad_of_type<float, __bf16, FROM>(a, stream, ev) : grad_of_type<float, float, FROM>(a, stream, ev);
+}
+
+// Whether the gradient's kernel sums up the pairs itself, each row those of its own, and its first block all of them: one launch
+// less, as long as sums of all rows in a row's lanes, or in a pair's of the first block, stay short (a pair may have all rows).
+// In one stream, us, sequences of one length and all rows in the first, with a launch for the pairs and without: 300 x 983 fp32,
+// 4 pairs 13.6 / 10.9 and 13.1 / 10.9; 2048 x 983, 16 pairs 18.2 / 15.4 and 20.7 / 17.4; 1024 x 32000 bf16, 16 pairs 53.5 / 50.9 and
+// 53.9 / 52.2; beyond the lines 4096 x 983, 16 pairs 22.4 / 20.4 and 29.0 / 30.6, 64 pairs 22.4 / 19.9 and 29.0 / 63.7; 1024 x 7, 64
+// pairs 9.3 / 8.2 and 10.0 / 27.1.
+bool pairs_in_grad(const ChoiceRows &r, int pairs)
+{
+    const int lanes = grad_lanes(r) < 64 ? grad_lanes(r) : 64;
+    return pairs <= FEW && r.B <= 32 * lanes && r.B * pairs <= 128 * NT;
 }
 
 // more: room for SUM_SLICES
@@ -1074,7 +1224,7 @@ hipError_t launch_logprob_grad(const ChoiceRows &r, const float *logp, const flo
     a.logp = logp;
     a.lse = lse;
     a.g = g;
-    return logit_grad(a, stream, ev);
+    return logit_grad<GRAD_ROWS>(a, stream, ev);
 }
 
 hipError_t launch_policy(const ChoiceRows &r, const PolicyTerms &t, const ChoiceGrad &d, void *ws, hipStream_t stream,
@@ -1096,17 +1246,30 @@ hipError_t launch_policy(const ChoiceRows &r, const PolicyTerms &t, const Choice
         const hipError_t e = rows(a, &fin.n, stream, ev);
         return e != hipSuccess || fin.n == 1 ? e : add_sums(fin, more, stream);
     }
-    a.h.coef = d.dZ ? w.coef : nullptr;
-    const hipError_t e = chunked_rows(a, split_for(r), w.partial, &fin.n, stream, ev);
-    if (e != hipSuccess) return e;
-    if (fin.n == 1) fin.n = 0;
-    if (!d.dZ) return fin.n ? add_sums(fin, nullptr, stream) : hipSuccess;
     GradArgs g = {};
     g.r = r;
     g.d = d;
+    const Split s = split_for(r);
+    // Chunks of few rows: their gradient's kernel joins them itself, and one block of it makes the sums (in one stream, with a launch
+    // for that and without, us: 24 x 131072 fp32 19.1 / 16.1, 1 x 131072 10.3 / 9.3, 64 x 500000 bf16 54.9 / 51.9).
+    if (d.dZ && r.B <= FEW) {
+        float *const chosen = reinterpret_cast<float *>(w.coef);
+        const hipError_t e = row_sums(a, s, w.partial, chosen, stream, ev);
+        if (e != hipSuccess) return e;
+        g.h = a.h;
+        g.partial = w.partial;
+        g.chosen = chosen;
+        g.fin.stats = t.stats;
+        return logit_grad<GRAD_CHUNKS>(g, stream, LaunchEvents());
+    }
+    a.h.coef = d.dZ ? w.coef : nullptr;
+    const hipError_t e = chunked_rows(a, s, w.partial, &fin.n, stream, ev);
+    if (e != hipSuccess) return e;
+    if (fin.n == 1) fin.n = 0;
+    if (!d.dZ) return fin.n ? add_sums(fin, nullptr, stream) : hipSuccess;
     g.coef = w.coef;
     g.fin = fin;
-    return logit_grad(g, stream, LaunchEvents());
+    return logit_grad<GRAD_ROWS>(g, stream, LaunchEvents());
 }
 
 hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, const ChoiceGrad &d, void *ws, hipStream_t stream,
@@ -1121,20 +1284,25 @@ hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, cons
     int blocks = 0;
     hipError_t e = hipSuccess;
     if (r.B > 0) e = rows_in_registers(r, false) ? rows(a, &blocks, stream, ev) : chunked_rows(a, split_for(r), w.partial, &blocks, stream, ev);
-    if (e == hipSuccess)
-        e = launch_kernel(preference_kernel, dim3((unsigned)t.pairs), dim3(NT), stream, LaunchEvents(), t, r.B,
-                          (const double *)w.row_lp, d.dZ ? w.coef : nullptr, w.sums);
-    const SumFour fin = {w.sums, t.pairs, t.stats};
     if (e != hipSuccess) return e;
-    if (!d.dZ || r.B == 0) return launch_kernel(sum_four_kernel, dim3(1), dim3(SUM_THREADS), stream, LaunchEvents(), fin);
     GradArgs g = {};
     g.r = r;
     g.d = d;
     g.coef = w.coef;
     g.first_row = t.seq;
     g.end_row = t.seq + 2 * t.pairs;
-    g.fin = fin;
-    return logit_grad(g, stream, LaunchEvents());
+    if (d.dZ && r.B > 0 && pairs_in_grad(r, t.pairs)) {
+        g.p = t;
+        g.row_lp = w.row_lp;
+        g.fin.stats = t.stats;
+        return logit_grad<GRAD_PAIRS>(g, stream, LaunchEvents());
+    }
+    e = launch_kernel(preference_kernel, dim3((unsigned)t.pairs), dim3(NT), stream, LaunchEvents(), t, r.B, (const double *)w.row_lp,
+                      d.dZ ? w.coef : nullptr, w.sums);
+    g.fin = {w.sums, t.pairs, t.stats};
+    if (e != hipSuccess) return e;
+    if (!d.dZ || r.B == 0) return launch_kernel(sum_four_kernel, dim3(1), dim3(SUM_THREADS), stream, LaunchEvents(), g.fin);
+    return logit_grad<GRAD_ROWS>(g, stream, LaunchEvents());
 }
 
 }  // namespace hb

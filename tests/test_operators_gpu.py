@@ -320,7 +320,7 @@ def policy_tols(z, y, old, adv, refs, w, clip, kl, stats, lp, want, g, K, dtype)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("B,K", SHAPES + [(2000, 7), (1100, 130)])
+@pytest.mark.parametrize("B,K", SHAPES + [(2000, 7), (1100, 130), (1, 100001), (33, 99991), (64, 49999)])
 def test_policy_loss_and_its_gradient(B, K, dtype):
     rng = np.random.default_rng(B + 31 * K)
     z, y, old, adv, refs, w = policy_inputs(B, K, rng, dtype)
@@ -425,6 +425,7 @@ def near_on_device(got, want, Z, g, K, dtype, what):
     (17000, 4099, "bf16"),    # ... of odd rows
     (1030, 50001, "f32"),     # long rows, many: whole rows by a block where they are only read
     (1030, 82003, "f32"),     # too long for registers, one chunk a row
+    (66, 82003, "f32"),       # ... several
     (70, 52000, "f32"), (66, 70003, "f32"), (70, 110001, "bf16"), (66, 150001, "bf16"),  # a row in 1024 lanes
     (4, 300007, "bf16"), (1, 1 << 20, "f32"),
 ])
@@ -524,7 +525,8 @@ def preference_tols(z, y, seq, refs, beta, eps, stats, s, want, g, K, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("B,K,pairs", [(1, 3, 1), (2, 7, 1), (40, 7, 3), (167, 983, 4), (64, 64, 40), (90, 2050, 2), (9, 33000, 2),
-                                       (5, 70001, 1), (700, 20, 1), (2500, 5, 7)])
+                                       (5, 70001, 1), (700, 20, 1), (2500, 5, 7), (300, 983, 70), (130, 2050, 65), (70, 9001, 66), (1500, 300, 50),
+                                       (128, 9, 64), (2300, 600, 3)])
 def test_preference_loss_and_its_gradient(B, K, pairs, dtype):
     rng = np.random.default_rng(B + K * 3 + pairs)
     z, y, seq, refs = preference_case(B, K, pairs, rng, dtype)
