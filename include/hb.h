@@ -209,8 +209,9 @@ int hb_batch_loss_csr_async(hb_model *m, const int32_t *d_row_ptr, const int32_t
  * gradient read them, and the gradient on its way back through them with the mask that hb_dropout_async has for (seed, offset
  * 32 n + l) and a B x d_l matrix, so a call can be made again, here or elsewhere.  p as there; 0 switches it off.
  * bf16 mode: what a layer keeps is rounded once more.  A replay of a captured step repeats the masks of the captured call.
- * The first call with p > 0 allocates one more buffer for each hidden layer.  hb_model_get_activations gives the activations before
- * dropout.  The network then runs layer by layer (not in the kernels of whole small networks or fused output layers).
+ * The first call with p > 0 allocates one more buffer for each hidden layer (the handle's device has to be current).
+ * hb_model_get_activations gives the activations before dropout.  The network then runs layer by layer (not in the kernels of
+ * whole small networks or fused output layers).
  */
 int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call);
 
@@ -224,7 +225,7 @@ int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call
  *   hb_policy_grad_async      its gradient instead (d_grad_flat: P floats, flat layout); the replica is left untouched
  *   hb_preference_step_async, hb_preference_grad_async   the same of the preference loss
  * Nothing is synchronised; the calls enqueue kernels only and may be captured once one ordinary call of them has been made (the
- * first allocates the handle's workspace for them).
+ * first allocates the handle's workspace for them).  The handle's device has to be current.
  */
 struct hb_policy;
 struct hb_preference;
@@ -485,7 +486,8 @@ int hb_hogbatch_run_epoch(hb_sched *s, hb_model *gpu, int32_t gpu_worker, int32_
  * base address that is aligned to the elements, any ld).  The calls only enqueue kernels on
  * hip_stream (a hipStream_t, NULL = the default stream): nothing is allocated, copied, cleared or synchronised, so they may be
  * captured.  Everything has to be on the device that is current at the call, the stream too: pointers that are not in
- * its memory are HB_ERR_INVALID, as is a stream of another device.  Inputs are only read, and only in stream order.
+ * its memory are HB_ERR_INVALID, as is a stream of another device.  Inputs are only read, and only in stream order.  What a
+ * call writes must not overlap what it reads or what else it writes (HB_ERR_INVALID), but where it says so.
  */
 enum { HB_TENSOR_F32 = 0, HB_TENSOR_BF16 = 1 };
 

@@ -1806,6 +1806,15 @@ float hb_batch_grad_csr(hb_model *m, const int32_t *d_row_ptr, const int32_t *d_
     return out;
 }
 
+// Calls that may allocate do so on the current device: it has to be the handle's.
+static int check_current_device(const hb_model *m)
+{
+    int dev = -1;
+    HB_HIP(hipGetDevice(&dev));
+    if (dev != m->device) return fail(HB_ERR_INVALID, "the handle is of device %d, the current device is %d", m->device, dev);
+    return HB_OK;
+}
+
 int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call)
 {
     int rc = check_handle(m, true);
@@ -1814,6 +1823,8 @@ int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call
     rc = check_dropout_p(p, &threshold);
     if (rc != HB_OK) return rc;
     if (next_call >> 59) return fail(HB_ERR_INVALID, "next_call = %llu is not below 2^59", (unsigned long long)next_call);
+    rc = check_current_device(m);
+    if (rc != HB_OK) return rc;
     if (threshold > 0 && m->drop.empty()) {
         std::vector<void *> buffers((size_t)m->L + 1, nullptr);
         for (int l = 1; l < m->L; ++l) {
@@ -1842,7 +1853,7 @@ static int validate_head_call(hb_model *m, const void *dX, const int32_t *dy, in
     int rc = validate_batch_call(m, dX, dy, B, false, false);
     if (rc != HB_OK) return rc;
     if (m->loss != HB_LOSS_SOFTMAX_CE) return fail(HB_ERR_INVALID, "this call needs a model with HB_LOSS_SOFTMAX_CE");
-    return HB_OK;
+    return check_current_device(m);
 }
 
 static int run_head_call(hb_model *m, const void *dX, const int32_t *dy, int64_t B, float lr, StepMode mode, float *d_grad_flat,
@@ -1868,6 +1879,7 @@ int hb_batch_logprob_async(hb_model *m, const void *dX, const int32_t *dy, int64
     const int rc = validate_head_call(m, dX, dy, B);
     if (rc != HB_OK) return rc;
     if (!d_logp) return fail(HB_ERR_INVALID, "d_logp is NULL");
+    if (d_lse == d_logp) return fail(HB_ERR_INVALID, "d_lse overlaps d_logp");
     Head head;
     head.logp = d_logp;
     head.lse = d_lse;
@@ -1882,6 +1894,8 @@ static int policy_call(hb_model *m, const void *dX, const int32_t *dy, int64_t B
     if (rc != HB_OK) return rc;
     if (!policy->d_old_logp || !policy->d_adv) return fail(HB_ERR_INVALID, "d_old_logp or d_adv is NULL");
     if (!d_stats) return fail(HB_ERR_INVALID, "d_stats is NULL");
+    rc = check_policy_apart(policy, dy, B, d_stats, d_logp, nullptr, 0, nullptr, 0, 0, TENSOR_F32, nullptr, 0);
+    if (rc != HB_OK) return rc;
     const PolicyTerms t = policy_terms(policy, B, d_stats, d_logp);
     Head head;
     head.policy = &t;
@@ -1910,6 +1924,8 @@ static int preference_call(hb_model *m, const void *dX, const int32_t *dy, int64
     if (preference->pairs > m->max_B)
         return fail(HB_ERR_INVALID, "pairs = %d is more than max_B = %lld", preference->pairs, (long long)m->max_B);
     if (!d_stats) return fail(HB_ERR_INVALID, "d_stats is NULL");
+    rc = check_preference_apart(preference, dy, B, d_stats, d_seq_logp, nullptr, 0, nullptr, 0, 0, TENSOR_F32, nullptr, 0);
+    if (rc != HB_OK) return rc;
     const PreferenceTerms t = preference_terms(preference, d_stats, d_seq_logp);
     Head head;
     head.preference = &t;

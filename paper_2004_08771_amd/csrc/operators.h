@@ -80,6 +80,12 @@ hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, cons
 int check_dropout_p(float p, unsigned *threshold);
 int check_policy(const hb_policy *p);
 int check_preference(const hb_preference *p);
+// what they write apart from what they read, but for d_dZ and d_Z; Z, dZ and ws may be null
+int check_policy_apart(const hb_policy *p, const int32_t *y, int64_t B, const float *stats, const float *logp, const void *Z,
+                       int64_t ldz, const void *dZ, int64_t lddz, int64_t K, int tensor, const void *ws, size_t ws_bytes);
+int check_preference_apart(const hb_preference *p, const int32_t *y, int64_t B, const float *stats, const float *seq_logp,
+                           const void *Z, int64_t ldz, const void *dZ, int64_t lddz, int64_t K, int tensor, const void *ws,
+                           size_t ws_bytes);
 PolicyTerms policy_terms(const hb_policy *p, int64_t B, float *d_stats, float *d_logp);
 PreferenceTerms preference_terms(const hb_preference *p, float *d_stats, float *d_seq_logp);
 

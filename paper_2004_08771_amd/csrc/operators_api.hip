@@ -21,16 +21,33 @@ int check_type(int tensor)
 
 bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// rows x cols elements of `size` bytes from p on, `ld` apart
+// rows x cols elements of `size` bytes from p on, `ld` apart; or n bytes.  A null pointer has none.
 struct Block {
     const char *begin, *end;
-    Block(const void *p, int64_t rows, int64_t cols, int64_t ld, size_t size)
+    const char *name;
+    Block(const void *p, int64_t rows, int64_t cols, int64_t ld, size_t size, const char *name_ = "")
         : begin(static_cast<const char *>(p)),
-          end(begin + (rows > 0 && cols > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * size : 0))
+          end(begin + (p && rows > 0 && cols > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * size : 0)), name(name_)
     {
     }
+    Block(const void *p, size_t bytes, const char *name_) : begin(static_cast<const char *>(p)), end(begin + (p ? bytes : 0)), name(name_) {}
     bool meets(const Block &o) const { return begin < o.end && o.begin < end; }
 };
+
+// What a call writes has to be apart from what it reads, and from what else it writes.  (A block of the launch may have written
+// where another still has to read.)  skip: that many of either list may be the same memory
+template <int N, int M>
+int check_apart(const Block (&outs)[N], const Block (&ins)[M], int skip = 0)
+{
+    for (int i = 0; i < N; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (outs[i].meets(outs[j])) return set_error(HB_ERR_INVALID, "%s overlaps %s", outs[i].name, outs[j].name);
+        for (int j = 0; j < M; ++j)
+            if ((i >= skip || j >= skip) && outs[i].meets(ins[j]))
+                return set_error(HB_ERR_INVALID, "%s overlaps %s", outs[i].name, ins[j].name);
+    }
+    return HB_OK;
+}
 
 // in place (the same rows), or apart
 int check_out(const void *in, int64_t ldi, const void *out, int64_t ldo, int64_t rows, int64_t cols, size_t size, const char *what)
@@ -168,6 +185,26 @@ int check_preference(const hb_preference *p)
     return HB_OK;
 }
 
+int check_policy_apart(const hb_policy *p, const int32_t *y, int64_t B, const float *stats, const float *logp, const void *Z,
+                       int64_t ldz, const void *dZ, int64_t lddz, int64_t K, int tensor, const void *ws, size_t ws_bytes)
+{
+    const size_t n = sizeof(float) * (size_t)B, size = size_of(tensor);
+    return check_apart<4, 6>({{dZ, B, K, lddz, size, "d_dZ"}, {stats, 4 * sizeof(float), "d_stats"}, {logp, n, "d_logp"}, {ws, ws_bytes, "d_ws"}},
+                             {{Z, B, K, ldz, size, "d_Z"}, {y, n, "d_y"}, {p->d_old_logp, n, "d_old_logp"}, {p->d_ref_logp, n, "d_ref_logp"},
+                              {p->d_adv, n, "d_adv"}, {p->d_weight, n, "d_weight"}}, 1);
+}
+
+int check_preference_apart(const hb_preference *p, const int32_t *y, int64_t B, const float *stats, const float *seq_logp,
+                           const void *Z, int64_t ldz, const void *dZ, int64_t lddz, int64_t K, int tensor, const void *ws,
+                           size_t ws_bytes)
+{
+    const size_t n = sizeof(float) * (size_t)B, pairs = 2 * sizeof(float) * (size_t)p->pairs, size = size_of(tensor);
+    return check_apart<4, 4>({{dZ, B, K, lddz, size, "d_dZ"}, {stats, 4 * sizeof(float), "d_stats"}, {seq_logp, pairs, "d_seq_logp"},
+                              {ws, ws_bytes, "d_ws"}},
+                             {{Z, B, K, ldz, size, "d_Z"}, {y, n, "d_y"}, {p->d_seq, pairs + sizeof(int32_t), "d_seq"},
+                              {p->d_ref_logp, pairs, "d_ref_logp"}}, 1);
+}
+
 PolicyTerms policy_terms(const hb_policy *p, int64_t B, float *d_stats, float *d_logp)
 {
     PolicyTerms t = {};
@@ -239,6 +276,10 @@ int hb_logprob_async(const void *d_Z, int64_t ldz, int tensor, const int32_t *d_
     if (rc != HB_OK) return rc;
     if (B == 0) return HB_OK;
     if (!d_logp) return set_error(HB_ERR_INVALID, "d_logp is NULL");
+    const size_t n = sizeof(float) * (size_t)B;
+    rc = check_apart<3, 2>({{d_logp, n, "d_logp"}, {d_lse, n, "d_lse"}, {d_ws, choice_workspace(B, 0), "d_ws"}},
+                           {{d_Z, B, K, ldz, size_of(tensor), "d_Z"}, {d_y, n, "d_y"}});
+    if (rc != HB_OK) return rc;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     rc = check_device({{d_Z, "d_Z"}, {d_y, "d_y"}, {d_logp, "d_logp"}, {d_lse, "d_lse"}, {d_ws, "d_ws"}}, stream);
     if (rc != HB_OK) return rc;
@@ -253,6 +294,10 @@ int hb_logprob_grad_async(const void *d_Z, int64_t ldz, int tensor, const int32_
     if (rc != HB_OK) return rc;
     if (B == 0) return HB_OK;
     if (!d_logp || !d_lse || !d_g || !d_dZ) return set_error(HB_ERR_INVALID, "d_logp, d_lse, d_g or d_dZ is NULL");
+    const size_t n = sizeof(float) * (size_t)B;
+    rc = check_apart<1, 4>({{d_dZ, B, K, lddz, size_of(tensor), "d_dZ"}},
+                           {{d_y, n, "d_y"}, {d_logp, n, "d_logp"}, {d_lse, n, "d_lse"}, {d_g, n, "d_g"}});
+    if (rc != HB_OK) return rc;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     rc = check_device({{d_Z, "d_Z"}, {d_y, "d_y"}, {d_logp, "d_logp"}, {d_lse, "d_lse"}, {d_g, "d_g"}, {d_dZ, "d_dZ"}}, stream);
     if (rc != HB_OK) return rc;
@@ -272,6 +317,8 @@ int hb_policy_loss_async(const void *d_Z, int64_t ldz, int tensor, const int32_t
     if (rc != HB_OK) return rc;
     if (!d_stats) return set_error(HB_ERR_INVALID, "d_stats is NULL");
     if (B > 0 && (!policy->d_old_logp || !policy->d_adv)) return set_error(HB_ERR_INVALID, "d_old_logp or d_adv is NULL");
+    rc = check_policy_apart(policy, d_y, B, d_stats, d_logp, d_Z, ldz, d_dZ, lddz, K, tensor, d_ws, choice_workspace(B, 0));
+    if (rc != HB_OK) return rc;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     rc = check_device({{d_Z, "d_Z"}, {d_y, "d_y"}, {policy->d_old_logp, "d_old_logp"}, {policy->d_ref_logp, "d_ref_logp"},
                        {policy->d_adv, "d_adv"}, {policy->d_weight, "d_weight"}, {d_stats, "d_stats"}, {d_logp, "d_logp"},
@@ -293,6 +340,9 @@ int hb_preference_loss_async(const void *d_Z, int64_t ldz, int tensor, const int
     if (rc == HB_OK) rc = check_workspace(d_ws, ws_bytes, B, preference->pairs);
     if (rc != HB_OK) return rc;
     if (!d_stats) return set_error(HB_ERR_INVALID, "d_stats is NULL");
+    rc = check_preference_apart(preference, d_y, B, d_stats, d_seq_logp, d_Z, ldz, d_dZ, lddz, K, tensor, d_ws,
+                                choice_workspace(B, preference->pairs));
+    if (rc != HB_OK) return rc;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     rc = check_device({{d_Z, "d_Z"}, {d_y, "d_y"}, {preference->d_seq, "d_seq"}, {preference->d_ref_logp, "d_ref_logp"},
                        {d_stats, "d_stats"}, {d_seq_logp, "d_seq_logp"}, {d_dZ, "d_dZ"}, {d_ws, "d_ws"}},

@@ -354,6 +354,8 @@ def test_refusals_of_a_handle():
                  lambda: m.policy_step_async(X, y, 32, 0.1, bad_pol, st), lambda: m.policy_grad_async(X, y, 32, pol, None, st),
                  lambda: m.preference_step_async(X, y, 32, 0.1, many, st), lambda: m.preference_grad_async(X, y, 32, prf, None, st),
                  lambda: m.preference_grad_async(X, y, 32, prf, g, None), lambda: m.batch_logprob_async(X, y, 32, None),
+                 lambda: m.policy_step_async(X, y, 32, 0.1, pol, st, v), lambda: m.policy_step_async(X, y, 32, 0.1, pol, v),
+                 lambda: m.preference_step_async(X, y, 32, 0.1, prf, st, st), lambda: m.batch_logprob_async(X, y, 32, v, v),
                  lambda: m.set_dropout(1.0), lambda: m.set_dropout(-0.1), lambda: m.set_dropout(0.1, 0, 1 << 59)):
         with pytest.raises(hb.HbError) as e:
             call()

@@ -91,6 +91,26 @@ def test_losses_refuse_operands():
     refused(lambda: hb.policy_loss(Z, Y, ROW, ROW, STATS[:3], ws=WS))
 
 
+def test_losses_refuse_outputs_that_overlap():
+    r, d = torch.zeros(4, 6), torch.zeros_like(Z)
+    far = torch.zeros(64)
+    both, four = far[:6], far[3:7]
+    for call in (lambda: hb.logprob(Z, Y, r[0], r[0], ws=WS), lambda: hb.logprob(Z, Y, both, far[5:11], ws=WS),
+                 lambda: hb.logprob(Z, Y, Z.view(-1)[54:], None, ws=WS), lambda: hb.logprob(Z, Y, WS.view(torch.float32)[:6], None, ws=WS),
+                 lambda: hb.logprob_grad(Z, Y, r[0], r[1], d.view(-1)[:6], d), lambda: hb.logprob_grad(Z, Y, d.view(-1)[54:], r[1], r[2], d),
+                 lambda: hb.policy_loss(Z, Y, r[0], r[1], STATS, logp=r[0], ws=WS),
+                 lambda: hb.policy_loss(Z, Y, r[0], r[1], STATS, logp=r[1], ws=WS),
+                 lambda: hb.policy_loss(Z, Y, r[0], r[1], STATS, logp=r[2], ref=r[2], ws=WS),
+                 lambda: hb.policy_loss(Z, Y, r[0], r[1], STATS, logp=r[2], weight=r[2], ws=WS),
+                 lambda: hb.policy_loss(Z, Y, r[0], r[1], four, logp=both, ws=WS),
+                 lambda: hb.policy_loss(Z, Y, r[0], r[1], d.view(-1)[:4], dZ=d, ws=WS),
+                 lambda: hb.policy_loss(Z, Y, r[0], r[1], STATS, dZ=d, logp=Z.view(-1)[:6], ws=WS),
+                 lambda: hb.preference_loss(Z, Y, SEQ, STATS, seq_logp=STATS[:2], ws=WS),
+                 lambda: hb.preference_loss(Z, Y, SEQ, STATS, seq_logp=r[0][:2], ref=r[0][:2], ws=WS),
+                 lambda: hb.preference_loss(Z, Y, SEQ, d.view(-1)[:4], dZ=d, ws=WS)):
+        refused(call, text="overlaps")
+
+
 @pytest.mark.parametrize("more", [dict(clip=(-0.1, 0.2)), dict(clip=(1.1, 0.2)), dict(clip=(0.2, -0.2)),
                                   dict(clip=(float("nan"), 0.2)), dict(clip=(0.2, float("inf"))), dict(kl_coef=0.1),
                                   dict(kl_coef=-0.1, ref=ROW), dict(kl_coef=float("nan"), ref=ROW)])
