@@ -623,12 +623,6 @@ __device__ __forceinline__ float rescale(float from, float to)
     return f.far == t.far ? exp2_of(f.shift - t.shift) : 0.f;
 }
 
-__device__ __forceinline__ TopSum join(TopSum a, TopSum b)
-{
-    const float top = fmaxf(a.top, b.top);
-    return {top, a.sum * rescale(a.top, top) + b.sum * rescale(b.top, top)};
-}
-
 template <int N>
 struct Count {
     static constexpr int value = N;
@@ -640,7 +634,7 @@ template <typename T>
 __global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, int pieces_per_chunk, TopSum *partial, float *chosen)
 {
     constexpr int V = Piece<T>::V, U = 4;
-    __shared__ TopSum red[NT / 64];
+    __shared__ float red_top[NT / 64], red_sum[NT / 64];
     const ChoiceRows &r = a.r;
     const long long row = blockIdx.x / chunks;
     const int c = blockIdx.x % chunks;
@@ -688,19 +682,23 @@ __global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, in
     int p = c * pieces_per_chunk + (int)threadIdx.x;
     for (; p + (U - 1) * NT < end; p += U * NT) pieces(Count<U>(), p);
     for (; p < end; p += NT) pieces(Count<1>(), p);
+    // The maximum first, so that every sum is rescaled once more, not at each step of the way
+    const bool whole = chunks == 1 && a.h.kind != HEAD_POLICY;  // (its sums are added up over the rows)
+    const float zy = logit(r, row, y);
+    float top = max_of_row<NT, NT / 64>(whole ? fmaxf(t.top, zy) : t.top, red_top);
+    t.sum *= rescale(t.top, top);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) t = join(t, TopSum{__shfl_xor(t.top, o, 64), __shfl_xor(t.sum, o, 64)});
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = t;
+    for (int o = 32; o > 0; o >>= 1) t.sum += __shfl_xor(t.sum, o, 64);
+    if ((threadIdx.x & 63) == 0) red_sum[threadIdx.x >> 6] = t.sum;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < NT / 64; ++w) t = join(t, red[w]);
-        if (chunks == 1 && a.h.kind != HEAD_POLICY) {  // (its sums are added up over the rows)
-            const float zy = logit(r, row, y), top = fmaxf(t.top, zy);
+        for (int w = 1; w < NT / 64; ++w) t.sum += red_sum[w];
+        if (whole) {
             Four sums = {};
-            head_row(a.h, in, row, finish_row(zy, top, t.sum * rescale(t.top, top)), true, sums);
+            head_row(a.h, in, row, finish_row(zy, top, t.sum), true, sums);
         } else {
-            partial[blockIdx.x] = t;
-            if (chosen && c == 0) chosen[row] = logit(r, row, y);
+            partial[blockIdx.x] = TopSum{top, t.sum};
+            if (chosen && c == 0) chosen[row] = zy;
         }
     }
 }
@@ -708,11 +706,12 @@ __global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, in
 // The terms of a row from its chunks, in `lanes` neighbouring lanes (a power of two up to 64), of which this is number g.
 __device__ __forceinline__ RowTerms terms_of_chunks(const TopSum *partial, int chunks, float zy, int g, int lanes)
 {
-    TopSum s = {-INFINITY, 0.f};
-    for (int c = g; c < chunks; c += lanes) s = join(s, partial[c]);
-    for (int o = lanes / 2; o > 0; o >>= 1) s = join(s, TopSum{__shfl_xor(s.top, o, 64), __shfl_xor(s.sum, o, 64)});
-    const float top = fmaxf(s.top, zy);
-    return finish_row(zy, top, s.sum * rescale(s.top, top));
+    float top = zy, others = 0.f;
+    for (int c = g; c < chunks; c += lanes) top = fmaxf(top, partial[c].top);
+    for (int o = lanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    for (int c = g; c < chunks; c += lanes) others += partial[c].sum * rescale(partial[c].top, top);
+    for (int o = lanes / 2; o > 0; o >>= 1) others += __shfl_xor(others, o, 64);
+    return finish_row(zy, top, others);
 }
 
 // The rows' terms from their chunks, G lanes a row.
