@@ -853,7 +853,7 @@ struct GradArgs {
 };
 
 // What a call on few rows has its first block do instead of one more launch: the statistics and what else is returned
-constexpr int FEW = NT / 4;
+constexpr int FEW = NT;
 __device__ __forceinline__ void few_rows(const GradArgs &a, Four *red)
 {
     int lanes = 64;
@@ -1026,14 +1026,16 @@ constexpr int ROW_PIECES = 20 * 1024;  // the longest row that rows_kernel has a
 
 // Rows go through registers, but for long ones that are few (a workgroup each leaves most of the device idle) or, where they are only
 // read, many (one workgroup of 1024 a compute unit waits between its rows), and those too long for a workgroup.
-// Measured on both sides of the lines, data from memory, us, registers against chunks (bf16): policy loss 4 x 32000 12.0 / 13.2,
-// 16 x 65000 15.1 / 15.9, 64 x 65000 18.1 / 19.8 (4 x 65000 14.6 / 13.2); 16 x 128000 22.7 / 17.6, 64 x 128000 25.9 / 23.5, 128 x 128000
-// 27.5 / 31.9, 256 x 128000 39.3 / 56.8; log-probabilities 64 x 65000 9.2 / 10.7, 1000 x 65000 33.2 / 35.8, 16 x 128000 12.1 / 9.8,
-// 1000 x 128000 74.9 / 57.7.
+// Measured on both sides of the lines, data from memory, us, registers against chunks: policy loss 4 x 32000 bf16 11.9 / 9.7, 16 x 32000
+// fp32 11.2 / 11.3, 64 x 32000 14.2 / 13.5 and 14.2 / 15.3, 4 x 65000 bf16 14.7 / 11.3, 64 x 65000 18.0 / 15.6, 64 x 49000 fp32 18.1 / 17.1,
+// 64 x 16000 bf16 10.2 / 12.0; 128 x 65000 19.8 / 19.6, 128 x 130000 27.1 / 28.1, 256 x 130000 40.2 / 52.7, 128 x 80000 fp32
+// 29.4 / 33.3; log-probabilities 4 x 32000 bf16 6.3 / 6.9, 4 x 65000 8.5 / 6.9, 64 x 65000 9.2 / 9.5, 64 x 49000 fp32 10.3 / 9.6,
+// 1000 x 65000 bf16 33.2 / 35.8, 1000 x 128000 74.9 / 57.7.
 bool rows_in_registers(const ChoiceRows &r, bool grad)
 {
+    if (r.B <= 64 && r.K > 32768) return false;
     const int n = most_pieces(r);
-    return n <= 12288 || (grad && n <= ROW_PIECES && r.B > 64);
+    return n <= 12288 || (grad && n <= ROW_PIECES);
 }
 
 Split split_for(const ChoiceRows &r)
@@ -1114,11 +1116,15 @@ hipError_t chunked_rows(RowsArgs a, const Split &s, TopSum *partial, int *blocks
     const dim3 block(NT);
     const hipError_t e = row_sums(a, s, partial, nullptr, stream, ev);
     if (e != hipSuccess || (s.chunks == 1 && a.h.kind != HEAD_POLICY)) return e;
-    *blocks = ceil_div(a.r.B, s.chunks == 1 ? NT : NT / 64);
+    // One block makes a loss' sums itself, if fewer lanes a row make it one
+    const int lanes = s.chunks == 1 ? 1 : a.h.kind != HEAD_POLICY || a.r.B <= 4 || a.r.B > 64 ? 64 : a.r.B <= 16 ? 16 : 4;
+    *blocks = ceil_div(a.r.B, NT / lanes);
     if (*blocks > MAX_SUM_BLOCKS) *blocks = MAX_SUM_BLOCKS;
     if (*blocks > 1) a.stats = nullptr;
     const dim3 merge((unsigned)*blocks);
-    return s.chunks == 1 ? launch_kernel(merge_kernel<1>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial)
+    if (lanes == 16) return launch_kernel(merge_kernel<16>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial);
+    if (lanes == 4) return launch_kernel(merge_kernel<4>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial);
+    return lanes == 1 ? launch_kernel(merge_kernel<1>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial)
                          : launch_kernel(merge_kernel<64>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial);
 }
 

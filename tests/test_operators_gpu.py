@@ -320,7 +320,7 @@ def policy_tols(z, y, old, adv, refs, w, clip, kl, stats, lp, want, g, K, dtype)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("B,K", SHAPES + [(2000, 7), (1100, 130), (1, 100001), (33, 99991), (64, 49999)])
+@pytest.mark.parametrize("B,K", SHAPES + [(2000, 7), (1100, 130), (1, 100001), (33, 99991), (64, 49999), (65, 32770), (14, 40001), (200, 82011)])
 def test_policy_loss_and_its_gradient(B, K, dtype):
     rng = np.random.default_rng(B + 31 * K)
     z, y, old, adv, refs, w = policy_inputs(B, K, rng, dtype)
@@ -526,7 +526,7 @@ def preference_tols(z, y, seq, refs, beta, eps, stats, s, want, g, K, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("B,K,pairs", [(1, 3, 1), (2, 7, 1), (40, 7, 3), (167, 983, 4), (64, 64, 40), (90, 2050, 2), (9, 33000, 2),
                                        (5, 70001, 1), (700, 20, 1), (2500, 5, 7), (300, 983, 70), (130, 2050, 65), (70, 9001, 66), (1500, 300, 50),
-                                       (128, 9, 64), (2300, 600, 3)])
+                                       (128, 9, 64), (2300, 600, 3), (300, 983, 200), (130, 2050, 300), (70, 9001, 300)])
 def test_preference_loss_and_its_gradient(B, K, pairs, dtype):
     rng = np.random.default_rng(B + K * 3 + pairs)
     z, y, seq, refs = preference_case(B, K, pairs, rng, dtype)
