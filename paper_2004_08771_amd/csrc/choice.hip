@@ -155,12 +155,6 @@ __device__ __forceinline__ void store_buffer(__amdgpu_buffer_rsrc_t rs, int lane
     else __builtin_amdgcn_raw_buffer_store_b64(u, rs, B * lane_piece, B * first_piece, POLICY);
 }
 
-__device__ __forceinline__ float logit(const ChoiceRows &r, long long row, int k)
-{
-    const long long i = row * r.ldz + k;
-    return r.tensor == TENSOR_BF16 ? (float)static_cast<const __bf16 *>(r.Z)[i] : static_cast<const float *>(r.Z)[i];
-}
-
 // Exponentials are powers of two of z * LOG2E - top * LOG2E: one fused multiply-add and one v_exp_f32.  LOG2E is log2 e to 24
 // bits, so what is added up is the softmax of logits that are 1.3e-8 smaller; log-probabilities are made of z_y * LOG2E
 // and that sum in the same way, which leaves an error of 1.3e-8 (E z - z_y) in them, of both signs (with the exact factor
@@ -294,49 +288,79 @@ struct SumFour {
 
 // What is done with a row's terms
 enum { HEAD_LOGPROB, HEAD_TERMS, HEAD_POLICY };
-struct RowHead {
-    int kind;
-    float *logp, *lse;  // LOGPROB: results (lse may be null).  POLICY: in p
-    double *row_lp;     // TERMS: 0 where a row takes no part
-    RowCoef *coef;      // TERMS: {shift, factor, 1 / s, 1 - p_y}.  POLICY: null, or the gradient's coefficients
-    PolicyTerms p;
+
+// What the kernels that read the logits first are given.  With up to 112 bytes of arguments, and no block size among them, a
+// launch takes 2.8 us on the host, with more 3.5 in most processes (a call of hb_logprob_async 3.95 -> 3.24 us, a policy loss of 300 x 7,
+// two launches, 5.17 -> 4.84).
+struct RowsArgs {
+    const void *Z;
+    const int32_t *y;
+    const float *weight;
+    int ldz, B, K;
+    unsigned char head, tensor;
+    bool past;             // POLICY: of dZ, as in ChoiceGrad
+    bool one;              // POLICY, one block: out is the statistics
+    union {
+        struct {
+            float *logp, *lse;  // lse may be null
+        } l;
+        struct {
+            double *row_lp;     // 0 where a row takes no part
+            RowCoef *coef;      // {shift, factor, 1 / s, 1 - p_y}; null: none
+        } t;
+        struct {
+            const float *old_logp, *ref_logp, *adv;
+            float *logp;
+            float clip_low, clip_high, kl_coef, uniform;
+        } p;
+    };
+    void *out;             // POLICY: four sums a block, or with one block the statistics
+    void *dZ;              // POLICY, whole rows: as in ChoiceGrad
+    int lddz, pad;
 };
+static_assert(sizeof(RowsArgs) == 112, "more arguments cost every launch up to 0.7 us");
+
+__device__ __forceinline__ float logit(const RowsArgs &a, long long row, int k)
+{
+    const long long i = row * a.ldz + k;
+    return a.tensor == TENSOR_BF16 ? (float)static_cast<const __bf16 *>(a.Z)[i] : static_cast<const float *>(a.Z)[i];
+}
 
 // What a row has besides its logits, asked for together
 struct RowInputs {
     int y;
     float w, old_logp, adv, ref_logp;  // POLICY
-    __device__ __forceinline__ RowInputs(const RowHead &h, const ChoiceRows &r, long long row)
-        : y(r.y[row]), w(1.f), old_logp(0.f), adv(0.f), ref_logp(0.f)
+    __device__ __forceinline__ RowInputs(const RowsArgs &a, long long row)
+        : y(a.y[row]), w(1.f), old_logp(0.f), adv(0.f), ref_logp(0.f)
     {
-        if (h.kind != HEAD_POLICY) return;
-        w = r.weight ? r.weight[row] : h.p.uniform;
-        old_logp = h.p.old_logp[row];
-        adv = h.p.adv[row];
-        if (h.p.ref_logp) ref_logp = h.p.ref_logp[row];
+        if (a.head != HEAD_POLICY) return;
+        w = a.weight ? a.weight[row] : a.p.uniform;
+        old_logp = a.p.old_logp[row];
+        adv = a.p.adv[row];
+        if (a.p.ref_logp) ref_logp = a.p.ref_logp[row];
     }
     __device__ __forceinline__ bool choice(int K) const { return y >= 0 && y < K && w != 0.f; }
 };
 
-__device__ __forceinline__ RowCoef head_row(const RowHead &h, const RowInputs &in, long long row, const RowTerms &t, bool write,
+__device__ __forceinline__ RowCoef head_row(const RowsArgs &a, const RowInputs &in, long long row, const RowTerms &t, bool write,
                                             Four &sums)
 {
     RowCoef c = {0.f, 0.f, 0.f, 0.f};
-    if (h.kind == HEAD_LOGPROB) {
+    if (a.head == HEAD_LOGPROB) {
         if (write) {
-            h.logp[row] = (float)t.lp;
-            if (h.lse) h.lse[row] = (float)t.lse;
+            a.l.logp[row] = (float)t.lp;
+            if (a.l.lse) a.l.lse[row] = (float)t.lse;
         }
         return c;
     }
-    if (h.kind == HEAD_TERMS) {
+    if (a.head == HEAD_TERMS) {
         if (write) {
-            h.row_lp[row] = t.part ? t.lp : 0.0;
-            if (h.coef) h.coef[row] = RowCoef{t.under.shift, t.under.factor, t.inv_sum, t.others};
+            a.t.row_lp[row] = t.part ? t.lp : 0.0;
+            if (a.t.coef) a.t.coef[row] = RowCoef{t.under.shift, t.under.factor, t.inv_sum, t.others};
         }
         return c;
     }
-    const PolicyTerms &p = h.p;
+    const auto &p = a.p;
     if (t.part) {
         const float A = in.adv;
         float pg = 0.f, g = 0.f, kl = 0.f;
@@ -364,15 +388,12 @@ __device__ __forceinline__ RowCoef head_row(const RowHead &h, const RowInputs &i
         c.scale = -g * t.inv_sum;
         c.chosen = g * t.others;
     }
-    if (write) {
-        if (p.logp) p.logp[row] = (float)t.lp;
-        if (h.coef) h.coef[row] = c;
-    }
+    if (write && p.logp) p.logp[row] = (float)t.lp;
     return c;
 }
 
 // Every G-th lane has something to add.  red: a wavefront each
-template <int G = 1>
+template <int THREADS, int G = 1>
 __device__ __forceinline__ Four sum_block(Four s, Four *red)
 {
 #pragma unroll
@@ -383,7 +404,7 @@ __device__ __forceinline__ Four sum_block(Four s, Four *red)
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
     s = red[0];
-    for (int w = 1; w < (int)(blockDim.x >> 6); ++w) s = add_four(s, red[w]);
+    for (int w = 1; w < THREADS / 64; ++w) s = add_four(s, red[w]);
     return s;
 }
 
@@ -394,18 +415,20 @@ __device__ __forceinline__ void store_stats(float *stats, const Four &s)
         for (int i = 0; i < 4; ++i) stats[i] = (float)s.v[i];
 }
 
+template <int THREADS>
 __device__ __forceinline__ void sum_four(const SumFour &f, Four *red)
 {
     Four s = {};
 #pragma unroll 8
-    for (int i = threadIdx.x; i < f.n; i += blockDim.x) s = add_four(s, f.partial[i]);
-    store_stats(f.stats, sum_block(s, red));
+    for (int i = threadIdx.x; i < f.n; i += THREADS) s = add_four(s, f.partial[i]);
+    store_stats(f.stats, sum_block<THREADS>(s, red));
 }
 
-__global__ __launch_bounds__(SUM_THREADS) void sum_four_kernel(SumFour f)
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void sum_four_kernel(SumFour f)
 {
-    __shared__ Four red[SUM_THREADS / 64];
-    sum_four(f, red);
+    __shared__ Four red[THREADS / 64];
+    sum_four<THREADS>(f, red);
 }
 
 // One of SUM_SLICES neighbouring parts of the sums a block
@@ -415,28 +438,27 @@ __global__ __launch_bounds__(NT) void sum_slices_kernel(const Four *partial, int
     const int per = (n + SUM_SLICES - 1) / SUM_SLICES, end = min(n, ((int)blockIdx.x + 1) * per);
     Four s = {};
     for (int i = (int)blockIdx.x * per + threadIdx.x; i < end; i += NT) s = add_four(s, partial[i]);
-    s = sum_block(s, red);
+    s = sum_block<NT>(s, red);
     if (threadIdx.x == 0) out[blockIdx.x] = s;
 }
 
 // ---------------------------------------------------------------- whole rows in registers
-struct RowsArgs {
-    ChoiceRows r;
-    RowHead h;
-    ChoiceGrad d;   // POLICY
-    Four *sums;     // POLICY: one a block, or with one block ...
-    float *stats;   // ... the statistics themselves
-};
+// What a block leaves of a policy loss
+__device__ __forceinline__ void store_sums(const RowsArgs &a, const Four &sums)
+{
+    if (a.one) store_stats(static_cast<float *>(a.out), sums);
+    else if (threadIdx.x == 0) static_cast<Four *>(a.out)[blockIdx.x] = sums;
+}
 
 // wavefronts a SIMD that the registers have to leave room for
-constexpr int row_waves(int g, int n) { return g == 1 || n > 4 ? (n > 8 ? 4 : 5) : 6; }
+constexpr int row_waves(int g, int n) { return g <= 4 || n > 4 ? (n > 8 ? 4 : 5) : 6; }
 
 // A row of dZ and its padding
 template <int G, typename TO>
 __device__ __forceinline__ void zero_row(TO *dz, const RowsArgs &a, int g)
 {
     constexpr int V = 16 / sizeof(TO);
-    const int n = max(a.r.K, a.d.pad), off = (int)((reinterpret_cast<uintptr_t>(dz) & 15) / sizeof(TO));
+    const int n = max(a.K, a.pad), off = (int)((reinterpret_cast<uintptr_t>(dz) & 15) / sizeof(TO));
     const int head = off ? min(V - off, n) : 0, pieces = (n - head) / V;
     const v4u zero = {0u, 0u, 0u, 0u};
     for (int p = g; p < pieces; p += G) reinterpret_cast<v4u *>(dz + head)[p] = zero;
@@ -471,28 +493,28 @@ __device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long ro
     // The exponentials stay in registers, too, where they take the place of the logits or there is room for them; else they
     // are made again for the gradient.
     constexpr bool KEEP = sizeof(T) == 4 || N <= 4;
-    const Row<T> z(a.r.Z, a.r.ldz, row, a.r.K);
-    const RowInputs in(a.h, a.r, row);
+    const Row<T> z(a.Z, a.ldz, row, a.K);
+    const RowInputs in(a, row);
     const int y = in.y;
     // the choice: its place in the pieces (if it is in one), the lane that has it, and which piece of that lane's it is
     const int ay = y - z.head, py = ay / V, iy = py / G;
     const bool own = ay >= 0 && py < z.pieces && py % G == g;
-    TO *dz = static_cast<TO *>(a.d.dZ) + row * a.d.ld;
-    if (!in.choice(a.r.K)) {
+    TO *dz = static_cast<TO *>(a.dZ) + row * a.lddz;
+    if (!in.choice(a.K)) {
         const RowTerms t = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
-        if (g == 0) head_row(a.h, in, row, t, true, sums);
-        if (a.d.dZ) zero_row<G>(dz, a, g);
+        if (g == 0) head_row(a, in, row, t, true, sums);
+        if (a.dZ) zero_row<G>(dz, a, g);
         return;
     }
-    const float zy = logit(a.r, row, y);
+    const float zy = logit(a, row, y);
     Piece<T> x[N];
     float edge[E];
-    const int most = a.r.K / V;  // pieces of any row; one less is in all of them
+    const int most = a.K / V;  // pieces of any row; one less is in all of them
     if constexpr (G >= 64) {
         const __amdgpu_buffer_rsrc_t rs = z.buffer();
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            if (i * G < most) x[i] = a.d.past ? Row<T>::template load<PAST>(rs, g, i * G) : Row<T>::template load<0>(rs, g, i * G);
+            if (i * G < most) x[i] = a.past ? Row<T>::template load<PAST>(rs, g, i * G) : Row<T>::template load<0>(rs, g, i * G);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -545,7 +567,7 @@ __device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long ro
     for (int o = (G < 64 ? G : 64) / 2; o > 0; o >>= 1) others += __shfl_xor(others, o, 64);
     RowCoef c;
     if (G <= 64) {
-        c = head_row(a.h, in, row, finish_row(zy, top, others), g == 0, sums);
+        c = head_row(a, in, row, finish_row(zy, top, others), g == 0, sums);
     } else {
         if ((threadIdx.x & 63) == 0) red_sum[threadIdx.x >> 6] = others;
         __syncthreads();
@@ -553,13 +575,13 @@ __device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long ro
             others = red_sum[0];
 #pragma unroll
             for (int w = 1; w < WAVES; ++w) others += red_sum[w];
-            c = head_row(a.h, in, row, finish_row(zy, top, others), g == 0, sums);
+            c = head_row(a, in, row, finish_row(zy, top, others), g == 0, sums);
             if (threadIdx.x == 0) *red_coef = c;
         }
         __syncthreads();
         c = *red_coef;
     }
-    if (!a.d.dZ) return;
+    if (!a.dZ) return;
     if (c.scale == 0.f && c.chosen == 0.f) {
         zero_row<G>(dz, a, g);
         return;
@@ -576,7 +598,7 @@ __device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long ro
         float out[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) out[e] = c.scale * (KEEP ? v[i][e] : under.exp(x[i].get(e)));
-        if (through && a.d.past) store_buffer<TO, V, PAST>(rs, g, i * G, out);
+        if (through && a.past) store_buffer<TO, V, PAST>(rs, g, i * G, out);
         else if (through) store_buffer<TO, V, 0>(rs, g, i * G, out);
         else if (i * G + g < z.pieces) store<TO, V>(to + (i * G + g) * V, out, false);
         __builtin_amdgcn_sched_barrier(0);
@@ -587,7 +609,7 @@ __device__ __forceinline__ void row_in_registers(const RowsArgs &a, long long ro
         const int j = z.edge(i * G + g);
         if (j >= 0) dz[j] = TO(j == y ? c.chosen : c.scale * edge[i]);
     }
-    for (int j = a.r.K + g; j < a.d.pad; j += G) dz[j] = TO(0.f);
+    for (int j = a.K + g; j < a.pad; j += G) dz[j] = TO(0.f);
 }
 
 template <typename T, typename TO, int G, int N, int THREADS>
@@ -601,11 +623,10 @@ __global__ __launch_bounds__(THREADS, row_waves(G, N)) void rows_kernel(RowsArgs
     const long long row = (long long)blockIdx.x * ROWS + sub;
     // (a loop over rows would keep registers for the row before)
     Four sums = {};
-    if (row < a.r.B) row_in_registers<T, TO, G, N, WAVES>(a, row, g, red_top, red_sum, &red_coef, sums);
-    if (a.h.kind == HEAD_POLICY) {
-        if constexpr (G <= 64) sums = sum_block<G>(sums, red_four);  // else the first thread's
-        if (a.stats) store_stats(a.stats, sums);
-        else if (threadIdx.x == 0) a.sums[blockIdx.x] = sums;
+    if (row < a.B) row_in_registers<T, TO, G, N, WAVES>(a, row, g, red_top, red_sum, &red_coef, sums);
+    if (a.head == HEAD_POLICY) {
+        if constexpr (G <= 64) sums = sum_block<THREADS, G>(sums, red_four);  // else the first thread's
+        store_sums(a, sums);
     }
 }
 
@@ -635,17 +656,16 @@ __global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, in
 {
     constexpr int V = Piece<T>::V, U = 4;
     __shared__ float red_top[NT / 64], red_sum[NT / 64];
-    const ChoiceRows &r = a.r;
     const long long row = blockIdx.x / chunks;
     const int c = blockIdx.x % chunks;
-    const RowInputs in(a.h, r, row);
-    if (!in.choice(r.K)) {
+    const RowInputs in(a, row);
+    if (!in.choice(a.K)) {
         const RowTerms none = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
         Four sums = {};
-        if (chunks == 1 && a.h.kind != HEAD_POLICY && threadIdx.x == 0) head_row(a.h, in, row, none, true, sums);
+        if (chunks == 1 && a.head != HEAD_POLICY && threadIdx.x == 0) head_row(a, in, row, none, true, sums);
         return;
     }
-    const Row<T> z(r.Z, r.ldz, row, r.K);
+    const Row<T> z(a.Z, a.ldz, row, a.K);
     const int y = in.y, end = min(z.pieces, (c + 1) * pieces_per_chunk);
     TopSum t = {-INFINITY, 0.f};
     if (c == 0) {
@@ -683,8 +703,8 @@ __global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, in
     for (; p + (U - 1) * NT < end; p += U * NT) pieces(Count<U>(), p);
     for (; p < end; p += NT) pieces(Count<1>(), p);
     // The maximum first, so that every sum is rescaled once more, not at each step of the way
-    const bool whole = chunks == 1 && a.h.kind != HEAD_POLICY;  // (its sums are added up over the rows)
-    const float zy = logit(r, row, y);
+    const bool whole = chunks == 1 && a.head != HEAD_POLICY;  // (its sums are added up over the rows)
+    const float zy = logit(a, row, y);
     float top = max_of_row<NT, NT / 64>(whole ? fmaxf(t.top, zy) : t.top, red_top);
     t.sum *= rescale(t.top, top);
 #pragma unroll
@@ -695,7 +715,7 @@ __global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, in
         for (int w = 1; w < NT / 64; ++w) t.sum += red_sum[w];
         if (whole) {
             Four sums = {};
-            head_row(a.h, in, row, finish_row(zy, top, t.sum), true, sums);
+            head_row(a, in, row, finish_row(zy, top, t.sum), true, sums);
         } else {
             partial[blockIdx.x] = TopSum{top, t.sum};
             if (chosen && c == 0) chosen[row] = zy;
@@ -714,25 +734,22 @@ __device__ __forceinline__ RowTerms terms_of_chunks(const TopSum *partial, int c
     return finish_row(zy, top, others);
 }
 
-// The rows' terms from their chunks, G lanes a row.
+// The rows' terms from their chunks, G lanes a row.  coef (may be null): POLICY, the gradient's coefficients
 template <int G>
-__global__ __launch_bounds__(NT) void merge_kernel(RowsArgs a, int chunks, const TopSum *partial)
+__global__ __launch_bounds__(NT) void merge_kernel(RowsArgs a, int blocks, int chunks, const TopSum *partial, RowCoef *coef)
 {
     __shared__ Four red[NT / 64];
     Four sums = {};
     const int g = threadIdx.x % G;
-    const long long per_grid = (long long)gridDim.x * (NT / G);
-    for (long long row = (long long)blockIdx.x * (NT / G) + threadIdx.x / G; row < a.r.B; row += per_grid) {
+    const long long per_grid = (long long)blocks * (NT / G);
+    for (long long row = (long long)blockIdx.x * (NT / G) + threadIdx.x / G; row < a.B; row += per_grid) {
         RowTerms t = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
-        const RowInputs in(a.h, a.r, row);
-        if (in.choice(a.r.K)) t = terms_of_chunks(partial + row * chunks, chunks, logit(a.r, row, in.y), g, G);
-        head_row(a.h, in, row, t, g == 0, sums);
+        const RowInputs in(a, row);
+        if (in.choice(a.K)) t = terms_of_chunks(partial + row * chunks, chunks, logit(a, row, in.y), g, G);
+        const RowCoef c = head_row(a, in, row, t, g == 0, sums);
+        if (coef && g == 0) coef[row] = c;
     }
-    if (a.h.kind == HEAD_POLICY) {
-        sums = sum_block(sums, red);
-        if (a.stats) store_stats(a.stats, sums);
-        else if (threadIdx.x == 0) a.sums[blockIdx.x] = sums;
-    }
+    if (a.head == HEAD_POLICY) store_sums(a, sum_block<NT>(sums, red));
 }
 
 // ---------------------------------------------------------------- pairs of sequences
@@ -771,7 +788,7 @@ struct Pair {
     }
 };
 
-__device__ __forceinline__ void store_sums(const PreferenceTerms &p, int n, double s0, double s1)
+__device__ __forceinline__ void store_pair(const PreferenceTerms &p, int n, double s0, double s1)
 {
     if (!p.seq_logp) return;
     p.seq_logp[2 * n] = (float)s0;
@@ -798,11 +815,11 @@ __global__ __launch_bounds__(NT) void preference_kernel(PreferenceTerms p, long 
 #pragma unroll
     for (int q = 0; q < 2; ++q)
         for (long long row = rows.at[q] + threadIdx.x; row < rows.at[q + 1]; row += NT) s.v[q] += row_lp[row];
-    s = sum_block(s, red);
+    s = sum_block<NT>(s, red);
     const Pair pair(p, n, s.v[0], s.v[1]);
     if (threadIdx.x == 0) {
         sums[n] = pair.stats(p);
-        store_sums(p, n, s.v[0], s.v[1]);
+        store_pair(p, n, s.v[0], s.v[1]);
     }
     if (!coef) return;
     const double slope = pair.slope(p);
@@ -835,76 +852,44 @@ enum {
     GRAD_PAIRS    // preference: the rows' terms
 };
 struct GradArgs {
-    ChoiceRows r;
-    ChoiceGrad d;
-    const RowCoef *coef;              // ROWS: or
-    const float *logp, *lse, *g;      // ... of hb_logprob_grad
-    const int32_t *first_row, *end_row;
-    int chunks, pieces_per_chunk;     // G = NT
-    int first;                        // the first block does something else: it adds up the sums (ROWS), or makes them
-    SumFour fin;
-    // CHUNKS: pieces are divided in row_sums_kernel as they are here
-    RowHead h;
-    const TopSum *partial;
+    const void *Z;
+    const int32_t *y;
+    void *dZ;
+    union {
+        const RowCoef *coef;  // of the rows, or (lse not null) ...
+        const float *logp;    // ... what hb_logprob_grad is given
+    };
+    const float *lse, *g;
+    const int32_t *seq;      // rows [seq[0], seq[last]) only; null: all
+    const Four *partial;     // ROWS: what the first block adds up, if there is one
+    float *stats;
+    int ldz, lddz, B, K, pad;
+    int chunks, pieces_per_chunk;  // G = NT
+    int last, sums;
+    bool first;              // the first block does something else: it adds up the sums (ROWS), or makes them
+    bool all_rows, past;     // as in ChoiceGrad
+};
+template <int FROM>
+struct GradFrom : GradArgs {};
+template <>
+struct GradFrom<GRAD_CHUNKS> : GradArgs {  // pieces are divided in row_sums_kernel as they are here
+    RowsArgs rows;
+    const TopSum *partial_rows;
     const float *chosen;
-    // PAIRS
+};
+template <>
+struct GradFrom<GRAD_PAIRS> : GradArgs {
     PreferenceTerms p;
     const double *row_lp;
 };
-
-// What a call on few rows has its first block do instead of one more launch: the statistics and what else is returned
-constexpr int FEW = NT;
-__device__ __forceinline__ void few_rows(const GradArgs &a, Four *red)
-{
-    int lanes = 64;
-    while (lanes * a.r.B > NT) lanes /= 2;
-    const int row = threadIdx.x / lanes, g = threadIdx.x % lanes;
-    Four sums = {};
-    if (row < a.r.B) {
-        RowTerms t = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
-        const RowInputs in(a.h, a.r, row);
-        if (in.choice(a.r.K)) t = terms_of_chunks(a.partial + row * a.chunks, a.chunks, a.chosen[row], g, lanes);
-        head_row(a.h, in, row, t, g == 0, sums);
-    }
-    store_stats(a.fin.stats, sum_block(sums, red));
-}
-__device__ __forceinline__ void few_pairs(const GradArgs &a, Four *red)
-{
-    int lanes = 64;
-    while (lanes * a.p.pairs > NT) lanes /= 2;
-    const int n = threadIdx.x / lanes, g = threadIdx.x % lanes;
-    Four sums = {};
-    if (n < a.p.pairs) {
-        double s[2];
-        sums_of_pair(PairRows(a.p, a.r.B, n), a.row_lp, g, lanes, s);
-        if (g == 0) {
-            sums = Pair(a.p, n, s[0], s[1]).stats(a.p);
-            store_sums(a.p, n, s[0], s[1]);
-        }
-    }
-    store_stats(a.fin.stats, sum_block(sums, red));
-}
-
-// The coefficients of a row of one of the pairs, in `lanes` neighbouring lanes.
-__device__ __forceinline__ RowCoef coef_in_pair(const GradArgs &a, long long row, int g, int lanes)
-{
-    int n = 0;  // pairs that end in front of it
-    for (int i = g; i < a.p.pairs; i += lanes) n += a.p.seq[2 * i + 2] <= row;
-    for (int o = lanes / 2; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
-    n = min(n, a.p.pairs - 1);
-    const PairRows rows(a.p, a.r.B, n);
-    double s[2];
-    sums_of_pair(rows, a.row_lp, g, lanes, s);
-    const double slope = Pair(a.p, n, s[0], s[1]).slope(a.p);
-    return slope_of_row(a.coef[row], (float)(row < rows.at[1] ? slope : -slope));
-}
+static_assert(sizeof(GradFrom<GRAD_ROWS>) == 112, "more arguments cost every launch up to 0.7 us");
 
 __device__ __forceinline__ RowCoef coef_of(const GradArgs &a, long long row, int y)
 {
-    if (a.coef) return a.coef[row];
+    if (!a.lse) return a.coef[row];
     RowCoef c = {0.f, 0.f, 0.f, 0.f};
     const float lse = a.lse[row], g = a.g[row];
-    if (y < 0 || y >= a.r.K || lse == -INFINITY || g == 0.f) return c;
+    if (y < 0 || y >= a.K || lse == -INFINITY || g == 0.f) return c;
     const Under under(lse);
     c.shift = under.shift;
     c.factor = under.factor;
@@ -913,17 +898,64 @@ __device__ __forceinline__ RowCoef coef_of(const GradArgs &a, long long row, int
     return c;
 }
 
+// What a call on few rows has its first block do instead of one more launch: the statistics and what else is returned
+constexpr int FEW = NT;
+__device__ __forceinline__ void few_rows(const GradFrom<GRAD_CHUNKS> &a, Four *red)
+{
+    int lanes = 64;
+    while (lanes * a.B > NT) lanes /= 2;
+    const int row = threadIdx.x / lanes, g = threadIdx.x % lanes;
+    Four sums = {};
+    if (row < a.B) {
+        RowTerms t = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
+        const RowInputs in(a.rows, row);
+        if (in.choice(a.K)) t = terms_of_chunks(a.partial_rows + row * a.chunks, a.chunks, a.chosen[row], g, lanes);
+        head_row(a.rows, in, row, t, g == 0, sums);
+    }
+    store_stats(a.stats, sum_block<NT>(sums, red));
+}
+__device__ __forceinline__ void few_pairs(const GradFrom<GRAD_PAIRS> &a, Four *red)
+{
+    int lanes = 64;
+    while (lanes * a.p.pairs > NT) lanes /= 2;
+    const int n = threadIdx.x / lanes, g = threadIdx.x % lanes;
+    Four sums = {};
+    if (n < a.p.pairs) {
+        double s[2];
+        sums_of_pair(PairRows(a.p, a.B, n), a.row_lp, g, lanes, s);
+        if (g == 0) {
+            sums = Pair(a.p, n, s[0], s[1]).stats(a.p);
+            store_pair(a.p, n, s[0], s[1]);
+        }
+    }
+    store_stats(a.stats, sum_block<NT>(sums, red));
+}
+
+// The coefficients of a row of one of the pairs, in `lanes` neighbouring lanes.
+__device__ __forceinline__ RowCoef coef_in_pair(const GradFrom<GRAD_PAIRS> &a, long long row, int g, int lanes)
+{
+    int n = 0;  // pairs that end in front of it
+    for (int i = g; i < a.p.pairs; i += lanes) n += a.p.seq[2 * i + 2] <= row;
+    for (int o = lanes / 2; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+    n = min(n, a.p.pairs - 1);
+    const PairRows rows(a.p, a.B, n);
+    double s[2];
+    sums_of_pair(rows, a.row_lp, g, lanes, s);
+    const double slope = Pair(a.p, n, s[0], s[1]).slope(a.p);
+    return slope_of_row(a.coef[row], (float)(row < rows.at[1] ? slope : -slope));
+}
+
 // G lanes have a row, or a chunk of one, between them.  The last rows come first: they are what the pass over the logits
 // before this one has left in the caches.
 template <typename T, typename TO, int G, int FROM>
-__global__ __launch_bounds__(NT) void logit_grad_kernel(GradArgs a)
+__global__ __launch_bounds__(NT) void logit_grad_kernel(GradFrom<FROM> a)
 {
     constexpr int V = Piece<T>::V, U = 4, LANES = G < 64 ? G : 64;
     __shared__ Four red[NT / 64];
     if ((int)blockIdx.x < a.first) {
-        if (FROM == GRAD_CHUNKS) few_rows(a, red);
-        else if (FROM == GRAD_PAIRS) few_pairs(a, red);
-        else sum_four(a.fin, red);
+        if constexpr (FROM == GRAD_CHUNKS) few_rows(a, red);
+        else if constexpr (FROM == GRAD_PAIRS) few_pairs(a, red);
+        else sum_four<NT>(SumFour{a.partial, a.sums, a.stats}, red);
         return;
     }
     const int g = threadIdx.x % G;
@@ -934,28 +966,32 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradArgs a)
         row /= a.chunks;
     } else {
         row = row * (NT / G) + threadIdx.x / G;
-        if (row >= a.r.B) return;
+        if (row >= a.B) return;
     }
-    row = a.r.B - 1 - row;
-    const bool outside = a.first_row && (row < *a.first_row || row >= *a.end_row);
-    if (outside && !a.d.all_rows) return;
-    const Row<T> z(a.r.Z, a.r.ldz, row, a.r.K);
-    TO *dz = static_cast<TO *>(a.d.dZ) + row * a.d.ld;
-    const int y = a.r.y[row];
+    row = a.B - 1 - row;
+    const bool outside = a.seq && (row < a.seq[0] || row >= a.seq[a.last]);
+    if (outside && !a.all_rows) return;
+    const Row<T> z(a.Z, a.ldz, row, a.K);
+    TO *dz = static_cast<TO *>(a.dZ) + row * a.lddz;
+    const int y = a.y[row];
     RowCoef k = {0.f, 0.f, 0.f, 0.f};
-    if (FROM == GRAD_CHUNKS) {
-        const RowInputs in(a.h, a.r, row);
+    if constexpr (FROM == GRAD_CHUNKS) {
+        const RowInputs in(a.rows, row);
         Four sums;
-        if (in.choice(a.r.K))
-            k = head_row(a.h, in, row, terms_of_chunks(a.partial + row * a.chunks, a.chunks, a.chosen[row], g % 64, 64), false, sums);
-    } else if (!outside) {
-        k = FROM == GRAD_PAIRS ? coef_in_pair(a, row, g % LANES, LANES) : coef_of(a, row, y);
+        if (in.choice(a.K)) {
+            const RowTerms t = terms_of_chunks(a.partial_rows + row * a.chunks, a.chunks, a.chosen[row], g % 64, 64);
+            k = head_row(a.rows, in, row, t, false, sums);
+        }
+    } else if constexpr (FROM == GRAD_PAIRS) {
+        if (!outside) k = coef_in_pair(a, row, g % LANES, LANES);
+    } else {
+        if (!outside) k = coef_of(a, row, y);
     }
     const int end = G == NT ? min(z.pieces, (c + 1) * a.pieces_per_chunk) : z.pieces;
     const bool none = k.scale == 0.f && k.chosen == 0.f;
     const Under under(k.shift, k.factor);
     TO *to = dz + z.head;
-    const bool past = a.d.past && (reinterpret_cast<uintptr_t>(to) & (V * sizeof(TO) - 1)) == 0;
+    const bool past = a.past && (reinterpret_cast<uintptr_t>(to) & (V * sizeof(TO) - 1)) == 0;
     auto pieces = [&](auto count, int p) {
         constexpr int n = decltype(count)::value;
         Piece<T> x[n];
@@ -983,7 +1019,7 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradArgs a)
             if (j < 0) continue;
             dz[j] = TO(none ? 0.f : j == y ? k.chosen : k.scale * under.exp(z.at(j)));
         }
-        for (int j = a.r.K + g; j < a.d.pad; j += G) dz[j] = TO(0.f);
+        for (int j = a.K + g; j < a.pad; j += G) dz[j] = TO(0.f);
     }
 }
 
@@ -1007,7 +1043,8 @@ struct Workspace {
 };
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
-int most_pieces(const ChoiceRows &r) { return r.K / (r.tensor == TENSOR_BF16 ? 8 : 4); }  // of a row, wherever it begins
+int most_pieces(int K, int tensor) { return K / (tensor == TENSOR_BF16 ? 8 : 4); }  // of a row, wherever it begins
+int most_pieces(const ChoiceRows &r) { return most_pieces(r.K, r.tensor); }
 
 // Whether a gradient goes past the caches: up to half of the last one (256 MB) it is left there for who reads it next, and
 // storing it past them gains little (classes 32000 in bf16, log-probabilities and their gradient: 65 MB 42.6 -> 43.1 us, 131 MB
@@ -1047,11 +1084,22 @@ Split split_for(const ChoiceRows &r)
     return {chunks, ceil_div(pieces, chunks)};
 }
 
+// Where the blocks of a policy loss leave their sums
+struct Results {
+    Four *sums;
+    float *stats;
+    void of(RowsArgs &a, int blocks) const
+    {
+        a.one = blocks == 1;
+        a.out = a.one ? static_cast<void *>(stats) : static_cast<void *>(sums);
+    }
+};
+
 template <typename T, typename TO, int G, int N, int THREADS>
-hipError_t rows_launch(RowsArgs a, int *blocks_out, hipStream_t stream, const LaunchEvents &ev)
+hipError_t rows_launch(RowsArgs a, const Results &to, int *blocks_out, hipStream_t stream, const LaunchEvents &ev)
 {
-    const int blocks = ceil_div(a.r.B, THREADS / G);
-    if (blocks > 1) a.stats = nullptr;
+    const int blocks = ceil_div(a.B, THREADS / G);
+    to.of(a, blocks);
     *blocks_out = blocks;
     return launch_kernel(rows_kernel<T, TO, G, N, THREADS>, dim3((unsigned)blocks), dim3(THREADS), stream, ev, a);
 }
@@ -1059,15 +1107,15 @@ hipError_t rows_launch(RowsArgs a, int *blocks_out, hipStream_t stream, const La
 // A loss whose rows fit a block of 1024 needs no second launch for its sums: 256 rows of 7 classes 8.8 us a call, 257 rows 11.5 us,
 // and 11.1 us for 256 rows in four blocks; 64 rows of 983 classes 8.8 and 11.3 us (one call alone 24.9 and 23.7 us).
 template <typename T, typename TO, int G, int N>
-hipError_t rows_form(const RowsArgs &a, int *blocks, hipStream_t s, const LaunchEvents &ev)
+hipError_t rows_form(const RowsArgs &a, const Results &to, int *blocks, hipStream_t s, const LaunchEvents &ev)
 {
     if constexpr (G < 64)
-        if (a.h.kind == HEAD_POLICY && a.r.B > NT / G && a.r.B <= 1024 / G) return rows_launch<T, TO, G, N, 1024>(a, blocks, s, ev);
-    return rows_launch<T, TO, G, N, (G > 64 ? G : NT)>(a, blocks, s, ev);
+        if (a.head == HEAD_POLICY && a.B > NT / G && a.B <= 1024 / G) return rows_launch<T, TO, G, N, 1024>(a, to, blocks, s, ev);
+    return rows_launch<T, TO, G, N, (G > 64 ? G : NT)>(a, to, blocks, s, ev);
 }
 
 template <typename T, typename TO>
-hipError_t rows_of_type(const RowsArgs &a, int *blocks, hipStream_t s, const LaunchEvents &ev)
+hipError_t rows_of_type(const RowsArgs &a, const Results &to, int *blocks, hipStream_t s, const LaunchEvents &ev)
 {
     // Four pieces a lane, in as many lanes as that takes, more pieces where a row would need more than 256 lanes.  Fewer lanes
     // with more pieces make fewer wavefronts than it takes to wait for the memory, more lanes compute more of what is the same in all
@@ -1076,63 +1124,94 @@ hipError_t rows_of_type(const RowsArgs &a, int *blocks, hipStream_t s, const Lau
     // bf16 128 x 4 26.9, 64 x 8 29.6, 256 x 2 29.7; 2048 x 32000 bf16 256 x 16 55.0, 512 x 8 55.4, 1024 x 4 57.7; the whole call:
     // 65536 x 7 fp32 1 x 2 7.9, 2 x 1 10.5, 4 x 1 11.2).  Long rows in blocks that a compute unit has room for two of: 4000 x
     // 83793 bf16 512 x 24 271, 1024 x 12 307.
-    const int n = most_pieces(a.r);
-    if (n <= 2) return rows_form<T, TO, 1, 2>(a, blocks, s, ev);
-    if (n <= 4) return rows_form<T, TO, 2, 2>(a, blocks, s, ev);
-    if (n <= 16) return rows_form<T, TO, 4, 4>(a, blocks, s, ev);
-    if (n <= 32) return rows_form<T, TO, 8, 4>(a, blocks, s, ev);
-    if (n <= 64) return rows_form<T, TO, 16, 4>(a, blocks, s, ev);
-    if (n <= 128) return rows_form<T, TO, 32, 4>(a, blocks, s, ev);
-    if (n <= 256) return rows_form<T, TO, 64, 4>(a, blocks, s, ev);
-    if (n <= 512) return rows_form<T, TO, 128, 4>(a, blocks, s, ev);
-    if (n <= 1024) return rows_form<T, TO, 256, 4>(a, blocks, s, ev);
-    if (n <= 2048) return rows_form<T, TO, 256, 8>(a, blocks, s, ev);
-    if (n <= 4096) return rows_form<T, TO, 256, 16>(a, blocks, s, ev);
-    if (n <= 6656) return rows_form<T, TO, 512, 13>(a, blocks, s, ev);
-    if (n <= 8192) return rows_form<T, TO, 512, 16>(a, blocks, s, ev);
-    if (n <= 12288) return rows_form<T, TO, 512, 24>(a, blocks, s, ev);
-    if (n <= 16384) return rows_form<T, TO, 1024, 16>(a, blocks, s, ev);
-    return rows_form<T, TO, 1024, 20>(a, blocks, s, ev);
+    const int n = most_pieces(a.K, a.tensor);
+    if (n <= 2) return rows_form<T, TO, 1, 2>(a, to, blocks, s, ev);
+    if (n <= 4) return rows_form<T, TO, 2, 2>(a, to, blocks, s, ev);
+    if (n <= 16) return rows_form<T, TO, 4, 4>(a, to, blocks, s, ev);
+    if (n <= 32) return rows_form<T, TO, 8, 4>(a, to, blocks, s, ev);
+    if (n <= 64) return rows_form<T, TO, 16, 4>(a, to, blocks, s, ev);
+    if (n <= 128) return rows_form<T, TO, 32, 4>(a, to, blocks, s, ev);
+    if (n <= 256) return rows_form<T, TO, 64, 4>(a, to, blocks, s, ev);
+    if (n <= 512) return rows_form<T, TO, 128, 4>(a, to, blocks, s, ev);
+    if (n <= 1024) return rows_form<T, TO, 256, 4>(a, to, blocks, s, ev);
+    if (n <= 2048) return rows_form<T, TO, 256, 8>(a, to, blocks, s, ev);
+    if (n <= 4096) return rows_form<T, TO, 256, 16>(a, to, blocks, s, ev);
+    if (n <= 6656) return rows_form<T, TO, 512, 13>(a, to, blocks, s, ev);
+    if (n <= 8192) return rows_form<T, TO, 512, 16>(a, to, blocks, s, ev);
+    if (n <= 12288) return rows_form<T, TO, 512, 24>(a, to, blocks, s, ev);
+    if (n <= 16384) return rows_form<T, TO, 1024, 16>(a, to, blocks, s, ev);
+    return rows_form<T, TO, 1024, 20>(a, to, blocks, s, ev);
 }
 
-hipError_t rows(const RowsArgs &a, int *blocks, hipStream_t stream, const LaunchEvents &ev)
+// dz: the type of the gradient, if there is one
+hipError_t rows(const RowsArgs &a, int dz, const Results &to, int *blocks, hipStream_t stream, const LaunchEvents &ev)
 {
-    if (a.r.tensor == TENSOR_BF16) return rows_of_type<__bf16, __bf16>(a, blocks, stream, ev);
-    return a.d.dZ && a.d.tensor == TENSOR_BF16 ? rows_of_type<float, __bf16>(a, blocks, stream, ev)
-                                               : rows_of_type<float, float>(a, blocks, stream, ev);
+    if (a.tensor == TENSOR_BF16) return rows_of_type<__bf16, __bf16>(a, to, blocks, stream, ev);
+    return a.dZ && dz == TENSOR_BF16 ? rows_of_type<float, __bf16>(a, to, blocks, stream, ev)
+                                     : rows_of_type<float, float>(a, to, blocks, stream, ev);
+}
+
+RowsArgs rows_args(const ChoiceRows &r, int head)
+{
+    RowsArgs a = {};
+    a.Z = r.Z;
+    a.y = r.y;
+    a.weight = r.weight;
+    a.ldz = (int)r.ldz;
+    a.B = (int)r.B;
+    a.K = r.K;
+    a.tensor = (unsigned char)r.tensor;
+    a.head = (unsigned char)head;
+    return a;
+}
+
+template <int FROM>
+GradFrom<FROM> grad_args(const ChoiceRows &r, const ChoiceGrad &d)
+{
+    GradFrom<FROM> a = {};
+    a.Z = r.Z;
+    a.y = r.y;
+    a.ldz = (int)r.ldz;
+    a.B = (int)r.B;
+    a.K = r.K;
+    a.dZ = d.dZ;
+    a.lddz = (int)d.ld;
+    a.pad = d.pad;
+    a.all_rows = d.all_rows;
+    a.past = past_caches(r, d);
+    return a;
 }
 
 // The heads of rows in chunks.  blocks: those that leave sums
 hipError_t row_sums(const RowsArgs &a, const Split &s, TopSum *partial, float *chosen, hipStream_t stream, const LaunchEvents &ev)
 {
-    const dim3 grid((unsigned)(a.r.B * s.chunks)), block(NT);
-    return a.r.tensor == TENSOR_BF16
+    const dim3 grid((unsigned)((long long)a.B * s.chunks)), block(NT);
+    return a.tensor == TENSOR_BF16
                ? launch_kernel(row_sums_kernel<__bf16>, grid, block, stream, ev, a, s.chunks, s.pieces_per_chunk, partial, chosen)
                : launch_kernel(row_sums_kernel<float>, grid, block, stream, ev, a, s.chunks, s.pieces_per_chunk, partial, chosen);
 }
 
-hipError_t chunked_rows(RowsArgs a, const Split &s, TopSum *partial, int *blocks, hipStream_t stream, const LaunchEvents &ev)
+hipError_t chunked_rows(RowsArgs a, const Split &s, TopSum *partial, RowCoef *coef, const Results &to, int *blocks, hipStream_t stream,
+                        const LaunchEvents &ev)
 {
     const dim3 block(NT);
     const hipError_t e = row_sums(a, s, partial, nullptr, stream, ev);
-    if (e != hipSuccess || (s.chunks == 1 && a.h.kind != HEAD_POLICY)) return e;
+    if (e != hipSuccess || (s.chunks == 1 && a.head != HEAD_POLICY)) return e;
     // One block makes a loss' sums itself, if fewer lanes a row make it one
-    const int lanes = s.chunks == 1 ? 1 : a.h.kind != HEAD_POLICY || a.r.B <= 4 || a.r.B > 64 ? 64 : a.r.B <= 16 ? 16 : 4;
-    *blocks = ceil_div(a.r.B, NT / lanes);
+    const int lanes = s.chunks == 1 ? 1 : a.head != HEAD_POLICY || a.B <= 4 || a.B > 64 ? 64 : a.B <= 16 ? 16 : 4;
+    *blocks = ceil_div(a.B, NT / lanes);
     if (*blocks > MAX_SUM_BLOCKS) *blocks = MAX_SUM_BLOCKS;
-    if (*blocks > 1) a.stats = nullptr;
+    to.of(a, *blocks);
     const dim3 merge((unsigned)*blocks);
-    if (lanes == 16) return launch_kernel(merge_kernel<16>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial);
-    if (lanes == 4) return launch_kernel(merge_kernel<4>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial);
-    return lanes == 1 ? launch_kernel(merge_kernel<1>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial)
-                         : launch_kernel(merge_kernel<64>, merge, block, stream, LaunchEvents(), a, s.chunks, (const TopSum *)partial);
+    const auto kernel = lanes == 64 ? merge_kernel<64> : lanes == 16 ? merge_kernel<16> : lanes == 4 ? merge_kernel<4> : merge_kernel<1>;
+    return launch_kernel(kernel, merge, block, stream, LaunchEvents(), a, *blocks, s.chunks, (const TopSum *)partial, coef);
 }
 
 // A row in G lanes
 template <typename T, typename TO, int G, int FROM>
-hipError_t grad_form(const GradArgs &a, hipStream_t stream, const LaunchEvents &ev)
+hipError_t grad_form(const GradFrom<FROM> &a, hipStream_t stream, const LaunchEvents &ev)
 {
-    const int blocks = ceil_div(a.r.B, NT / G) + a.first;
+    const int blocks = ceil_div(a.B, NT / G) + a.first;
     return launch_kernel(logit_grad_kernel<T, TO, G, FROM>, dim3((unsigned)blocks), dim3(NT), stream, ev, a);
 }
 
@@ -1143,12 +1222,11 @@ int grad_lanes(const ChoiceRows &r)
 }
 
 template <typename T, typename TO, int FROM>
-hipError_t grad_of_type(GradArgs a, hipStream_t stream, const LaunchEvents &ev)
+hipError_t grad_of_type(const ChoiceRows &r, GradFrom<FROM> a, hipStream_t stream, const LaunchEvents &ev)
 {
     a.chunks = 1;
-    a.pieces_per_chunk = 0;
     if constexpr (FROM != GRAD_CHUNKS) {
-        switch (grad_lanes(a.r)) {
+        switch (grad_lanes(r)) {
         case 4: return grad_form<T, TO, 4, FROM>(a, stream, ev);
         case 8: return grad_form<T, TO, 8, FROM>(a, stream, ev);
         case 16: return grad_form<T, TO, 16, FROM>(a, stream, ev);
@@ -1156,19 +1234,18 @@ hipError_t grad_of_type(GradArgs a, hipStream_t stream, const LaunchEvents &ev)
         case 64: return grad_form<T, TO, 64, FROM>(a, stream, ev);
         }
     }
-    const Split s = split_for(a.r);
+    const Split s = split_for(r);
     a.chunks = s.chunks;
     a.pieces_per_chunk = s.pieces_per_chunk;
-    return launch_kernel(logit_grad_kernel<T, TO, NT, FROM>, dim3((unsigned)(a.r.B * s.chunks + a.first)), dim3(NT), stream, ev, a);
+    return launch_kernel(logit_grad_kernel<T, TO, NT, FROM>, dim3((unsigned)(r.B * s.chunks + a.first)), dim3(NT), stream, ev, a);
 }
 
 template <int FROM>
-hipError_t logit_grad(GradArgs a, hipStream_t stream, const LaunchEvents &ev)
+hipError_t logit_grad(const ChoiceRows &r, int dz, GradFrom<FROM> a, hipStream_t stream, const LaunchEvents &ev)
 {
-    a.d.past = past_caches(a.r, a.d);
-    a.first = FROM != GRAD_ROWS || a.fin.n > 0;
-    if (a.r.tensor == TENSOR_BF16) return grad_of_type<__bf16, __bf16, FROM>(a, stream, ev);
-    return a.d.tensor == TENSOR_BF16 ? grad_of_type<float, __bf16, FROM>(a, stream, ev) : grad_of_type<float, float, FROM>(a, stream, ev);
+    a.first = FROM != GRAD_ROWS || a.sums > 0;
+    if (r.tensor == TENSOR_BF16) return grad_of_type<__bf16, __bf16, FROM>(r, a, stream, ev);
+    return dz == TENSOR_BF16 ? grad_of_type<float, __bf16, FROM>(r, a, stream, ev) : grad_of_type<float, float, FROM>(r, a, stream, ev);
 }
 
 // Whether the gradient's kernel sums up the pairs itself, each row those of its own, and its first block all of them: one launch
@@ -1193,7 +1270,8 @@ hipError_t add_sums(SumFour f, Four *more, hipStream_t stream)
         f.partial = more;
         f.n = SUM_SLICES;
     }
-    return launch_kernel(sum_four_kernel, dim3(1), dim3(f.n > NT ? SUM_THREADS : NT), stream, LaunchEvents(), f);
+    return f.n > NT ? launch_kernel(sum_four_kernel<SUM_THREADS>, dim3(1), dim3(SUM_THREADS), stream, LaunchEvents(), f)
+                    : launch_kernel(sum_four_kernel<NT>, dim3(1), dim3(NT), stream, LaunchEvents(), f);
 }
 
 }  // namespace
@@ -1209,51 +1287,50 @@ size_t choice_workspace(long long B, int pairs)
 hipError_t launch_logprob(const ChoiceRows &r, float *logp, float *lse, void *ws, hipStream_t stream, const LaunchEvents &ev)
 {
     if (r.B == 0) return hipSuccess;
-    RowsArgs a = {};
-    a.r = r;
-    a.h.kind = HEAD_LOGPROB;
-    a.h.logp = logp;
-    a.h.lse = lse;
+    RowsArgs a = rows_args(r, HEAD_LOGPROB);
+    a.l.logp = logp;
+    a.l.lse = lse;
     int blocks = 0;
-    if (rows_in_registers(r, false)) return rows(a, &blocks, stream, ev);
-    return chunked_rows(a, split_for(r), Workspace(ws, r.B, 0).partial, &blocks, stream, ev);
+    if (rows_in_registers(r, false)) return rows(a, 0, Results{}, &blocks, stream, ev);
+    return chunked_rows(a, split_for(r), Workspace(ws, r.B, 0).partial, nullptr, Results{}, &blocks, stream, ev);
 }
 
 hipError_t launch_logprob_grad(const ChoiceRows &r, const float *logp, const float *lse, const float *g, const ChoiceGrad &d,
                                hipStream_t stream, const LaunchEvents &ev)
 {
     if (r.B == 0) return hipSuccess;
-    GradArgs a = {};
-    a.r = r;
-    a.d = d;
+    auto a = grad_args<GRAD_ROWS>(r, d);
     a.logp = logp;
     a.lse = lse;
     a.g = g;
-    return logit_grad<GRAD_ROWS>(a, stream, ev);
+    return logit_grad(r, d.tensor, a, stream, ev);
 }
 
 hipError_t launch_policy(const ChoiceRows &r, const PolicyTerms &t, const ChoiceGrad &d, void *ws, hipStream_t stream,
                          const LaunchEvents &ev)
 {
     const Workspace w(ws, r.B, 0);
+    const Results to = {w.sums, t.stats};
     SumFour fin = {w.sums, 0, t.stats};
     Four *const more = w.sums + r.B;  // (rows_kernel leaves a sum a row at most, in all of the workspace)
     if (r.B == 0) return add_sums(fin, more, stream);
-    RowsArgs a = {};
-    a.r = r;
-    a.h.kind = HEAD_POLICY;
-    a.h.p = t;
-    a.sums = w.sums;
-    a.stats = t.stats;
+    RowsArgs a = rows_args(r, HEAD_POLICY);
+    a.p.old_logp = t.old_logp;
+    a.p.ref_logp = t.ref_logp;
+    a.p.adv = t.adv;
+    a.p.logp = t.logp;
+    a.p.clip_low = t.clip_low;
+    a.p.clip_high = t.clip_high;
+    a.p.kl_coef = t.kl_coef;
+    a.p.uniform = t.uniform;
     if (rows_in_registers(r, d.dZ != nullptr)) {
-        a.d = d;
-        a.d.past = past_caches(r, d);
-        const hipError_t e = rows(a, &fin.n, stream, ev);
+        a.dZ = d.dZ;
+        a.lddz = (int)d.ld;
+        a.pad = d.pad;
+        a.past = past_caches(r, d);
+        const hipError_t e = rows(a, d.tensor, to, &fin.n, stream, ev);
         return e != hipSuccess || fin.n == 1 ? e : add_sums(fin, more, stream);
     }
-    GradArgs g = {};
-    g.r = r;
-    g.d = d;
     const Split s = split_for(r);
     // Chunks of few rows: their gradient's kernel joins them itself, and one block of it makes the sums (in one stream, with a launch
     // for that and without, us: 24 x 131072 fp32 19.1 / 16.1, 1 x 131072 10.3 / 9.3, 64 x 500000 bf16 54.9 / 51.9).
@@ -1261,53 +1338,65 @@ hipError_t launch_policy(const ChoiceRows &r, const PolicyTerms &t, const Choice
         float *const chosen = reinterpret_cast<float *>(w.coef);
         const hipError_t e = row_sums(a, s, w.partial, chosen, stream, ev);
         if (e != hipSuccess) return e;
-        g.h = a.h;
-        g.partial = w.partial;
+        auto g = grad_args<GRAD_CHUNKS>(r, d);
+        g.rows = a;
+        g.partial_rows = w.partial;
         g.chosen = chosen;
-        g.fin.stats = t.stats;
-        return logit_grad<GRAD_CHUNKS>(g, stream, LaunchEvents());
+        g.stats = t.stats;
+        return logit_grad(r, d.tensor, g, stream, LaunchEvents());
     }
-    a.h.coef = d.dZ ? w.coef : nullptr;
-    const hipError_t e = chunked_rows(a, s, w.partial, &fin.n, stream, ev);
+    const hipError_t e = chunked_rows(a, s, w.partial, d.dZ ? w.coef : nullptr, to, &fin.n, stream, ev);
     if (e != hipSuccess) return e;
     if (fin.n == 1) fin.n = 0;
     if (!d.dZ) return fin.n ? add_sums(fin, nullptr, stream) : hipSuccess;
+    auto g = grad_args<GRAD_ROWS>(r, d);
     g.coef = w.coef;
-    g.fin = fin;
-    return logit_grad<GRAD_ROWS>(g, stream, LaunchEvents());
+    g.partial = fin.partial;
+    g.sums = fin.n;
+    g.stats = t.stats;
+    return logit_grad(r, d.tensor, g, stream, LaunchEvents());
+}
+
+template <int FROM>
+static GradFrom<FROM> grad_of_pairs(const ChoiceRows &r, const PreferenceTerms &t, const ChoiceGrad &d, const Workspace &w)
+{
+    auto g = grad_args<FROM>(r, d);
+    g.coef = w.coef;
+    g.seq = t.seq;
+    g.last = 2 * t.pairs;
+    g.stats = t.stats;
+    return g;
 }
 
 hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, const ChoiceGrad &d, void *ws, hipStream_t stream,
                              const LaunchEvents &ev)
 {
     const Workspace w(ws, r.B, t.pairs);
-    RowsArgs a = {};
-    a.r = r;
-    a.h.kind = HEAD_TERMS;
-    a.h.row_lp = w.row_lp;
-    a.h.coef = d.dZ ? w.coef : nullptr;
-    int blocks = 0;
     hipError_t e = hipSuccess;
-    if (r.B > 0) e = rows_in_registers(r, false) ? rows(a, &blocks, stream, ev) : chunked_rows(a, split_for(r), w.partial, &blocks, stream, ev);
-    if (e != hipSuccess) return e;
-    GradArgs g = {};
-    g.r = r;
-    g.d = d;
-    g.coef = w.coef;
-    g.first_row = t.seq;
-    g.end_row = t.seq + 2 * t.pairs;
+    if (r.B > 0) {
+        RowsArgs a = rows_args(r, HEAD_TERMS);
+        a.t.row_lp = w.row_lp;
+        a.t.coef = d.dZ ? w.coef : nullptr;
+        int blocks = 0;
+        e = rows_in_registers(r, false) ? rows(a, 0, Results{}, &blocks, stream, ev)
+                                        : chunked_rows(a, split_for(r), w.partial, nullptr, Results{}, &blocks, stream, ev);
+        if (e != hipSuccess) return e;
+    }
     if (d.dZ && r.B > 0 && pairs_in_grad(r, t.pairs)) {
+        auto g = grad_of_pairs<GRAD_PAIRS>(r, t, d, w);
         g.p = t;
         g.row_lp = w.row_lp;
-        g.fin.stats = t.stats;
-        return logit_grad<GRAD_PAIRS>(g, stream, LaunchEvents());
+        return logit_grad(r, d.tensor, g, stream, LaunchEvents());
     }
     e = launch_kernel(preference_kernel, dim3((unsigned)t.pairs), dim3(NT), stream, LaunchEvents(), t, r.B, (const double *)w.row_lp,
                       d.dZ ? w.coef : nullptr, w.sums);
-    g.fin = {w.sums, t.pairs, t.stats};
     if (e != hipSuccess) return e;
-    if (!d.dZ || r.B == 0) return launch_kernel(sum_four_kernel, dim3(1), dim3(SUM_THREADS), stream, LaunchEvents(), g.fin);
-    return logit_grad<GRAD_ROWS>(g, stream, LaunchEvents());
+    if (!d.dZ || r.B == 0)
+        return launch_kernel(sum_four_kernel<SUM_THREADS>, dim3(1), dim3(SUM_THREADS), stream, LaunchEvents(), SumFour{w.sums, t.pairs, t.stats});
+    auto g = grad_of_pairs<GRAD_ROWS>(r, t, d, w);
+    g.partial = w.sums;
+    g.sums = t.pairs;
+    return logit_grad(r, d.tensor, g, stream, LaunchEvents());
 }
 
 }  // namespace hb
