@@ -428,6 +428,7 @@ def near_on_device(got, want, Z, g, K, dtype, what):
     (66, 82003, "f32"),       # ... several
     (70, 52000, "f32"), (66, 70003, "f32"), (70, 110001, "bf16"), (66, 150001, "bf16"),  # a row in 1024 lanes
     (4, 300007, "bf16"), (1, 1 << 20, "f32"),
+    (1, 1 << 24, "f32"), (1 << 22, 2, "f32"), (1 << 22, 3, "bf16"),  # the limits
 ])
 def test_large_calls(B, K, dtype):
     g0 = torch.Generator(device="cuda").manual_seed(B + K)
