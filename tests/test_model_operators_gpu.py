@@ -126,9 +126,12 @@ NETS = [
     ((300, 1024, 1024, 33), SIG, BF16, 1001), ((128, 256, 1000), SIG, BF16, 200), ((64, 20, 24, 20, 16, 10), SIG, BF16, 65),
 ]
 
+# outputs so wide that few rows are cut into chunks; bf16: their padding
+WIDE = [((24, 16, 33001), SIG, F32, 6), ((24, 16, 33001), SIG, BF16, 6), ((24, 16, 50003), SIG, BF16, 70)]
+
 
 @pytest.mark.parametrize("p", [0.0, 0.3])
-@pytest.mark.parametrize("dims,act,dtype,B", NETS)
+@pytest.mark.parametrize("dims,act,dtype,B", NETS + WIDE)
 def test_policy_gradient_of_a_network(dims, act, dtype, B, p):
     rng = np.random.default_rng(B + len(dims))
     seed, call, K = 987654321012345, 11, dims[-1]
@@ -172,7 +175,7 @@ def test_policy_gradient_of_a_network(dims, act, dtype, B, p):
 
 
 @pytest.mark.parametrize("p", [0.0, 0.2])
-@pytest.mark.parametrize("dims,act,dtype,B", [NETS[0], NETS[3], NETS[5], NETS[8], NETS[9], NETS[12]])
+@pytest.mark.parametrize("dims,act,dtype,B", [NETS[0], NETS[3], NETS[5], NETS[8], NETS[9], NETS[12]] + WIDE)
 def test_preference_gradient_of_a_network(dims, act, dtype, B, p):
     rng = np.random.default_rng(7 * B + len(dims))
     seed, call, K, pairs = 5, 2 ** 40, dims[-1], 3
