@@ -558,16 +558,19 @@ def test_preference_loss_and_its_gradient(B, K, pairs, dtype):
         assert np.array_equal(got[:seq[0]], keep[:seq[0]], equal_nan=True) and np.array_equal(got[seq[-1]:], keep[seq[-1]:], equal_nan=True)
 
 
-def test_preference_rows_that_take_no_part_get_zeros_whatever_the_loss():
+@pytest.mark.parametrize("B,K", [(6, 40), (200, 3)])    # with a launch less, and with one for the pairs
+def test_preference_rows_that_take_no_part_get_zeros_whatever_the_loss(B, K):
     """A sequence of log-probability -inf: its loss is infinite or undefined, the gradients of padding are zeros all the same."""
-    z = np.zeros((6, 40))
+    z = np.zeros((B, K))
     z[1, 0] = z[3, 0] = -np.inf
-    y = np.array([-1, 0, 0, 0, 40, 5], np.int32)    # both sequences have an impossible choice, and padding
-    dZ, _ = matrix(np.full((6, 40), 7.0), "f32")
+    y = np.zeros(B, np.int32)
+    y[:6] = [-1, 0, 0, 0, K, K - 1]                       # both sequences have an impossible choice, and padding
+    dZ, _ = matrix(np.full((B, K), 7.0), "f32")
     st = torch.zeros(4, device="cuda")
-    hb.preference_loss(matrix(z, "f32")[0], vec(y, torch.int32), vec([0, 3, 6], torch.int32), st, dZ=dZ, ws=ws(6, 1))
+    hb.preference_loss(matrix(z, "f32")[0], vec(y, torch.int32), vec([0, 3, 6], torch.int32), st, dZ=dZ, ws=ws(B, 1))
     got = host(dZ)
     assert not got[0].any() and not got[4].any() and np.isnan(host(st)[0])
+    assert (got[6:] == 7.0).all()
 
 
 def test_preference_gradient_against_differences():
@@ -596,12 +599,12 @@ def test_preference_gradient_against_differences():
     assert truncation < 0.1 * abs(along) + 1e-3
 
 
-def test_preference_offsets_out_of_range_write_nothing_outside():
+@pytest.mark.parametrize("B,K", [(12, 100), (200, 3)])
+def test_preference_offsets_out_of_range_write_nothing_outside(B, K):
     """Offsets beyond the rows are cut to them, decreasing ones make a sequence empty: no access outside, whatever they say."""
     rng = np.random.default_rng(3)
-    B, K = 12, 100
     z, y = logits(B, K, rng, "f32", masked=False)
-    for seq, same in [([-5, 4, 99], [0, 4, 12]), ([0, 12, 12], None), ([12, 12, 12], None), ([50, 60, 70], [12, 12, 12])]:
+    for seq, same in [([-5, 4, B + 87], [0, 4, B]), ([0, B, B], None), ([B, B, B], None), ([B + 38, B + 48, B + 58], [B, B, B])]:
         out = []
         for q in (seq, same or seq):
             dZ, flat = matrix(np.full((B, K), np.nan), "f32", K + 1, 2)
@@ -635,7 +638,7 @@ def test_refusals_that_need_a_device():
         assert e.value.code == hb.HB_ERR_INVALID and "device pointer" in str(e.value)
 
 
-@pytest.mark.parametrize("B,K", [(40, 7), (300, 1500), (3, 60000), (20, 20000)])
+@pytest.mark.parametrize("B,K", [(40, 7), (300, 1500), (3, 60000), (20, 20000), (2100, 600)])
 def test_captured_and_replayed_beside_eager_work(B, K):
     """One graph with all of them, replayed five times with other inputs, eager calls and synchronisations between."""
     rng = np.random.default_rng(B)
