@@ -644,9 +644,9 @@ __device__ __forceinline__ float rescale(float from, float to)
     return f.far == t.far ? exp2_of(f.shift - t.shift) : 0.f;
 }
 
-template <int N>
-struct Count {
-    static constexpr int value = N;
+template <bool B>
+struct Flag {
+    static constexpr bool value = B;
 };
 
 // A block a chunk, without the chosen class; the first chunk has the edges.  A row of one chunk is finished here.
@@ -674,14 +674,17 @@ __global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, in
         t.top = v == v ? v : -INFINITY;
         t.sum = Under(t.top).exp(v);
     }
-    auto pieces = [&](auto count, int p) {
-        constexpr int n = decltype(count)::value;
-        Piece<T> x[n];
+    // U pieces a lane; guard: not all lanes have that many left, and their loads are sent together all the same
+    auto pieces = [&](auto guard, int p) {
+        Piece<T> x[U];
 #pragma unroll
-        for (int u = 0; u < n; ++u) x[u] = z.load(p + u * NT);
+        for (int u = 0; u < U; ++u) {
+            if (!decltype(guard)::value || p + u * NT < end) x[u] = z.load(p + u * NT);
+            else x[u].set_none();
+        }
         float top = t.top;
 #pragma unroll
-        for (int u = 0; u < n; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int at = y - z.first(p + u * NT);
             if ((unsigned)at < (unsigned)V) x[u].drop(at, true);
 #pragma unroll
@@ -692,16 +695,16 @@ __global__ __launch_bounds__(NT) void row_sums_kernel(RowsArgs a, int chunks, in
         const Under under(top);
         float o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < n; ++u) {
+        for (int u = 0; u < U; ++u) {
             x[u].forget();
 #pragma unroll
             for (int e = 0; e < V; ++e) o[e & 3] += under.exp(x[u].get(e));
         }
         t.sum += (o[0] + o[1]) + (o[2] + o[3]);
     };
-    int p = c * pieces_per_chunk + (int)threadIdx.x;
-    for (; p + (U - 1) * NT < end; p += U * NT) pieces(Count<U>(), p);
-    for (; p < end; p += NT) pieces(Count<1>(), p);
+    int p = c * pieces_per_chunk;
+    for (; p + U * NT <= end; p += U * NT) pieces(Flag<false>(), p + (int)threadIdx.x);
+    if (p < end) pieces(Flag<true>(), p + (int)threadIdx.x);
     // The maximum first, so that every sum is rescaled once more, not at each step of the way
     const bool whole = chunks == 1 && a.head != HEAD_POLICY;  // (its sums are added up over the rows)
     const float zy = logit(a, row, y);
@@ -992,14 +995,16 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradFrom<FROM> a)
     const Under under(k.shift, k.factor);
     TO *to = dz + z.head;
     const bool past = a.past && (reinterpret_cast<uintptr_t>(to) & (V * sizeof(TO) - 1)) == 0;
-    auto pieces = [&](auto count, int p) {
-        constexpr int n = decltype(count)::value;
-        Piece<T> x[n];
+    // U pieces a lane; guard: not all lanes have that many left, and their loads are sent together all the same
+    auto pieces = [&](auto guard, int p) {
+        Piece<T> x[U];
         if (!none)
 #pragma unroll
-            for (int u = 0; u < n; ++u) x[u] = z.load(p + u * G);
+            for (int u = 0; u < U; ++u)
+                if (!decltype(guard)::value || p + u * G < end) x[u] = z.load(p + u * G);
 #pragma unroll
-        for (int u = 0; u < n; ++u) {
+        for (int u = 0; u < U; ++u) {
+            if (decltype(guard)::value && p + u * G >= end) continue;
             float out[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) out[e] = none ? 0.f : k.scale * under.exp(x[u].get(e));
@@ -1008,9 +1013,9 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradFrom<FROM> a)
             if ((unsigned)at < (unsigned)V) dz[y] = TO(k.chosen);  // over what this lane has just stored there
         }
     };
-    int p = c * a.pieces_per_chunk + g;
-    for (; p + (U - 1) * G < end; p += U * G) pieces(Count<U>(), p);
-    for (; p < end; p += G) pieces(Count<1>(), p);
+    int p = c * a.pieces_per_chunk;
+    for (; p + U * G <= end; p += U * G) pieces(Flag<false>(), p + g);
+    if (p < end) pieces(Flag<true>(), p + g);
     if (c == a.chunks - 1) {
         constexpr int E = G < Row<T>::EDGE ? Row<T>::EDGE / G : 1;
 #pragma unroll
