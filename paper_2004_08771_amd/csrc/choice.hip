@@ -282,7 +282,7 @@ __device__ __forceinline__ Four add_four(const Four &a, const Four &b)
 // stats = sum of n partial sums in a fixed order
 struct SumFour {
     const Four *partial;
-    int n;  // 0: nothing to do
+    int n;
     float *stats;
 };
 
@@ -848,9 +848,9 @@ __device__ __forceinline__ void sums_of_pair(const PairRows &rows, const double 
 }
 
 // ---------------------------------------------------------------- the gradient in the logits, from the rows' coefficients
-// Rows [*first_row, *end_row) only where there are bounds.
+// What the coefficients are made from
 enum {
-    GRAD_ROWS,    // coefficients, or log-probabilities and what they are multiplied with
+    GRAD_ROWS,    // they are there, or log-probabilities and what these are multiplied with
     GRAD_CHUNKS,  // policy: what row_sums_kernel leaves
     GRAD_PAIRS    // preference: the rows' terms
 };
