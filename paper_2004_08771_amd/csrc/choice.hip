@@ -155,28 +155,20 @@ __device__ __forceinline__ void store_buffer(__amdgpu_buffer_rsrc_t rs, int lane
     else __builtin_amdgcn_raw_buffer_store_b64(u, rs, B * lane_piece, B * first_piece, POLICY);
 }
 
-// Exponentials are powers of two of z * LOG2E - top * LOG2E: one fused multiply-add and one v_exp_f32.  LOG2E is log2 e to 24
-// bits, so what is added up is the softmax of logits that are 1.3e-8 smaller; log-probabilities are made of z_y * LOG2E
-// and that sum in the same way, which leaves an error of 1.3e-8 (E z - z_y) in them, of both signs (with the exact factor
-// outside it would be 1.3e-8 times the entropy, always of one sign, which the tokens of a sequence add up).
+// Exponentials are powers of two of (z - top) * LOG2E: the difference first, since it is exact near the maximum and 0 there whatever the
+// logits' size, where z * LOG2E - top * LOG2E would leave the rounding error of a product (+-64 at 1e9, past fp32's range from
+// 1e10 on).  LOG2E is log2 e to 24 bits, so what is added up is the softmax of logits that are 1.3e-8 smaller; log-probabilities
+// are made of (z_y - top) * LOG2E and that sum in the same way, which leaves an error of 1.3e-8 (E z - z_y) in them, of both signs
+// (with the exact factor outside it would be 1.3e-8 times the entropy, always of one sign, which the tokens of a sequence add up).
 constexpr float LOG2E = 0x1.715476p+0f;
 constexpr double LN2 = 0.693147180559945309;
 __device__ __forceinline__ float exp2_of(float u) { return __builtin_amdgcn_exp2f(u); }
 
-// The exponent u = z * factor - shift under a maximum (0 where that is -inf).  From 2^100 on top * LOG2E could leave the range,
-// but logits differ from it by 0 or by 2^76 and more: any power of two as the factor tells these apart, exactly.
+// Exponentials under a maximum (under 0 where that is -inf)
 struct Under {
-    float shift, factor;
-    bool far;
-    __device__ __forceinline__ explicit Under(float top)
-    {
-        const float ref = top == -INFINITY ? 0.f : top;
-        far = fabsf(ref) >= 0x1p100f;
-        factor = far ? 0x1p-40f : LOG2E;
-        shift = ref * factor;
-    }
-    __device__ __forceinline__ Under(float shift_, float factor_) : shift(shift_), factor(factor_), far(false) {}
-    __device__ __forceinline__ float exp(float z) const { return exp2_of(__builtin_fmaf(z, factor, -shift)); }
+    float ref;
+    __device__ __forceinline__ explicit Under(float top) : ref(top == -INFINITY ? 0.f : top) {}
+    __device__ __forceinline__ float exp(float z) const { return exp2_of((z - ref) * LOG2E); }
 };
 
 // log2(s) for a positive s, in two parts: an integer, and at most 1 with an error of 2^-24
@@ -237,7 +229,8 @@ struct RowTerms {
 };
 
 // zy: the chosen logit; top: the maximum; o: the sum over the others under it.
-// 64-bit additions, but no function of 64 bits: those would take more registers than the rows do.
+// 64-bit additions, but no function of 64 bits: those would take more registers than the rows do.  The log-probability starts from the
+// distance to the maximum, not from lse: beside a large maximum log s would be rounded away.
 __device__ __forceinline__ RowTerms finish_row(float zy, float top, float o)
 {
     RowTerms t = {false, Under(0.f), 0.f, 0.f, 0.0, 0.0};
@@ -252,21 +245,15 @@ __device__ __forceinline__ RowTerms finish_row(float zy, float top, float o)
     t.inv_sum = __builtin_amdgcn_rcpf(s);  // off by a rounding
     t.others = o * t.inv_sum;
     const double log2_s = (double)l.hi + (double)l.lo;
-    if (t.under.far) {
-        t.lse = (double)top + LN2 * log2_s;
-        t.lp = (double)zy - t.lse;
-    } else {
-        const double lse2 = (double)t.under.shift + log2_s;
-        t.lse = LN2 * lse2;
-        t.lp = LN2 * ((double)zy * (double)LOG2E - lse2);
-    }
+    t.lse = (double)t.under.ref + LN2 * log2_s;
+    t.lp = LN2 * (((double)zy - (double)t.under.ref) * (double)LOG2E - log2_s);
     if (o < e) t.lp = -(double)log1p_of(o * __builtin_amdgcn_rcpf(e));
     return t;
 }
 
-// The gradient of a row: dz_k = scale * 2^(z_k * factor - shift) for k != y and `chosen` for k = y; all zero where both are
+// The gradient of a row: dz_k = scale * exp(z_k - ref) for k != y and `chosen` for k = y; all zero where both are
 struct RowCoef {
-    float shift, factor, scale, chosen;
+    float ref, scale, chosen, pad;
 };
 
 struct Four {
@@ -306,7 +293,7 @@ struct RowsArgs {
         } l;
         struct {
             double *row_lp;     // 0 where a row takes no part
-            RowCoef *coef;      // {shift, factor, 1 / s, 1 - p_y}; null: none
+            RowCoef *coef;      // {maximum, 1 / s, 1 - p_y}; null: none
         } t;
         struct {
             const float *old_logp, *ref_logp, *adv;
@@ -356,7 +343,7 @@ __device__ __forceinline__ RowCoef head_row(const RowsArgs &a, const RowInputs &
     if (a.head == HEAD_TERMS) {
         if (write) {
             a.t.row_lp[row] = t.part ? t.lp : 0.0;
-            if (a.t.coef) a.t.coef[row] = RowCoef{t.under.shift, t.under.factor, t.inv_sum, t.others};
+            if (a.t.coef) a.t.coef[row] = RowCoef{t.under.ref, t.inv_sum, t.others, 0.f};
         }
         return c;
     }
@@ -383,8 +370,7 @@ __device__ __forceinline__ RowCoef head_row(const RowsArgs &a, const RowInputs &
             sums = add_four(sums, Four{{p.kl_coef != 0.f ? pgw + (double)p.kl_coef * klw : pgw, pgw, klw, cut ? (double)w : 0.0}});
         }
         g *= w;
-        c.shift = t.under.shift;
-        c.factor = t.under.factor;
+        c.ref = t.under.ref;
         c.scale = -g * t.inv_sum;
         c.chosen = g * t.others;
     }
@@ -636,12 +622,10 @@ struct TopSum {
     float top, sum;
 };
 
-// What a sum under `from` is multiplied with to be one under `to` >= from: the difference of their shifts, as rounded
+// What a sum under `from` is multiplied with to be one under `to` >= from
 __device__ __forceinline__ float rescale(float from, float to)
 {
-    if (from == to || from == -INFINITY) return 1.f;
-    const Under f(from), t(to);
-    return f.far == t.far ? exp2_of(f.shift - t.shift) : 0.f;
+    return from == to || from == -INFINITY ? 1.f : exp2_of((from - to) * LOG2E);
 }
 
 template <bool B>
@@ -893,9 +877,7 @@ __device__ __forceinline__ RowCoef coef_of(const GradArgs &a, long long row, int
     RowCoef c = {0.f, 0.f, 0.f, 0.f};
     const float lse = a.lse[row], g = a.g[row];
     if (y < 0 || y >= a.K || lse == -INFINITY || g == 0.f) return c;
-    const Under under(lse);
-    c.shift = under.shift;
-    c.factor = under.factor;
+    c.ref = lse;
     c.scale = -g;
     c.chosen = -g * expm1f(a.logp[row]);
     return c;
@@ -992,7 +974,7 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradFrom<FROM> a)
     }
     const int end = G == NT ? min(z.pieces, (c + 1) * a.pieces_per_chunk) : z.pieces;
     const bool none = k.scale == 0.f && k.chosen == 0.f;
-    const Under under(k.shift, k.factor);
+    const Under under(k.ref);
     TO *to = dz + z.head;
     const bool past = a.past && (reinterpret_cast<uintptr_t>(to) & (V * sizeof(TO) - 1)) == 0;
     // U pieces a lane; guard: not all lanes have that many left, and their loads are sent together all the same
