@@ -518,7 +518,9 @@ int hb_logprob_async(const void *d_Z, int64_t ldz, int tensor, const int32_t *d_
                      float *d_lse, void *d_ws, size_t ws_bytes, void *hip_stream);
 /*
  * Its gradient: dZ_i[k] = g_i ([k = y_i] - exp(z_i[k] - lse_i)), with d_logp and d_lse as hb_logprob_async left them for the
- * same d_Z and d_y, and d_g the gradient of each log-probability.  Rows without a choice, without an
+ * same d_Z and d_y, and d_g the gradient of each log-probability.  (lse_i is z_i[y_i] - logp_i where that is the more exact of the two,
+ * so logits far from 0 cost no precision; where logp_i is as far from 0 as lse_i, exponents are off by 2^-24 of it, and no
+ * probability is more than 1 - exp(logp_i).)  Rows without a choice, without an
  * allowed class, or with g_i = 0 get zeros, whatever their logits hold.  d_dZ has the type of d_Z; it may be d_Z
  * itself with lddz = ldz, otherwise they must not overlap.
  */

@@ -251,9 +251,9 @@ __device__ __forceinline__ RowTerms finish_row(float zy, float top, float o)
     return t;
 }
 
-// The gradient of a row: dz_k = scale * exp(z_k - ref) for k != y and `chosen` for k = y; all zero where both are
+// The gradient of a row: dz_k = scale * exp(z_k - ref) 2^add for k != y and `chosen` for k = y; all zero where both are
 struct RowCoef {
-    float ref, scale, chosen, pad;
+    float ref, scale, chosen, add;
 };
 
 struct Four {
@@ -834,7 +834,8 @@ __device__ __forceinline__ void sums_of_pair(const PairRows &rows, const double 
 // ---------------------------------------------------------------- the gradient in the logits, from the rows' coefficients
 // What the coefficients are made from
 enum {
-    GRAD_ROWS,    // they are there, or log-probabilities and what these are multiplied with
+    GRAD_ROWS,    // they are there
+    GRAD_LOGPROB, // log-probabilities and what these are multiplied with
     GRAD_CHUNKS,  // policy: what row_sums_kernel leaves
     GRAD_PAIRS    // preference: the rows' terms
 };
@@ -843,8 +844,8 @@ struct GradArgs {
     const int32_t *y;
     void *dZ;
     union {
-        const RowCoef *coef;  // of the rows, or (lse not null) ...
-        const float *logp;    // ... what hb_logprob_grad is given
+        const RowCoef *coef;  // ROWS, PAIRS
+        const float *logp;    // LOGPROB, with:
     };
     const float *lse, *g;
     const int32_t *seq;      // rows [seq[0], seq[last]) only; null: all
@@ -855,6 +856,7 @@ struct GradArgs {
     int last, sums;
     bool first;              // the first block does something else: it adds up the sums (ROWS), or makes them
     bool all_rows, past;     // as in ChoiceGrad
+    bool keep;               // LOGPROB: the chosen logits stay where they are, for what else reads them
 };
 template <int FROM>
 struct GradFrom : GradArgs {};
@@ -869,18 +871,41 @@ struct GradFrom<GRAD_PAIRS> : GradArgs {
     PreferenceTerms p;
     const double *row_lp;
 };
-static_assert(sizeof(GradFrom<GRAD_ROWS>) == 112, "more arguments cost every launch up to 0.7 us");
+static_assert(sizeof(GradFrom<GRAD_ROWS>) == 112 && sizeof(GradFrom<GRAD_LOGPROB>) == 112, "more arguments cost every launch up to 0.7 us");
 
-__device__ __forceinline__ RowCoef coef_of(const GradArgs &a, long long row, int y)
+// p_k = exp(z_k - lse) from what hb_logprob_async has left.  As fp32 numbers lse and logp are each off by 2^-25 of themselves, and
+// lse = z_y - logp: the smaller one says more.  With lse alone an offset of the logits goes into every p_k (three classes at 1e7, 1e7 + 1 and 1e7 + 2:
+// 1.07 instead of 0.665); with z_y - logp only the distance of the choice does.  Where both are large p_k is still at most 1 - p_y.
+struct LogprobCoef {
+    RowCoef c;
+    float others;  // 1 - p_y
+};
+template <typename T>
+__device__ __forceinline__ LogprobCoef coef_of_logprob(const GradArgs &a, const Row<T> &z, long long row, int y)
 {
-    if (!a.lse) return a.coef[row];
-    RowCoef c = {0.f, 0.f, 0.f, 0.f};
-    const float lse = a.lse[row], g = a.g[row];
-    if (y < 0 || y >= a.K || lse == -INFINITY || g == 0.f) return c;
-    c.ref = lse;
-    c.scale = -g;
-    c.chosen = -g * expm1f(a.logp[row]);
-    return c;
+    LogprobCoef k = {{0.f, 0.f, 0.f, 0.f}, 0.f};
+    const float lse = a.lse[row], g = a.g[row], lp = a.logp[row];
+    const float zy = (float)z.z[min(max(y, 0), a.K - 1)];  // (asked for first: it has a load in front of it)
+    if (y < 0 || y >= a.K || lse == -INFINITY || g == 0.f) return k;
+    const bool near = 2.f * fabsf(lp) <= fabsf(lse);
+    k.others = -expm1f(lp);
+    k.c.ref = near ? zy : lse;
+    k.c.add = near ? lp * LOG2E : 0.f;
+    k.c.scale = -g;
+    k.c.chosen = g * k.others;
+    return k;
+}
+
+// The chosen elements of a gradient in place of the logits whose rows go in several chunks: all of those read them
+template <typename T>
+__global__ __launch_bounds__(NT) void chosen_grad_kernel(GradArgs a)
+{
+    const int row = blockIdx.x * NT + threadIdx.x;
+    if (row >= a.B) return;
+    const int y = a.y[row];
+    const float g = a.g[row];
+    if (y < 0 || y >= a.K || a.lse[row] == -INFINITY || g == 0.f) return;
+    static_cast<T *>(a.dZ)[(long long)row * a.lddz + y] = T(g * -expm1f(a.logp[row]));
 }
 
 // What a call on few rows has its first block do instead of one more launch: the statistics and what else is returned
@@ -940,7 +965,7 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradFrom<FROM> a)
     if ((int)blockIdx.x < a.first) {
         if constexpr (FROM == GRAD_CHUNKS) few_rows(a, red);
         else if constexpr (FROM == GRAD_PAIRS) few_pairs(a, red);
-        else sum_four<NT>(SumFour{a.partial, a.sums, a.stats}, red);
+        else if constexpr (FROM == GRAD_ROWS) sum_four<NT>(SumFour{a.partial, a.sums, a.stats}, red);
         return;
     }
     const int g = threadIdx.x % G;
@@ -960,7 +985,16 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradFrom<FROM> a)
     TO *dz = static_cast<TO *>(a.dZ) + row * a.lddz;
     const int y = a.y[row];
     RowCoef k = {0.f, 0.f, 0.f, 0.f};
-    if constexpr (FROM == GRAD_CHUNKS) {
+    float others = INFINITY;  // at most this of a class that is not chosen
+    if constexpr (FROM == GRAD_LOGPROB) {
+        const LogprobCoef l = coef_of_logprob(a, z, row, y);
+        k = l.c;
+        others = l.others;
+        if (G == NT && a.Z == a.dZ) {  // all wavefronts have the chosen logit before one of them writes over it
+            asm volatile("" : "+v"(k.ref));
+            __syncthreads();
+        }
+    } else if constexpr (FROM == GRAD_CHUNKS) {
         const RowInputs in(a.rows, row);
         Four sums;
         if (in.choice(a.K)) {
@@ -970,11 +1004,14 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradFrom<FROM> a)
     } else if constexpr (FROM == GRAD_PAIRS) {
         if (!outside) k = coef_in_pair(a, row, g % LANES, LANES);
     } else {
-        if (!outside) k = coef_of(a, row, y);
+        if (!outside) k = a.coef[row];
     }
     const int end = G == NT ? min(z.pieces, (c + 1) * a.pieces_per_chunk) : z.pieces;
     const bool none = k.scale == 0.f && k.chosen == 0.f;
-    const Under under(k.ref);
+    auto other = [&](float v) {
+        const float e = exp2_of(__builtin_fmaf(v - k.ref, LOG2E, k.add));
+        return k.scale * (FROM == GRAD_LOGPROB ? fminf(e, others) : e);
+    };
     TO *to = dz + z.head;
     const bool past = a.past && (reinterpret_cast<uintptr_t>(to) & (V * sizeof(TO) - 1)) == 0;
     // U pieces a lane; guard: not all lanes have that many left, and their loads are sent together all the same
@@ -989,10 +1026,18 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradFrom<FROM> a)
             if (decltype(guard)::value && p + u * G >= end) continue;
             float out[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) out[e] = none ? 0.f : k.scale * under.exp(x[u].get(e));
-            store<TO, V>(to + (long long)(p + u * G) * V, out, past);
+            for (int e = 0; e < V; ++e) out[e] = none ? 0.f : other(x[u].get(e));
+            TO *const piece = to + (long long)(p + u * G) * V;
             const int at = y - z.first(p + u * G);
-            if ((unsigned)at < (unsigned)V) dz[y] = TO(k.chosen);  // over what this lane has just stored there
+            const bool own = (unsigned)at < (unsigned)V;
+            if (FROM == GRAD_LOGPROB && own && a.keep && !none) {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (e != at) piece[e] = TO(out[e]);
+                continue;
+            }
+            store<TO, V>(piece, out, past);
+            if (own) dz[y] = TO(k.chosen);  // over what this lane has just stored there
         }
     };
     int p = c * a.pieces_per_chunk;
@@ -1003,8 +1048,8 @@ __global__ __launch_bounds__(NT) void logit_grad_kernel(GradFrom<FROM> a)
 #pragma unroll
         for (int i = 0; i < E; ++i) {
             const int j = z.edge(i * G + g);
-            if (j < 0) continue;
-            dz[j] = TO(none ? 0.f : j == y ? k.chosen : k.scale * under.exp(z.at(j)));
+            if (j < 0 || (FROM == GRAD_LOGPROB && j == y && a.keep && !none)) continue;
+            dz[j] = TO(none ? 0.f : j == y ? k.chosen : other(z.at(j)));
         }
         for (int j = a.K + g; j < a.pad; j += G) dz[j] = TO(0.f);
     }
@@ -1212,6 +1257,7 @@ template <typename T, typename TO, int FROM>
 hipError_t grad_of_type(const ChoiceRows &r, GradFrom<FROM> a, hipStream_t stream, const LaunchEvents &ev)
 {
     a.chunks = 1;
+    a.keep = false;
     if constexpr (FROM != GRAD_CHUNKS) {
         switch (grad_lanes(r)) {
         case 4: return grad_form<T, TO, 4, FROM>(a, stream, ev);
@@ -1224,15 +1270,20 @@ hipError_t grad_of_type(const ChoiceRows &r, GradFrom<FROM> a, hipStream_t strea
     const Split s = split_for(r);
     a.chunks = s.chunks;
     a.pieces_per_chunk = s.pieces_per_chunk;
-    return launch_kernel(logit_grad_kernel<T, TO, NT, FROM>, dim3((unsigned)(r.B * s.chunks + a.first)), dim3(NT), stream, ev, a);
+    a.keep = FROM == GRAD_LOGPROB && a.Z == a.dZ && s.chunks > 1;
+    const hipError_t e =
+        launch_kernel(logit_grad_kernel<T, TO, NT, FROM>, dim3((unsigned)(r.B * s.chunks + a.first)), dim3(NT), stream, ev, a);
+    if (e != hipSuccess || !a.keep) return e;
+    return launch_kernel(chosen_grad_kernel<TO>, dim3((unsigned)ceil_div(r.B, NT)), dim3(NT), stream, LaunchEvents(), GradArgs(a));
 }
 
 template <int FROM>
 hipError_t logit_grad(const ChoiceRows &r, int dz, GradFrom<FROM> a, hipStream_t stream, const LaunchEvents &ev)
 {
-    a.first = FROM != GRAD_ROWS || a.sums > 0;
+    a.first = FROM == GRAD_CHUNKS || FROM == GRAD_PAIRS || (FROM == GRAD_ROWS && a.sums > 0);
     if (r.tensor == TENSOR_BF16) return grad_of_type<__bf16, __bf16, FROM>(r, a, stream, ev);
-    return dz == TENSOR_BF16 ? grad_of_type<float, __bf16, FROM>(r, a, stream, ev) : grad_of_type<float, float, FROM>(r, a, stream, ev);
+    if constexpr (FROM == GRAD_LOGPROB) return grad_of_type<float, float, FROM>(r, a, stream, ev);
+    else return dz == TENSOR_BF16 ? grad_of_type<float, __bf16, FROM>(r, a, stream, ev) : grad_of_type<float, float, FROM>(r, a, stream, ev);
 }
 
 // Whether the gradient's kernel sums up the pairs itself, each row those of its own, and its first block all of them: one launch
@@ -1286,7 +1337,7 @@ hipError_t launch_logprob_grad(const ChoiceRows &r, const float *logp, const flo
                                hipStream_t stream, const LaunchEvents &ev)
 {
     if (r.B == 0) return hipSuccess;
-    auto a = grad_args<GRAD_ROWS>(r, d);
+    auto a = grad_args<GRAD_LOGPROB>(r, d);
     a.logp = logp;
     a.lse = lse;
     a.g = g;

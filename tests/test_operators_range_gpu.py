@@ -127,6 +127,51 @@ def test_logprob_of_logits_of_any_size(B, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,K", SHAPES + [(84, 9001), (300, 20011)])
+def test_gradient_of_log_probabilities_of_any_size(B, K, dtype):
+    """exp(z - lse) from lse or z_y - logp, n the smaller of |logp| and |lse|: what n is rounded to, what is subtracted from it and its
+    product with log2 e add 4 u n to an exponent.  Where that is not small the probability is still at most 1 - p_y."""
+    rng = np.random.default_rng(B + 7 * K)
+    z, y = rows(B, K, dtype, rng)
+    lp, lse, p, m = softmax_ref(z, y)
+    g = rng.standard_normal(B).astype(np.float32).astype(np.float64)
+    g[1::13] = 0.0
+    unit = unit_grad(p.copy(), y)
+    others = unit[np.arange(B), y]
+    off = eps(K) + (2 * np.minimum(m[:, None] - z, 104.0) + 16 + 4 * np.minimum(np.abs(lp), np.abs(lse))[:, None]) * U
+    off = np.minimum(np.abs(unit) * np.expm1(np.minimum(off, 80.0)), np.maximum(others, p.max(1))[:, None] + 0.0 * unit)
+    off[np.arange(B), y] = (2 * eps(K) + 16 * U) * others
+    tol = np.abs(g)[:, None] * (off + 4 * U * np.abs(unit) + TINY) + 2.0 ** -126
+    if dtype == "bf16":
+        tol = tol + 2.0 ** -8 * (np.abs(unit * g[:, None]) + tol)
+    Z, dy, a, b = device(z, dtype), vec(y, torch.int32), torch.zeros(B, device="cuda"), torch.zeros(B, device="cuda")
+    hb.logprob(Z, dy, a, b, ws=ws(B))
+    dZ = torch.full_like(Z, 7.0)
+    hb.logprob_grad(Z, dy, a, b, vec(g), dZ)
+    near(dZ, unit * g[:, None], tol, "dZ")
+    assert torch.isfinite(dZ).all()
+    wide = torch.full((B, K + 5), 7.0, device="cuda", dtype=TYPES[dtype])     # in place, other edges
+    wide[:, 3:K + 3] = Z
+    hb.logprob_grad(wide[:, 3:K + 3], dy, a, b, vec(g), wide[:, 3:K + 3])
+    near(wide[:, 3:K + 3], unit * g[:, None], tol, "dZ in place")
+    assert bool((wide[:, :3] == 7.0).all()) and bool((wide[:, K + 3:] == 7.0).all())
+    hb.logprob_grad(Z, dy, a, b, vec(g), Z)
+    assert torch.equal(Z, dZ)
+
+
+@pytest.mark.parametrize("c", [0.0, 1e4, 1e5, 1e7, -1e7])
+def test_an_offset_of_the_logits_costs_a_gradient_nothing(c):
+    """Three classes at c, c + 1, c + 2: softmax 0.0900, 0.2447, 0.6652, whatever c; off by the exponentials' roundings."""
+    z = np.array([[c, c + 1, c + 2]] * 3)
+    y = np.arange(3, dtype=np.int32)
+    a, b, dZ = torch.zeros(3, device="cuda"), torch.zeros(3, device="cuda"), torch.zeros(3, 3, device="cuda")
+    hb.logprob(device(z, "f32"), vec(y, torch.int32), a, b, ws=ws(3))
+    hb.logprob_grad(device(z, "f32"), vec(y, torch.int32), a, b, torch.ones(3, device="cuda"), dZ)
+    p = np.exp([0.0, 1.0, 2.0])
+    near(dZ, np.eye(3) - p / p.sum(), 32 * U, "dZ")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("B,K", SHAPES)
 def test_policy_loss_on_logits_of_any_size(B, K, dtype):
     """Advantages of both signs, log-ratios away from the borders of the clip; a choice that is all but impossible has ratio 0."""
