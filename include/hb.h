@@ -225,7 +225,8 @@ int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call
  *   hb_policy_grad_async      its gradient instead (d_grad_flat: P floats, flat layout); the replica is left untouched
  *   hb_preference_step_async, hb_preference_grad_async   the same of the preference loss
  * Nothing is synchronised; the calls enqueue kernels only and may be captured once one ordinary call of them has been made (the
- * first allocates the handle's workspace for them).  The handle's device has to be current.
+ * first allocates the handle's workspace for them).  The handle's device has to be current.  What a call writes must not overlap
+ * what it reads or what else it writes (HB_ERR_INVALID).
  */
 struct hb_policy;
 struct hb_preference;

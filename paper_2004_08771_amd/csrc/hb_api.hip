@@ -1856,6 +1856,12 @@ static int validate_head_call(hb_model *m, const void *dX, const int32_t *dy, in
     return check_current_device(m);
 }
 
+// X as it is read
+static Block input_block(const hb_model *m, const void *dX, int64_t B)
+{
+    return Block(dX, (size_t)B * (size_t)m->dims[0] * (m->dtype == HB_BF16_F32MASTER ? 2 : 4), "dX");
+}
+
 static int run_head_call(hb_model *m, const void *dX, const int32_t *dy, int64_t B, float lr, StepMode mode, float *d_grad_flat,
                          const Head &head)
 {
@@ -1879,7 +1885,9 @@ int hb_batch_logprob_async(hb_model *m, const void *dX, const int32_t *dy, int64
     const int rc = validate_head_call(m, dX, dy, B);
     if (rc != HB_OK) return rc;
     if (!d_logp) return fail(HB_ERR_INVALID, "d_logp is NULL");
-    if (d_lse == d_logp) return fail(HB_ERR_INVALID, "d_lse overlaps d_logp");
+    const size_t n = sizeof(float) * (size_t)B;
+    const int rc_a = check_apart<2, 2>({{d_logp, n, "d_logp"}, {d_lse, n, "d_lse"}}, {input_block(m, dX, B), {dy, n, "dy"}});
+    if (rc_a != HB_OK) return rc_a;
     Head head;
     head.logp = d_logp;
     head.lse = d_lse;
@@ -1894,7 +1902,11 @@ static int policy_call(hb_model *m, const void *dX, const int32_t *dy, int64_t B
     if (rc != HB_OK) return rc;
     if (!policy->d_old_logp || !policy->d_adv) return fail(HB_ERR_INVALID, "d_old_logp or d_adv is NULL");
     if (!d_stats) return fail(HB_ERR_INVALID, "d_stats is NULL");
-    rc = check_policy_apart(policy, dy, B, d_stats, d_logp, nullptr, 0, nullptr, 0, 0, TENSOR_F32, nullptr, 0);
+    const size_t n = sizeof(float) * (size_t)B;
+    rc = check_apart<3, 6>({{d_grad_flat, sizeof(float) * (size_t)m->P, "d_grad_flat"}, {d_stats, 4 * sizeof(float), "d_stats"},
+                            {d_logp, n, "d_logp"}},
+                           {input_block(m, dX, B), {dy, n, "dy"}, {policy->d_old_logp, n, "d_old_logp"}, {policy->d_ref_logp, n, "d_ref_logp"},
+                            {policy->d_adv, n, "d_adv"}, {policy->d_weight, n, "d_weight"}});
     if (rc != HB_OK) return rc;
     const PolicyTerms t = policy_terms(policy, B, d_stats, d_logp);
     Head head;
@@ -1924,7 +1936,11 @@ static int preference_call(hb_model *m, const void *dX, const int32_t *dy, int64
     if (preference->pairs > m->max_B)
         return fail(HB_ERR_INVALID, "pairs = %d is more than max_B = %lld", preference->pairs, (long long)m->max_B);
     if (!d_stats) return fail(HB_ERR_INVALID, "d_stats is NULL");
-    rc = check_preference_apart(preference, dy, B, d_stats, d_seq_logp, nullptr, 0, nullptr, 0, 0, TENSOR_F32, nullptr, 0);
+    const size_t pairs = 2 * sizeof(float) * (size_t)preference->pairs;
+    rc = check_apart<3, 4>({{d_grad_flat, sizeof(float) * (size_t)m->P, "d_grad_flat"}, {d_stats, 4 * sizeof(float), "d_stats"},
+                            {d_seq_logp, pairs, "d_seq_logp"}},
+                           {input_block(m, dX, B), {dy, sizeof(float) * (size_t)B, "dy"},
+                            {preference->d_seq, pairs + sizeof(int32_t), "d_seq"}, {preference->d_ref_logp, pairs, "d_ref_logp"}});
     if (rc != HB_OK) return rc;
     const PreferenceTerms t = preference_terms(preference, d_stats, d_seq_logp);
     Head head;

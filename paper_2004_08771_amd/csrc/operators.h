@@ -3,6 +3,7 @@
 #pragma once
 
 #include <stddef.h>
+#include <stdint.h>
 
 #include "../../include/hb.h"
 #include "hb_internal.h"
@@ -76,16 +77,38 @@ hipError_t launch_policy(const ChoiceRows &r, const PolicyTerms &t, const Choice
 hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, const ChoiceGrad &d, void *ws, hipStream_t stream,
                              const LaunchEvents &ev = LaunchEvents());
 
+// rows x cols elements of `size` bytes from p on, `ld` apart; or n bytes.  A null pointer has none.
+struct Block {
+    const char *begin, *end;
+    const char *name;
+    Block(const void *p, int64_t rows, int64_t cols, int64_t ld, size_t size, const char *name_ = "")
+        : begin(static_cast<const char *>(p)),
+          end(begin + (p && rows > 0 && cols > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * size : 0)), name(name_)
+    {
+    }
+    Block(const void *p, size_t bytes, const char *name_) : begin(static_cast<const char *>(p)), end(begin + (p ? bytes : 0)), name(name_) {}
+    bool meets(const Block &o) const { return begin < o.end && o.begin < end; }
+};
+
+// What a call writes has to be apart from what it reads, and from what else it writes.  (A block of the launch may have written
+// where another still has to read.)  skip: that many of either list may be the same memory
+template <int N, int M>
+int check_apart(const Block (&outs)[N], const Block (&ins)[M], int skip = 0)
+{
+    for (int i = 0; i < N; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (outs[i].meets(outs[j])) return set_error(HB_ERR_INVALID, "%s overlaps %s", outs[i].name, outs[j].name);
+        for (int j = 0; j < M; ++j)
+            if ((i >= skip || j >= skip) && outs[i].meets(ins[j]))
+                return set_error(HB_ERR_INVALID, "%s overlaps %s", outs[i].name, ins[j].name);
+    }
+    return HB_OK;
+}
+
 // what the entry points check and pass on of their arguments (operators_api.hip)
 int check_dropout_p(float p, unsigned *threshold);
 int check_policy(const hb_policy *p);
 int check_preference(const hb_preference *p);
-// what they write apart from what they read, but for d_dZ and d_Z; Z, dZ and ws may be null
-int check_policy_apart(const hb_policy *p, const int32_t *y, int64_t B, const float *stats, const float *logp, const void *Z,
-                       int64_t ldz, const void *dZ, int64_t lddz, int64_t K, int tensor, const void *ws, size_t ws_bytes);
-int check_preference_apart(const hb_preference *p, const int32_t *y, int64_t B, const float *stats, const float *seq_logp,
-                           const void *Z, int64_t ldz, const void *dZ, int64_t lddz, int64_t K, int tensor, const void *ws,
-                           size_t ws_bytes);
 PolicyTerms policy_terms(const hb_policy *p, int64_t B, float *d_stats, float *d_logp);
 PreferenceTerms preference_terms(const hb_preference *p, float *d_stats, float *d_seq_logp);
 

@@ -21,34 +21,6 @@ int check_type(int tensor)
 
 bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// rows x cols elements of `size` bytes from p on, `ld` apart; or n bytes.  A null pointer has none.
-struct Block {
-    const char *begin, *end;
-    const char *name;
-    Block(const void *p, int64_t rows, int64_t cols, int64_t ld, size_t size, const char *name_ = "")
-        : begin(static_cast<const char *>(p)),
-          end(begin + (p && rows > 0 && cols > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * size : 0)), name(name_)
-    {
-    }
-    Block(const void *p, size_t bytes, const char *name_) : begin(static_cast<const char *>(p)), end(begin + (p ? bytes : 0)), name(name_) {}
-    bool meets(const Block &o) const { return begin < o.end && o.begin < end; }
-};
-
-// What a call writes has to be apart from what it reads, and from what else it writes.  (A block of the launch may have written
-// where another still has to read.)  skip: that many of either list may be the same memory
-template <int N, int M>
-int check_apart(const Block (&outs)[N], const Block (&ins)[M], int skip = 0)
-{
-    for (int i = 0; i < N; ++i) {
-        for (int j = 0; j < i; ++j)
-            if (outs[i].meets(outs[j])) return set_error(HB_ERR_INVALID, "%s overlaps %s", outs[i].name, outs[j].name);
-        for (int j = 0; j < M; ++j)
-            if ((i >= skip || j >= skip) && outs[i].meets(ins[j]))
-                return set_error(HB_ERR_INVALID, "%s overlaps %s", outs[i].name, ins[j].name);
-    }
-    return HB_OK;
-}
-
 // in place (the same rows), or apart
 int check_out(const void *in, int64_t ldi, const void *out, int64_t ldo, int64_t rows, int64_t cols, size_t size, const char *what)
 {
@@ -128,6 +100,27 @@ int check_workspace(const void *ws, size_t ws_bytes, int64_t B, int32_t pairs)
     return HB_OK;
 }
 
+// What they write apart from what they read, but for d_dZ and d_Z
+int check_policy_apart(const hb_policy *p, const int32_t *y, int64_t B, const float *stats, const float *logp, const void *Z,
+                       int64_t ldz, const void *dZ, int64_t lddz, int64_t K, int tensor, const void *ws, size_t ws_bytes)
+{
+    const size_t n = sizeof(float) * (size_t)B, size = size_of(tensor);
+    return check_apart<4, 6>({{dZ, B, K, lddz, size, "d_dZ"}, {stats, 4 * sizeof(float), "d_stats"}, {logp, n, "d_logp"}, {ws, ws_bytes, "d_ws"}},
+                             {{Z, B, K, ldz, size, "d_Z"}, {y, n, "d_y"}, {p->d_old_logp, n, "d_old_logp"}, {p->d_ref_logp, n, "d_ref_logp"},
+                              {p->d_adv, n, "d_adv"}, {p->d_weight, n, "d_weight"}}, 1);
+}
+
+int check_preference_apart(const hb_preference *p, const int32_t *y, int64_t B, const float *stats, const float *seq_logp,
+                           const void *Z, int64_t ldz, const void *dZ, int64_t lddz, int64_t K, int tensor, const void *ws,
+                           size_t ws_bytes)
+{
+    const size_t n = sizeof(float) * (size_t)B, pairs = 2 * sizeof(float) * (size_t)p->pairs, size = size_of(tensor);
+    return check_apart<4, 4>({{dZ, B, K, lddz, size, "d_dZ"}, {stats, 4 * sizeof(float), "d_stats"}, {seq_logp, pairs, "d_seq_logp"},
+                              {ws, ws_bytes, "d_ws"}},
+                             {{Z, B, K, ldz, size, "d_Z"}, {y, n, "d_y"}, {p->d_seq, pairs + sizeof(int32_t), "d_seq"},
+                              {p->d_ref_logp, pairs, "d_ref_logp"}}, 1);
+}
+
 ChoiceRows rows_of(const void *Z, int64_t ldz, int tensor, const int32_t *y, const float *weight, int64_t B, int32_t K)
 {
     ChoiceRows r = {};
@@ -183,26 +176,6 @@ int check_preference(const hb_preference *p)
     if (!(p->smoothing >= 0.f && p->smoothing <= 0.5f))
         return set_error(HB_ERR_INVALID, "smoothing = %g is outside [0, 0.5]", (double)p->smoothing);
     return HB_OK;
-}
-
-int check_policy_apart(const hb_policy *p, const int32_t *y, int64_t B, const float *stats, const float *logp, const void *Z,
-                       int64_t ldz, const void *dZ, int64_t lddz, int64_t K, int tensor, const void *ws, size_t ws_bytes)
-{
-    const size_t n = sizeof(float) * (size_t)B, size = size_of(tensor);
-    return check_apart<4, 6>({{dZ, B, K, lddz, size, "d_dZ"}, {stats, 4 * sizeof(float), "d_stats"}, {logp, n, "d_logp"}, {ws, ws_bytes, "d_ws"}},
-                             {{Z, B, K, ldz, size, "d_Z"}, {y, n, "d_y"}, {p->d_old_logp, n, "d_old_logp"}, {p->d_ref_logp, n, "d_ref_logp"},
-                              {p->d_adv, n, "d_adv"}, {p->d_weight, n, "d_weight"}}, 1);
-}
-
-int check_preference_apart(const hb_preference *p, const int32_t *y, int64_t B, const float *stats, const float *seq_logp,
-                           const void *Z, int64_t ldz, const void *dZ, int64_t lddz, int64_t K, int tensor, const void *ws,
-                           size_t ws_bytes)
-{
-    const size_t n = sizeof(float) * (size_t)B, pairs = 2 * sizeof(float) * (size_t)p->pairs, size = size_of(tensor);
-    return check_apart<4, 4>({{dZ, B, K, lddz, size, "d_dZ"}, {stats, 4 * sizeof(float), "d_stats"}, {seq_logp, pairs, "d_seq_logp"},
-                              {ws, ws_bytes, "d_ws"}},
-                             {{Z, B, K, ldz, size, "d_Z"}, {y, n, "d_y"}, {p->d_seq, pairs + sizeof(int32_t), "d_seq"},
-                              {p->d_ref_logp, pairs, "d_ref_logp"}}, 1);
 }
 
 PolicyTerms policy_terms(const hb_policy *p, int64_t B, float *d_stats, float *d_logp)

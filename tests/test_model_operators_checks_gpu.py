@@ -1,0 +1,51 @@
+"""What the calls of a handle with a loss of their own refuse, and what its profile says of them."""
+import pytest
+import torch
+
+import hb_inputs as hi
+import paper_2004_08771_amd as hb
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = hb.HB_F32, hb.HB_BF16_F32MASTER
+CE = hi.LOSS_SOFTMAX_CE
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_outputs_of_a_handle_that_overlap_are_refused(dtype):
+    """One allocation cut into pieces that meet: outputs with each other, with the labels, the input, and what a row has besides."""
+    B, dims = 32, (8, 16, 4)
+    m = hb.Model(dims, hi.ACT_SIGMOID, CE).configure(dtype, B)
+    P = m.num_params
+    X = torch.zeros(B, 8, device="cuda", dtype=torch.float32 if dtype == F32 else torch.bfloat16)
+    flat_x = X.view(-1).view(torch.float32)
+    y = torch.zeros(B, dtype=torch.int32, device="cuda")
+    buf = torch.zeros(P + 100, device="cuda")
+    v, w, r, st = [torch.zeros(B, device="cuda") for _ in range(4)]
+    seq, pref = torch.tensor([0, 5, 32], dtype=torch.int32, device="cuda"), torch.zeros(2, device="cuda")
+    pol = hb.policy_args(B, v, w, ref=r, weight=buf[:B], kl_coef=0.1)
+    prf = hb.preference_args(seq, pref)
+    labels = y.view(torch.float32)
+    refused = [
+        lambda: m.batch_logprob_async(X, y, B, buf[:B], buf[B - 1:2 * B - 1]), lambda: m.batch_logprob_async(X, y, B, buf[1:], buf[:B]),
+        lambda: m.batch_logprob_async(X, y, B, labels), lambda: m.batch_logprob_async(X, y, B, v, labels),
+        lambda: m.batch_logprob_async(X, y, B, flat_x[-B:]), lambda: m.batch_logprob_async(X, y, B, v, flat_x),
+        lambda: m.policy_step_async(X, y, B, 0.1, pol, flat_x[-4:]), lambda: m.policy_step_async(X, y, B, 0.1, pol, st, labels),
+        lambda: m.policy_step_async(X, y, B, 0.1, pol, st, buf[B - 1:]), lambda: m.policy_step_async(X, y, B, 0.1, pol, st[4:], st[:B]),
+        lambda: m.policy_grad_async(X, y, B, pol, buf, st), lambda: m.policy_grad_async(X, y, B, pol, buf[B:], buf[B + P - 1:]),
+        lambda: m.policy_grad_async(X, y, B, pol, buf[B:], st, buf[B + 3:]),
+        lambda: m.preference_step_async(X, y, B, 0.1, prf, st, st[3:]), lambda: m.preference_step_async(X, y, B, 0.1, prf, labels),
+        lambda: m.preference_step_async(X, y, B, 0.1, prf, st, pref), lambda: m.preference_grad_async(X, y, B, prf, buf, buf[P - 1:]),
+        lambda: m.preference_grad_async(X, y, B, prf, buf, st, buf[7:]), lambda: m.preference_grad_async(X, y, B, prf, flat_x[-1:], st),
+    ]
+    for i, call in enumerate(refused):
+        with pytest.raises(hb.HbError) as e:
+            call()
+        assert e.value.code == hb.HB_ERR_INVALID and "overlaps" in str(e.value), i
+    # side by side is fine
+    m.batch_logprob_async(X, y, B, buf[:B], buf[B:2 * B])
+    m.policy_grad_async(X, y, B, pol, buf[B:B + P], buf[B + P:B + P + 4], buf[B + P + 4:B + P + 4 + B])
+    m.preference_grad_async(X, y, B, prf, buf[B:B + P], buf[B + P:B + P + 4], buf[B + P + 4:B + P + 6])
+    torch.cuda.synchronize()
+    assert torch.isfinite(buf).all()
+    m.destroy()
