@@ -488,7 +488,8 @@ int hb_hogbatch_run_epoch(hb_sched *s, hb_model *gpu, int32_t gpu_worker, int32_
  * hip_stream (a hipStream_t, NULL = the default stream): nothing is allocated, copied, cleared or synchronised, so they may be
  * captured.  Everything has to be on the device that is current at the call, the stream too: pointers that are not in
  * its memory are HB_ERR_INVALID, as is a stream of another device.  Inputs are only read, and only in stream order.  What a
- * call writes must not overlap what it reads or what else it writes (HB_ERR_INVALID), but where it says so.
+ * call writes must not overlap what it reads or what else it writes (HB_ERR_INVALID), but where it says so; what lies between the rows of a
+ * matrix is not part of it (two halves of the columns of one buffer do not overlap).
  */
 enum { HB_TENSOR_F32 = 0, HB_TENSOR_BF16 = 1 };
 

@@ -81,13 +81,22 @@ hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, cons
 struct Block {
     const char *begin, *end;
     const char *name;
-    Block(const void *p, int64_t rows, int64_t cols, int64_t ld, size_t size, const char *name_ = "")
-        : begin(static_cast<const char *>(p)),
-          end(begin + (p && rows > 0 && cols > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * size : 0)), name(name_)
+    int64_t rows, row, pitch;  // bytes of a row, and from one to the next
+    Block(const void *p, int64_t rows_, int64_t cols, int64_t ld, size_t size, const char *name_ = "")
+        : begin(static_cast<const char *>(p)), end(begin), name(name_), rows(rows_), row(cols * (int64_t)size), pitch(ld * (int64_t)size)
+    {
+        if (p && rows > 0 && cols > 0) end = begin + (size_t)(rows - 1) * (size_t)pitch + (size_t)row;
+        if (rows == 1 || pitch == row) {  // one piece
+            row = pitch = end - begin;
+            rows = 1;
+        }
+    }
+    Block(const void *p, size_t bytes, const char *name_)
+        : begin(static_cast<const char *>(p)), end(begin + (p ? bytes : 0)), name(name_), rows(1), row(end - begin), pitch(row)
     {
     }
-    Block(const void *p, size_t bytes, const char *name_) : begin(static_cast<const char *>(p)), end(begin + (p ? bytes : 0)), name(name_) {}
-    bool meets(const Block &o) const { return begin < o.end && o.begin < end; }
+    bool meets(const Block &o) const { return begin < o.end && o.begin < end && ((rows == 1 && o.rows == 1) || rows_meet(o)); }
+    bool rows_meet(const Block &o) const;  // what of the two ranges is between rows is not counted
 };
 
 // What a call writes has to be apart from what it reads, and from what else it writes.  (A block of the launch may have written

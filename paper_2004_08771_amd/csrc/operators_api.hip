@@ -147,6 +147,40 @@ ChoiceGrad grad_of(void *dZ, int64_t lddz, int tensor)
 
 namespace hb {
 
+// Sum over i = 0 .. n - 1 of floor((a i + b) / m), a, b >= 0: the lattice points under a line.  What a and b hold of whole m is
+// counted at once, the rest with the axes exchanged, as in Euclid's algorithm.
+static __int128 floor_sum(__int128 n, __int128 m, __int128 a, __int128 b)
+{
+    __int128 sum = 0;
+    for (;;) {
+        sum += n * (n - 1) / 2 * (a / m) + n * (b / m);
+        a %= m;
+        b %= m;
+        const __int128 top = a * n + b;
+        if (top < m) return sum;
+        n = top / m;
+        b = top % m;
+        const __int128 t = m;
+        m = a;
+        a = t;
+    }
+}
+
+// Row i of this block begins s = c + i pitch behind the other one and meets row j of it if j o.pitch < s + row and j o.pitch + o.row > s:
+// floor((s + row - 1) / o.pitch) - floor((s - o.row) / o.pitch) whole numbers j.  Of the rows that are within the other one's range, one that
+// meets a row in front of its first or behind its last meets that one, too, so the sum of these is 0 if they are apart.
+bool Block::rows_meet(const Block &o) const
+{
+    const __int128 c = (__int128)(begin - o.begin), range = o.end - o.begin;
+    __int128 i0 = 0, i1 = rows - 1;
+    if (c <= -row) i0 = (-row - c) / pitch + 1;                                   // the first with s > -row
+    if (c + i1 * pitch >= range) i1 = c >= range ? -1 : (range - 1 - c) / pitch;  // the last with s < range
+    if (i0 > i1) return false;
+    const __int128 shift = ((__int128)row + o.row) / o.pitch + 1;                 // whole pitches, so that nothing below is negative
+    const __int128 first = c + i0 * pitch + shift * o.pitch;
+    return floor_sum(i1 - i0 + 1, o.pitch, pitch, first + row - 1) > floor_sum(i1 - i0 + 1, o.pitch, pitch, first - o.row);
+}
+
 int check_dropout_p(float p, unsigned *threshold)
 {
     if (!(p >= 0.f && p < 1.f)) return set_error(HB_ERR_INVALID, "p = %g is outside [0, 1)", (double)p);

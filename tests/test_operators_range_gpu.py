@@ -251,3 +251,24 @@ def test_a_plain_implementation_agrees_with_its_own_definition():
     part, lp2, lse2, p2 = ref.rows_ref(z, y)
     assert np.allclose(lp, lp2, atol=1e-13) and np.allclose(lse, lse2, atol=1e-13) and np.allclose(p, p2, atol=1e-15)
     assert np.allclose(unit_grad(p, y), ref.grad_ref(part, p2, y, np.ones(9)), atol=1e-15)
+
+
+def test_matrices_side_by_side_in_one_buffer():
+    """Input and output as the two halves of a buffer's columns: as apart (the logits aligned alike: a row's sum is made in pieces that
+    begin at 16-byte boundaries), and nothing else is written."""
+    rng = np.random.default_rng(4)
+    B, K = 37, 203
+    z, y = rows(B, K, "f32", rng)
+    buf = torch.full((B, 2 * K + 7), 7.0, device="cuda")
+    left, right = buf[:, 1:K + 1], buf[:, K + 1:2 * K + 1]
+    left.copy_(torch.as_tensor(z))
+    Z, dy, apart = buf.clone()[:, 1:K + 1], vec(y, torch.int32), torch.full((B, K), 7.0, device="cuda")
+    a, b, g = torch.zeros(B, device="cuda"), torch.zeros(B, device="cuda"), torch.ones(B, device="cuda")
+    st = torch.zeros(4, device="cuda")
+    hb.logprob(left, dy, a, b, ws=ws(B))
+    for call in (lambda z, d: hb.dropout(z, d, 0.25, 3, 1), lambda z, d: hb.logprob_grad(z, dy, a, b, g, d),
+                 lambda z, d: hb.policy_loss(z, dy, a, g, st, dZ=d, ws=ws(B))):
+        call(left, right)
+        call(Z, apart)
+        assert torch.equal(right, apart) and torch.equal(left, Z)
+        assert bool((buf[:, 0] == 7.0).all()) and bool((buf[:, 2 * K + 1:] == 7.0).all())
