@@ -564,8 +564,8 @@ int hb_policy_loss_async(const void *d_Z, int64_t ldz, int tensor, const int32_t
  * device, non-decreasing, within [0, B]; a sequence may be empty); sequence 2n was preferred over 2n + 1.
  * With s_q = the sum of logp over the rows of sequence q that have a choice and h_n = (s_2n - ref_2n) - (s_2n+1 - ref_2n+1):
  *     loss = mean over the pairs of -(1 - smoothing) log sigma(beta h_n) - smoothing log sigma(-beta h_n)
- * and dZ is its gradient.  Rows without a choice or without an allowed class add nothing and get zeros.  Rows in front
- * of the first and behind the last sequence are neither read nor written.  Offsets out of range are cut to it;
+ * and dZ is its gradient.  Rows without a choice or without an allowed class add nothing and get zeros.  In rows in front
+ * of the first and behind the last sequence the logits are not read and the gradient is not written.  Offsets out of range are cut to it;
  * decreasing ones make a sequence empty, and the results of its neighbours mean nothing then.
  * d_stats (4 floats): loss, share of the pairs with h_n > 0, mean of beta (s_2n - ref_2n), mean of beta
  * (s_2n+1 - ref_2n+1).  d_seq_logp (may be NULL): 2 pairs floats, s_q.  d_dZ: as for hb_logprob_grad_async; NULL: the loss

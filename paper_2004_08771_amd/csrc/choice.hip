@@ -293,7 +293,9 @@ struct RowsArgs {
         } l;
         struct {
             double *row_lp;     // 0 where a row takes no part
+            const int32_t *seq; // rows in front of seq[0] and from seq[last] on are not looked at
             RowCoef *coef;      // {maximum, 1 / s, 1 - p_y}; null: none
+            int last;
         } t;
         struct {
             const float *old_logp, *ref_logp, *adv;
@@ -320,6 +322,7 @@ struct RowInputs {
     __device__ __forceinline__ RowInputs(const RowsArgs &a, long long row)
         : y(a.y[row]), w(1.f), old_logp(0.f), adv(0.f), ref_logp(0.f)
     {
+        if (a.head == HEAD_TERMS && (row < a.t.seq[0] || row >= a.t.seq[a.t.last])) y = -1;
         if (a.head != HEAD_POLICY) return;
         w = a.weight ? a.weight[row] : a.p.uniform;
         old_logp = a.p.old_logp[row];
@@ -1415,6 +1418,8 @@ hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, cons
         RowsArgs a = rows_args(r, HEAD_TERMS);
         a.t.row_lp = w.row_lp;
         a.t.coef = d.dZ ? w.coef : nullptr;
+        a.t.seq = t.seq;
+        a.t.last = 2 * t.pairs;
         int blocks = 0;
         e = rows_in_registers(r, false) ? rows(a, 0, Results{}, &blocks, stream, ev)
                                         : chunked_rows(a, split_for(r), w.partial, nullptr, Results{}, &blocks, stream, ev);
