@@ -390,7 +390,8 @@ def cpu_worker_run_epoch(sched, worker, layer_dims, activation, loss, host_X, ho
     return u.value, nb.value, ls.value
 
 
-# ---- operators on device tensors: torch tensors in, nothing returned, everything enqueued on `stream`
+# ---- operators on device tensors: torch tensors in, nothing returned, everything enqueued on `stream`: a hipStream_t as int (0: the
+# default stream), or None for the stream that torch has current, in whose order the tensors have been made
 
 _types = {}  # torch's types as objects -> HB_TENSOR_* or "int32"; they are known once a tensor has come
 
@@ -454,10 +455,21 @@ def _workspace(ws):
     return ws.data_ptr(), ws.nbytes
 
 
-def _call(name, *args):
-    rc = getattr(_lib or lib(), name)(*args)
-    if rc != HB_OK:
-        _check(rc)
+def _current(device):
+    """torch's current stream of a device, as int."""
+    import torch
+    global _current
+    _current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _current(device)
+
+
+def _stream(stream, t):
+    """The stream of a call on t."""
+    if stream is None:
+        device = t.get_device()
+        if device >= 0:
+            stream = _current(device)
+    return stream or None
 
 
 def choice_workspace_bytes(B, pairs=0) -> int:
@@ -469,23 +481,29 @@ def dropout(x, out, p, seed, offset=0, stream=None):
     """hb_dropout_async on matrices x and out (out may be x).  The gradient of x is the same call on the gradient of out."""
     m = px, ldx, kind, rows, cols = _matrix(x, "x")
     po, ldo = _out_matrix(out, "out", m)
-    _call("hb_dropout_async", px, ldx, po, ldo, kind, rows, cols, p, seed, offset, stream or None)
+    rc = (_lib or lib()).hb_dropout_async(px, ldx, po, ldo, kind, rows, cols, p, seed, offset, _stream(stream, x))
+    if rc != HB_OK:
+        _check(rc)
 
 
 def logprob(Z, y, logp, lse=None, ws=None, stream=None):
     """hb_logprob_async: log-probabilities of the classes y (int32) in rows of logits Z."""
     pz, ldz, kind, B, K = _matrix(Z, "Z")
     pw, nw = _workspace(ws)
-    _call("hb_logprob_async", pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, _vector(logp, "logp", B), _vector(lse, "lse", B),
-          pw, nw, stream or None)
+    rc = (_lib or lib()).hb_logprob_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, _vector(logp, "logp", B),
+                                         _vector(lse, "lse", B), pw, nw, _stream(stream, Z))
+    if rc != HB_OK:
+        _check(rc)
 
 
 def logprob_grad(Z, y, logp, lse, g, dZ, stream=None):
     """hb_logprob_grad_async: dZ = g d logp / d Z (dZ may be Z)."""
     m = pz, ldz, kind, B, K = _matrix(Z, "Z")
     pd, ldd = _out_matrix(dZ, "dZ", m)
-    _call("hb_logprob_grad_async", pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, _vector(logp, "logp", B),
-          _vector(lse, "lse", B), _vector(g, "g", B), pd, ldd, stream or None)
+    rc = (_lib or lib()).hb_logprob_grad_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, _vector(logp, "logp", B),
+                                              _vector(lse, "lse", B), _vector(g, "g", B), pd, ldd, _stream(stream, Z))
+    if rc != HB_OK:
+        _check(rc)
 
 
 def policy_args(B, old, adv, ref=None, weight=None, clip=(0.2, 0.2), kl_coef=0.0) -> Policy:
@@ -501,8 +519,10 @@ def policy_loss(Z, y, old, adv, stats, dZ=None, ref=None, weight=None, clip=(0.2
     pd, ldd = (None, ldz) if dZ is None else _out_matrix(dZ, "dZ", m)
     pw, nw = _workspace(ws)
     args = policy_args(B, old, adv, ref, weight, clip, kl_coef)
-    _call("hb_policy_loss_async", pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, ctypes.byref(args), _vector(stats, "stats", 4),
-          _vector(logp, "logp", B), pd, ldd, pw, nw, stream or None)
+    rc = (_lib or lib()).hb_policy_loss_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, ctypes.byref(args),
+                                             _vector(stats, "stats", 4), _vector(logp, "logp", B), pd, ldd, pw, nw, _stream(stream, Z))
+    if rc != HB_OK:
+        _check(rc)
 
 
 def preference_args(seq, ref=None, beta=0.1, smoothing=0.0) -> Preference:
@@ -519,5 +539,8 @@ def preference_loss(Z, y, seq, stats, dZ=None, ref=None, beta=0.1, smoothing=0.0
     pd, ldd = (None, ldz) if dZ is None else _out_matrix(dZ, "dZ", m)
     pw, nw = _workspace(ws)
     args = preference_args(seq, ref, beta, smoothing)
-    _call("hb_preference_loss_async", pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, ctypes.byref(args),
-          _vector(stats, "stats", 4), _vector(seq_logp, "seq_logp", 2 * args.pairs), pd, ldd, pw, nw, stream or None)
+    rc = (_lib or lib()).hb_preference_loss_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, ctypes.byref(args),
+                                                 _vector(stats, "stats", 4), _vector(seq_logp, "seq_logp", 2 * args.pairs), pd, ldd,
+                                                 pw, nw, _stream(stream, Z))
+    if rc != HB_OK:
+        _check(rc)
