@@ -268,7 +268,9 @@ enum {
     HB_K_FWD_GEMM = 0,   /* Z_l = A_{l-1} W_l^T + b_l, activation          (Eq. (1)) */
     HB_K_DA_GEMM = 1,    /* delta_{l-1} = (delta_l W_l) * f'                (Eq. (2)) */
     HB_K_DW_GEMM = 2,    /* dW_l = delta_l^T A_{l-1}, db_l (split-K partials) (Eq. (2)) */
-    HB_K_LOSS = 3,       /* loss and output delta                           (Section 7.1) */
+    HB_K_LOSS = 3,       /* loss and output delta                           (Section 7.1); policy and preference losses and log-
+                            probabilities: `layer` 0 the pass over the logits, 1 sums over rows and pairs, 2 a second pass
+                            over the logits for the gradient */
     HB_K_UPDATE = 4,     /* W <- W - lr * sum of partials, all tensors      (Eq. (3)) */
     HB_K_SPMM_FWD = 5,   /* CSR first layer, forward */
     HB_K_SPARSE_DW = 6,  /* CSR first layer, gradient + update of the touched columns */

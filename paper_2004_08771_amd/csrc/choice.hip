@@ -1227,10 +1227,10 @@ hipError_t row_sums(const RowsArgs &a, const Split &s, TopSum *partial, float *c
 }
 
 hipError_t chunked_rows(RowsArgs a, const Split &s, TopSum *partial, RowCoef *coef, const Results &to, int *blocks, hipStream_t stream,
-                        const LaunchEvents &ev)
+                        const PassEvents &ev, double bytes)
 {
     const dim3 block(NT);
-    const hipError_t e = row_sums(a, s, partial, nullptr, stream, ev);
+    const hipError_t e = row_sums(a, s, partial, nullptr, stream, ev(PASS_LOGITS, bytes));
     if (e != hipSuccess || (s.chunks == 1 && a.head != HEAD_POLICY)) return e;
     // One block makes a loss' sums itself, if fewer lanes a row make it one
     const int lanes = s.chunks == 1 ? 1 : a.head != HEAD_POLICY || a.B <= 4 || a.B > 64 ? 64 : a.B <= 16 ? 16 : 4;
@@ -1239,7 +1239,8 @@ hipError_t chunked_rows(RowsArgs a, const Split &s, TopSum *partial, RowCoef *co
     to.of(a, *blocks);
     const dim3 merge((unsigned)*blocks);
     const auto kernel = lanes == 64 ? merge_kernel<64> : lanes == 16 ? merge_kernel<16> : lanes == 4 ? merge_kernel<4> : merge_kernel<1>;
-    return launch_kernel(kernel, merge, block, stream, LaunchEvents(), a, *blocks, s.chunks, (const TopSum *)partial, coef);
+    return launch_kernel(kernel, merge, block, stream, ev(PASS_SUMS, (double)sizeof(TopSum) * s.chunks * a.B), a, *blocks, s.chunks,
+                         (const TopSum *)partial, coef);
 }
 
 // A row in G lanes
@@ -1302,18 +1303,23 @@ bool pairs_in_grad(const ChoiceRows &r, int pairs)
 }
 
 // more: room for SUM_SLICES
-hipError_t add_sums(SumFour f, Four *more, hipStream_t stream)
+hipError_t add_sums(SumFour f, Four *more, hipStream_t stream, const PassEvents &ev)
 {
     if (f.n > 16 * SUM_THREADS) {
         const hipError_t e =
-            launch_kernel(sum_slices_kernel, dim3(SUM_SLICES), dim3(NT), stream, LaunchEvents(), f.partial, f.n, more);
+            launch_kernel(sum_slices_kernel, dim3(SUM_SLICES), dim3(NT), stream, ev(PASS_SUMS, (double)sizeof(Four) * f.n), f.partial, f.n, more);
         if (e != hipSuccess) return e;
         f.partial = more;
         f.n = SUM_SLICES;
     }
-    return f.n > NT ? launch_kernel(sum_four_kernel<SUM_THREADS>, dim3(1), dim3(SUM_THREADS), stream, LaunchEvents(), f)
-                    : launch_kernel(sum_four_kernel<NT>, dim3(1), dim3(NT), stream, LaunchEvents(), f);
+    const LaunchEvents le = ev(PASS_SUMS, (double)sizeof(Four) * f.n);
+    return f.n > NT ? launch_kernel(sum_four_kernel<SUM_THREADS>, dim3(1), dim3(SUM_THREADS), stream, le, f)
+                    : launch_kernel(sum_four_kernel<NT>, dim3(1), dim3(NT), stream, le, f);
 }
+
+// What a pass over the logits, and one that writes their gradient, cannot do without
+double logits_bytes(const ChoiceRows &r) { return ((r.tensor == TENSOR_BF16 ? 2.0 : 4.0) * r.K + 4.0) * (double)r.B; }
+double grad_bytes(const ChoiceRows &r, const ChoiceGrad &d) { return d.dZ ? (d.tensor == TENSOR_BF16 ? 2.0 : 4.0) * r.K * (double)r.B : 0.0; }
 
 }  // namespace
 
@@ -1325,36 +1331,36 @@ size_t choice_workspace(long long B, int pairs)
            sizeof(TopSum) * (size_t)(B > MAX_CHUNKED ? B : MAX_CHUNKED);
 }
 
-hipError_t launch_logprob(const ChoiceRows &r, float *logp, float *lse, void *ws, hipStream_t stream, const LaunchEvents &ev)
+hipError_t launch_logprob(const ChoiceRows &r, float *logp, float *lse, void *ws, hipStream_t stream, const PassEvents &ev)
 {
     if (r.B == 0) return hipSuccess;
     RowsArgs a = rows_args(r, HEAD_LOGPROB);
     a.l.logp = logp;
     a.l.lse = lse;
     int blocks = 0;
-    if (rows_in_registers(r, false)) return rows(a, 0, Results{}, &blocks, stream, ev);
-    return chunked_rows(a, split_for(r), Workspace(ws, r.B, 0).partial, nullptr, Results{}, &blocks, stream, ev);
+    if (rows_in_registers(r, false)) return rows(a, 0, Results{}, &blocks, stream, ev(PASS_LOGITS, logits_bytes(r)));
+    return chunked_rows(a, split_for(r), Workspace(ws, r.B, 0).partial, nullptr, Results{}, &blocks, stream, ev, logits_bytes(r));
 }
 
 hipError_t launch_logprob_grad(const ChoiceRows &r, const float *logp, const float *lse, const float *g, const ChoiceGrad &d,
-                               hipStream_t stream, const LaunchEvents &ev)
+                               hipStream_t stream, const PassEvents &ev)
 {
     if (r.B == 0) return hipSuccess;
     auto a = grad_args<GRAD_LOGPROB>(r, d);
     a.logp = logp;
     a.lse = lse;
     a.g = g;
-    return logit_grad(r, d.tensor, a, stream, ev);
+    return logit_grad(r, d.tensor, a, stream, ev(PASS_GRAD, logits_bytes(r) + grad_bytes(r, d)));
 }
 
 hipError_t launch_policy(const ChoiceRows &r, const PolicyTerms &t, const ChoiceGrad &d, void *ws, hipStream_t stream,
-                         const LaunchEvents &ev)
+                         const PassEvents &ev)
 {
     const Workspace w(ws, r.B, 0);
     const Results to = {w.sums, t.stats};
     SumFour fin = {w.sums, 0, t.stats};
     Four *const more = w.sums + r.B;  // (rows_kernel leaves a sum a row at most, in all of the workspace)
-    if (r.B == 0) return add_sums(fin, more, stream);
+    if (r.B == 0) return add_sums(fin, more, stream, ev);
     RowsArgs a = rows_args(r, HEAD_POLICY);
     a.p.old_logp = t.old_logp;
     a.p.ref_logp = t.ref_logp;
@@ -1369,33 +1375,33 @@ hipError_t launch_policy(const ChoiceRows &r, const PolicyTerms &t, const Choice
         a.lddz = (int)d.ld;
         a.pad = d.pad;
         a.past = past_caches(r, d);
-        const hipError_t e = rows(a, d.tensor, to, &fin.n, stream, ev);
-        return e != hipSuccess || fin.n == 1 ? e : add_sums(fin, more, stream);
+        const hipError_t e = rows(a, d.tensor, to, &fin.n, stream, ev(PASS_LOGITS, logits_bytes(r) + grad_bytes(r, d)));
+        return e != hipSuccess || fin.n == 1 ? e : add_sums(fin, more, stream, ev);
     }
     const Split s = split_for(r);
     // Chunks of few rows: their gradient's kernel joins them itself, and one block of it makes the sums (in one stream, with a launch
     // for that and without, us: 24 x 131072 fp32 19.1 / 16.1, 1 x 131072 10.3 / 9.3, 64 x 500000 bf16 54.9 / 51.9).
     if (d.dZ && r.B <= FEW) {
         float *const chosen = reinterpret_cast<float *>(w.coef);
-        const hipError_t e = row_sums(a, s, w.partial, chosen, stream, ev);
+        const hipError_t e = row_sums(a, s, w.partial, chosen, stream, ev(PASS_LOGITS, logits_bytes(r)));
         if (e != hipSuccess) return e;
         auto g = grad_args<GRAD_CHUNKS>(r, d);
         g.rows = a;
         g.partial_rows = w.partial;
         g.chosen = chosen;
         g.stats = t.stats;
-        return logit_grad(r, d.tensor, g, stream, LaunchEvents());
+        return logit_grad(r, d.tensor, g, stream, ev(PASS_GRAD, logits_bytes(r) + grad_bytes(r, d)));
     }
-    const hipError_t e = chunked_rows(a, s, w.partial, d.dZ ? w.coef : nullptr, to, &fin.n, stream, ev);
+    const hipError_t e = chunked_rows(a, s, w.partial, d.dZ ? w.coef : nullptr, to, &fin.n, stream, ev, logits_bytes(r));
     if (e != hipSuccess) return e;
     if (fin.n == 1) fin.n = 0;
-    if (!d.dZ) return fin.n ? add_sums(fin, nullptr, stream) : hipSuccess;
+    if (!d.dZ) return fin.n ? add_sums(fin, nullptr, stream, ev) : hipSuccess;
     auto g = grad_args<GRAD_ROWS>(r, d);
     g.coef = w.coef;
     g.partial = fin.partial;
     g.sums = fin.n;
     g.stats = t.stats;
-    return logit_grad(r, d.tensor, g, stream, LaunchEvents());
+    return logit_grad(r, d.tensor, g, stream, ev(PASS_GRAD, logits_bytes(r) + grad_bytes(r, d)));
 }
 
 template <int FROM>
@@ -1410,7 +1416,7 @@ static GradFrom<FROM> grad_of_pairs(const ChoiceRows &r, const PreferenceTerms &
 }
 
 hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, const ChoiceGrad &d, void *ws, hipStream_t stream,
-                             const LaunchEvents &ev)
+                             const PassEvents &ev)
 {
     const Workspace w(ws, r.B, t.pairs);
     hipError_t e = hipSuccess;
@@ -1421,25 +1427,27 @@ hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, cons
         a.t.seq = t.seq;
         a.t.last = 2 * t.pairs;
         int blocks = 0;
-        e = rows_in_registers(r, false) ? rows(a, 0, Results{}, &blocks, stream, ev)
-                                        : chunked_rows(a, split_for(r), w.partial, nullptr, Results{}, &blocks, stream, ev);
+        e = rows_in_registers(r, false) ? rows(a, 0, Results{}, &blocks, stream, ev(PASS_LOGITS, logits_bytes(r)))
+                                        : chunked_rows(a, split_for(r), w.partial, nullptr, Results{}, &blocks, stream, ev, logits_bytes(r));
         if (e != hipSuccess) return e;
     }
     if (d.dZ && r.B > 0 && pairs_in_grad(r, t.pairs)) {
         auto g = grad_of_pairs<GRAD_PAIRS>(r, t, d, w);
         g.p = t;
         g.row_lp = w.row_lp;
-        return logit_grad(r, d.tensor, g, stream, LaunchEvents());
+        return logit_grad(r, d.tensor, g, stream, ev(PASS_GRAD, logits_bytes(r) + grad_bytes(r, d)));
     }
-    e = launch_kernel(preference_kernel, dim3((unsigned)t.pairs), dim3(NT), stream, LaunchEvents(), t, r.B, (const double *)w.row_lp,
+    e = launch_kernel(preference_kernel, dim3((unsigned)t.pairs), dim3(NT), stream,
+                      ev(PASS_SUMS, (sizeof(double) + (d.dZ ? 2.0 * sizeof(RowCoef) : 0.0)) * (double)r.B), t, r.B, (const double *)w.row_lp,
                       d.dZ ? w.coef : nullptr, w.sums);
     if (e != hipSuccess) return e;
     if (!d.dZ || r.B == 0)
-        return launch_kernel(sum_four_kernel<SUM_THREADS>, dim3(1), dim3(SUM_THREADS), stream, LaunchEvents(), SumFour{w.sums, t.pairs, t.stats});
+        return launch_kernel(sum_four_kernel<SUM_THREADS>, dim3(1), dim3(SUM_THREADS), stream, ev(PASS_SUMS, (double)sizeof(Four) * t.pairs),
+                             SumFour{w.sums, t.pairs, t.stats});
     auto g = grad_of_pairs<GRAD_ROWS>(r, t, d, w);
     g.partial = w.sums;
     g.sums = t.pairs;
-    return logit_grad(r, d.tensor, g, stream, LaunchEvents());
+    return logit_grad(r, d.tensor, g, stream, ev(PASS_GRAD, logits_bytes(r) + grad_bytes(r, d)));
 }
 
 }  // namespace hb

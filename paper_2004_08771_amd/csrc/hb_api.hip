@@ -301,7 +301,10 @@ int run_head(hb_model *m, const Head &head, const int32_t *y, int64_t B, void *d
     d.tensor = delta_tensor;
     d.pad = pad;
     d.all_rows = true;
-    const LaunchEvents ev = prof_begin(m, HB_K_LOSS, 0, 0, 0, 0, 0.0, 4.0 * B * (r.K * (delta ? 2.0 : 1.0) + 1.0));
+    PassEvents ev;
+    if (m->prof_on) ev = {m, [](void *who, int pass, double bytes) {
+                              return prof_begin(static_cast<hb_model *>(who), HB_K_LOSS, pass, 0, 0, 0, 0.0, bytes);
+                          }};
     if (head.policy) HB_HIP(launch_policy(r, *head.policy, d, m->head_ws, m->stream, ev));
     else if (head.preference) HB_HIP(launch_preference(r, *head.preference, d, m->head_ws, m->stream, ev));
     else HB_HIP(launch_logprob(r, head.logp, head.lse, m->head_ws, m->stream, ev));

@@ -67,15 +67,22 @@ struct PreferenceTerms {
     float *stats;          // 4
     float *seq_logp;       // 2 pairs, may be null
 };
+// Who asks for the times of a call's launches: events for each, as it is made
+enum { PASS_LOGITS = 0, PASS_SUMS = 1, PASS_GRAD = 2 };  // over the logits; over rows and pairs; over the logits again, for the gradient
+struct PassEvents {
+    void *who = nullptr;
+    LaunchEvents (*events)(void *who, int pass, double bytes) = nullptr;
+    LaunchEvents operator()(int pass, double bytes) const { return events ? events(who, pass, bytes) : LaunchEvents(); }
+};
 size_t choice_workspace(long long B, int pairs);  // bytes, for all of the calls below
 hipError_t launch_logprob(const ChoiceRows &r, float *logp, float *lse, void *ws, hipStream_t stream,
-                          const LaunchEvents &ev = LaunchEvents());
+                          const PassEvents &ev = PassEvents());
 hipError_t launch_logprob_grad(const ChoiceRows &r, const float *logp, const float *lse, const float *g, const ChoiceGrad &d,
-                               hipStream_t stream, const LaunchEvents &ev = LaunchEvents());
+                               hipStream_t stream, const PassEvents &ev = PassEvents());
 hipError_t launch_policy(const ChoiceRows &r, const PolicyTerms &t, const ChoiceGrad &d, void *ws, hipStream_t stream,
-                         const LaunchEvents &ev = LaunchEvents());
+                         const PassEvents &ev = PassEvents());
 hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, const ChoiceGrad &d, void *ws, hipStream_t stream,
-                             const LaunchEvents &ev = LaunchEvents());
+                             const PassEvents &ev = PassEvents());
 
 // rows x cols elements of `size` bytes from p on, `ld` apart; or n bytes.  A null pointer has none.
 struct Block {

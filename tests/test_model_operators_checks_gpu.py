@@ -49,3 +49,47 @@ def test_outputs_of_a_handle_that_overlap_are_refused(dtype):
     torch.cuda.synchronize()
     assert torch.isfinite(buf).all()
     m.destroy()
+
+
+# calls whose rows go through registers once, are cut into chunks that the gradient's kernel or one of their own joins; few pairs, whose
+# sums the gradient's kernel makes, and many
+PROFILED = [
+    ("policy", (24, 16, 1000), 200, 0, {0: "rw", 1: ""}), ("policy", (24, 16, 7), 32, 0, {0: "rw"}), ("policy", (24, 16, 50003), 20, 0, {0: "r", 2: "rw"}),
+    ("logprob", (24, 16, 1000), 200, 0, {0: "r"}), ("logprob", (24, 16, 50003), 20, 0, {0: "r", 1: ""}),
+    ("preference", (24, 16, 1000), 200, 2, {0: "r", 2: "rw"}), ("preference", (24, 16, 7), 3000, 2, {0: "r", 1: "", 2: "rw"}),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind,dims,B,pairs,passes", PROFILED)
+def test_profile_has_every_launch_of_a_loss(kind, dims, B, pairs, passes, dtype):
+    """An entry for each pass, with what it has to move: the logits are fp32, the gradient is of the handle's type."""
+    K = dims[-1]
+    m = hb.Model(dims, hi.ACT_SIGMOID, CE).configure(dtype, B)
+    m.set_params(torch.zeros(m.num_params).numpy())
+    X = torch.randn(B, dims[0], device="cuda").to(torch.float32 if dtype == F32 else torch.bfloat16)
+    y = torch.zeros(B, dtype=torch.int32, device="cuda")
+    v, st, g = torch.zeros(B, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros(m.num_params, device="cuda")
+    seq = torch.linspace(0, B, 2 * pairs + 1).to(torch.int32).cuda() if pairs else None
+
+    def call():
+        if kind == "policy":
+            m.policy_grad_async(X, y, B, hb.policy_args(B, v, v), g, st)
+        elif kind == "preference":
+            m.preference_grad_async(X, y, B, hb.preference_args(seq), g, st)
+        else:
+            m.batch_logprob_async(X, y, B, v)
+
+    call()
+    m.profile_enable(True)
+    call()
+    call()
+    got = {s["layer"]: s for s in m.profile_read() if s["kind"] == 3}
+    m.profile_enable(False)
+    assert set(got) == set(passes)
+    for i, moved in passes.items():
+        s = got[i]
+        assert s["launches"] == 2 and s["total_ms"] > 0
+        want = (4 * B * (K + 1) if "r" in moved else 0) + ((4 if dtype == F32 else 2) * B * K if "w" in moved else 0)
+        assert s["bytes_per_launch"] == want or (not moved and s["bytes_per_launch"] > 0)
+    m.destroy()
