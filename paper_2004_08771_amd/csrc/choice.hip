@@ -1302,6 +1302,11 @@ bool pairs_in_grad(const ChoiceRows &r, int pairs)
     return pairs <= FEW && r.B <= 32 * lanes && r.B * pairs <= 128 * NT;
 }
 
+// Up to this many pairs the first block of a gradient's kernel adds up their sums beside the other blocks; one block's reading of more
+// outlasts them (us, so and with launches of their own: 16385 pairs of 4 rows x 7 46.9 / 45.8, x 983 152.6 / 156.6; 40000 pairs 102.8 /
+// 96.0 and 403 / 408; 262144 pairs x 7 572 / 499; 2^22 pairs 9490 / 7050, the loss alone there 7180 / 5140).
+constexpr int FEW_SUMS = 65536;
+
 // more: room for SUM_SLICES
 hipError_t add_sums(SumFour f, Four *more, hipStream_t stream, const PassEvents &ev)
 {
@@ -1327,6 +1332,7 @@ size_t choice_workspace(long long B, int pairs)
 {
     static_assert(sizeof(RowCoef) + sizeof(double) + sizeof(TopSum) == sizeof(Four) && MAX_SUM_BLOCKS >= SUM_SLICES,
                   "a sum for each row, and SUM_SLICES more");
+    static_assert(sizeof(TopSum) * MAX_CHUNKED >= sizeof(Four) * SUM_SLICES, "SUM_SLICES in the place of the chunks");
     return sizeof(Four) * (size_t)(pairs > MAX_SUM_BLOCKS ? pairs : MAX_SUM_BLOCKS) + (sizeof(RowCoef) + sizeof(double)) * (size_t)B +
            sizeof(TopSum) * (size_t)(B > MAX_CHUNKED ? B : MAX_CHUNKED);
 }
@@ -1441,12 +1447,13 @@ hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, cons
                       ev(PASS_SUMS, (sizeof(double) + (d.dZ ? 2.0 * sizeof(RowCoef) : 0.0)) * (double)r.B), t, r.B, (const double *)w.row_lp,
                       d.dZ ? w.coef : nullptr, w.sums);
     if (e != hipSuccess) return e;
-    if (!d.dZ || r.B == 0)
-        return launch_kernel(sum_four_kernel<SUM_THREADS>, dim3(1), dim3(SUM_THREADS), stream, ev(PASS_SUMS, (double)sizeof(Four) * t.pairs),
-                             SumFour{w.sums, t.pairs, t.stats});
+    const SumFour fin = {w.sums, t.pairs, t.stats};
+    const bool apart = !d.dZ || r.B == 0 || t.pairs > FEW_SUMS;
+    if (apart) e = add_sums(fin, reinterpret_cast<Four *>(w.partial), stream, ev);  // (what was in chunks has been joined)
+    if (e != hipSuccess || !d.dZ || r.B == 0) return e;
     auto g = grad_of_pairs<GRAD_ROWS>(r, t, d, w);
     g.partial = w.sums;
-    g.sums = t.pairs;
+    g.sums = apart ? 0 : t.pairs;
     return logit_grad(r, d.tensor, g, stream, ev(PASS_GRAD, logits_bytes(r) + grad_bytes(r, d)));
 }
 
