@@ -1095,17 +1095,25 @@ struct Split {
 };
 
 constexpr int ROW_PIECES = 20 * 1024;  // the longest row that rows_kernel has a form for
+constexpr int MAX_ROW = 8 * ROW_PIECES;
 
 // Rows go through registers, but for long ones that are few (a workgroup each leaves most of the device idle) or, where they are only
 // read, many (one workgroup of 1024 a compute unit waits between its rows), and those too long for a workgroup.
-// Measured on both sides of the lines, data from memory, us, registers against chunks: policy loss 4 x 32000 bf16 11.9 / 9.7, 16 x 32000
-// fp32 11.2 / 11.3, 64 x 32000 14.2 / 13.5 and 14.2 / 15.3, 4 x 65000 bf16 14.7 / 11.3, 64 x 65000 18.0 / 15.6, 64 x 49000 fp32 18.1 / 17.1,
-// 64 x 16000 bf16 10.2 / 12.0; 128 x 65000 19.8 / 19.6, 128 x 130000 27.1 / 28.1, 256 x 130000 40.2 / 52.7, 128 x 80000 fp32
-// 29.4 / 33.3; log-probabilities 4 x 32000 bf16 6.3 / 6.9, 4 x 65000 8.5 / 6.9, 64 x 65000 9.2 / 9.5, 64 x 49000 fp32 10.3 / 9.6,
-// 1000 x 65000 bf16 33.2 / 35.8, 1000 x 128000 74.9 / 57.7.
+// Chunks are a launch more (but for a gradient of several rows, which has a second one anyway), so the lines are further out where
+// logits are only read, or where there is one row.  us a call in a stream, the same input again and again, registers / chunks:
+//   policy loss and gradient, bf16: 4 x 24000 11.4 / 12.2, 2 x 28000 12.1 / 11.8, 64 x 28000 12.5 / 11.6, 4 x 32000 12.4 / 11.9, 64 x 32000
+//   13.2 / 11.7, 4 x 52000 12.6 / 10.3, 64 x 65000 15.7 / 10.4; fp32: 4 x 33000 11.5 / 12.1, 4 x 40000 11.8 / 12.1, 64 x 40000 12.6 / 11.5,
+//   4 x 44000 12.1 / 12.0, 64 x 49000 13.6 / 11.4; one row: bf16 40000 9.4 / 11.3, 52000 10.2 / 10.4, 65000 11.9 / 10.3, fp32 49000 10.1 / 11.3
+//   log-probabilities, bf16: 4 x 52000 6.9 / 8.4, 64 x 65000 8.1 / 8.5, 64 x 80000 9.4 / 8.5; policy loss alone 4 x 52000 9.6 / 9.7, 4 x 65000
+//   10.5 / 9.7; preference loss and gradient 4 x 52000 12.0 / 12.4, 64 x 65000 15.4 / 14.2; fp32: 4 x 49000 7.9 / 9.6, 10.9 / 11.5, 12.2 / 14.4
+// With data from memory the figures on the left are 0 to 3 us higher, those on the right 0 to 2.  More rows (data from memory):
+//   policy loss 128 x 65000 bf16 19.8 / 19.6, 128 x 130000 27.1 / 28.1, 256 x 130000 40.2 / 52.7, 128 x 80000 fp32 29.4 / 33.3;
+//   log-probabilities 1000 x 65000 bf16 33.2 / 35.8, 1000 x 128000 74.9 / 57.7.
 bool rows_in_registers(const ChoiceRows &r, bool grad)
 {
-    if (r.B <= 64 && r.K > 32768) return false;
+    const bool bf16 = r.tensor == TENSOR_BF16;
+    const int few = !grad ? (bf16 ? 60000 : MAX_ROW) : r.B == 1 ? 52000 : bf16 ? 27000 : 40000;
+    if (r.B <= 64 && r.K > few) return false;
     const int n = most_pieces(r);
     return n <= 12288 || (grad && n <= ROW_PIECES);
 }

@@ -4,6 +4,7 @@ import torch
 
 import hb_inputs as hi
 import paper_2004_08771_amd as hb
+import test_model_operators_gpu as networks
 
 pytestmark = pytest.mark.gpu
 
@@ -93,3 +94,12 @@ def test_profile_has_every_launch_of_a_loss(kind, dims, B, pairs, passes, dtype)
         want = (4 * B * (K + 1) if "r" in moved else 0) + ((4 if dtype == F32 else 2) * B * K if "w" in moved else 0)
         assert s["bytes_per_launch"] == want or (not moved and s["bytes_per_launch"] > 0)
     m.destroy()
+
+
+@pytest.mark.parametrize("p", [0.0, 0.3])
+@pytest.mark.parametrize("dims,act,dtype,B", [((24, 16, 53001), hi.ACT_SIGMOID, F32, 6), ((24, 16, 53001), hi.ACT_SIGMOID, BF16, 6),
+                                              ((24, 16, 40003), hi.ACT_SIGMOID, BF16, 20)])
+def test_losses_of_networks_whose_rows_are_cut_into_chunks(dims, act, dtype, B, p):
+    """The tests of a handle's gradients, with outputs so wide that few rows go in chunks whatever they are read for."""
+    networks.test_policy_gradient_of_a_network(dims, act, dtype, B, p)
+    networks.test_preference_gradient_of_a_network(dims, act, dtype, B, p)
