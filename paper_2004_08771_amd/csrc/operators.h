@@ -102,7 +102,11 @@ struct Block {
         : begin(static_cast<const char *>(p)), end(begin + (p ? bytes : 0)), name(name_), rows(1), row(end - begin), pitch(row)
     {
     }
-    bool meets(const Block &o) const { return begin < o.end && o.begin < end && ((rows == 1 && o.rows == 1) || rows_meet(o)); }
+    bool meets(const Block &o) const
+    {
+        if (begin >= end || o.begin >= o.end || begin >= o.end || o.begin >= end) return false;
+        return (rows == 1 && o.rows == 1) || rows_meet(o);
+    }
     bool rows_meet(const Block &o) const;  // what of the two ranges is between rows is not counted
 };
 

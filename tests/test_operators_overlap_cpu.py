@@ -62,3 +62,13 @@ def test_halves_of_a_buffer():
             with pytest.raises(hb.HbError) as e:
                 call(a, b) if len(a) == 6 else hb.dropout(a, b, 0.5, 1)
             assert ("overlaps" in str(e.value)) == meet
+
+
+def test_what_is_empty_overlaps_nothing():
+    """No rows: the pointers to what a row has may be anything, inside the statistics as well."""
+    st, ws = torch.zeros(4), torch.zeros(1 << 17, dtype=torch.uint8)
+    inside = st.data_ptr() + 4
+    policy = hb.binding.Policy(inside, None, inside, None, 0.2, 0.2, 0.0)
+    rc = hb.lib().hb_policy_loss_async(inside, 5, hb.HB_TENSOR_F32, inside, 0, 5, policy, st.data_ptr(), inside, inside, 5, ws.data_ptr(),
+                                       ws.nbytes, None)
+    assert rc != hb.HB_OK and "overlaps" not in hb.binding.last_error()      # (there is no device here)
