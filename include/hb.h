@@ -502,7 +502,7 @@ enum { HB_TENSOR_F32 = 0, HB_TENSOR_BF16 = 1 };
  * the gradient of out gives the gradient of x.  The generator is Philox4x32-10 (Salmon et al., SC 2011) with the
  * key (low, high half of seed) and the counter (column / 8, row, low, high half of offset); of its four
  * words, the element in column c takes half c % 8, low halves first, and is kept if that is at least 65536 p'.
- * Another offset (or seed) is another mask.  d_out may be d_x with ldo = ldx; otherwise they must not overlap.
+ * Another offset (or seed) is another mask; both are values of the call, so a replay of a captured call repeats its mask.  d_out may be d_x with ldo = ldx; otherwise they must not overlap.
  * bf16: the product is rounded once.  rows, cols, ldx, ldo < 2^31; rows or cols 0: nothing to do.
  */
 int hb_dropout_async(const void *d_x, int64_t ldx, void *d_out, int64_t ldo, int tensor, int64_t rows, int64_t cols, float p,
