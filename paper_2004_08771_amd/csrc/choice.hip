@@ -10,7 +10,7 @@
 //
 // All of it is bound by memory (but for short rows, whose once-a-row part counts, and small calls, which are launches).  Measured on
 // one MI355X, a large copy there 5.2 TB/s: policy loss 8192 x 50257 bf16 288 us (10 % of the rows padding; 1.56 GB, 5.4 TB/s),
-// 100000 x 2000 bf16 143 us (5.6 TB/s); log-probabilities 8192 x 32000 bf16 80 us (5.9 TB/s); of 4096 x 32000 bf16 38 us, and their
+// 100000 x 2000 bf16 120 us (800 MB, partly from the last cache); log-probabilities 8192 x 32000 bf16 80 us (5.9 TB/s); of 4096 x 32000 bf16 38 us, and their
 // gradient 75 us; preference loss of 16 pairs x 32000 bf16, 8111 rows, 246 us: the logits come twice, because
 // a token's gradient takes the whole pair (1.43 GB, 5.8 TB/s; splitting the call by pairs, so that the second pass finds the logits in
 // the last cache, costs more in launches than it saves: 286 -> 311 us in two parts, 347 us in four).

@@ -794,6 +794,10 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
             bmaj[l] = (char)gemm_bf16_dw_form(m->dims[l], m->dims[l - 1], Bi, m->ld8[l],
                                               (l == 1) ? (long long)m->dims[0] : (long long)m->ld8[l - 1],
                                               m->delta_bf[l & 1], (l == 1) ? X : input_of_next(l - 1));
+    // With dropout the transposed copy of layer l's activations is free for their derivative, unless the weight gradient of layer
+    // l + 1 needs one of what dropout leaves of them.  (Without a copy the backward-data product reads them across its rows: 16384 x
+    // 4096 x 4096 683 us instead of 437, 16384 x 4096 x 1024 405 instead of 176.)
+    auto derivative_t = [&](int l) { return m->act == ACT_SIGMOID && bmaj[l + 1]; };
     // D_l: while its weight gradient reads it, the backward-data product beside that reads D_{l-1} and writes D_{l-2}.  The third
     // buffer is that of the transposed copies of even layers, where none of those needs one.
     bool three = true;
@@ -820,7 +824,7 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
             g.C_bf16 = m->act_bf[l];
             g.ldcb = m->ld8[l];
             if (back) {
-                if (!drop && (!bmaj[l + 1] || m->act == ACT_SIGMOID)) {
+                if (drop ? derivative_t(l) : !bmaj[l + 1] || m->act == ACT_SIGMOID) {
                     g.Ct_bf16 = m->act_t[l];
                     g.ldct = ldB;
                 }
@@ -888,7 +892,7 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
         g.b_vec = 1;
         g.aux = m->act_bf[l - 1];
         g.ldaux = m->ld8[l - 1];
-        if (!drop) g.aux_t = m->act_t[l - 1];  // written by the forward pass of layer l-1
+        if (!drop || derivative_t(l - 1)) g.aux_t = m->act_t[l - 1];  // written by the forward pass of layer l-1
         g.ldauxt = ldB;
         if (m->act == ACT_RELU) {
             g.mask_in = m->relu_mask[l - 1];
