@@ -10,10 +10,10 @@
 //
 // All of it is bound by memory (but for short rows, whose once-a-row part counts, and small calls, which are launches).  Measured on
 // one MI355X, a large copy there 5.2 TB/s: policy loss 8192 x 50257 bf16 288 us (10 % of the rows padding; 1.56 GB, 5.4 TB/s),
-// 100000 x 2000 bf16 120 us (800 MB, partly from the last cache); log-probabilities 8192 x 32000 bf16 80 us (5.9 TB/s); of 4096 x 32000 bf16 38 us, and their
-// gradient 75 us; preference loss of 16 pairs x 32000 bf16, 8111 rows, 246 us: the logits come twice, because
-// a token's gradient takes the whole pair (1.43 GB, 5.8 TB/s; splitting the call by pairs, so that the second pass finds the logits in
-// the last cache, costs more in launches than it saves: 286 -> 311 us in two parts, 347 us in four).
+// 100000 x 2000 bf16 120 us (800 MB, partly from the last cache); log-probabilities 8192 x 32000 bf16 80 us (5.9 TB/s); of
+// 4096 x 32000 bf16 38 us, and their gradient 75 us; preference loss of 16 pairs x 32000 bf16, 8111 rows, 246 us: the logits come
+// twice, because a token's gradient takes the whole pair (1.43 GB, 5.8 TB/s; splitting the call by pairs, so that the second pass
+// finds the logits in the last cache, costs more in launches than it saves: 286 -> 311 us in two parts, 347 us in four).
 #include "operators.h"
 
 namespace hb {
@@ -876,9 +876,10 @@ struct GradFrom<GRAD_PAIRS> : GradArgs {
 };
 static_assert(sizeof(GradFrom<GRAD_ROWS>) == 112 && sizeof(GradFrom<GRAD_LOGPROB>) == 112, "more arguments cost every launch up to 0.7 us");
 
-// p_k = exp(z_k - lse) from what hb_logprob_async has left.  As fp32 numbers lse and logp are each off by 2^-25 of themselves, and
-// lse = z_y - logp: the smaller one says more.  With lse alone an offset of the logits goes into every p_k (three classes at 1e7, 1e7 + 1 and 1e7 + 2:
-// 1.07 instead of 0.665); with z_y - logp only the distance of the choice does.  Where both are large p_k is still at most 1 - p_y.
+// p_k = exp(z_k - lse) from what hb_logprob_async has left.  As fp32 numbers lse and logp are each off by up to 2^-24 of themselves, and
+// lse = z_y - logp: the smaller one says more.  With lse alone an offset of the logits goes into every p_k (three classes at 1e7,
+// 1e7 + 1 and 1e7 + 2: 1.07 instead of 0.665); with z_y - logp only the distance of the choice does.  Where both are large p_k is
+// still at most 1 - p_y.
 struct LogprobCoef {
     RowCoef c;
     float others;  // 1 - p_y
