@@ -587,6 +587,67 @@ int hb_preference_loss_async(const void *d_Z, int64_t ldz, int tensor, const int
 /* Bytes of workspace for the calls above (pairs: 0 but for the preference loss); 0 for arguments that they refuse. */
 size_t hb_choice_workspace_bytes(int64_t B, int32_t pairs);
 
+/*
+ * ---- Orthogonalised updates -----------------------------------------------------------------
+ *
+ * G with its singular values brought near 1 and its singular vectors kept, by Newton-Schulz products: with X = G / (|G| + eps)
+ * (|G|: the square root of the sum of squares), then for each of `steps` steps (a, b, c)
+ *     A = X X^T,   X <- a X + (b A + c A^2) X
+ * where X is G^T if G has more rows than columns; the result has G's shape.  A step maps every singular value s to a s + b s^3 +
+ * c s^5.  n matrices go through the same launches, so a network's are given in one call (a matrix without rows or columns is left out).
+ *   steps   1 .. 32
+ *   coef    HOST pointer, read before the call returns: a, b, c of all steps (n_coef = 1) or of each (n_coef = steps), finite and within
+ *           [-32, 32]; NULL (n_coef = 0): (3.4445, -4.7750, 2.0315), five steps of which bring singular values between 1e-2 and 1 to 0.7 .. 1.2
+ *   eps     >= 0, finite; a matrix of zeros has a result of zeros if it is not 0 (NaN, 0 / 0, if it is)
+ *   products  HB_TENSOR_F32: errors as of fp32 products (a few 1e-6 of the result's norm for five of the usual steps), or HB_TENSOR_BF16: operands of 11 bits, the
+ *           linear term a X in 22: about 1e-3, a third of the work
+ * What a rounding adds to a singular value near 0 is multiplied by up to a^steps, as the value itself.  Coefficients that let singular values grow beyond 16
+ * overflow (inf or NaN); so does a G with inf or NaN anywhere, whose whole result is NaN.  Entries of X below 2^-36 count as 0.
+ * 1 <= rows, cols <= 32768, rows cols <= 2^30; ld < 2^31.
+ */
+typedef struct hb_ortho {
+    int32_t steps, n_coef;
+    const float *coef;
+    float eps;
+    int32_t products;
+} hb_ortho;
+typedef struct hb_ortho_matrix {
+    int64_t rows, cols;
+    const void *d_g;       /* rows x cols */
+    int64_t ldg;
+    void *d_out;           /* rows x cols; may be d_g if the types and ldo = ldg are the same, must not overlap anything else */
+    int64_t ldo;
+} hb_ortho_matrix;
+/* g_tensor, out_tensor: HB_TENSOR_* of every d_g, every d_out.  d_ws: hb_ortho_workspace_bytes() bytes, as for the calls above. */
+int hb_orthogonalize_async(const hb_ortho_matrix *list, int32_t n, int g_tensor, int out_tensor, const hb_ortho *how, void *d_ws,
+                           size_t ws_bytes, void *hip_stream);
+/*
+ * A training step with it: for every matrix W (fp32) with gradient G and momentum M (fp32)
+ *     M <- momentum M + G,   U = G + momentum M if nesterov, else M   (the new M)
+ *     W <- W - lr weight_decay W - lr scale O,   O: U orthogonalised
+ * lr, momentum, weight_decay >= 0 and finite, momentum < 1; scale finite (what brings updates of different shapes to one size: 0.2
+ * sqrt(max(rows, cols)) gives O's entries the root mean square 0.2).  W, M and G must not overlap anything.
+ */
+typedef struct hb_muon {
+    hb_ortho ortho;
+    float lr, momentum, weight_decay;
+    int32_t nesterov;
+} hb_muon;
+typedef struct hb_muon_matrix {
+    int64_t rows, cols;
+    const void *d_g;
+    int64_t ldg;
+    float *d_m;
+    int64_t ldm;
+    float *d_w;
+    int64_t ldw;
+    float scale;
+} hb_muon_matrix;
+int hb_muon_async(const hb_muon_matrix *list, int32_t n, int g_tensor, const hb_muon *how, void *d_ws, size_t ws_bytes,
+                  void *hip_stream);
+/* Bytes of workspace for n matrices of these shapes (HOST arrays); 0 for arguments that the calls refuse. */
+size_t hb_ortho_workspace_bytes(const int64_t *rows, const int64_t *cols, int32_t n, int products);
+
 #ifdef __cplusplus
 }
 #endif

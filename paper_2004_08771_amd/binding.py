@@ -110,6 +110,33 @@ SIGNATURES["hb_policy_loss_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _
 SIGNATURES["hb_preference_loss_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _prfp, _vp, _vp, _vp,
                                                  _i64, _vp, _sz, _vp])
 
+
+
+class Ortho(ctypes.Structure):
+    """Mirror of hb_ortho."""
+    _fields_ = [("steps", _i32), ("n_coef", _i32), ("coef", ctypes.POINTER(_f32)), ("eps", _f32), ("products", _i32)]
+
+
+class OrthoMatrix(ctypes.Structure):
+    """Mirror of hb_ortho_matrix."""
+    _fields_ = [("rows", _i64), ("cols", _i64), ("d_g", _vp), ("ldg", _i64), ("d_out", _vp), ("ldo", _i64)]
+
+
+class Muon(ctypes.Structure):
+    """Mirror of hb_muon."""
+    _fields_ = [("ortho", Ortho), ("lr", _f32), ("momentum", _f32), ("weight_decay", _f32), ("nesterov", _i32)]
+
+
+class MuonMatrix(ctypes.Structure):
+    """Mirror of hb_muon_matrix."""
+    _fields_ = [("rows", _i64), ("cols", _i64), ("d_g", _vp), ("ldg", _i64), ("d_m", _vp), ("ldm", _i64), ("d_w", _vp), ("ldw", _i64),
+                ("scale", _f32)]
+
+
+SIGNATURES["hb_ortho_workspace_bytes"] = (_sz, [_i64p, _i64p, _i32, _int])
+SIGNATURES["hb_orthogonalize_async"] = (_int, [ctypes.POINTER(OrthoMatrix), _i32, _int, _int, ctypes.POINTER(Ortho), _vp, _sz, _vp])
+SIGNATURES["hb_muon_async"] = (_int, [ctypes.POINTER(MuonMatrix), _i32, _int, ctypes.POINTER(Muon), _vp, _sz, _vp])
+
 _lib = None
 
 
@@ -420,7 +447,7 @@ def _matrix(t, name):
         _invalid(f"{name} has {len(shape)} dimensions: a matrix is needed")
     rows, cols = shape
     step, along = t.stride()
-    if along != 1 and cols > 1:
+    if along != 1 and cols > 1 and rows > 0:
         _invalid(f"{name}: the elements of a row must be next to each other")
     if rows < 2:
         step = cols if cols > 1 else 1
@@ -447,9 +474,9 @@ def _vector(t, name, n, kind=HB_TENSOR_F32):
     return t.data_ptr()
 
 
-def _workspace(ws):
+def _workspace(ws, size="choice_workspace_bytes()"):
     if ws is None:
-        _invalid("ws is needed: a tensor of choice_workspace_bytes() bytes")
+        _invalid(f"ws is needed: a tensor of {size} bytes")
     if not ws.is_contiguous():
         _invalid("ws must be contiguous")
     return ws.data_ptr(), ws.nbytes
@@ -544,3 +571,77 @@ def preference_loss(Z, y, seq, stats, dZ=None, ref=None, beta=0.1, smoothing=0.0
                                                  pw, nw, _stream(stream, Z))
     if rc != HB_OK:
         _check(rc)
+
+
+ORTHO_COEF = (3.4445, -4.7750, 2.0315)
+
+
+def ortho_args(steps=5, coef=ORTHO_COEF, eps=1e-7, products=HB_TENSOR_F32) -> Ortho:
+    """hb_ortho.  coef: (a, b, c), or such a triple for every step."""
+    flat = [float(v) for c in coef for v in (c if hasattr(c, "__len__") else (c,))]
+    if len(flat) not in (3, 3 * steps):
+        _invalid(f"coef has {len(flat)} numbers: 3, or 3 for each of {steps} steps are needed")
+    return Ortho(steps, len(flat) // 3, (_f32 * len(flat))(*flat), eps, products)
+
+
+def ortho_workspace_bytes(shapes, products=HB_TENSOR_F32) -> int:
+    """hb_ortho_workspace_bytes of [(rows, cols), ...]: what `ws` of orthogonalize and muon_update has to hold."""
+    shapes = [tuple(int(d) for d in s) for s in shapes]
+    n = len(shapes)
+    return int(lib().hb_ortho_workspace_bytes((_i64 * n)(*[s[0] for s in shapes]), (_i64 * n)(*[s[1] for s in shapes]), n, int(products)))
+
+
+def _list(t, name, n=None):
+    t = list(t) if isinstance(t, (list, tuple)) else [t]
+    if n is not None and len(t) != n:
+        _invalid(f"{name} has {len(t)} matrices: {n} are needed")
+    return t
+
+
+def _one_type(kinds, name):
+    if len(set(kinds)) > 1:
+        _invalid(f"{name}: one type for all matrices is needed")
+    return kinds[0] if kinds else HB_TENSOR_F32
+
+
+def orthogonalize(G, out, steps=5, coef=ORTHO_COEF, eps=1e-7, products=None, ws=None, stream=None):
+    """hb_orthogonalize_async of a matrix or a list of them; out (may be G) has their shapes.  products: HB_TENSOR_F32 or HB_TENSOR_BF16, by
+    default the type of out."""
+    G = _list(G, "G")
+    out = _list(out, "out", len(G))
+    a, o = [_matrix(t, "G") for t in G], [_matrix(t, "out") for t in out]
+    for x, y in zip(a, o):
+        if x[3:] != y[3:]:
+            _invalid(f"out is {y[3]} x {y[4]}: G's shape, {x[3]} x {x[4]}, is needed")
+    g_kind, o_kind = _one_type([x[2] for x in a], "G"), _one_type([y[2] for y in o], "out")
+    how = ortho_args(steps, coef, eps, o_kind if products is None else products)
+    pw, nw = _workspace(ws, "ortho_workspace_bytes()")
+    mats = (OrthoMatrix * len(a))(*[(x[3], x[4], x[0], x[1], y[0], y[1]) for x, y in zip(a, o)])
+    _check((_lib or lib()).hb_orthogonalize_async(mats, len(a), g_kind, o_kind, ctypes.byref(how), pw, nw, _stream(stream, ws)))
+
+
+def muon_args(lr, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5, coef=ORTHO_COEF, eps=1e-7, products=HB_TENSOR_F32) -> Muon:
+    """hb_muon."""
+    return Muon(ortho_args(steps, coef, eps, products), lr, momentum, weight_decay, int(bool(nesterov)))
+
+
+def muon_update(W, G, M, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale=None, steps=5, coef=ORTHO_COEF, eps=1e-7,
+                products=HB_TENSOR_F32, ws=None, stream=None):
+    """hb_muon_async: one step of weights W (float32) with gradients G and momenta M (float32), each a matrix or a list of them.  scale: a
+    factor of the update for each, by default 0.2 sqrt(max(rows, cols))."""
+    W = _list(W, "W")
+    n = len(W)
+    w, g, m = [_matrix(t, "W") for t in W], [_matrix(t, "G") for t in _list(G, "G", n)], [_matrix(t, "M") for t in _list(M, "M", n)]
+    for x, y, z in zip(w, g, m):
+        if y[3:] != x[3:] or z[2:] != x[2:] or x[2] != HB_TENSOR_F32:
+            _invalid("W and M have to be float32, and W, G and M of one shape")
+    if scale is None:
+        scale = [0.2 * max(x[3], x[4]) ** 0.5 for x in w]
+    elif not hasattr(scale, "__len__"):
+        scale = [scale] * n
+    if len(scale) != n:
+        _invalid(f"scale has {len(scale)} numbers: {n} are needed")
+    how = muon_args(lr, momentum, nesterov, weight_decay, steps, coef, eps, products)
+    pw, nw = _workspace(ws, "ortho_workspace_bytes()")
+    mats = (MuonMatrix * n)(*[(x[3], x[4], y[0], y[1], z[0], z[1], x[0], x[1], s) for x, y, z, s in zip(w, g, m, scale)])
+    _check((_lib or lib()).hb_muon_async(mats, n, _one_type([y[2] for y in g], "G"), ctypes.byref(how), pw, nw, _stream(stream, ws)))

@@ -84,6 +84,34 @@ hipError_t launch_policy(const ChoiceRows &r, const PolicyTerms &t, const Choice
 hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, const ChoiceGrad &d, void *ws, hipStream_t stream,
                              const PassEvents &ev = PassEvents());
 
+// ---------------------------------------------------------------- orthogonalised updates
+constexpr int ORTHO_GROUP = 16;  // matrices that go through the same launches, at most
+struct OrthoShape {
+    int rows, cols;            // both at least 1
+    int m() const { return rows < cols ? rows : cols; }
+    int n() const { return rows < cols ? cols : rows; }
+};
+struct OrthoMatrix {
+    const void *g;
+    long long ldg;
+    void *out;                 // the result, or (muon) the fp32 weights
+    long long ldo;
+    float *momentum;           // muon
+    long long ldm;
+    float scale;               // muon: factor of the update
+};
+struct OrthoSteps {
+    int g_tensor, out_tensor;  // of G and of the result
+    int products;              // TENSOR_F32: products of 22 bits, TENSOR_BF16: of 11
+    int steps, n_coef;
+    const float *coef;         // host: a, b, c of every step (n_coef = steps), or of all (1)
+    float eps;
+    bool muon, nesterov;
+    float lr, momentum, weight_decay;
+};
+size_t ortho_workspace(const OrthoShape *shapes, int n, int products);
+hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n, const OrthoSteps &how, void *ws, hipStream_t stream);
+
 // rows x cols elements of `size` bytes from p on, `ld` apart; or n bytes.  A null pointer has none.
 struct Block {
     const char *begin, *end;
@@ -129,6 +157,10 @@ int check_apart(const Block (&outs)[N], const Block (&ins)[M], int skip = 0)
 int check_dropout_p(float p, unsigned *threshold);
 int check_policy(const hb_policy *p);
 int check_preference(const hb_preference *p);
+int check_ortho(const hb_ortho *o);
+int check_muon(const hb_muon *h);
+OrthoSteps ortho_steps(const hb_ortho *o);
+OrthoSteps muon_steps(const hb_muon *h, int g_tensor);
 PolicyTerms policy_terms(const hb_policy *p, int64_t B, float *d_stats, float *d_logp);
 PreferenceTerms preference_terms(const hb_preference *p, float *d_stats, float *d_seq_logp);
 

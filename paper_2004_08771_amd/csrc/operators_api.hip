@@ -2,7 +2,10 @@
 #include "../../include/hb.h"
 #include "operators.h"
 
+#include <algorithm>
 #include <cmath>
+#include <new>
+#include <vector>
 
 using namespace hb;
 
@@ -143,6 +146,68 @@ ChoiceGrad grad_of(void *dZ, int64_t lddz, int tensor)
     return d;
 }
 
+constexpr int64_t MAX_ORTHO_DIM = 32768, MAX_ORTHO_SIZE = 1 << 30;
+constexpr int MAX_ORTHO_LIST = 4096, MAX_ORTHO_STEPS = 32;
+const float USUAL_COEF[3] = {3.4445f, -4.7750f, 2.0315f};
+
+int check_ortho_shape(int64_t rows, int64_t cols, int k)
+{
+    if (rows < 0 || rows > MAX_ORTHO_DIM || cols < 0 || cols > MAX_ORTHO_DIM || rows * cols > MAX_ORTHO_SIZE)
+        return set_error(HB_ERR_INVALID, "matrix %d is %lld x %lld: at most %lld rows and columns and %lld elements are supported", k, (long long)rows,
+                         (long long)cols, (long long)MAX_ORTHO_DIM, (long long)MAX_ORTHO_SIZE);
+    return HB_OK;
+}
+
+int check_ortho_operand(const void *p, int64_t ld, int64_t cols, size_t size, const char *name, int k)
+{
+    if (!p) return set_error(HB_ERR_INVALID, "%s of matrix %d is NULL", name, k);
+    if (ld < cols || ld > MAX_COLS)
+        return set_error(HB_ERR_INVALID, "the pitch of %s of matrix %d, %lld, is outside [cols = %lld, 2^31)", name, k, (long long)ld, (long long)cols);
+    if (!aligned_to(p, size)) return set_error(HB_ERR_INVALID, "%s of matrix %d is not aligned to its elements", name, k);
+    return HB_OK;
+}
+
+// What a list writes, and the workspace, apart from everything else in it.  Sorted by where they begin, so that only those that begin within another are compared
+int check_list_apart(std::vector<Block> &outs, std::vector<Block> &ins, const void *ws, size_t ws_bytes)
+{
+    struct Part {
+        const Block *b;
+        bool out;
+    };
+    std::vector<Part> all;
+    const Block work(ws, ws_bytes, "d_ws");
+    all.reserve(outs.size() + ins.size() + 1);
+    for (const Block &b : outs) all.push_back({&b, true});
+    for (const Block &b : ins) all.push_back({&b, false});
+    all.push_back({&work, true});
+    std::sort(all.begin(), all.end(), [](const Part &x, const Part &y) { return x.b->begin < y.b->begin; });
+    for (size_t i = 0; i < all.size(); ++i)
+        for (size_t j = i + 1; j < all.size() && all[j].b->begin < all[i].b->end; ++j)
+            if ((all[i].out || all[j].out) && all[i].b->meets(*all[j].b))
+                return set_error(HB_ERR_INVALID, "%s overlaps %s", all[i].b->name, all[j].b->name);
+    return HB_OK;
+}
+
+int check_ortho_workspace(const void *ws, size_t ws_bytes, const std::vector<OrthoShape> &shapes, int products, size_t *need)
+{
+    if (!ws) return set_error(HB_ERR_INVALID, "d_ws is NULL");
+    if (!aligned_to(ws, 16)) return set_error(HB_ERR_INVALID, "d_ws must be 16-byte aligned");
+    *need = ortho_workspace(shapes.data(), (int)shapes.size(), products);
+    if (ws_bytes < *need)
+        return set_error(HB_ERR_INVALID, "the workspace has %zu bytes, %zu are needed (hb_ortho_workspace_bytes)", ws_bytes, *need);
+    return HB_OK;
+}
+
+// of a list
+int check_pointers(const std::vector<Pointer> &list, hipStream_t stream)
+{
+    for (const Pointer &p : list) {
+        const int rc = check_device<1>({p}, nullptr);
+        if (rc != HB_OK) return rc;
+    }
+    return check_device<1>({{nullptr, ""}}, stream);
+}
+
 }  // namespace
 
 namespace hb {
@@ -210,6 +275,51 @@ int check_preference(const hb_preference *p)
     if (!(p->smoothing >= 0.f && p->smoothing <= 0.5f))
         return set_error(HB_ERR_INVALID, "smoothing = %g is outside [0, 0.5]", (double)p->smoothing);
     return HB_OK;
+}
+
+int check_ortho(const hb_ortho *o)
+{
+    if (!o) return set_error(HB_ERR_INVALID, "the arguments of the steps are NULL");
+    if (o->steps < 1 || o->steps > MAX_ORTHO_STEPS) return set_error(HB_ERR_INVALID, "steps = %d is outside [1, %d]", o->steps, MAX_ORTHO_STEPS);
+    if (o->coef ? (o->n_coef != 1 && o->n_coef != o->steps) : o->n_coef != 0)
+        return set_error(HB_ERR_INVALID, "n_coef = %d: 1 or steps = %d are needed with coef, 0 without", o->n_coef, o->steps);
+    for (int i = 0; o->coef && i < 3 * o->n_coef; ++i)
+        if (!(std::fabs(o->coef[i]) <= 32.f)) return set_error(HB_ERR_INVALID, "coefficient %d, %g, is outside [-32, 32]", i, (double)o->coef[i]);
+    if (!(o->eps >= 0.f) || !std::isfinite(o->eps)) return set_error(HB_ERR_INVALID, "eps = %g is negative or not finite", (double)o->eps);
+    return check_type(o->products);
+}
+
+int check_muon(const hb_muon *h)
+{
+    if (!h) return set_error(HB_ERR_INVALID, "the arguments of the update are NULL");
+    if (!(h->lr >= 0.f) || !std::isfinite(h->lr)) return set_error(HB_ERR_INVALID, "lr = %g is negative or not finite", (double)h->lr);
+    if (!(h->momentum >= 0.f && h->momentum < 1.f)) return set_error(HB_ERR_INVALID, "momentum = %g is outside [0, 1)", (double)h->momentum);
+    if (!(h->weight_decay >= 0.f) || !std::isfinite(h->weight_decay) || !std::isfinite(h->lr * h->weight_decay))
+        return set_error(HB_ERR_INVALID, "weight_decay = %g is negative or not finite", (double)h->weight_decay);
+    return check_ortho(&h->ortho);
+}
+
+OrthoSteps ortho_steps(const hb_ortho *o)
+{
+    OrthoSteps s = {};
+    s.products = o->products;
+    s.steps = o->steps;
+    s.n_coef = o->coef ? o->n_coef : 1;
+    s.coef = o->coef ? o->coef : USUAL_COEF;
+    s.eps = o->eps;
+    return s;
+}
+
+OrthoSteps muon_steps(const hb_muon *h, int g_tensor)
+{
+    OrthoSteps s = ortho_steps(&h->ortho);
+    s.g_tensor = g_tensor;
+    s.muon = true;
+    s.nesterov = h->nesterov != 0;
+    s.lr = h->lr;
+    s.momentum = h->momentum;
+    s.weight_decay = h->weight_decay;
+    return s;
 }
 
 PolicyTerms policy_terms(const hb_policy *p, int64_t B, float *d_stats, float *d_logp)
@@ -358,6 +468,130 @@ int hb_preference_loss_async(const void *d_Z, int64_t ldz, int tensor, const int
     return launched(launch_preference(rows_of(d_Z, ldz, tensor, d_y, nullptr, B, K),
                                       preference_terms(preference, d_stats, d_seq_logp), grad_of(d_dZ, lddz, tensor), d_ws, stream),
                     "hb_preference_loss_async");
+}
+
+size_t hb_ortho_workspace_bytes(const int64_t *rows, const int64_t *cols, int32_t n, int products)
+{
+    if (n < 0 || n > MAX_ORTHO_LIST || check_type(products) != HB_OK || (n > 0 && (!rows || !cols))) return 0;
+    try {
+        std::vector<OrthoShape> shapes;
+        for (int k = 0; k < n; ++k) {
+            if (check_ortho_shape(rows[k], cols[k], k) != HB_OK) return 0;
+            if (rows[k] > 0 && cols[k] > 0) shapes.push_back({(int)rows[k], (int)cols[k]});
+        }
+        return std::max<size_t>(16, ortho_workspace(shapes.data(), (int)shapes.size(), products));
+    } catch (const std::bad_alloc &) {
+        return 0;
+    }
+}
+
+int hb_orthogonalize_async(const hb_ortho_matrix *list, int32_t n, int g_tensor, int out_tensor, const hb_ortho *how, void *d_ws,
+                           size_t ws_bytes, void *hip_stream)
+{
+    int rc = check_type(g_tensor);
+    if (rc == HB_OK) rc = check_type(out_tensor);
+    if (rc == HB_OK) rc = check_ortho(how);
+    if (rc != HB_OK) return rc;
+    if (n < 0 || n > MAX_ORTHO_LIST) return set_error(HB_ERR_INVALID, "n = %d is outside [0, %d]", n, MAX_ORTHO_LIST);
+    if (n > 0 && !list) return set_error(HB_ERR_INVALID, "the list is NULL");
+    try {
+        std::vector<OrthoMatrix> mats;
+        std::vector<OrthoShape> shapes;
+        std::vector<Block> outs, ins;
+        std::vector<Pointer> pointers;
+        for (int k = 0; k < n; ++k) {
+            const hb_ortho_matrix &a = list[k];
+            rc = check_ortho_shape(a.rows, a.cols, k);
+            if (rc != HB_OK) return rc;
+            if (a.rows == 0 || a.cols == 0) continue;
+            rc = check_ortho_operand(a.d_g, a.ldg, a.cols, size_of(g_tensor), "d_g", k);
+            if (rc == HB_OK) rc = check_ortho_operand(a.d_out, a.ldo, a.cols, size_of(out_tensor), "d_out", k);
+            if (rc != HB_OK) return rc;
+            outs.emplace_back(a.d_out, a.rows, a.cols, a.ldo, size_of(out_tensor), "d_out");
+            // in place: all of G has been read when the first of the result is written
+            if (a.d_g != a.d_out || a.ldg != a.ldo || g_tensor != out_tensor) ins.emplace_back(a.d_g, a.rows, a.cols, a.ldg, size_of(g_tensor), "d_g");
+            pointers.push_back({a.d_g, "d_g"});
+            pointers.push_back({a.d_out, "d_out"});
+            OrthoMatrix m = {};
+            m.g = a.d_g;
+            m.ldg = a.ldg;
+            m.out = a.d_out;
+            m.ldo = a.ldo;
+            mats.push_back(m);
+            shapes.push_back({(int)a.rows, (int)a.cols});
+        }
+        if (mats.empty()) return HB_OK;
+        size_t need = 0;
+        rc = check_ortho_workspace(d_ws, ws_bytes, shapes, how->products, &need);
+        if (rc == HB_OK) rc = check_list_apart(outs, ins, d_ws, need);
+        if (rc != HB_OK) return rc;
+        pointers.push_back({d_ws, "d_ws"});
+        hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+        rc = check_pointers(pointers, stream);
+        if (rc != HB_OK) return rc;
+        OrthoSteps steps = ortho_steps(how);
+        steps.g_tensor = g_tensor;
+        steps.out_tensor = out_tensor;
+        return launched(launch_ortho(mats.data(), shapes.data(), (int)mats.size(), steps, d_ws, stream), "hb_orthogonalize_async");
+    } catch (const std::bad_alloc &) {
+        return set_error(HB_ERR_ALLOC, "out of host memory");
+    }
+}
+
+int hb_muon_async(const hb_muon_matrix *list, int32_t n, int g_tensor, const hb_muon *how, void *d_ws, size_t ws_bytes,
+                  void *hip_stream)
+{
+    int rc = check_type(g_tensor);
+    if (rc == HB_OK) rc = check_muon(how);
+    if (rc != HB_OK) return rc;
+    if (n < 0 || n > MAX_ORTHO_LIST) return set_error(HB_ERR_INVALID, "n = %d is outside [0, %d]", n, MAX_ORTHO_LIST);
+    if (n > 0 && !list) return set_error(HB_ERR_INVALID, "the list is NULL");
+    try {
+        std::vector<OrthoMatrix> mats;
+        std::vector<OrthoShape> shapes;
+        std::vector<Block> outs, ins;
+        std::vector<Pointer> pointers;
+        for (int k = 0; k < n; ++k) {
+            const hb_muon_matrix &a = list[k];
+            rc = check_ortho_shape(a.rows, a.cols, k);
+            if (rc == HB_OK && !(std::isfinite(a.scale) && std::isfinite(how->lr * a.scale)))
+                rc = set_error(HB_ERR_INVALID, "scale = %g of matrix %d is not finite", (double)a.scale, k);
+            if (rc != HB_OK) return rc;
+            if (a.rows == 0 || a.cols == 0) continue;
+            rc = check_ortho_operand(a.d_g, a.ldg, a.cols, size_of(g_tensor), "d_g", k);
+            if (rc == HB_OK) rc = check_ortho_operand(a.d_m, a.ldm, a.cols, sizeof(float), "d_m", k);
+            if (rc == HB_OK) rc = check_ortho_operand(a.d_w, a.ldw, a.cols, sizeof(float), "d_w", k);
+            if (rc != HB_OK) return rc;
+            outs.emplace_back(a.d_m, a.rows, a.cols, a.ldm, sizeof(float), "d_m");
+            outs.emplace_back(a.d_w, a.rows, a.cols, a.ldw, sizeof(float), "d_w");
+            ins.emplace_back(a.d_g, a.rows, a.cols, a.ldg, size_of(g_tensor), "d_g");
+            pointers.push_back({a.d_g, "d_g"});
+            pointers.push_back({a.d_m, "d_m"});
+            pointers.push_back({a.d_w, "d_w"});
+            OrthoMatrix m = {};
+            m.g = a.d_g;
+            m.ldg = a.ldg;
+            m.out = a.d_w;
+            m.ldo = a.ldw;
+            m.momentum = a.d_m;
+            m.ldm = a.ldm;
+            m.scale = a.scale;
+            mats.push_back(m);
+            shapes.push_back({(int)a.rows, (int)a.cols});
+        }
+        if (mats.empty()) return HB_OK;
+        size_t need = 0;
+        rc = check_ortho_workspace(d_ws, ws_bytes, shapes, how->ortho.products, &need);
+        if (rc == HB_OK) rc = check_list_apart(outs, ins, d_ws, need);
+        if (rc != HB_OK) return rc;
+        pointers.push_back({d_ws, "d_ws"});
+        hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+        rc = check_pointers(pointers, stream);
+        if (rc != HB_OK) return rc;
+        return launched(launch_ortho(mats.data(), shapes.data(), (int)mats.size(), muon_steps(how, g_tensor), d_ws, stream), "hb_muon_async");
+    } catch (const std::bad_alloc &) {
+        return set_error(HB_ERR_ALLOC, "out of host memory");
+    }
 }
 
 }  // extern "C"

@@ -1,0 +1,81 @@
+"""Orthogonalised updates and scores of rows of logits from their definitions, in 64 bits on the host (numpy)."""
+import numpy as np
+
+COEF = (3.4445, -4.7750, 2.0315)
+
+
+def _triples(coef, steps):
+    c = np.asarray(np.float32(coef), np.float64).reshape(-1, 3)  # as the calls take them
+    return np.broadcast_to(c, (steps, 3)) if len(c) == 1 else c
+
+
+def ortho_ref(G, steps=5, coef=COEF, eps=1e-7):
+    G = np.asarray(G, np.float64)
+    X = G.T if G.shape[0] > G.shape[1] else G
+    with np.errstate(all="ignore"):
+        X = X / (np.sqrt((X * X).sum()) + float(np.float32(eps)))
+        for a, b, c in _triples(coef, steps):
+            A = X @ X.T
+            X = a * X + (b * A + c * (A @ A)) @ X
+    return X.T if G.shape[0] > G.shape[1] else X
+
+
+def _high(x, scale):
+    return (x * scale).astype(np.float16).astype(np.float64) / scale
+
+
+def _both(x, scale):
+    hi = (x * scale).astype(np.float16).astype(np.float64)
+    return (hi + (x * scale - hi).astype(np.float16).astype(np.float64)) / scale
+
+
+def ortho_rounded(G, steps=5, coef=COEF, eps=1e-7, planes=1):
+    """The same with what is stored in 11 or 22 bits rounded to them, and nothing else: the linear term in 22, diagonals not at all."""
+    G = np.asarray(G, np.float64)
+    flip = G.shape[0] > G.shape[1]
+    X = G.T if flip else G
+    X = _both(X / (np.sqrt((X * X).sum()) + float(np.float32(eps))), 4096)
+    q = _high if planes == 1 else _both
+    for k, (a, b, c) in enumerate(_triples(coef, steps)):
+        Xq = q(X, 4096)
+        A = Xq @ Xq.T
+        d = np.diag(A).copy()
+        F = q(A - np.diag(d), 4096)
+        B = b * F + c * (F @ F + (d[:, None] + d[None, :]) * F)
+        e = b * d + c * (d * d + np.diag(F @ F))
+        H = q(B - np.diag(np.diag(B)), 1024)
+        X = (a + e)[:, None] * X + H @ Xq
+        if k + 1 < steps:
+            X = _both(X, 4096)
+    return X.T if flip else X
+
+
+def fp32_sums(G, steps=5, coef=COEF, eps=1e-7):
+    """What the fp32 sums of the products may add to the result, in Frobenius norm.  A sum of n terms in chains of n / 32 rounds about that often
+    plus a few times; roundings of many entries are independent, so those of a matrix add up like sqrt(n / 32 + 8) 2^-24 of its norm, 4
+    times that at most.  A later step multiplies what is there by at most max |p'| = p'(0) = a (usual steps; the divided
+    differences of the odd p bound the derivative of the matrix function in this norm)."""
+    G = np.asarray(G, np.float64)
+    X = G.T if G.shape[0] > G.shape[1] else G
+    norm = np.sqrt((X * X).sum()) + float(np.float32(eps))
+    s = np.linalg.svd(X / norm, compute_uv=False)
+    m, n = X.shape
+    u = 4 * np.sqrt(max(m, n) / 32 + 8) * 2.0 ** -24
+    off = 2.0 ** -24
+    for a, b, c in _triples(coef, steps):
+        top, size = s.max(), np.sqrt((s * s).sum())
+        slope = np.abs(a + 3 * b * np.linspace(0, top, 100) ** 2 + 5 * c * np.linspace(0, top, 100) ** 4).max()
+        dA = u * top * size
+        dB = (abs(b) + 2 * abs(c) * top ** 2) * dA + u * (abs(b) + abs(c) * top ** 2) * top * size
+        s = np.abs(a * s + b * s ** 3 + c * s ** 5)
+        off = slope * off + dB * top + 2 * u * (abs(a) + abs(b) * top ** 2 + abs(c) * top ** 4) * size
+    return off
+
+
+def muon_ref(W, G, M, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale=1.0, steps=5, coef=COEF, eps=1e-7, ortho=ortho_ref):
+    """(W, M, O) after a step."""
+    f = lambda v: float(np.float32(v))  # noqa: E731
+    W, G, M = (np.asarray(t, np.float64) for t in (W, G, M))
+    M = f(momentum) * M + G
+    O = ortho(G + f(momentum) * M if nesterov else M, steps, coef, eps)
+    return W - f(lr) * f(weight_decay) * W - f(lr) * f(scale) * O, M, O
