@@ -588,6 +588,36 @@ int hb_preference_loss_async(const void *d_Z, int64_t ldz, int tensor, const int
 size_t hb_choice_workspace_bytes(int64_t B, int32_t pairs);
 
 /*
+ * ---- Scores of rows of logits ---------------------------------------------------------------
+ *
+ * What a model says besides the class it was asked for: of each of B rows of K logits (as for hb_logprob_async)
+ *     logp = z[y] - lse,   lse = log of the sum over k of exp(z[k]),   entropy = -sum over k of p_k log p_k,   p = softmax(z)
+ * and the `top` most likely classes in order (of equal logits the lowest class; -0 and 0 are equal) with their log-probabilities.
+ * d_y NULL: every row is looked at, there is no logp.  Otherwise a row whose class is outside [0, K) (padding) has logp = lse = entropy = 0,
+ * and alternatives of class -1 and log-probability 0.  A logit of -inf is a class that is not allowed: it adds nothing and is no alternative;
+ * behind the last allowed class, alternatives are class -1 with -inf.  A row whose logits are all -inf has logp = lse = -inf and entropy 0.  A NaN or +inf
+ * makes logp, lse, entropy and the alternatives' log-probabilities of its row NaN; a NaN is no alternative.
+ * d_logp, d_lse, d_entropy: B floats, each may be NULL; d_top_class (B x top int32, row-major; not NULL if top > 0), d_top_logp (B x top floats, may
+ * be NULL).  0 <= top <= 64.  0 <= B <= 2^22, 1 <= K <= 2^24, ldz < 2^31.  The same call gives the same bits.
+ * d_ws: hb_scores_workspace_bytes(B, K, top) bytes, as for hb_logprob_async.
+ */
+int hb_scores_async(const void *d_Z, int64_t ldz, int tensor, const int32_t *d_y, int64_t B, int32_t K, int32_t top, float *d_logp,
+                    float *d_lse, float *d_entropy, int32_t *d_top_class, float *d_top_logp, void *d_ws, size_t ws_bytes,
+                    void *hip_stream);
+/*
+ * The gradient in the logits of sum over the rows of g_logp logp + g_entropy entropy (a policy's loss with an entropy bonus):
+ *     dZ[k] = g_logp ([k = y] - p_k) - g_entropy p_k (log p_k + entropy)
+ * d_g_logp, d_g_entropy: B floats; one of them may be NULL (all 0).  d_y may be NULL if d_g_logp is.  Rows whose class is outside
+ * [0, K), rows without an allowed class and rows whose weights are both 0 get zeros, whatever their logits hold.  Nothing of
+ * hb_scores_async is needed.  d_dZ has the type of d_Z; it may be d_Z itself with lddz = ldz, otherwise they must not overlap.
+ * d_ws: hb_scores_workspace_bytes(B, K, 0) bytes.
+ */
+int hb_scores_grad_async(const void *d_Z, int64_t ldz, int tensor, const int32_t *d_y, int64_t B, int32_t K, const float *d_g_logp,
+                         const float *d_g_entropy, void *d_dZ, int64_t lddz, void *d_ws, size_t ws_bytes, void *hip_stream);
+/* Bytes of workspace for the calls above; 0 for arguments that they refuse. */
+size_t hb_scores_workspace_bytes(int64_t B, int32_t K, int32_t top);
+
+/*
  * ---- Orthogonalised updates -----------------------------------------------------------------
  *
  * G with its singular values brought near 1 and its singular vectors kept, by Newton-Schulz products: with X = G / (|G| + eps)

@@ -11,4 +11,5 @@ from .binding import (  # noqa: F401
     HB_LOSS_SOFTMAX_CE, HB_OK, HB_TENSOR_BF16, HB_TENSOR_F32, HbError, Model, Sched, batch_loss_static,
     choice_workspace_bytes, cpu_worker_run_epoch, dropout, hogbatch_run_epoch, lib, lib_path, logprob, logprob_grad,
     muon_args, muon_update, ortho_args, ortho_workspace_bytes, orthogonalize, policy_args, policy_loss, preference_args, preference_loss,
+    scores, scores_grad, scores_workspace_bytes,
 )

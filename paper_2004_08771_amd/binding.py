@@ -133,6 +133,9 @@ class MuonMatrix(ctypes.Structure):
                 ("scale", _f32)]
 
 
+SIGNATURES["hb_scores_workspace_bytes"] = (_sz, [_i64, _i32, _i32])
+SIGNATURES["hb_scores_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp])
+SIGNATURES["hb_scores_grad_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _vp, _vp, _vp, _i64, _vp, _sz, _vp])
 SIGNATURES["hb_ortho_workspace_bytes"] = (_sz, [_i64p, _i64p, _i32, _int])
 SIGNATURES["hb_orthogonalize_async"] = (_int, [ctypes.POINTER(OrthoMatrix), _i32, _int, _int, ctypes.POINTER(Ortho), _vp, _sz, _vp])
 SIGNATURES["hb_muon_async"] = (_int, [ctypes.POINTER(MuonMatrix), _i32, _int, ctypes.POINTER(Muon), _vp, _sz, _vp])
@@ -569,6 +572,48 @@ def preference_loss(Z, y, seq, stats, dZ=None, ref=None, beta=0.1, smoothing=0.0
     rc = (_lib or lib()).hb_preference_loss_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, ctypes.byref(args),
                                                  _vector(stats, "stats", 4), _vector(seq_logp, "seq_logp", 2 * args.pairs), pd, ldd,
                                                  pw, nw, _stream(stream, Z))
+    if rc != HB_OK:
+        _check(rc)
+
+
+def scores_workspace_bytes(B, K, top=0) -> int:
+    """hb_scores_workspace_bytes: what `ws` of scores and scores_grad (top = 0) has to hold."""
+    return int(lib().hb_scores_workspace_bytes(int(B), int(K), int(top)))
+
+
+def _table(t, name, rows, cols=None, kind=HB_TENSOR_F32):
+    """(address, columns) of a matrix of rows x cols elements one behind the other, or (None, 0)."""
+    if t is None:
+        return None, 0
+    shape = t.shape
+    if _type(t) != kind or len(shape) != 2 or shape[0] != rows or (cols is not None and shape[1] != cols) or not t.is_contiguous():
+        _invalid(f"{name} is {tuple(shape)} {t.dtype}: {rows} rows{'' if cols is None else f' of {cols}'} {'int32' if kind == 'int32' else 'float32'}, "
+                 "one behind the other, are needed")
+    return t.data_ptr(), shape[1]
+
+
+def scores(Z, y=None, logp=None, lse=None, entropy=None, top_class=None, top_logp=None, ws=None, stream=None):
+    """hb_scores_async: log-probabilities of the classes y (int32; None: no classes), normalisers, entropies and, as many as top_class (int32) has
+    columns, the most likely classes of rows of logits Z."""
+    pz, ldz, kind, B, K = _matrix(Z, "Z")
+    pc, top = _table(top_class, "top_class", B, kind="int32")
+    if pc is None and top_logp is not None:
+        _invalid("top_logp without top_class")
+    pl, _ = _table(top_logp, "top_logp", B, top)
+    pw, nw = _workspace(ws, "scores_workspace_bytes()")
+    rc = (_lib or lib()).hb_scores_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, top, _vector(logp, "logp", B), _vector(lse, "lse", B),
+                                        _vector(entropy, "entropy", B), pc, pl, pw, nw, _stream(stream, Z))
+    if rc != HB_OK:
+        _check(rc)
+
+
+def scores_grad(Z, dZ, y=None, g_logp=None, g_entropy=None, ws=None, stream=None):
+    """hb_scores_grad_async: dZ = d (g_logp logp + g_entropy entropy) / d Z (dZ may be Z)."""
+    m = pz, ldz, kind, B, K = _matrix(Z, "Z")
+    pd, ldd = _out_matrix(dZ, "dZ", m)
+    pw, nw = _workspace(ws, "scores_workspace_bytes()")
+    rc = (_lib or lib()).hb_scores_grad_async(pz, ldz, kind, _vector(y, "y", B, "int32"), B, K, _vector(g_logp, "g_logp", B),
+                                             _vector(g_entropy, "g_entropy", B), pd, ldd, pw, nw, _stream(stream, Z))
     if rc != HB_OK:
         _check(rc)
 

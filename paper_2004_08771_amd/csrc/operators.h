@@ -84,6 +84,20 @@ hipError_t launch_policy(const ChoiceRows &r, const PolicyTerms &t, const Choice
 hipError_t launch_preference(const ChoiceRows &r, const PreferenceTerms &t, const ChoiceGrad &d, void *ws, hipStream_t stream,
                              const PassEvents &ev = PassEvents());
 
+// ---------------------------------------------------------------- scores of rows
+// ChoiceRows::y may be null (every row takes part, without a class), ChoiceRows::weight is not looked at
+struct ScoreOut {
+    float *logp, *lse, *entropy;  // B entries; each may be null
+    int32_t *top_class;           // B x top
+    float *top_logp;              // may be null
+};
+size_t scores_workspace(long long B, int K, int top);
+hipError_t launch_scores(const ChoiceRows &r, const ScoreOut &out, int top, void *ws, hipStream_t stream,
+                         const PassEvents &ev = PassEvents());
+// d.pad and d.all_rows are not looked at; the gradient has the type of the logits
+hipError_t launch_scores_grad(const ChoiceRows &r, const float *g_logp, const float *g_entropy, const ChoiceGrad &d, void *ws,
+                              hipStream_t stream, const PassEvents &ev = PassEvents());
+
 // ---------------------------------------------------------------- orthogonalised updates
 constexpr int ORTHO_GROUP = 16;  // matrices that go through the same launches, at most
 struct OrthoShape {

@@ -70,7 +70,7 @@ int launched(hipError_t e, const char *what)
     return HB_OK;
 }
 
-int check_rows(const void *Z, int64_t ldz, int tensor, const int32_t *y, int64_t B, int64_t K)
+int check_rows(const void *Z, int64_t ldz, int tensor, const int32_t *y, int64_t B, int64_t K, bool needs_y = true)
 {
     const int rc = check_type(tensor);
     if (rc != HB_OK) return rc;
@@ -80,7 +80,7 @@ int check_rows(const void *Z, int64_t ldz, int tensor, const int32_t *y, int64_t
     if (ldz < K) return set_error(HB_ERR_INVALID, "ldz = %lld is less than K = %lld", (long long)ldz, (long long)K);
     if (ldz > MAX_COLS) return set_error(HB_ERR_INVALID, "ldz = %lld is more than %lld", (long long)ldz, (long long)MAX_COLS);
     if (B > 0 && !Z) return set_error(HB_ERR_INVALID, "d_Z is NULL");
-    if (B > 0 && !y) return set_error(HB_ERR_INVALID, "d_y is NULL");
+    if (B > 0 && needs_y && !y) return set_error(HB_ERR_INVALID, "d_y is NULL");
     if (!aligned_to(Z, size_of(tensor))) return set_error(HB_ERR_INVALID, "d_Z is not aligned to its elements");
     return HB_OK;
 }
@@ -144,6 +144,18 @@ ChoiceGrad grad_of(void *dZ, int64_t lddz, int tensor)
     d.ld = lddz;
     d.tensor = tensor;
     return d;
+}
+
+constexpr int32_t MAX_TOP = 64;
+
+int check_scores_workspace(const void *ws, size_t ws_bytes, int64_t B, int32_t K, int32_t top)
+{
+    if (!ws) return set_error(HB_ERR_INVALID, "d_ws is NULL");
+    if (!aligned_to(ws, 16)) return set_error(HB_ERR_INVALID, "d_ws must be 16-byte aligned");
+    const size_t need = scores_workspace(B, K, top);
+    if (ws_bytes < need)
+        return set_error(HB_ERR_INVALID, "the workspace has %zu bytes, %zu are needed (hb_scores_workspace_bytes)", ws_bytes, need);
+    return HB_OK;
 }
 
 constexpr int64_t MAX_ORTHO_DIM = 32768, MAX_ORTHO_SIZE = 1 << 30;
@@ -468,6 +480,65 @@ int hb_preference_loss_async(const void *d_Z, int64_t ldz, int tensor, const int
     return launched(launch_preference(rows_of(d_Z, ldz, tensor, d_y, nullptr, B, K),
                                       preference_terms(preference, d_stats, d_seq_logp), grad_of(d_dZ, lddz, tensor), d_ws, stream),
                     "hb_preference_loss_async");
+}
+
+size_t hb_scores_workspace_bytes(int64_t B, int32_t K, int32_t top)
+{
+    if (B < 0 || B > MAX_CHOICE_ROWS || K < 1 || K > MAX_CLASSES || top < 0 || top > MAX_TOP) return 0;
+    return scores_workspace(B, K, top);
+}
+
+int hb_scores_async(const void *d_Z, int64_t ldz, int tensor, const int32_t *d_y, int64_t B, int32_t K, int32_t top, float *d_logp,
+                    float *d_lse, float *d_entropy, int32_t *d_top_class, float *d_top_logp, void *d_ws, size_t ws_bytes,
+                    void *hip_stream)
+{
+    int rc = check_rows(d_Z, ldz, tensor, d_y, B, K, d_logp != nullptr);
+    if (rc != HB_OK) return rc;
+    if (top < 0 || top > MAX_TOP) return set_error(HB_ERR_INVALID, "top = %d is outside [0, %d]", top, MAX_TOP);
+    rc = check_scores_workspace(d_ws, ws_bytes, B, K, top);
+    if (rc != HB_OK) return rc;
+    if (B == 0) return HB_OK;
+    if (top > 0 && !d_top_class) return set_error(HB_ERR_INVALID, "d_top_class is NULL");
+    if (top == 0) {
+        d_top_class = nullptr;
+        d_top_logp = nullptr;
+    }
+    const size_t n = sizeof(float) * (size_t)B, t = n * (size_t)top;
+    rc = check_apart<6, 2>({{d_logp, n, "d_logp"}, {d_lse, n, "d_lse"}, {d_entropy, n, "d_entropy"}, {d_top_class, t, "d_top_class"},
+                            {d_top_logp, t, "d_top_logp"}, {d_ws, scores_workspace(B, K, top), "d_ws"}},
+                           {{d_Z, B, K, ldz, size_of(tensor), "d_Z"}, {d_y, n, "d_y"}});
+    if (rc != HB_OK) return rc;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    rc = check_device({{d_Z, "d_Z"}, {d_y, "d_y"}, {d_logp, "d_logp"}, {d_lse, "d_lse"}, {d_entropy, "d_entropy"},
+                       {d_top_class, "d_top_class"}, {d_top_logp, "d_top_logp"}, {d_ws, "d_ws"}},
+                      stream);
+    if (rc != HB_OK) return rc;
+    return launched(launch_scores(rows_of(d_Z, ldz, tensor, d_y, nullptr, B, K), {d_logp, d_lse, d_entropy, d_top_class, d_top_logp}, top,
+                                  d_ws, stream),
+                    "hb_scores_async");
+}
+
+int hb_scores_grad_async(const void *d_Z, int64_t ldz, int tensor, const int32_t *d_y, int64_t B, int32_t K, const float *d_g_logp,
+                         const float *d_g_entropy, void *d_dZ, int64_t lddz, void *d_ws, size_t ws_bytes, void *hip_stream)
+{
+    int rc = check_rows(d_Z, ldz, tensor, d_y, B, K, d_g_logp != nullptr);
+    if (rc == HB_OK) rc = check_grad(d_Z, ldz, tensor, B, K, d_dZ, lddz);
+    if (rc == HB_OK) rc = check_scores_workspace(d_ws, ws_bytes, B, K, 0);
+    if (rc != HB_OK) return rc;
+    if (B == 0) return HB_OK;
+    if (!d_dZ) return set_error(HB_ERR_INVALID, "d_dZ is NULL");
+    if (!d_g_logp && !d_g_entropy) return set_error(HB_ERR_INVALID, "d_g_logp and d_g_entropy are NULL");
+    const size_t n = sizeof(float) * (size_t)B;
+    rc = check_apart<2, 4>({{d_dZ, B, K, lddz, size_of(tensor), "d_dZ"}, {d_ws, scores_workspace(B, K, 0), "d_ws"}},
+                           {{d_Z, B, K, ldz, size_of(tensor), "d_Z"}, {d_y, n, "d_y"}, {d_g_logp, n, "d_g_logp"}, {d_g_entropy, n, "d_g_entropy"}},
+                           1);
+    if (rc != HB_OK) return rc;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    rc = check_device({{d_Z, "d_Z"}, {d_y, "d_y"}, {d_g_logp, "d_g_logp"}, {d_g_entropy, "d_g_entropy"}, {d_dZ, "d_dZ"}, {d_ws, "d_ws"}}, stream);
+    if (rc != HB_OK) return rc;
+    return launched(launch_scores_grad(rows_of(d_Z, ldz, tensor, d_y, nullptr, B, K), d_g_logp, d_g_entropy, grad_of(d_dZ, lddz, tensor),
+                                       d_ws, stream),
+                    "hb_scores_grad_async");
 }
 
 size_t hb_ortho_workspace_bytes(const int64_t *rows, const int64_t *cols, int32_t n, int products)

@@ -79,3 +79,57 @@ def muon_ref(W, G, M, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale=
     M = f(momentum) * M + G
     O = ortho(G + f(momentum) * M if nesterov else M, steps, coef, eps)
     return W - f(lr) * f(weight_decay) * W - f(lr) * f(scale) * O, M, O
+
+
+def scores_ref(Z, y, top):
+    """part, logp, lse, entropy, classes, their log-probabilities, p, log p: all in 64 bits, row by row from the definitions."""
+    Z = np.asarray(Z, np.float64)
+    B, K = Z.shape
+    part = np.ones(B, bool) if y is None else (np.asarray(y) >= 0) & (np.asarray(y) < K)
+    logp, lse, H = np.zeros(B), np.zeros(B), np.zeros(B)
+    classes, tops = np.full((B, top), -1), np.zeros((B, top))
+    p, lp = np.zeros((B, K)), np.zeros((B, K))
+    for i in np.nonzero(part)[0]:
+        z = Z[i]
+        order = np.argsort(-np.where(np.isnan(z), -np.inf, z), kind="stable")
+        order = order[(z[order] > -np.inf)][:top]
+        classes[i, :len(order)] = order
+        tops[i] = -np.inf
+        if np.isnan(z).any() or (z == np.inf).any():
+            logp[i] = lse[i] = H[i] = p[i] = lp[i] = np.nan
+            tops[i, :len(order)] = np.nan
+            continue
+        if (z == -np.inf).all():
+            logp[i] = lse[i] = -np.inf
+            lp[i] = -np.inf
+            continue
+        w = int(np.argmax(z))
+        d = z - z[w]
+        e = np.exp(d)
+        o = np.delete(e, w).sum()
+        lp[i] = d - np.log1p(o)
+        p[i] = e / (1 + o)
+        lse[i] = z[w] + np.log1p(o)
+        few = np.where(e > 0, d, 0.0)
+        H[i] = np.log1p(o) - (e * few).sum() / (1 + o)
+        tops[i, :len(order)] = lp[i, order]
+        if y is not None:
+            logp[i] = lp[i, y[i]]
+    return part, logp, lse, H, classes, tops, p, lp
+
+
+def scores_grad_ref(ref, y, g_logp, g_entropy):
+    """From what scores_ref gives; 1 - p_y as the sum of the others."""
+    part, _, _, H, _, _, p, lp = ref
+    B, K = p.shape
+    d = np.zeros((B, K))
+    for i in range(B):
+        gl, gh = (0.0 if g is None else float(g[i]) for g in (g_logp, g_entropy))
+        if not part[i] or (gl == 0 and gh == 0) or (p[i] == 0).all():
+            continue
+        d[i] = -gl * p[i] - gh * p[i] * (np.where(p[i] == 0, 0.0, lp[i]) + H[i])
+        if gl:
+            q = p[i].copy()
+            q[y[i]] = 0
+            d[i, y[i]] += gl * (p[i, y[i]] + q.sum())
+    return d
