@@ -100,6 +100,7 @@ hipError_t launch_scores_grad(const ChoiceRows &r, const float *g_logp, const fl
 
 // ---------------------------------------------------------------- orthogonalised updates
 constexpr int ORTHO_GROUP = 16;  // matrices that go through the same launches, at most
+constexpr int ORTHO_STEPS = 32;
 struct OrthoShape {
     int rows, cols;            // both at least 1
     int m() const { return rows < cols ? rows : cols; }

@@ -159,7 +159,7 @@ int check_scores_workspace(const void *ws, size_t ws_bytes, int64_t B, int32_t K
 }
 
 constexpr int64_t MAX_ORTHO_DIM = 32768, MAX_ORTHO_SIZE = 1 << 30;
-constexpr int MAX_ORTHO_LIST = 4096, MAX_ORTHO_STEPS = 32;
+constexpr int MAX_ORTHO_LIST = 4096, MAX_ORTHO_STEPS = ORTHO_STEPS;
 const float USUAL_COEF[3] = {3.4445f, -4.7750f, 2.0315f};
 
 int check_ortho_shape(int64_t rows, int64_t cols, int k)

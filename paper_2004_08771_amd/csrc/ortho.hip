@@ -17,10 +17,14 @@
 // HB_TENSOR_F32 takes the products of high and low parts, too (three products of the four; low times low is 2^-22): the errors are
 // those of fp32 products.
 // Operands are scaled by powers of two so that neither what they hold nor its low part leaves fp16's range: X by 2^12 (entries are at most the largest
-// singular value, 1.2, and around (m n)^-1/2 at the start), A by 2^12, B by 2^10 (entries up to the range of b s^2 + c s^4).
+// singular value s, 1.2 for the usual steps, and around (m n)^-1/2 at the start), A by 2^8 and B by 2^10 (entries beside the diagonal are at most half
+// the range of s^2, and of b s^2 + c s^4): s up to 16 and b s^2 + c s^4 up to 64 have room.
 // Everything in the workspace is padded with zeros to whole tiles, which the steps keep zero: no kernel between the first and the last
 // has a bounds check.
+#include "gemm_device.h"
 #include "operators.h"
+#include <math.h>
+#include <stdlib.h>
 
 namespace hb {
 namespace {
@@ -32,39 +36,82 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(1))) const void *gptr_t;
 typedef __attribute__((address_space(3))) void *lptr_t;
 
-constexpr float SX = 4096.f, SA = 4096.f, SB = 1024.f;
+constexpr float SX = 4096.f, SA = 256.f, SB = 1024.f;
 constexpr int BK = 64, ROW_BYTES = 2 * BK;  // a row of an operand tile: one cache line
-constexpr int SUM_NT = 256, SUM_BLOCKS = 256, SUM_MIN = 8192;
+constexpr int SUM_NT = 256, SUM_BLOCKS = 1024, SUM_MIN = 4096;
 constexpr int PREP = 64;  // tiles of the kernel that lays X out
 
-// one matrix: what the kernels read of it, in the workspace
-struct Mat {
+// a matrix as the caller has it
+struct Matrix {
+    int rows, cols;
+    bool flip;                // X is its transpose
+    bool whole_g, whole_m;    // four elements at a time lie at boundaries of their size
+    bool whole_out;           // and of the result: four of four bytes, eight of two
+    float scale;              // lr times the matrix's factor
+    const void *g;
+    void *out;                // the result, or the weights
+    float *mom;
+    long long ldg, ldo, ldm;
+};
+// and what is the same for all of them
+struct How {
+    int g_tensor, out_tensor;  // TENSOR_* of G and of the result
+    bool muon, nesterov;
+    float momentum, eps, decay;  // decay: lr weight_decay
+};
+// what the kernels of the products read of it besides, in the workspace
+struct Mat : Matrix {
     int m, n, mp, np;         // rows and columns of X, and padded to whole tiles
-    int rows, cols, flip;     // of G; X is its transpose
     int sums, sum0;           // blocks of the sum of squares, and the first
     int prep0, sym0, all0;    // first block of the others: X's layout, tiles on and below the diagonal of m x m, tiles of m x n
     size_t x[2], xt[2], f, h; // byte offsets from the workspace: X and X^T (two of each, in turn), A and B; low parts follow
     size_t d, e;              // diagonals of A and B
-    const void *g;
-    long long ldg;
-    void *out;                // the result, or the weights
-    long long ldo;
-    float *mom;
-    long long ldm;
-    float scale;              // lr times the matrix's factor
 };
-struct List {
+struct List : How {
     int count, tile, planes;
-    int g_tensor, out_tensor, step_kind;  // HB_TENSOR_* of G and of the result
-    int nesterov;
-    float momentum, eps, decay;           // lr weight_decay
     Mat mat[ORTHO_GROUP];
 };
-enum { PLAIN = 0, MUON = 1 };  // step_kind
 
-__device__ __forceinline__ float load_one(const void *p, long long at, int tensor)
+typedef __bf16 v4b __attribute__((ext_vector_type(4)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+
+// elements at .. at + 3 of a row of which `left` are there (0 for the others); whole: 4 elements lie at a boundary of their size
+__device__ __forceinline__ v4f load_four(const void *p, long long at, int tensor, int left, bool whole)
 {
-    return tensor == TENSOR_BF16 ? (float)static_cast<const __bf16 *>(p)[at] : static_cast<const float *>(p)[at];
+    v4f x = {0.f, 0.f, 0.f, 0.f};
+    if (tensor == TENSOR_BF16) {
+        const __bf16 *q = static_cast<const __bf16 *>(p) + at;
+        if (whole && left >= 4) {
+            const v4b u = *reinterpret_cast<const v4b *>(q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = (float)u[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < left) x[e] = (float)q[e];
+        }
+    } else {
+        const float *q = static_cast<const float *>(p) + at;
+        if (whole && left >= 4) {
+            x = *reinterpret_cast<const v4f *>(q);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < left) x[e] = q[e];
+        }
+    }
+    return x;
+}
+
+__device__ __forceinline__ void store_four(float *q, const v4f &x, int left, bool whole)
+{
+    if (whole && left >= 4) {
+        *reinterpret_cast<v4f *>(q) = x;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) q[e] = x[e];
+    }
 }
 
 // the matrix of a block, from the first blocks of each
@@ -77,42 +124,75 @@ __device__ __forceinline__ int find(const List &l, int block, F first)
 }
 
 // what is orthogonalised: G, or with momentum m' = mu m + g (the new one): g + mu m' or m'
-__device__ __forceinline__ float updated(const List &l, float g, float m_new)
+__device__ __forceinline__ float updated(const How &l, float g, float m_new)
 {
-    if (l.step_kind == PLAIN) return g;
+    if (!l.muon) return g;
     return l.nesterov ? __builtin_fmaf(l.momentum, m_new, g) : m_new;
 }
 
 // ---------------------------------------------------------------- the norm
 // Sums of squares in 64 bits (neither 1e30 nor 1e-30 leaves their range), a fixed part of the rows a block; the momentum on the way.
+// A power of two of lanes has a row, four elements each at a time, and loads four times before it waits; a matrix without gaps is one long row.
 // The first block puts the list where the other kernels read it: it is longer than what a launch should carry.
+template <int NT>
+__device__ __forceinline__ double sum_of_block(const How &l, const Matrix &a, int block, int blocks, double *red)
+{
+    const bool gaps = a.ldg != a.cols || (l.muon && a.ldm != a.cols);
+    const int rows = gaps ? a.rows : 1, cols = gaps ? a.cols : a.rows * a.cols;
+    int lanes = NT;
+    while (lanes > 1 && 2 * lanes >= cols) lanes >>= 1;
+    const int per_block = NT / lanes, step = 4 * lanes;
+    // one long row goes to all blocks in turn, else rows do
+    const int stride = rows == 1 ? blocks * step : step, c0 = 4 * ((int)threadIdx.x % lanes) + (rows == 1 ? block * step : 0);
+    const int r0 = rows == 1 ? (int)threadIdx.x / lanes : block * per_block + (int)threadIdx.x / lanes;
+    double s = 0.0;
+    for (int r = r0; r < rows; r += blocks * per_block) {
+        const long long g = (long long)r * a.ldg, m = (long long)r * a.ldm;
+        for (long long c = c0; c < cols; c += 4LL * stride) {
+            v4f x[4], y[4];
+            int left[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const long long at = c + (long long)u * stride;
+                left[u] = at < cols ? (int)min(4LL, cols - at) : 0;
+                x[u] = load_four(a.g, g + at, l.g_tensor, left[u], a.whole_g);
+                if (l.muon) y[u] = load_four(a.mom, m + at, TENSOR_F32, left[u], a.whole_m);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (l.muon) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        y[u][e] = __builtin_fmaf(l.momentum, y[u][e], x[u][e]);
+                        x[u][e] = updated(l, x[u][e], y[u][e]);
+                    }
+                    store_four(a.mom + m + c + (long long)u * stride, y[u], left[u], a.whole_m);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s += (double)x[u][e] * (double)x[u][e];
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = red[0];
+#pragma unroll
+    for (int i = 1; i < NT / 64; ++i) s += red[i];
+    return s;
+}
+
 __global__ __launch_bounds__(SUM_NT) void sum_kernel(List l, List *to, double *partial)
 {
     if (blockIdx.x == 0) {
         const unsigned *from = reinterpret_cast<const unsigned *>(&l);
         for (unsigned i = threadIdx.x; i < sizeof(List) / 4; i += SUM_NT) reinterpret_cast<unsigned *>(to)[i] = from[i];
     }
-    const int k = find(l, blockIdx.x, [](const Mat &a) { return a.sum0; });
-    const Mat &a = l.mat[k];
-    const int b = blockIdx.x - a.sum0;
-    const long long total = (long long)a.rows * a.cols;
-    double s = 0.0;
-    for (long long i = (long long)b * SUM_NT + threadIdx.x; i < total; i += (long long)a.sums * SUM_NT) {
-        const long long r = i / a.cols, c = i - r * a.cols;
-        float v = load_one(a.g, r * a.ldg + c, l.g_tensor);
-        if (l.step_kind == MUON) {
-            const float m_new = __builtin_fmaf(l.momentum, a.mom[r * a.ldm + c], v);
-            a.mom[r * a.ldm + c] = m_new;
-            v = updated(l, v, m_new);
-        }
-        s += (double)v * (double)v;
-    }
     __shared__ double red[SUM_NT / 64];
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) partial[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+    const Mat &a = l.mat[find(l, blockIdx.x, [](const Mat &x) { return x.sum0; })];
+    const double s = sum_of_block<SUM_NT>(l, a, blockIdx.x - a.sum0, a.sums, red);
+    if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
 __device__ __forceinline__ void split(float x, half_t &hi, half_t &lo)
@@ -130,7 +210,8 @@ __global__ __launch_bounds__(256) void prep_kernel(const List *lp, unsigned char
     __shared__ double red[4];
     __shared__ float tile[PREP][PREP + 1];
     const int tid = threadIdx.x;
-    double s = tid < a.sums ? partial[a.sum0 + tid] : 0.0;
+    double s = 0.0;
+    for (int i = tid; i < a.sums; i += 256) s += partial[a.sum0 + i];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
     if ((tid & 63) == 0) red[tid >> 6] = s;
@@ -140,16 +221,24 @@ __global__ __launch_bounds__(256) void prep_kernel(const List *lp, unsigned char
     const int per_row = a.np / PREP, t = blockIdx.x - a.prep0;
     const int i0 = (t / per_row) * PREP, j0 = (t % per_row) * PREP;
     const int r0 = a.flip ? j0 : i0, c0 = a.flip ? i0 : j0;
-    for (int q = tid; q < PREP * PREP; q += 256) {
-        const int r = q / PREP, c = q % PREP;
-        float v = 0.f;
-        if (r0 + r < a.rows && c0 + c < a.cols) {
-            v = load_one(a.g, (long long)(r0 + r) * a.ldg + c0 + c, l.g_tensor);
-            if (l.step_kind == MUON) v = updated(l, v, a.mom[(long long)(r0 + r) * a.ldm + c0 + c]);
-            v = (float)((double)v * inv);
+    v4f x[PREP / 16], y[PREP / 16];
+    const int c = 4 * (tid & 15), there = a.cols - (c0 + c);
+#pragma unroll
+    for (int i = 0; i < PREP / 16; ++i) {
+        const int r = 16 * i + (tid >> 4), left = r0 + r < a.rows ? there : 0;
+        x[i] = load_four(a.g, (long long)(r0 + r) * a.ldg + c0 + c, l.g_tensor, left, a.whole_g);
+        if (l.muon) y[i] = load_four(a.mom, (long long)(r0 + r) * a.ldm + c0 + c, TENSOR_F32, left, a.whole_m);
+    }
+#pragma unroll
+    for (int i = 0; i < PREP / 16; ++i) {
+        const int r = 16 * i + (tid >> 4), left = r0 + r < a.rows ? there : 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float u = l.muon ? updated(l, x[i][e], y[i][e]) : x[i][e];
+            const float v = e < left ? (float)((double)u * inv) : 0.f;  // (inv may be inf)
+            if (a.flip) tile[c + e][r] = v;
+            else tile[r][c + e] = v;
         }
-        if (a.flip) tile[c][r] = v;
-        else tile[r][c] = v;
     }
     __syncthreads();
     half_t *const X = reinterpret_cast<half_t *>(ws + a.x[0]), *const XT = reinterpret_cast<half_t *>(ws + a.xt[0]);
@@ -194,7 +283,8 @@ struct Product {
     static constexpr int RM = T / WM, RN = T / WN, MB = RM / 16, NB = RN / 16;
     static constexpr int LOADS = T * 8 / NT;  // 16-byte loads a lane and operand tile
     static constexpr int OPERAND = T * ROW_BYTES, STAGE = 2 * OPERAND;
-    static constexpr size_t LDS = (size_t)S * STAGE;
+    static constexpr int HM = RM < 64 ? RM : 64, AHEAD = 2, REGION = RN * (HM + 4) * 4;  // of the results: rows at a time, loads before one is used
+    static constexpr size_t LDS = (size_t)(S * STAGE > NW * REGION ? S * STAGE : NW * REGION);
     v4f acc[MB][NB];
 
     // P, Q: first rows of the tile, of `pitch` bytes; segments of nk k-tiles with the offsets (bytes) of their operands
@@ -256,6 +346,113 @@ struct Product {
     }
 };
 
+// 256 x 256 tiles of eight wavefronts, as 2 x 4, of 128 x 64 each: two stages of the left operand and three of the right one (all 160 KB of LDS).
+// The sixteen products of a group (half of the rows at one k-step of 32) are issued with the requests of the next group's fragments and two
+// loads from memory between them, so that neither the LDS nor the address unit gets them all at once; loads have two groups or more to land.
+template <>
+struct Product<256, 2, 4, 2> {
+    static constexpr int T = 256, WM = 2, NW = 8, NT = 512, RM = 128, RN = 64, MB = 8, NB = 4;
+    static constexpr int OPERAND = T * ROW_BYTES, Q_BASE = 2 * OPERAND;
+    static constexpr int HM = 64, AHEAD = 4, REGION = RN * (HM + 4) * 4;
+    static constexpr size_t LDS = 5 * (size_t)OPERAND;
+    static_assert(NW * REGION <= (int)LDS, "LDS");
+    v4f acc[MB][NB];
+
+    __device__ __forceinline__ void run(unsigned char *lds, const unsigned char *P, const unsigned char *Q, unsigned pitch, int nk, int segs,
+                                        size_t low_p, size_t low_q, int tid)
+    {
+        const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int wm = wave % WM, wn = wave / WM;
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+        unsigned off[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int R = (wave + NW * v) * 8 + (lane >> 3);
+            off[v] = (unsigned)R * pitch + (((lane & 7) ^ swz(R)) << 4);
+        }
+        const int total = nk * segs;
+        auto issue_p = [&](int t, int stage, int v) {
+            const int seg = t >= 2 * nk ? 2 : t >= nk ? 1 : 0;
+            const unsigned char *p = P + (seg == 2 ? low_p : 0) + (size_t)(t - seg * nk) * ROW_BYTES;
+            __builtin_amdgcn_global_load_lds((gptr_t)(p + off[v]), (lptr_t)(lds + stage * OPERAND + (wave + NW * v) * 1024), 16, 0, 0);
+        };
+        auto issue_q = [&](int t, int stage, int v) {
+            const int seg = t >= 2 * nk ? 2 : t >= nk ? 1 : 0;
+            const unsigned char *q = Q + (seg == 1 ? low_q : 0) + (size_t)(t - seg * nk) * ROW_BYTES;
+            __builtin_amdgcn_global_load_lds((gptr_t)(q + off[v]), (lptr_t)(lds + Q_BASE + stage * OPERAND + (wave + NW * v) * 1024), 16, 0, 0);
+        };
+        const int c16 = lane & 15, g4 = lane >> 4;
+        const int p_off = (wm * RM + c16) * ROW_BYTES + ((g4 ^ swz(c16)) << 4);
+        const int q_off = Q_BASE + (wn * RN + c16) * ROW_BYTES + ((g4 ^ swz(c16)) << 4);
+        v8h fp[2][4], fq[2][4];  // half of the rows, all columns at one k-step
+        auto read = [&](int off_, int q, int kk) { return *reinterpret_cast<const v8h *>(lds + ((off_ ^ (kk << 6)) + q * 16 * ROW_BYTES)); };
+        auto group = [&](auto half_c, int bs, bool rd, int sp, int sq, int kk, bool ld, bool is_p, int t, int stage, int first) {
+            constexpr int half = decltype(half_c)::value;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    acc[4 * half + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[half][i], fq[bs][j], acc[4 * half + i][j], 0, 0, 0);
+                    const int b = 4 * i + j;
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (rd) {
+                        if (b < 4) fp[half ^ 1][b] = read(p_off + sp * OPERAND, b + (half ? 0 : 4), kk);
+                        else if (half && b < 8) fq[bs ^ 1][b - 4] = read(q_off + sq * OPERAND, b - 4, kk);
+                    }
+                    if (ld && (b == (half ? 10 : 5) || b == (half ? 14 : 10))) {
+                        const int v = first + (b == (half ? 14 : 10) ? 1 : 0);
+                        if (is_p) issue_p(t, stage, v);
+                        else issue_q(t, stage, v);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        };
+        constexpr IntC<0> LO = {};
+        constexpr IntC<1> HI = {};
+#pragma unroll
+        for (int v = 0; v < 4; ++v) issue_p(0, 0, v);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) issue_q(0, 0, v);
+        if (total > 1) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) issue_q(1, 1, v);
+            issue_p(1, 1, 0);
+            issue_p(1, 1, 1);
+            wait_loads_and_meet<6>();  // tile 0 has landed
+        } else {
+            wait_loads_and_meet<0>();
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) fp[0][q] = read(p_off, q, 0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) fq[0][q] = read(q_off, q, 0);
+        int q_cur = 0, q_nxt = 1, q_ld = 2;  // stages of the right operand of tiles t, t + 1, t + 2
+        for (int t = 0; t < total; ++t) {
+            const int cur = t & 1;
+            const bool next = t + 1 < total, next2 = t + 2 < total;
+            // (the fragments of a group were requested during the one before; the compiler cannot tell across the branches)
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            group(LO, 0, true, cur, q_cur, 0, next, true, t + 1, cur ^ 1, 2);  // + second half of the left tile t + 1
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            group(HI, 0, true, cur, q_cur, 1, next2, false, t + 2, q_ld, 0);   // + the right tile t + 2, whose stage held t - 1
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            group(LO, 1, true, cur, q_cur, 1, next2, false, t + 2, q_ld, 2);
+            // tile t + 1 has landed (the right tile t + 2 may be on its way), and nobody reads tile t any more
+            if (next2) wait_loads_and_meet<4>();
+            else wait_loads_and_meet<0>();
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            group(HI, 1, next, cur ^ 1, q_nxt, 0, next2, true, t + 2, cur, 0);  // + first half of the left tile t + 2
+            const int u = q_cur;
+            q_cur = q_nxt;
+            q_nxt = q_ld;
+            q_ld = u;
+        }
+    }
+};
+
 // row of tile t of the tiles on and below the diagonal, in row order
 __device__ __forceinline__ int triangle_row(int t)
 {
@@ -265,17 +462,64 @@ __device__ __forceinline__ int triangle_row(int t)
     return r;
 }
 
-// 4 values of a row: high parts, and low ones `low` elements further on
-__device__ __forceinline__ v4f load4(const half_t *p, size_t low, bool two)
-{
-    const v4h hi = *reinterpret_cast<const v4h *>(p);
-    v4f x = {(float)hi[0], (float)hi[1], (float)hi[2], (float)hi[3]};
-    if (two) {
-        const v4h lo = *reinterpret_cast<const v4h *>(p + low);
+// eight values of a row: high parts, and low ones `low` elements further on
+struct Eight {
+    float v[8];
+    __device__ __forceinline__ void load(const half_t *p, size_t low, bool two)
+    {
+        const v8h hi = *reinterpret_cast<const v8h *>(p);
+        v8h lo = {};
+        if (two) lo = *reinterpret_cast<const v8h *>(p + low);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] += (float)lo[e];
+        for (int e = 0; e < 8; ++e) v[e] = (float)hi[e] + (float)lo[e];
     }
-    return x;
+    __device__ __forceinline__ void store(half_t *p, size_t low, bool two) const
+    {
+        v8h hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            half_t u, w;
+            split(v[e], u, w);
+            hi[e] = u;
+            lo[e] = w;
+        }
+        *reinterpret_cast<v8h *>(p) = hi;
+        if (two) *reinterpret_cast<v8h *>(p + low) = lo;
+    }
+};
+
+// Eight neighbours in a row of the result, of which `left` are there
+__device__ __forceinline__ void put_result(const How &l, const Matrix &a, int r, int c, const float *v)
+{
+    if (r >= a.rows || c >= a.cols) return;
+    const int left = a.cols - c;
+    const long long at = (long long)r * a.ldo + c;
+    if (l.out_tensor == TENSOR_BF16) {
+        __bf16 *const q = static_cast<__bf16 *>(a.out) + at;
+        if (a.whole_out && left >= 8) {
+            v8b u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = (__bf16)(v[e] * (1.f / SX));
+            *reinterpret_cast<v8b *>(q) = u;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < left) q[e] = (__bf16)(v[e] * (1.f / SX));
+        }
+        return;
+    }
+    float *const q = static_cast<float *>(a.out) + at;
+#pragma unroll
+    for (int h = 0; h < 8; h += 4) {
+        v4f x;
+        if (l.muon) x = load_four(q, h, TENSOR_F32, left - h, a.whole_out);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float o = v[h + e] * (1.f / SX);
+            x[e] = l.muon ? __builtin_fmaf(-a.scale, o, __builtin_fmaf(-l.decay, x[e], x[e])) : o;
+        }
+        store_four(q + h, x, left - h, a.whole_out);
+    }
 }
 
 template <int T, int WM, int WN, int S, int KIND>
@@ -309,97 +553,508 @@ __global__ __launch_bounds__(64 * WM *WN) void product_kernel(const List *lp, un
         p.run(lds, x + (size_t)i0 * pitch, y + (size_t)j0 * pitch, pitch, nk, planes == 2 ? 3 : 1, 2 * (KIND == GRAM ? xlow : alow),
               2 * (SYM ? (KIND == GRAM ? xlow : alow) : xlow), tid);
     }
-    // lane 16 g + c of a 16 x 16 block: column c, rows 4 g .. 4 g + 3
-    const int lane = tid & 63, wave = tid >> 6;
-    const int wi = i0 + (wave % WM) * P::RM + 4 * (lane >> 4), wj = j0 + (wave / WM) * P::RN + (lane & 15);
+    // The results leave through LDS, HM rows of the wavefront's block at a time: lane 16 g + c of a 16 x 16 block has column c, rows 4 g .. 4 g + 3, in LDS
+    // they lie a column after the other.  From there lanes take eight rows of a column each (whole lines of the transposed
+    // layouts, which the terms to be added are read from, too), and eight columns of a row.  Loops that are not unrolled throughout: code that every
+    // workgroup runs once comes from memory, a line after the other (unrolled for all blocks it took 40 to 80 us of a launch).
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int bi0 = i0 + (wave % WM) * P::RM, bj0 = j0 + (wave / WM) * P::RN;  // of this wavefront
     float *const D = reinterpret_cast<float *>(ws + a.d), *const E = reinterpret_cast<float *>(ws + a.e);
-    const half_t *const F = reinterpret_cast<const half_t *>(ws + a.f);
+    half_t *const F = reinterpret_cast<half_t *>(ws + a.f), *const H = reinterpret_cast<half_t *>(ws + a.h);
+    half_t *const xt = reinterpret_cast<half_t *>(ws + a.xt[from]);
+    half_t *const new_xt = reinterpret_cast<half_t *>(ws + a.xt[from ^ 1]), *const new_x = reinterpret_cast<half_t *>(ws + a.x[from ^ 1]);
+    constexpr int HM = P::HM, PITCH = HM + 4, PER = HM / 8, ITEMS = P::RN * PER / 64;
+    const bool two = planes == 2, rows_too = SYM ? ti != tj : KIND == NEXT || !a.flip;
+    __syncthreads();  // nobody reads the operands any more: their place is for the results
+    float *const mine = reinterpret_cast<float *>(lds + wave * P::REGION);
 #pragma unroll
-    for (int bj = 0; bj < P::NB; ++bj) {
-        const int j = wj + 16 * bj;
-        const float dj = KIND == SQUARE ? D[j] : 0.f;
+    for (int half = 0; half < P::RM / HM; ++half) {
 #pragma unroll
-        for (int bi = 0; bi < P::MB; ++bi) {
-            const int i = wi + 16 * bi;
-            v4f v = p.acc[bi][bj];
-            if (KIND == GRAM) {
+        for (int bj = 0; bj < P::NB; ++bj)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (i + e == j) {
-                        D[j] = v[e] * (1.f / (SX * SX));
-                        v[e] = 0.f;
-                    } else {
-                        v[e] *= SA / (SX * SX);
-                    }
+            for (int bi = 0; bi < HM / 16; ++bi)
+                *reinterpret_cast<v4f *>(mine + (16 * bj + (lane & 15)) * PITCH + 16 * bi + 4 * (lane >> 4)) = p.acc[half * (HM / 16) + bi][bj];
+        const int ih = bi0 + half * HM;
+#pragma unroll 1
+        for (int it0 = 0; it0 < ITEMS; it0 += P::AHEAD) {
+            Eight x[P::AHEAD];
+            if (KIND != GRAM) {
+#pragma unroll
+                for (int u = 0; u < P::AHEAD; ++u) {
+                    const int item = (it0 + u) * 64 + lane, j = bj0 + item / PER, i = ih + 8 * (item % PER);
+                    if (KIND == SQUARE) x[u].load(F + (size_t)j * a.mp + i, alow, two);
+                    else x[u].load(xt + (size_t)j * a.mp + i, xlow, true);
                 }
-            } else if (KIND == SQUARE) {
-                const v4f f = load4(F + (size_t)j * a.mp + i, alow, planes == 2);
-                const v4f di = *reinterpret_cast<const v4f *>(D + i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float sq = v[e] * (1.f / (SA * SA)), fe = f[e] * (1.f / SA);
-                    if (i + e == j) {
-                        E[j] = __builtin_fmaf(cc, __builtin_fmaf(dj, dj, sq), cb * dj);
-                        v[e] = 0.f;
-                    } else {
-                        v[e] = SB * __builtin_fmaf(cc, __builtin_fmaf(di[e] + dj, fe, sq), cb * fe);
-                    }
-                }
-            } else {
-                const v4f x = load4(reinterpret_cast<const half_t *>(ws + a.xt[from]) + (size_t)j * a.mp + i, xlow, true);
-                const v4f ei = *reinterpret_cast<const v4f *>(E + i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(ca + ei[e], x[e], v[e] * (1.f / SB));
             }
-            if (KIND == LAST) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = a.flip ? j : i + e, c = a.flip ? i + e : j;
-                    if (r < a.rows && c < a.cols) {
-                        const long long at = (long long)r * a.ldo + c;
-                        const float o = v[e] * (1.f / SX);
-                        if (l.step_kind == MUON) {
-                            float *const w = static_cast<float *>(a.out) + at;
-                            *w = __builtin_fmaf(-a.scale, o, __builtin_fmaf(-l.decay, *w, *w));
-                        } else if (l.out_tensor == TENSOR_BF16) {
-                            static_cast<__bf16 *>(a.out)[at] = (__bf16)o;
-                        } else {
-                            static_cast<float *>(a.out)[at] = o;
-                        }
+            for (int u = 0; u < P::AHEAD; ++u) {
+                const int item = (it0 + u) * 64 + lane, jl = item / PER, il = 8 * (item % PER), j = bj0 + jl, i = ih + il;
+                float *const at = mine + jl * PITCH + il;
+                Eight v;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v.v[e] = at[e];
+                const v4f *const di = reinterpret_cast<const v4f *>((KIND == SQUARE ? D : E) + i);
+                if (KIND == GRAM) {
+                    if (ti == tj && i <= j && j < i + 8) D[j] = at[j - i] * (1.f / (SX * SX));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v.v[e] *= SA / (SX * SX);
+                } else if (KIND == SQUARE) {
+                    const float dj = D[j];
+                    if (ti == tj && i <= j && j < i + 8) E[j] = __builtin_fmaf(cc, __builtin_fmaf(dj, dj, at[j - i] * (1.f / (SA * SA))), cb * dj);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float sq = v.v[e] * (1.f / (SA * SA)), f = x[u].v[e] * (1.f / SA);
+                        v.v[e] = SB * __builtin_fmaf(cc, __builtin_fmaf(di[e / 4][e % 4] + dj, f, sq), cb * f);
                     }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v.v[e] = __builtin_fmaf(ca + di[e / 4][e % 4], x[u].v[e], v.v[e] * (1.f / SB));
                 }
-                continue;
+                if (SYM && ti == tj) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v.v[e] = i + e == j ? 0.f : v.v[e];
+                }
+                if (SYM) v.store((KIND == GRAM ? F : H) + (size_t)j * a.mp + i, alow, two);
+                else if (KIND == NEXT) v.store(new_xt + (size_t)j * a.mp + i, xlow, true);
+                else if (a.flip) put_result(l, a, j, i, v.v);
+                if (rows_too) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) at[e] = v.v[e];
+                }
             }
-            v4h hi, lo;
+        }
+        if (rows_too) {
+#pragma unroll 1
+            for (int it = 0; it < ITEMS; ++it) {
+                const int item = it * 64 + lane, il = item / (P::RN / 8), jl = 8 * (item % (P::RN / 8)), i = ih + il, j = bj0 + jl;
+                Eight v;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v.v[e] = mine[(jl + e) * PITCH + il];
+                if (SYM) v.store((KIND == GRAM ? F : H) + (size_t)i * a.mp + j, alow, two);
+                else if (KIND == NEXT) v.store(new_x + (size_t)i * a.np + j, xlow, two);
+                else put_result(l, a, i, j, v.v);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- small matrices
+// X of up to 128 rows: a workgroup has a block of its columns (all of them where they are few: then one launch does everything), and
+// several steps need X once.  With A = X X^T and P_k = a + b A_k + c A_k^2,
+//     X_k+1 = P_k X_k,   A_k+1 = P_k A_k P_k,   X_k+l = Q X_k,   Q = P_k+l-1 ... P_k
+// so a run of steps is products of m x m matrices, which commute and are symmetric.  A value of A near 0 keeps an absolute error while A_k+1 gives it the factor
+// p(0)^2, so the error of a long run is as of a square root of the precision: runs end where the product of the largest factors
+// passes 12 (HB_TENSOR_F32: two of the usual steps; the errors are those of single steps), or 500 (HB_TENSOR_BF16: five, 5e-4 at most).
+// Everything is held in 22 bits.  A wavefront has a strip of 16 columns of the m x m matrices in its registers.  A result of the matrix core holds four rows of a column a
+// lane, so two blocks of a strip are its operand of 32 values of k (in an order of their own, the same for both operands); rows go through LDS.
+constexpr int SMALL_NT = 512, SMALL_WAVES = 8;
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+struct SmallStep {
+    float a, b, c;
+    float sa, sp, sq;  // powers of two: scales of A before the step, of its P, and of Q after it
+    int end;           // of a run
+};
+struct SmallMat : Matrix {
+    int m, n;
+    int blocks, block0;  // of columns, and the first workgroup
+    int sums, sum0;      // as in Mat
+    size_t x;            // byte offset in the workspace: X^T, between launches
+    size_t part[2];      // sums of X X^T over each block's columns, in turn
+};
+struct SmallArgs : How {
+    int count;
+    int steps;
+    SmallStep step[ORTHO_STEPS];
+    SmallMat mat[ORTHO_GROUP];
+};
+static_assert(sizeof(SmallArgs) < 4000, "arguments of a launch");
+
+// MP: rows of X, padded; NB: columns of a block
+template <int MP, int NB>
+struct Small {
+    static constexpr int S = MP / 16, PARTS = SMALL_WAVES / S, KS = (MP + 31) / 32;  // strips; parts that share a strip's sums; k-steps of m
+    static constexpr int CHUNKS = MP / 8, SHIFT = MP == 128 ? 0 : MP == 64 ? 1 : MP == 32 ? 2 : 3;
+    static constexpr int PLANE = NB * MP * 2, FILE = S * KS * 2 * 1024, RED = (PARTS - 1) * MP * MP * 4;
+    static constexpr int X = 0, SHARED = 2 * PLANE;  // X^T, high and low; then rows of the m x m matrices, or sums to be added up
+    static constexpr size_t LDS = 2 * (size_t)PLANE + (FILE > RED ? FILE : RED);
+
+    // byte of element (column j, row i) in a plane of X^T: the 16-byte pieces of a row are exchanged so that 16 rows lie on different banks
+    static __device__ __forceinline__ int at(int j, int i) { return j * (2 * MP) + ((((i >> 3) ^ (j >> SHIFT)) & (CHUNKS - 1)) << 4) + 2 * (i & 7); }
+
+    struct Strip {
+        v4f v[S];  // rows 16 i + 4 g + e of column 16 strip + c
+    };
+    struct Frag {
+        v8h hi[KS], lo[KS];
+    };
+
+    static __device__ __forceinline__ void frag_of(const Strip &m, float scale, Frag &f)
+    {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                half_t hi = 0, lo = 0;
+                if (2 * ks + e / 4 < S) split(m.v[2 * ks + e / 4 < S ? 2 * ks + e / 4 : 0][e % 4] * scale, hi, lo);
+                f.hi[ks][e] = hi;
+                f.lo[ks][e] = lo;
+            }
+    }
+    // The strip's part of the rows, for everybody, in the order in which the lanes ask for it.  (The matrices are symmetric but for roundings: columns in place of
+    // rows would save the exchange, but what is not symmetric grows from step to step then, 8e-4 of the result after five.)
+    static __device__ __forceinline__ void put_rows(unsigned char *file, const Strip &m, float scale, int strip, int lane)
+    {
+        const int g4 = lane >> 4, c16 = lane & 15, ks = strip >> 1;
+        unsigned char *const to = file + ks * 2048 + (16 * (c16 >> 2) + 4 * g4) * 16 + (4 * (strip & 1) + (c16 & 3)) * 2;
+#pragma unroll
+        for (int i = 0; i < S; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
+                half_t hi, lo;
+                split(m.v[i][e] * scale, hi, lo);
+                *reinterpret_cast<half_t *>(to + i * KS * 2048 + 16 * e) = hi;
+                *reinterpret_cast<half_t *>(to + i * KS * 2048 + 16 * e + 1024) = lo;
+            }
+        if (S == 1) {  // there is no second block of 16 values of k
+            *reinterpret_cast<v4h *>(file + 16 * lane + 8) = v4h{0, 0, 0, 0};
+            *reinterpret_cast<v4h *>(file + 1024 + 16 * lane + 8) = v4h{0, 0, 0, 0};
+        }
+    }
+    // rows in LDS times columns
+    static __device__ __forceinline__ void times(const unsigned char *file, const Frag &f, float scale, Strip &out, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            v4f acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const v8h hi = *reinterpret_cast<const v8h *>(file + ((i * KS + ks) * 2) * 1024 + 16 * lane);
+                const v8h lo = *reinterpret_cast<const v8h *>(file + ((i * KS + ks) * 2 + 1) * 1024 + 16 * lane);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, f.hi[ks], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, f.lo[ks], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, f.hi[ks], acc, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out.v[i][e] = acc[e] * scale;
+            if (S == 8) __builtin_amdgcn_sched_barrier(0);  // (requests for all rows at once leave no registers)
+        }
+    }
+
+    // columns j0 .. of X from G, or zeros behind its last
+    static __device__ __forceinline__ void load_g(unsigned char *lds, const How &l, const SmallMat &a, int j0, int columns, double inv)
+    {
+        for (int item = threadIdx.x; item < columns * CHUNKS; item += SMALL_NT) {
+            // lanes along what is next to each other in G
+            const int j = a.flip ? item / CHUNKS : item % columns, i = 8 * (a.flip ? item % CHUNKS : item / columns);
+            v8h hi, lo;
+            float v[8];
+            if (a.flip) {
+                const int r = j0 + j;
+#pragma unroll
+                for (int h = 0; h < 8; h += 4) {
+                    const int left = r < a.rows ? a.cols - i - h : 0;
+                    const v4f x = load_four(a.g, (long long)r * a.ldg + i + h, l.g_tensor, left, a.whole_g);
+                    v4f y = {0.f, 0.f, 0.f, 0.f};
+                    if (l.muon) y = load_four(a.mom, (long long)r * a.ldm + i + h, TENSOR_F32, left, a.whole_m);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[h + e] = e < left ? (float)((double)updated(l, x[e], y[e]) * inv) : 0.f;
+                }
+            } else {
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = y[e] = 0.f;
+                    if (i + e < a.rows && j0 + j < a.cols) {
+                        const long long at_g = (long long)(i + e) * a.ldg + j0 + j;
+                        v[e] = l.g_tensor == TENSOR_BF16 ? (float)static_cast<const __bf16 *>(a.g)[at_g] : static_cast<const float *>(a.g)[at_g];
+                        if (l.muon) y[e] = a.mom[(long long)(i + e) * a.ldm + j0 + j];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = i + e < a.rows && j0 + j < a.cols ? (float)((double)updated(l, v[e], y[e]) * inv) : 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
                 half_t u, w;
                 split(v[e], u, w);
                 hi[e] = u;
                 lo[e] = w;
             }
-            if (SYM) {
-                half_t *const to = reinterpret_cast<half_t *>(ws + (KIND == GRAM ? a.f : a.h));
-                *reinterpret_cast<v4h *>(to + (size_t)j * a.mp + i) = hi;
-                if (planes == 2) *reinterpret_cast<v4h *>(to + alow + (size_t)j * a.mp + i) = lo;
-                if (ti != tj) {
+            *reinterpret_cast<v8h *>(lds + at(j, i)) = hi;
+            *reinterpret_cast<v8h *>(lds + PLANE + at(j, i)) = lo;
+        }
+    }
+
+    // X X^T over the block's columns, a strip each; of several wavefronts with one strip the first has it
+    static __device__ __forceinline__ void gram(unsigned char *lds, int columns, Strip &m, int strip, int part, int lane)
+    {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        to[(size_t)(i + e) * a.mp + j] = hi[e];
-                        if (planes == 2) to[alow + (size_t)(i + e) * a.mp + j] = lo[e];
-                    }
-                }
-            } else {
-                half_t *const xt = reinterpret_cast<half_t *>(ws + a.xt[from ^ 1]), *const x = reinterpret_cast<half_t *>(ws + a.x[from ^ 1]);
-                *reinterpret_cast<v4h *>(xt + (size_t)j * a.mp + i) = hi;
-                *reinterpret_cast<v4h *>(xt + xlow + (size_t)j * a.mp + i) = lo;
+        for (int i = 0; i < S; ++i) m.v[i] = v4f{0.f, 0.f, 0.f, 0.f};
+        const int g4 = lane >> 4, row = (lane & 15) >> 2, col = 4 * (lane & 3);
+        for (int k = 32 * part; k < columns; k += 32 * PARTS) {
+            // the transposing read: lane 4 r + q of sixteen gives the place of columns 4 q .. of row r, and gets column lane of rows 0 .. 3
+            auto read = [&](int plane, int s) {
+                v8h f;
+                v4s u[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[(size_t)(i + e) * a.np + j] = hi[e];
-                    if (planes == 2) x[xlow + (size_t)(i + e) * a.np + j] = lo[e];
-                }
+                for (int t = 0; t < 2; ++t)
+                    u[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) v4s *)(lds + plane * PLANE + at(k + 8 * g4 + 4 * t + row, 16 * s + col)));
+                __builtin_memcpy(&f, u, sizeof(f));
+                return f;
+            };
+            const v8h hi = read(0, strip), lo = read(1, strip);
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                const v8h ph = read(0, i), pl = read(1, i);
+                m.v[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, hi, m.v[i], 0, 0, 0);
+                m.v[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, lo, m.v[i], 0, 0, 0);
+                m.v[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, hi, m.v[i], 0, 0, 0);
+                if (S == 8) __builtin_amdgcn_sched_barrier(0);
             }
         }
+    }
+    static __device__ __forceinline__ void add_parts(unsigned char *shared, Strip &m, int strip, int part, int lane)
+    {
+        if (PARTS == 1) return;
+        v4f *const red = reinterpret_cast<v4f *>(shared);
+        if (part > 0) {
+#pragma unroll
+            for (int i = 0; i < S; ++i) red[(((part - 1) * S + strip) * S + i) * 64 + lane] = m.v[i];
+        }
+        __syncthreads();
+        if (part == 0) {
+#pragma unroll 1
+            for (int q = 0; q < PARTS - 1; ++q)
+#pragma unroll
+                for (int i = 0; i < S; ++i) m.v[i] += red[((q * S + strip) * S + i) * 64 + lane];
+        }
+        __syncthreads();
+    }
+
+    // A run of steps from step k: A (in `m` of the first wavefronts) to the rows of Q in LDS; returns the step behind it
+    static __device__ __forceinline__ int run(const SmallArgs &l, unsigned char *file, Strip &m, int k, int strip, int part, int lane)
+    {
+        Strip q, p;
+        Frag f;
+        const bool mine = part == 0;
+        for (;; ++k) {
+            const SmallStep &s = l.step[k];
+            const bool first = k == 0 || l.step[k - 1].end != 0;
+            if (mine) {
+                put_rows(file, m, s.sa, strip, lane);
+                frag_of(m, s.sa, f);
+            }
+            __syncthreads();
+            if (mine) {
+                times(file, f, s.c / (s.sa * s.sa), p, lane);
+#pragma unroll
+                for (int i = 0; i < S; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p.v[i][e] = __builtin_fmaf(s.b, m.v[i][e], p.v[i][e]);
+                        if (i == strip && 4 * (lane >> 4) + e == (lane & 15)) p.v[i][e] += s.a;
+                    }
+            }
+            __syncthreads();
+            if (mine) put_rows(file, p, s.sp, strip, lane);
+            __syncthreads();
+            if (mine) {
+                if (first) {
+                    q = p;
+                } else {
+                    const float before = l.step[k - 1].sq;
+                    frag_of(q, before, f);
+                    times(file, f, 1.f / (s.sp * before), q, lane);
+                }
+                if (!s.end) {
+                    const float next = l.step[k + 1].sa;
+                    frag_of(m, s.sa, f);
+                    times(file, f, 1.f / (s.sp * s.sa), p, lane);  // P A
+                    frag_of(p, next, f);
+                    times(file, f, 1.f / (s.sp * next), m, lane);
+                }
+            }
+            __syncthreads();
+            if (s.end) {
+                if (mine) put_rows(file, q, s.sq, strip, lane);
+                __syncthreads();
+                return k + 1;
+            }
+        }
+    }
+
+    // Q X for the block's columns: in its place, or to the result
+    static __device__ __forceinline__ void apply(unsigned char *lds, const How &l, const SmallMat &a, int j0, int columns, float inv_sq, bool last,
+                                                 int wave, int lane)
+    {
+        const unsigned char *const file = lds + SHARED;
+        const int g4 = lane >> 4, c16 = lane & 15;
+#pragma unroll 1
+        for (int jb = 16 * wave; jb < columns; jb += 16 * SMALL_WAVES) {
+            const int j = jb + c16;
+            Frag f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    v4h hi = {0, 0, 0, 0}, lo = {0, 0, 0, 0};
+                    if (2 * ks + h < S) {
+                        hi = *reinterpret_cast<const v4h *>(lds + at(j, 32 * ks + 16 * h + 4 * g4));
+                        lo = *reinterpret_cast<const v4h *>(lds + PLANE + at(j, 32 * ks + 16 * h + 4 * g4));
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        f.hi[ks][4 * h + e] = hi[e];
+                        f.lo[ks][4 * h + e] = lo[e];
+                    }
+                }
+            Strip x;
+            times(file, f, inv_sq, x, lane);
+            if (!last) {
+#pragma unroll
+                for (int i = 0; i < S; ++i) {
+                    v4h hi, lo;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        half_t u, w;
+                        split(x.v[i][e], u, w);
+                        hi[e] = u;
+                        lo[e] = w;
+                    }
+                    *reinterpret_cast<v4h *>(lds + at(j, 16 * i + 4 * g4)) = hi;
+                    *reinterpret_cast<v4h *>(lds + PLANE + at(j, 16 * i + 4 * g4)) = lo;
+                }
+                continue;
+            }
+#pragma unroll
+            for (int i = 0; i < S; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int row = 16 * i + 4 * g4 + e, r = a.flip ? j0 + j : row, c = a.flip ? row : j0 + j;
+                    if (r >= a.rows || c >= a.cols) continue;
+                    const long long at_o = (long long)r * a.ldo + c;
+                    const float o = x.v[i][e] * (1.f / SX);
+                    if (l.muon) {
+                        float *const w = static_cast<float *>(a.out) + at_o;
+                        *w = __builtin_fmaf(-a.scale, o, __builtin_fmaf(-l.decay, *w, *w));
+                    } else if (l.out_tensor == TENSOR_BF16) {
+                        static_cast<__bf16 *>(a.out)[at_o] = (__bf16)o;
+                    } else {
+                        static_cast<float *>(a.out)[at_o] = o;
+                    }
+                }
+        }
+    }
+};
+
+__device__ __forceinline__ double factor_of(double sum, float eps) { return (double)SX / (sqrt(sum) + (double)eps); }
+
+template <typename F>
+__device__ __forceinline__ int find_small(const SmallArgs &l, int block, F first)
+{
+    int k = 0;
+    while (k + 1 < l.count && block >= first(l.mat[k + 1])) ++k;
+    return k;
+}
+
+// A matrix a workgroup, everything in one launch
+template <int MP, int NB>
+__global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallArgs l)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    typedef Small<MP, NB> M;
+    const SmallMat &a = l.mat[blockIdx.x];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), strip = wave % M::S, part = wave / M::S;
+    const double sum = sum_of_block<SMALL_NT>(l, a, 0, 1, reinterpret_cast<double *>(lds));
+    __syncthreads();  // the momenta are there, and the sums have been read
+    const int columns = (a.n + 31) / 32 * 32;
+    M::load_g(lds, l, a, 0, columns, factor_of(sum, l.eps));
+    __syncthreads();
+    typename M::Strip m;
+#pragma unroll 1
+    for (int k = 0; k < l.steps;) {
+        M::gram(lds, columns, m, strip, part, lane);
+        M::add_parts(lds + M::SHARED, m, strip, part, lane);
+#pragma unroll
+        for (int i = 0; i < M::S; ++i) m.v[i] *= 1.f / (SX * SX);
+        k = M::run(l, lds + M::SHARED, m, k, strip, part, lane);
+        M::apply(lds, l, a, 0, columns, 1.f / l.step[k - 1].sq, k == l.steps, wave, lane);
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(SUM_NT) void small_sum_kernel(SmallArgs l, double *partial)
+{
+    __shared__ double red[SUM_NT / 64];
+    const SmallMat &a = l.mat[find_small(l, blockIdx.x, [](const SmallMat &x) { return x.sum0; })];
+    const double s = sum_of_block<SUM_NT>(l, a, blockIdx.x - a.sum0, a.sums, red);
+    if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+// A workgroup a block of columns.  from = -1: X from G and the sums of its products; else the run of steps from `from` on (every workgroup makes its Q itself:
+// one more launch would take longer), X times Q, and for another run the sums of its products.  turn: which of the sums are read
+template <int MP, int NB>
+__global__ __launch_bounds__(SMALL_NT) void small_part_kernel(SmallArgs l, unsigned char *ws, const double *partial, int from, int turn)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    typedef Small<MP, NB> M;
+    const SmallMat &a = l.mat[find_small(l, blockIdx.x, [](const SmallMat &x) { return x.block0; })];
+    const int block = blockIdx.x - a.block0, j0 = block * NB, columns = (min(a.n - j0, NB) + 31) / 32 * 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), strip = wave % M::S, part = wave / M::S;
+    half_t *const kept = reinterpret_cast<half_t *>(ws + a.x) + (size_t)block * NB * MP * 2;  // the planes as they are in LDS
+    if (from <= 0) {
+        double *const red = reinterpret_cast<double *>(lds);
+        double s = 0.0;
+        for (int i = threadIdx.x; i < a.sums; i += SMALL_NT) s += partial[a.sum0 + i];
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+        if (lane == 0) red[wave] = s;
+        __syncthreads();
+        s = red[0];
+#pragma unroll
+        for (int i = 1; i < SMALL_WAVES; ++i) s += red[i];
+        __syncthreads();
+        M::load_g(lds, l, a, j0, columns, factor_of(s, l.eps));
+    } else {
+        const int n = columns * (2 * MP) / 16;
+        for (int plane = 0; plane < 2; ++plane)
+            for (int i = threadIdx.x; i < n; i += SMALL_NT)
+                reinterpret_cast<v8h *>(lds + plane * M::PLANE)[i] = reinterpret_cast<const v8h *>(kept + plane * NB * MP)[i];
+    }
+    typename M::Strip m;
+    int k = from;
+    if (from >= 0) {
+#pragma unroll
+        for (int i = 0; i < M::S; ++i) m.v[i] = v4f{0.f, 0.f, 0.f, 0.f};
+        const v4f *const sums = reinterpret_cast<const v4f *>(ws + a.part[turn]);
+#pragma unroll 2
+        for (int b = part; b < a.blocks; b += M::PARTS)
+#pragma unroll
+            for (int i = 0; i < M::S; ++i) m.v[i] += sums[((b * M::S + strip) * M::S + i) * 64 + lane];
+        M::add_parts(lds + M::SHARED, m, strip, part, lane);
+#pragma unroll
+        for (int i = 0; i < M::S; ++i) m.v[i] *= 1.f / (SX * SX);
+        k = M::run(l, lds + M::SHARED, m, from, strip, part, lane);
+        M::apply(lds, l, a, j0, columns, 1.f / l.step[k - 1].sq, k == l.steps, wave, lane);
+        if (k == l.steps) return;
+    } else {
+        k = 0;
+    }
+    __syncthreads();
+    if (from >= 0) {
+        const int n = columns * (2 * MP) / 16;
+        for (int plane = 0; plane < 2; ++plane)
+            for (int i = threadIdx.x; i < n; i += SMALL_NT)
+                reinterpret_cast<v8h *>(kept + plane * NB * MP)[i] = reinterpret_cast<const v8h *>(lds + plane * M::PLANE)[i];
+    }
+    M::gram(lds, columns, m, strip, part, lane);
+    M::add_parts(lds + M::SHARED, m, strip, part, lane);
+    if (part == 0) {
+        v4f *const sums = reinterpret_cast<v4f *>(ws + a.part[from < 0 ? turn : turn ^ 1]);
+#pragma unroll
+        for (int i = 0; i < M::S; ++i) sums[((block * M::S + strip) * M::S + i) * 64 + lane] = m.v[i];
     }
 }
 
@@ -438,7 +1093,8 @@ Layout lay_out(List &l, const OrthoShape *s, int n, int planes)
 {
     l.count = n;
     l.planes = planes;
-    l.tile = tile_of(s, n);
+    static const char *force = getenv("HB_ORTHO_TILE");
+    l.tile = force ? atoi(force) : tile_of(s, n);
     Layout y = {};
     size_t at = aligned(sizeof(List));
     y.partial = at;
@@ -447,7 +1103,6 @@ Layout lay_out(List &l, const OrthoShape *s, int n, int planes)
         Mat &a = l.mat[k];
         a.rows = s[k].rows;
         a.cols = s[k].cols;
-        a.flip = s[k].rows > s[k].cols;
         a.m = s[k].m();
         a.n = s[k].n();
         a.mp = (int)round_to(a.m, l.tile);
@@ -483,6 +1138,36 @@ Layout lay_out(List &l, const OrthoShape *s, int n, int planes)
     return y;
 }
 
+void describe(How &l, const OrthoSteps &how)
+{
+    l.g_tensor = how.g_tensor;
+    l.out_tensor = how.muon ? (int)TENSOR_F32 : how.out_tensor;
+    l.muon = how.muon;
+    l.nesterov = how.nesterov;
+    l.momentum = how.momentum;
+    l.eps = how.eps;
+    l.decay = how.lr * how.weight_decay;
+}
+
+void describe(Matrix &a, const OrthoMatrix &o, const OrthoShape &s, const OrthoSteps &how)
+{
+    const size_t size = how.g_tensor == TENSOR_BF16 ? 2 : 4;
+    a.rows = s.rows;
+    a.cols = s.cols;
+    a.flip = s.rows > s.cols;
+    a.g = o.g;
+    a.ldg = o.ldg;
+    a.out = o.out;
+    a.ldo = o.ldo;
+    a.mom = o.momentum;
+    a.ldm = o.ldm;
+    a.scale = how.lr * o.scale;
+    a.whole_g = reinterpret_cast<uintptr_t>(o.g) % (4 * size) == 0 && (o.ldg % 4 == 0 || a.rows == 1);
+    a.whole_m = reinterpret_cast<uintptr_t>(o.momentum) % 16 == 0 && (o.ldm % 4 == 0 || a.rows == 1);
+    a.whole_out = reinterpret_cast<uintptr_t>(o.out) % 16 == 0 &&
+                  (o.ldo % (how.out_tensor == TENSOR_BF16 && !how.muon ? 8 : 4) == 0 || a.rows == 1);
+}
+
 template <int T, int WM, int WN, int S>
 hipError_t products(const List *dl, unsigned char *ws, const Layout &y, const OrthoSteps &how, hipStream_t stream)
 {
@@ -504,12 +1189,138 @@ hipError_t products(const List *dl, unsigned char *ws, const Layout &y, const Or
     return e;
 }
 
+// Runs of steps, and the scales: singular values of X are at most 1 at the start; the largest factor and value of a step are looked for
+bool plan_steps(SmallArgs &l, const OrthoSteps &how)
+{
+    const double limit = how.products == TENSOR_F32 ? 12.0 : 500.0;
+    auto scale = [](double most, double cap) {  // a power of two that leaves room to 2^14
+        double s = cap;
+        while (s > 1.0 && most * s > 16384.0) s *= 0.5;
+        return (float)s;
+    };
+    double top = 1.002, last = top, product = 1.0;  // of the singular values, and before the step; of the factors in a run
+    l.steps = how.steps;
+    for (int k = 0; k < how.steps; ++k) {
+        const float *c = how.coef + 3 * (how.n_coef == 1 ? 0 : k);
+        SmallStep &s = l.step[k];
+        s.a = c[0];
+        s.b = c[1];
+        s.c = c[2];
+        double most = 0.0, next = 0.0;
+        for (int i = 0; i <= 256; ++i) {
+            const double x = top * i / 256, p = fabs(c[0] + x * x * (c[1] + x * x * c[2]));
+            most = p > most ? p : most;
+            next = p * x > next ? p * x : next;
+        }
+        if (k > 0) {
+            l.step[k - 1].end = product * most > limit;
+            if (l.step[k - 1].end) product = 1.0;
+        }
+        product *= most > 1.0 ? most : 1.0;
+        s.sa = scale(top * (top > last ? top : last), 4096.0);  // (P A of the step before, too)
+        s.sp = scale(most, 4096.0);
+        s.sq = scale(product, 4096.0);
+        s.end = k + 1 == how.steps;
+        last = top;
+        top = 1.002 * next;  // (between the places that are looked at)
+        if (!(top < 16.0) || most > 8192.0) return false;  // (or X leaves fp16 anyway)
+    }
+    return true;
+}
+
+struct SmallForm {
+    int rows, columns;
+};
+SmallForm small_form(int m)
+{
+    if (m <= 16) return {16, 1024};
+    if (m <= 32) return {32, 1024};
+    if (m <= 64) return {64, 512};
+    return {128, 128};
+}
+
+// The rows of the largest matrix of a call decide; 0: not for it
+int small_rows(const OrthoShape *s, int n)
+{
+    int m = 0;
+    for (int k = 0; k < n; ++k) m = s[k].m() > m ? s[k].m() : m;
+    return m <= 128 ? small_form(m).rows : 0;
+}
+
+struct SmallLayout {
+    size_t partial, end;
+    int sums, blocks;
+    bool one;  // every matrix is one block
+};
+SmallLayout lay_out_small(SmallArgs &l, const OrthoShape *s, int n, int rows)
+{
+    const int nb = small_form(rows).columns;
+    SmallLayout y = {};
+    l.count = n;
+    size_t at = 0;
+    y.partial = at;
+    at += aligned(sizeof(double) * SUM_BLOCKS * (size_t)n);
+    y.one = true;
+    for (int k = 0; k < n; ++k) {
+        SmallMat &a = l.mat[k];
+        a.m = s[k].m();
+        a.n = s[k].n();
+        a.blocks = (int)((a.n + nb - 1) / nb);
+        a.block0 = y.blocks;
+        y.blocks += a.blocks;
+        y.one = y.one && a.blocks == 1;
+        const long long total = (long long)s[k].rows * s[k].cols;
+        a.sums = (int)(total >= (long long)SUM_MIN * SUM_BLOCKS ? SUM_BLOCKS : (total + SUM_MIN - 1) / SUM_MIN);
+        a.sum0 = y.sums;
+        y.sums += a.sums;
+        a.x = at;
+        at = aligned(at + (size_t)a.blocks * nb * rows * 4);
+        for (int i = 0; i < 2; ++i) {
+            a.part[i] = at;
+            at = aligned(at + (size_t)a.blocks * rows * rows * 4);
+        }
+    }
+    y.end = y.one ? 16 : at;
+    return y;
+}
+
+template <int MP, int NB>
+hipError_t small_launches(const SmallArgs &l, const SmallLayout &y, unsigned char *ws, hipStream_t stream)
+{
+    typedef Small<MP, NB> M;
+    static LdsGrant grant;
+    hipError_t e = grant_lds(grant, M::LDS, small_kernel<MP, NB>, small_part_kernel<MP, NB>);
+    if (e != hipSuccess) return e;
+    if (y.one) {
+        hipLaunchKernelGGL((small_kernel<MP, NB>), dim3(l.count), dim3(SMALL_NT), M::LDS, stream, l);
+        return hipGetLastError();
+    }
+    double *const partial = reinterpret_cast<double *>(ws + y.partial);
+    hipLaunchKernelGGL(small_sum_kernel, dim3(y.sums), dim3(SUM_NT), 0, stream, l, partial);
+    hipLaunchKernelGGL((small_part_kernel<MP, NB>), dim3(y.blocks), dim3(SMALL_NT), M::LDS, stream, l, ws, partial, -1, 0);
+    int turn = 0;
+    for (int k = 0; k < l.steps;) {
+        hipLaunchKernelGGL((small_part_kernel<MP, NB>), dim3(y.blocks), dim3(SMALL_NT), M::LDS, stream, l, ws, partial, k, turn);
+        while (!l.step[k].end) ++k;
+        ++k;
+        turn ^= 1;
+    }
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t ortho_workspace(const OrthoShape *shapes, int n, int products)
 {
     size_t most = 0;
     List l;
+    const int rows = small_rows(shapes, n);
+    for (int k = 0; rows && k < n; k += ORTHO_GROUP) {
+        SmallArgs a;
+        const size_t b = lay_out_small(a, shapes + k, n - k < ORTHO_GROUP ? n - k : ORTHO_GROUP, rows).end;
+        most = b > most ? b : most;
+    }
+    // (also of small ones: the steps decide, too)
     for (int k = 0; k < n; k += ORTHO_GROUP) {
         const size_t b = lay_out(l, shapes + k, n - k < ORTHO_GROUP ? n - k : ORTHO_GROUP, products == TENSOR_F32 ? 2 : 1).end;
         most = b > most ? b : most;
@@ -520,27 +1331,32 @@ size_t ortho_workspace(const OrthoShape *shapes, int n, int products)
 // Groups of at most ORTHO_GROUP matrices, one after the other in the same workspace
 hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n, const OrthoSteps &how, void *ws, hipStream_t stream)
 {
+    const int rows = small_rows(shapes, n);
+    SmallArgs small = {};
+    if (rows && plan_steps(small, how)) {
+        describe(small, how);
+        for (int k0 = 0; k0 < n; k0 += ORTHO_GROUP) {
+            const int count = n - k0 < ORTHO_GROUP ? n - k0 : ORTHO_GROUP;
+            const SmallLayout y = lay_out_small(small, shapes + k0, count, rows);
+            for (int k = 0; k < count; ++k) describe(small.mat[k], list[k0 + k], shapes[k0 + k], how);
+            unsigned char *const w = static_cast<unsigned char *>(ws);
+            const hipError_t e = rows == 16   ? small_launches<16, 1024>(small, y, w, stream)
+                                 : rows == 32 ? small_launches<32, 1024>(small, y, w, stream)
+                                 : rows == 64 ? small_launches<64, 512>(small, y, w, stream)
+                                              : small_launches<128, 128>(small, y, w, stream);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
     for (int k0 = 0; k0 < n; k0 += ORTHO_GROUP) {
         const int count = n - k0 < ORTHO_GROUP ? n - k0 : ORTHO_GROUP;
         List l = {};
         const Layout y = lay_out(l, shapes + k0, count, how.products == TENSOR_F32 ? 2 : 1);
-        l.g_tensor = how.g_tensor;
-        l.out_tensor = how.out_tensor;
-        l.step_kind = how.muon ? MUON : PLAIN;
-        l.nesterov = how.nesterov;
-        l.momentum = how.momentum;
-        l.eps = how.eps;
-        l.decay = how.lr * how.weight_decay;
+        describe(l, how);
         for (int k = 0; k < count; ++k) {
             Mat &a = l.mat[k];
             const OrthoMatrix &o = list[k0 + k];
-            a.g = o.g;
-            a.ldg = o.ldg;
-            a.out = o.out;
-            a.ldo = o.ldo;
-            a.mom = o.momentum;
-            a.ldm = o.ldm;
-            a.scale = how.lr * o.scale;
+            describe(a, o, shapes[k0 + k], how);
         }
         unsigned char *const w = static_cast<unsigned char *>(ws);
         List *const dl = reinterpret_cast<List *>(w);

@@ -40,7 +40,7 @@ def ortho_rounded(G, steps=5, coef=COEF, eps=1e-7, planes=1):
         Xq = q(X, 4096)
         A = Xq @ Xq.T
         d = np.diag(A).copy()
-        F = q(A - np.diag(d), 4096)
+        F = q(A - np.diag(d), 256)
         B = b * F + c * (F @ F + (d[:, None] + d[None, :]) * F)
         e = b * d + c * (d * d + np.diag(F @ F))
         H = q(B - np.diag(np.diag(B)), 1024)
@@ -50,22 +50,61 @@ def ortho_rounded(G, steps=5, coef=COEF, eps=1e-7, planes=1):
     return X.T if flip else X
 
 
-def fp32_sums(G, steps=5, coef=COEF, eps=1e-7):
+def runs_of(coef, steps, limit):
+    """Where runs of steps end that are made on A = X X^T alone: the product of the largest factors |a + b s^2 + c s^4| is at most limit."""
+    ends, top, product = [False] * steps, 1.002, 1.0
+    for k, (a, b, c) in enumerate(_triples(coef, steps)):
+        x = top * np.arange(257) / 256
+        p = np.abs(a + b * x ** 2 + c * x ** 4)
+        if k and product * p.max() > limit:
+            ends[k - 1], product = True, 1.0
+        product *= max(1.0, p.max())
+        top = 1.002 * (p * x).max()
+    ends[-1] = True
+    return ends
+
+
+def ortho_runs(G, steps=5, coef=COEF, eps=1e-7, limit=12.0):
+    """The definition by runs of steps on A, with everything rounded to 22 bits as it is stored."""
+    G = np.asarray(G, np.float64)
+    flip = G.shape[0] > G.shape[1]
+    X = G.T if flip else G
+    X = _both(X / (np.sqrt((X * X).sum()) + float(np.float32(eps))), 4096)
+    I, A = np.eye(len(X)), None
+    for (a, b, c), end in zip(_triples(coef, steps), runs_of(coef, steps, limit)):
+        if A is None:
+            A, Q = X @ X.T, None
+        Aq = _both(A, 4096)
+        P = a * I + b * A + c * (Aq @ Aq)
+        Pq = _both(P, 4096)
+        Q = P if Q is None else Pq @ _both(Q, 32)
+        if not end:
+            A = Pq @ _both(Pq @ Aq, 4096)
+        else:
+            X, A = _both(_both(Q, 32) @ X, 4096), None
+    return X.T if flip else X
+
+
+def fp32_sums(G, steps=5, coef=COEF, eps=1e-7, limit=0.0):
     """What the fp32 sums of the products may add to the result, in Frobenius norm.  A sum of n terms in chains of n / 32 rounds about that often
     plus a few times; roundings of many entries are independent, so those of a matrix add up like sqrt(n / 32 + 8) 2^-24 of its norm, 4
     times that at most.  A later step multiplies what is there by at most max |p'| = p'(0) = a (usual steps; the divided
-    differences of the odd p bound the derivative of the matrix function in this norm)."""
+    differences of the odd p bound the derivative of the matrix function in this norm).  In a run of steps on A (limit) what A is off by goes on to the next A by at most the slope of
+    l p(l)^2."""
     G = np.asarray(G, np.float64)
     X = G.T if G.shape[0] > G.shape[1] else G
     norm = np.sqrt((X * X).sum()) + float(np.float32(eps))
     s = np.linalg.svd(X / norm, compute_uv=False)
     m, n = X.shape
     u = 4 * np.sqrt(max(m, n) / 32 + 8) * 2.0 ** -24
-    off = 2.0 ** -24
-    for a, b, c in _triples(coef, steps):
+    off, carried = 2.0 ** -24, 0.0
+    for (a, b, c), end in zip(_triples(coef, steps), runs_of(coef, steps, limit)):
         top, size = s.max(), np.sqrt((s * s).sum())
         slope = np.abs(a + 3 * b * np.linspace(0, top, 100) ** 2 + 5 * c * np.linspace(0, top, 100) ** 4).max()
-        dA = u * top * size
+        dA = u * top * size + carried
+        at = np.linspace(0, top, 100) ** 2
+        p, dp = a + b * at + c * at ** 2, b + 2 * c * at
+        carried = 0.0 if end else np.abs(p * p + 2 * at * p * dp).max() * dA
         dB = (abs(b) + 2 * abs(c) * top ** 2) * dA + u * (abs(b) + abs(c) * top ** 2) * top * size
         s = np.abs(a * s + b * s ** 3 + c * s ** 5)
         off = slope * off + dB * top + 2 * u * (abs(a) + abs(b) * top ** 2 + abs(c) * top ** 4) * size

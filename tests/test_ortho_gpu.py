@@ -1,7 +1,7 @@
 """Orthogonalised updates against their definition in 64 bits.
 
 Tolerances, in Frobenius norm: what the roundings of stored operands do is found by making the same roundings in the 64-bit computation
-(ortho_rounded); others may fall elsewhere by the order of fp32 sums, so twice its distance from the definition is allowed, and on top what fp32 sums
+(ortho_rounded, for small matrices ortho_runs); others may fall elsewhere by the order of fp32 sums, so twice its distance from the definition is allowed, and on top what fp32 sums
 may add (fp32_sums).  A bf16 result adds its rounding, 2^-8 relative to each entry.  Weights: the update's tolerance times lr scale, and three
 roundings of 2^-24 of |w| and of the update; momenta: one rounding of each term.
 """
@@ -42,10 +42,16 @@ def norm(x):
     return float(np.sqrt((x * x).sum()))
 
 
-def tolerance(G, products, out="f32", **how):
-    """(result, how far one may be from it in norm)"""
+def tolerance(G, products, out="f32", tiles=False, **how):
+    """(result, how far one may be from it in norm); tiles: beside larger matrices in a list"""
     want = ref.ortho_ref(G, **how)
-    tol = 2 * norm(ref.ortho_rounded(G, planes=2 if products == "f32" else 1, **how) - want) + ref.fp32_sums(G, **how)
+    limit = 0.0
+    if min(G.shape) <= 128 and not tiles:  # small matrices, by themselves: runs of steps
+        limit = 12.0 if products == "f32" else 500.0
+        rounded = ref.ortho_runs(G, limit=limit, **how)
+    else:
+        rounded = ref.ortho_rounded(G, planes=2 if products == "f32" else 1, **how)
+    tol = 2 * norm(rounded - want) + ref.fp32_sums(G, limit=limit, **how)
     return want, tol + (2.0 ** -8 * norm(want) if out == "bf16" else 2.0 ** -24 * norm(want)) + 2.0 ** -36 * np.sqrt(want.size)
 
 
@@ -105,6 +111,36 @@ def test_large_matrix_against_products_on_the_device():
             assert float((out.double() - want).norm() / want.norm()) <= tol, (rows, cols, products)
 
 
+SMALL = [(1, 1), (3, 40), (16, 16), (16, 1025), (17, 100), (32, 1024), (33, 5), (64, 512), (64, 513), (65, 65), (128, 128), (128, 129), (100, 1000), (5, 8192),
+         (9000, 20), (700, 128), (60, 3000), (127, 2000), (31, 33)]
+
+
+@pytest.mark.parametrize("products", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SMALL)
+def test_small_matrices(shape, products):
+    """One block of columns, several, and several matrices of which the largest decides."""
+    rng = np.random.default_rng(shape[0] + 7 * shape[1])
+    for shapes, how in [([shape], {}), ([shape, (shape[0], 2), (1, 1)], {"steps": 7}), ([shape[::-1], shape], {"steps": 1}),
+                        ([shape], {"steps": 9, "coef": (1.5, -0.5, 0.0)})]:
+        G = [gradient(r, c, rng, ("spread", "low", "holes")[(r + i) % 3]).astype(np.float32).astype(np.float64) for i, (r, c) in enumerate(shapes)]
+        out = [matrix(np.zeros(s), "f32", s[1] + 1, 1) for s in shapes]
+        hb.orthogonalize([matrix(x, "f32", x.shape[1] + 2, 3)[0] for x in G], [o[0] for o in out], products=KINDS[products],
+                         ws=work(shapes, products), **how)
+        for x, (o, flat) in zip(G, out):
+            check(o, *tolerance(x, products, **how), (shapes, how))
+            assert outside_is_nan(flat, o)
+
+
+def test_coefficients_that_grow_go_through_the_products():
+    """Factors too large for the runs of small matrices."""
+    rng = np.random.default_rng(8)
+    G = gradient(20, 30, rng, "plain").astype(np.float32).astype(np.float64)
+    how = {"steps": 2, "coef": ((30.0, 0.0, 0.0), (1.0, 0.0, 0.0))}
+    out = torch.empty(20, 30, device="cuda")
+    hb.orthogonalize(torch.as_tensor(G).float().cuda(), out, ws=work([(20, 30)], "f32"), **how)
+    check(out, *tolerance(G, "f32", tiles=True, **how), "grown")
+
+
 def test_lists_of_mixed_shapes():
     """More matrices than go through the same launches, tall and wide, some without rows."""
     rng = np.random.default_rng(5)
@@ -115,7 +151,7 @@ def test_lists_of_mixed_shapes():
     hb.orthogonalize(dG, out, ws=work(shapes, "f32"))
     for x, o, s in zip(G, out, shapes):
         if 0 not in s:
-            check(o, *tolerance(x, "f32"), s)
+            check(o, *tolerance(x, "f32", tiles=True), s)
 
 
 @pytest.mark.parametrize("how", [{"steps": 1}, {"steps": 2, "coef": (1.5, -0.5, 0.0)}, {"steps": 12, "coef": (1.5, -0.5, 0.0)},
@@ -201,7 +237,7 @@ def test_muon(nesterov, g_type, products):
             size = np.abs(momentum * m0) + np.abs(g)
             assert (np.abs(host(m) - want_m) <= 2 * U * size + 1e-30).all()
             u = g + float(np.float32(momentum)) * want_m if nesterov else want_m
-            _, tol = tolerance(u, products)
+            _, tol = tolerance(u, products, tiles=True)
             tol += 485 * 3 * U  # U from an M that has been rounded
             check(w, want_w, lr * abs(s) * tol + 3 * U * (norm(w0) + lr * abs(s) * norm(O)), w0.shape)
             assert outside_is_nan(fw, w) and outside_is_nan(fm, m)
