@@ -19,12 +19,11 @@
 // Operands are scaled by powers of two so that neither what they hold nor its low part leaves fp16's range: X by 2^12 (entries are at most the largest
 // singular value s, 1.2 for the usual steps, and around (m n)^-1/2 at the start), A by 2^8 and B by 2^10 (entries beside the diagonal are at most half
 // the range of s^2, and of b s^2 + c s^4): s up to 16 and b s^2 + c s^4 up to 64 have room.
-// Everything in the workspace is padded with zeros to whole tiles, which the steps keep zero: no kernel between the first and the last
-// has a bounds check.
+// X is padded with zeros to whole k-tiles, which the steps keep zero, and the workspace has whole tiles: no kernel between the first and the last has a bounds
+// check.  What a tile makes of the rows behind the last k-tile is not defined, but stays in such rows: no k gets that far.
 #include "gemm_device.h"
 #include "operators.h"
 #include <math.h>
-#include <stdlib.h>
 
 namespace hb {
 namespace {
@@ -61,14 +60,14 @@ struct How {
 };
 // what the kernels of the products read of it besides, in the workspace
 struct Mat : Matrix {
-    int m, n, mp, np;         // rows and columns of X, and padded to whole tiles
+    int m, n, mp, np;         // rows and columns of X in whole k-tiles (zeros behind the last), and pitches: whole tiles
     int sums, sum0;           // blocks of the sum of squares, and the first
     int prep0, sym0, all0;    // first block of the others: X's layout, tiles on and below the diagonal of m x m, tiles of m x n
     size_t x[2], xt[2], f, h; // byte offsets from the workspace: X and X^T (two of each, in turn), A and B; low parts follow
     size_t d, e;              // diagonals of A and B
 };
 struct List : How {
-    int count, tile, planes;
+    int count, planes;
     Mat mat[ORTHO_GROUP];
 };
 
@@ -218,7 +217,7 @@ __global__ __launch_bounds__(256) void prep_kernel(const List *lp, unsigned char
     __syncthreads();
     const double inv = (double)SX / (sqrt((red[0] + red[1]) + (red[2] + red[3])) + (double)l.eps);
     // tile of X: rows i0 .., columns j0 ..; of G the same or exchanged
-    const int per_row = a.np / PREP, t = blockIdx.x - a.prep0;
+    const int per_row = a.n / PREP, t = blockIdx.x - a.prep0;
     const int i0 = (t / per_row) * PREP, j0 = (t % per_row) * PREP;
     const int r0 = a.flip ? j0 : i0, c0 = a.flip ? i0 : j0;
     v4f x[PREP / 16], y[PREP / 16];
@@ -537,7 +536,7 @@ __global__ __launch_bounds__(64 * WM *WN) void product_kernel(const List *lp, un
         ti = triangle_row(t);
         tj = t - ti * (ti + 1) / 2;
     } else {
-        const int per_row = a.np / T;
+        const int per_row = (a.n + T - 1) / T;
         ti = t / per_row;
         tj = t - ti * per_row;
     }
@@ -549,7 +548,7 @@ __global__ __launch_bounds__(64 * WM *WN) void product_kernel(const List *lp, un
         const unsigned char *x = ws + (KIND == GRAM ? a.x[from] : KIND == SQUARE ? a.f : a.h);
         const unsigned char *y = KIND == GRAM || KIND == SQUARE ? x : ws + a.xt[from];
         const unsigned pitch = 2u * (unsigned)(KIND == GRAM ? a.np : a.mp);
-        const int nk = ((KIND == GRAM ? a.n : a.m) + BK - 1) / BK;
+        const int nk = (KIND == GRAM ? a.n : a.m) / BK;
         p.run(lds, x + (size_t)i0 * pitch, y + (size_t)j0 * pitch, pitch, nk, planes == 2 ? 3 : 1, 2 * (KIND == GRAM ? xlow : alow),
               2 * (SYM ? (KIND == GRAM ? xlow : alow) : xlow), tid);
     }
@@ -1062,40 +1061,62 @@ __global__ __launch_bounds__(SMALL_NT) void small_part_kernel(SmallArgs l, unsig
 long long round_to(long long v, int t) { return (v + t - 1) / t * t; }
 size_t aligned(size_t v) { return (v + 255) / 256 * 256; }
 
-// Tile size of a call
-int tile_of(const OrthoShape *s, int n)
+struct Tiles {
+    int sym, all;  // of the symmetric products, and of those with as many columns as X
+    int most() const { return sym > all ? sym : all; }
+};
+
+// Time of a product of `tiles` tiles of T x T over the longest k, in us, from what the kernels take: a k-tile of 64 with a workgroup or less a
+// compute unit 0.30 (T = 64), 0.68 (128), 1.40 us (256), with two 0.60, 1.20; first loads and results 4, 8, 18.
+double product_time(int T, double tiles, double k_tiles)
 {
-    double best = 0.0;
-    int tile = 64;
-    for (int t : {64, 128, 256}) {
-        double cost = 0.0, sym = 0.0, all = 0.0, depth = 0.0;
+    const double one = T == 64 ? 0.30 : T == 128 ? 0.68 : 1.40, two = T == 64 ? 0.60 : T == 128 ? 1.20 : 1.40;
+    const double at_once = T == 256 ? 256 : 512, rounds = floor(tiles / at_once), rest = tiles - rounds * at_once;
+    return k_tiles * (rounds * two + (rest == 0.0 ? 0.0 : rest <= 256 ? one : two)) + (T == 64 ? 4.0 : T == 128 ? 8.0 : 18.0);
+}
+
+// Large tiles read less for a product, small ones are more of them.  (4096 x 4096 bf16: sym 64 158, 128 120, 256 120 us, all 249, 165, 147;
+// 1000 x 4096: sym 23, 48, 105, all 22.6, 22.4, 43.)
+Tiles tiles_for(const OrthoShape *s, int n, int planes)
+{
+    Tiles best = {64, 64};
+    double sym_time = 0.0, all_time = 0.0;
+    for (int T : {64, 128, 256}) {
+        double sym = 0.0, all = 0.0, m_most = 0.0, n_most = 0.0;
         for (int k = 0; k < n; ++k) {
-            const double mt = (double)round_to(s[k].m(), t) / t, nt = (double)round_to(s[k].n(), t) / t;
+            const double mt = (double)((s[k].m() + T - 1) / T), nt = (double)((s[k].n() + T - 1) / T);
             sym += mt * (mt + 1) / 2;
             all += mt * nt;
-            depth = depth > (double)s[k].n() ? depth : (double)s[k].n();
+            m_most = fmax(m_most, s[k].m());
+            n_most = fmax(n_most, s[k].n());
         }
-        cost = (2 * ceil(sym / 256) + ceil(all / 256)) * t * t;
-        if (t == 64 || cost < best) {
-            best = cost;
-            tile = t;
+        const double km = ceil(m_most / BK) * (planes == 2 ? 3 : 1), kn = ceil(n_most / BK) * (planes == 2 ? 3 : 1);
+        const double ts = product_time(T, sym, kn) + product_time(T, sym, km), ta = product_time(T, all, km);
+        if (T == 64 || ts < sym_time) {
+            sym_time = ts;
+            best.sym = T;
+        }
+        if (T == 64 || ta < all_time) {
+            all_time = ta;
+            best.all = T;
         }
     }
-    return tile;
+    return best;
 }
 
 struct Layout {
     size_t partial, end;
     int sums, preps, syms, alls;
+    Tiles tiles;
 };
 
 Layout lay_out(List &l, const OrthoShape *s, int n, int planes)
 {
     l.count = n;
     l.planes = planes;
-    static const char *force = getenv("HB_ORTHO_TILE");
-    l.tile = force ? atoi(force) : tile_of(s, n);
+    const Tiles tiles = tiles_for(s, n, planes);
     Layout y = {};
+    y.tiles = tiles;
     size_t at = aligned(sizeof(List));
     y.partial = at;
     at += aligned(sizeof(double) * SUM_BLOCKS * (size_t)n);
@@ -1103,10 +1124,10 @@ Layout lay_out(List &l, const OrthoShape *s, int n, int planes)
         Mat &a = l.mat[k];
         a.rows = s[k].rows;
         a.cols = s[k].cols;
-        a.m = s[k].m();
-        a.n = s[k].n();
-        a.mp = (int)round_to(a.m, l.tile);
-        a.np = (int)round_to(a.n, l.tile);
+        a.m = (int)round_to(s[k].m(), BK);
+        a.n = (int)round_to(s[k].n(), BK);
+        a.mp = (int)round_to(a.m, tiles.most());
+        a.np = (int)round_to(a.n, tiles.all);
         const size_t x = 2 * (size_t)a.mp * a.np, sq = 2 * (size_t)a.mp * a.mp;
         for (int i = 0; i < 2; ++i) {
             a.x[i] = at;
@@ -1128,11 +1149,11 @@ Layout lay_out(List &l, const OrthoShape *s, int n, int planes)
         a.prep0 = y.preps;
         a.sym0 = y.syms;
         a.all0 = y.alls;
-        const int mt = a.mp / l.tile, nt = a.np / l.tile;
+        const int mt = (a.m + tiles.sym - 1) / tiles.sym;
         y.sums += a.sums;
-        y.preps += (a.mp / PREP) * (a.np / PREP);
+        y.preps += (a.m / PREP) * (a.n / PREP);
         y.syms += mt * (mt + 1) / 2;
-        y.alls += mt * nt;
+        y.alls += ((a.m + tiles.all - 1) / tiles.all) * ((a.n + tiles.all - 1) / tiles.all);
     }
     y.end = at;
     return y;
@@ -1168,23 +1189,56 @@ void describe(Matrix &a, const OrthoMatrix &o, const OrthoShape &s, const OrthoS
                   (o.ldo % (how.out_tensor == TENSOR_BF16 && !how.muon ? 8 : 4) == 0 || a.rows == 1);
 }
 
-template <int T, int WM, int WN, int S>
+template <int T>
+struct Form;
+template <>
+struct Form<64> {
+    typedef Product<64, 2, 2, 4> P;
+    template <int KIND>
+    static constexpr auto kernel = product_kernel<64, 2, 2, 4, KIND>;
+};
+template <>
+struct Form<128> {
+    typedef Product<128, 2, 2, 2> P;
+    template <int KIND>
+    static constexpr auto kernel = product_kernel<128, 2, 2, 2, KIND>;
+};
+template <>
+struct Form<256> {
+    typedef Product<256, 2, 4, 2> P;
+    template <int KIND>
+    static constexpr auto kernel = product_kernel<256, 2, 4, 2, KIND>;
+};
+
+template <int T, int KIND>
+hipError_t product(int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream)
+{
+    typedef Form<T> F;
+    static LdsGrant grant;
+    const hipError_t e = grant_lds(grant, F::P::LDS, F::template kernel<KIND>);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(F::template kernel<KIND>, dim3((unsigned)blocks), dim3(F::P::NT), F::P::LDS, stream, dl, ws, from, c[0], c[1], c[2]);
+    return hipGetLastError();
+}
+
+template <int KIND>
+hipError_t product(int tile, int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream)
+{
+    if (tile == 256) return product<256, KIND>(blocks, dl, ws, from, c, stream);
+    if (tile == 128) return product<128, KIND>(blocks, dl, ws, from, c, stream);
+    return product<64, KIND>(blocks, dl, ws, from, c, stream);
+}
+
 hipError_t products(const List *dl, unsigned char *ws, const Layout &y, const OrthoSteps &how, hipStream_t stream)
 {
-    typedef Product<T, WM, WN, S> P;
-    static LdsGrant grant;
-    hipError_t e = grant_lds(grant, P::LDS, product_kernel<T, WM, WN, S, GRAM>, product_kernel<T, WM, WN, S, SQUARE>,
-                             product_kernel<T, WM, WN, S, NEXT>, product_kernel<T, WM, WN, S, LAST>);
+    hipError_t e = hipSuccess;
     for (int i = 0; i < how.steps && e == hipSuccess; ++i) {
         const float *c = how.coef + 3 * (how.n_coef == 1 ? 0 : i);
         const int from = i & 1;
-        hipLaunchKernelGGL((product_kernel<T, WM, WN, S, GRAM>), dim3(y.syms), dim3(P::NT), P::LDS, stream, dl, ws, from, c[0], c[1], c[2]);
-        hipLaunchKernelGGL((product_kernel<T, WM, WN, S, SQUARE>), dim3(y.syms), dim3(P::NT), P::LDS, stream, dl, ws, from, c[0], c[1], c[2]);
-        if (i + 1 < how.steps)
-            hipLaunchKernelGGL((product_kernel<T, WM, WN, S, NEXT>), dim3(y.alls), dim3(P::NT), P::LDS, stream, dl, ws, from, c[0], c[1], c[2]);
-        else
-            hipLaunchKernelGGL((product_kernel<T, WM, WN, S, LAST>), dim3(y.alls), dim3(P::NT), P::LDS, stream, dl, ws, from, c[0], c[1], c[2]);
-        e = hipGetLastError();
+        e = product<GRAM>(y.tiles.sym, y.syms, dl, ws, from, c, stream);
+        if (e == hipSuccess) e = product<SQUARE>(y.tiles.sym, y.syms, dl, ws, from, c, stream);
+        if (e != hipSuccess) return e;
+        e = i + 1 < how.steps ? product<NEXT>(y.tiles.all, y.alls, dl, ws, from, c, stream) : product<LAST>(y.tiles.all, y.alls, dl, ws, from, c, stream);
     }
     return e;
 }
@@ -1365,9 +1419,7 @@ hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n
         hipLaunchKernelGGL(prep_kernel, dim3(y.preps), dim3(256), 0, stream, dl, w, partial);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        if (l.tile == 256) e = products<256, 2, 4, 2>(dl, w, y, how, stream);
-        else if (l.tile == 128) e = products<128, 2, 2, 2>(dl, w, y, how, stream);
-        else e = products<64, 2, 2, 4>(dl, w, y, how, stream);
+        e = products(dl, w, y, how, stream);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
