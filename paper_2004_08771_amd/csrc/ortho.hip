@@ -648,6 +648,7 @@ __global__ __launch_bounds__(64 * WM *WN) void product_kernel(const List *lp, un
 // lane, so two blocks of a strip are its operand of 32 values of k (in an order of their own, the same for both operands); rows go through LDS.
 constexpr int SMALL_NT = 512, SMALL_WAVES = 8;
 typedef short v4s __attribute__((ext_vector_type(4)));
+typedef short v8s __attribute__((ext_vector_type(8)));
 
 struct SmallStep {
     float a, b, c;
@@ -655,7 +656,7 @@ struct SmallStep {
     int end;           // of a run
 };
 struct SmallMat : Matrix {
-    int m, n;
+    int m, n;            // (whole_g, whole_m, whole_out: the matrix begins at a 16-byte boundary, 8 for two bytes)
     int blocks, block0;  // of columns, and the first workgroup
     int sums, sum0;      // as in Mat
     size_t x;            // byte offset in the workspace: X^T, between launches
@@ -673,13 +674,21 @@ static_assert(sizeof(SmallArgs) < 4000, "arguments of a launch");
 template <int MP, int NB>
 struct Small {
     static constexpr int S = MP / 16, PARTS = SMALL_WAVES / S, KS = (MP + 31) / 32;  // strips; parts that share a strip's sums; k-steps of m
-    static constexpr int CHUNKS = MP / 8, SHIFT = MP == 128 ? 0 : MP == 64 ? 1 : MP == 32 ? 2 : 3;
+    static constexpr int CHUNKS = MP / 8;
     static constexpr int PLANE = NB * MP * 2, FILE = S * KS * 2 * 1024, RED = (PARTS - 1) * MP * MP * 4;
     static constexpr int X = 0, SHARED = 2 * PLANE;  // X^T, high and low; then rows of the m x m matrices, or sums to be added up
     static constexpr size_t LDS = 2 * (size_t)PLANE + (FILE > RED ? FILE : RED);
 
-    // byte of element (column j, row i) in a plane of X^T: the 16-byte pieces of a row are exchanged so that 16 rows lie on different banks
-    static __device__ __forceinline__ int at(int j, int i) { return j * (2 * MP) + ((((i >> 3) ^ (j >> SHIFT)) & (CHUNKS - 1)) << 4) + 2 * (i & 7); }
+    // byte of element (column j, row i) in a plane of X^T: the 16-byte pieces of a row are exchanged so that 16 rows lie on different banks, and so do the four
+    // rows of 32 bytes of a transposing read
+    static __device__ __forceinline__ int turn(int j)
+    {
+        if (MP == 128) return ((j & 7) << 1) | ((j >> 3) & 1);
+        if (MP == 64) return (j & 6) | ((j >> 3) & 1);
+        if (MP == 32) return (j >> 2) & 3;
+        return (j >> 3) & 1;
+    }
+    static __device__ __forceinline__ int at(int j, int i) { return j * (2 * MP) + (((i >> 3) ^ turn(j)) << 4) + 2 * (i & 7); }
 
     struct Strip {
         v4f v[S];  // rows 16 i + 4 g + e of column 16 strip + c
@@ -740,48 +749,140 @@ struct Small {
         }
     }
 
-    // columns j0 .. of X from G, or zeros behind its last
-    static __device__ __forceinline__ void load_g(unsigned char *lds, const How &l, const SmallMat &a, int j0, int columns, double inv)
+    // A matrix as the caller has it, lanes along its rows: f(first row, column, step to the next row, rows) for ROWS_AT_ONCE rows at a time
+    static constexpr int ROWS_AT_ONCE = 8;
+    template <typename F>
+    static __device__ __forceinline__ void rows_of(const SmallMat &a, int j0, int columns, F f)
     {
-        for (int item = threadIdx.x; item < columns * CHUNKS; item += SMALL_NT) {
-            // lanes along what is next to each other in G
-            const int j = a.flip ? item / CHUNKS : item % columns, i = 8 * (a.flip ? item % CHUNKS : item / columns);
-            v8h hi, lo;
-            float v[8];
-            if (a.flip) {
-                const int r = j0 + j;
+        const int rows = a.flip ? min(columns, a.rows - j0) : a.rows, cols = a.flip ? a.cols : min(columns, a.cols - j0);
+        int shift = 9;  // of the lanes of a row
+        while (shift > 0 && (1 << (shift - 1)) >= cols) --shift;
+        const int step = SMALL_NT >> shift;
+#pragma unroll 1
+        for (int c = threadIdx.x & ((1 << shift) - 1); c < cols; c += 1 << shift)
+#pragma unroll 1
+            for (int r = threadIdx.x >> shift; r < rows; r += ROWS_AT_ONCE * step) f(r, c, step, rows);
+    }
+    // Rows without gaps between them, four elements at a time from a 16-byte boundary (8 for two bytes): f(first element, how many) for all of a thread's
+    static constexpr int FLAT = NB * MP / (4 * SMALL_NT);
+    static __device__ __forceinline__ int elements(const SmallMat &a, int j0, int columns) { return a.flip ? min(columns, a.rows - j0) * a.cols : a.rows * a.cols; }
+    static __device__ __forceinline__ bool flat(const SmallMat &a, long long ld, bool whole)
+    {
+        return ld == a.cols && whole && (a.flip || a.blocks == 1);  // (a block is then a run of rows that begins at a multiple of NB of them)
+    }
+    // the places in LDS of elements first .. first + 3
+    struct Places {
+        int r, c, cols;
+        bool flip;
+        __device__ __forceinline__ Places(const SmallMat &a, int first) : cols(a.cols), flip(a.flip)
+        {
+            r = (int)(((float)first + 0.5f) * __builtin_amdgcn_rcpf((float)cols));  // first < 2^16: off by less than 1 / (2 cols)
+            c = first - r * cols;
+        }
+        __device__ __forceinline__ int next()
+        {
+            const int p = flip ? at(r, c) : at(c, r);
+            if (++c == cols) {
+                c = 0;
+                ++r;
+            }
+            return p;
+        }
+    };
+    static __device__ __forceinline__ void keep(unsigned char *lds, int p, float x)
+    {
+        *reinterpret_cast<unsigned short *>(lds + p) = (unsigned short)(__float_as_uint(x) >> 16);
+        *reinterpret_cast<unsigned short *>(lds + PLANE + p) = (unsigned short)__float_as_uint(x);
+    }
+    static __device__ __forceinline__ float kept(const unsigned char *lds, int p)
+    {
+        return __uint_as_float((unsigned)*reinterpret_cast<const unsigned short *>(lds + p) << 16 | *reinterpret_cast<const unsigned short *>(lds + PLANE + p));
+    }
+    // Columns j0 .. of X as they are, a float in the two halves of an element's places in LDS, and this thread's part of the sum of their squares.
+    // with_momentum: M gets its new value on the way (else it has it)
+    static __device__ __forceinline__ double load_g(unsigned char *lds, const How &l, const SmallMat &a, int j0, int columns, bool with_momentum)
+    {
+        double sum = 0.0;
+        const bool bf16 = l.g_tensor == TENSOR_BF16;
+        const long long first_g = a.flip ? j0 * a.ldg : j0, first_m = a.flip ? j0 * a.ldm : j0;
+        if (flat(a, a.ldg, a.whole_g) && (!l.muon || flat(a, a.ldm, a.whole_m))) {
+            const int n = elements(a, j0, columns);
+            v4f x[FLAT];
 #pragma unroll
-                for (int h = 0; h < 8; h += 4) {
-                    const int left = r < a.rows ? a.cols - i - h : 0;
-                    const v4f x = load_four(a.g, (long long)r * a.ldg + i + h, l.g_tensor, left, a.whole_g);
-                    v4f y = {0.f, 0.f, 0.f, 0.f};
-                    if (l.muon) y = load_four(a.mom, (long long)r * a.ldm + i + h, TENSOR_F32, left, a.whole_m);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[h + e] = e < left ? (float)((double)updated(l, x[e], y[e]) * inv) : 0.f;
-                }
-            } else {
-                float y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] = y[e] = 0.f;
-                    if (i + e < a.rows && j0 + j < a.cols) {
-                        const long long at_g = (long long)(i + e) * a.ldg + j0 + j;
-                        v[e] = l.g_tensor == TENSOR_BF16 ? (float)static_cast<const __bf16 *>(a.g)[at_g] : static_cast<const float *>(a.g)[at_g];
-                        if (l.muon) y[e] = a.mom[(long long)(i + e) * a.ldm + j0 + j];
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = i + e < a.rows && j0 + j < a.cols ? (float)((double)updated(l, v[e], y[e]) * inv) : 0.f;
+            for (int u = 0; u < FLAT; ++u) {  // all of them are asked for before one is waited for
+                const int q = 4 * (threadIdx.x + u * SMALL_NT);
+                if (4 * u * SMALL_NT < n) x[u] = load_four(a.g, first_g + q, l.g_tensor, n - q, true);
             }
 #pragma unroll
+            for (int u = 0; u < FLAT; ++u) {
+                const int q = 4 * (threadIdx.x + u * SMALL_NT);
+                if (4 * u * SMALL_NT >= n) continue;
+                if (l.muon) {
+                    v4f y = load_four(a.mom, first_m + q, TENSOR_F32, n - q, true);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (with_momentum) y[e] = __builtin_fmaf(l.momentum, y[e], x[u][e]);
+                        x[u][e] = updated(l, x[u][e], y[e]);
+                    }
+                    if (with_momentum) store_four(a.mom + first_m + q, y, n - q, true);
+                }
+                Places at_x(a, q);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sum += (double)x[u][e] * (double)x[u][e];
+                    const int p = at_x.next();
+                    if (q + e < n) keep(lds, p, x[u][e]);
+                }
+            }
+            return sum;
+        }
+        rows_of(a, j0, columns, [&](int r, int c, int step, int rows) {
+            constexpr int U = ROWS_AT_ONCE;
+            float x[U], y[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long long q = first_g + min(r + u * step, rows - 1) * a.ldg + c;
+                x[u] = bf16 ? (float)static_cast<const __bf16 *>(a.g)[q] : static_cast<const float *>(a.g)[q];
+            }
+            if (l.muon) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) y[u] = a.mom[first_m + min(r + u * step, rows - 1) * a.ldm + c];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (r + u * step >= rows) continue;
+                if (l.muon) {
+                    if (with_momentum) {
+                        y[u] = __builtin_fmaf(l.momentum, y[u], x[u]);
+                        a.mom[first_m + (r + u * step) * a.ldm + c] = y[u];
+                    }
+                    x[u] = updated(l, x[u], y[u]);
+                }
+                sum += (double)x[u] * (double)x[u];
+                keep(lds, a.flip ? at(r + u * step, c) : at(c, r + u * step), x[u]);
+            }
+        });
+        return sum;
+    }
+    // ... and as X, with zeros behind its rows and columns
+    static __device__ __forceinline__ void scale_g(unsigned char *lds, const SmallMat &a, int j0, int columns, double inv)
+    {
+        const int n = (a.flip ? a.rows : a.cols) - j0, m = a.flip ? a.cols : a.rows;
+#pragma unroll 1
+        for (int item = threadIdx.x; item < columns * CHUNKS; item += SMALL_NT) {
+            const int j = item / CHUNKS, i = 8 * (item % CHUNKS), p = at(j, i);
+            const v8s up = *reinterpret_cast<const v8s *>(lds + p), down = *reinterpret_cast<const v8s *>(lds + PLANE + p);
+            v8h hi, lo;
+#pragma unroll
             for (int e = 0; e < 8; ++e) {
+                const float x = __uint_as_float((unsigned)(unsigned short)up[e] << 16 | (unsigned short)down[e]);
                 half_t u, w;
-                split(v[e], u, w);
+                split(j < n && i + e < m ? (float)((double)x * inv) : 0.f, u, w);  // (inv may be inf)
                 hi[e] = u;
                 lo[e] = w;
             }
-            *reinterpret_cast<v8h *>(lds + at(j, i)) = hi;
-            *reinterpret_cast<v8h *>(lds + PLANE + at(j, i)) = lo;
+            *reinterpret_cast<v8h *>(lds + p) = hi;
+            *reinterpret_cast<v8h *>(lds + PLANE + p) = lo;
         }
     }
 
@@ -833,14 +934,14 @@ struct Small {
     }
 
     // A run of steps from step k: A (in `m` of the first wavefronts) to the rows of Q in LDS; returns the step behind it
-    static __device__ __forceinline__ int run(const SmallArgs &l, unsigned char *file, Strip &m, int k, int strip, int part, int lane)
+    static __device__ __forceinline__ int run(const SmallStep *steps, unsigned char *file, Strip &m, int k, int strip, int part, int lane)
     {
         Strip q, p;
         Frag f;
         const bool mine = part == 0;
         for (;; ++k) {
-            const SmallStep &s = l.step[k];
-            const bool first = k == 0 || l.step[k - 1].end != 0;
+            const SmallStep s = steps[k];
+            const bool first = k == 0 || steps[k - 1].end != 0, end = __builtin_amdgcn_readfirstlane(s.end) != 0;
             if (mine) {
                 put_rows(file, m, s.sa, strip, lane);
                 frag_of(m, s.sa, f);
@@ -863,12 +964,12 @@ struct Small {
                 if (first) {
                     q = p;
                 } else {
-                    const float before = l.step[k - 1].sq;
+                    const float before = steps[k - 1].sq;
                     frag_of(q, before, f);
                     times(file, f, 1.f / (s.sp * before), q, lane);
                 }
-                if (!s.end) {
-                    const float next = l.step[k + 1].sa;
+                if (!end) {
+                    const float next = steps[k + 1].sa;
                     frag_of(m, s.sa, f);
                     times(file, f, 1.f / (s.sp * s.sa), p, lane);  // P A
                     frag_of(p, next, f);
@@ -876,7 +977,7 @@ struct Small {
                 }
             }
             __syncthreads();
-            if (s.end) {
+            if (end) {
                 if (mine) put_rows(file, q, s.sq, strip, lane);
                 __syncthreads();
                 return k + 1;
@@ -884,9 +985,8 @@ struct Small {
         }
     }
 
-    // Q X for the block's columns: in its place, or to the result
-    static __device__ __forceinline__ void apply(unsigned char *lds, const How &l, const SmallMat &a, int j0, int columns, float inv_sq, bool last,
-                                                 int wave, int lane)
+    // Q X for the block's columns, in its place
+    static __device__ __forceinline__ void apply(unsigned char *lds, int columns, float inv_sq, bool last, int wave, int lane)
     {
         const unsigned char *const file = lds + SHARED;
         const int g4 = lane >> 4, c16 = lane & 15;
@@ -911,40 +1011,89 @@ struct Small {
                 }
             Strip x;
             times(file, f, inv_sq, x, lane);
-            if (!last) {
 #pragma unroll
-                for (int i = 0; i < S; ++i) {
-                    v4h hi, lo;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        half_t u, w;
-                        split(x.v[i][e], u, w);
-                        hi[e] = u;
-                        lo[e] = w;
-                    }
-                    *reinterpret_cast<v4h *>(lds + at(j, 16 * i + 4 * g4)) = hi;
-                    *reinterpret_cast<v4h *>(lds + PLANE + at(j, 16 * i + 4 * g4)) = lo;
-                }
-                continue;
-            }
-#pragma unroll
-            for (int i = 0; i < S; ++i)
+            for (int i = 0; i < S; ++i) {
+                v4s hi, lo;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int row = 16 * i + 4 * g4 + e, r = a.flip ? j0 + j : row, c = a.flip ? row : j0 + j;
-                    if (r >= a.rows || c >= a.cols) continue;
-                    const long long at_o = (long long)r * a.ldo + c;
-                    const float o = x.v[i][e] * (1.f / SX);
-                    if (l.muon) {
-                        float *const w = static_cast<float *>(a.out) + at_o;
-                        *w = __builtin_fmaf(-a.scale, o, __builtin_fmaf(-l.decay, *w, *w));
-                    } else if (l.out_tensor == TENSOR_BF16) {
-                        static_cast<__bf16 *>(a.out)[at_o] = (__bf16)o;
+                    if (last) {  // the two halves of a float
+                        const unsigned bits = __float_as_uint(x.v[i][e] * (1.f / SX));
+                        hi[e] = (short)(bits >> 16);
+                        lo[e] = (short)(bits & 0xffffu);
                     } else {
-                        static_cast<float *>(a.out)[at_o] = o;
+                        half_t u, w;
+                        split(x.v[i][e], u, w);
+                        hi[e] = __builtin_bit_cast(short, u);
+                        lo[e] = __builtin_bit_cast(short, w);
                     }
                 }
+                *reinterpret_cast<v4s *>(lds + at(j, 16 * i + 4 * g4)) = hi;
+                *reinterpret_cast<v4s *>(lds + PLANE + at(j, 16 * i + 4 * g4)) = lo;
+            }
         }
+    }
+
+    // the result from there
+    static __device__ __forceinline__ void put_out(const unsigned char *lds, const How &l, const SmallMat &a, int j0, int columns)
+    {
+        const long long first = a.flip ? j0 * a.ldo : j0;
+        const bool bf16 = l.out_tensor == TENSOR_BF16;
+        if (flat(a, a.ldo, a.whole_out)) {
+            const int n = elements(a, j0, columns);
+            v4f w[FLAT];
+            if (l.muon) {
+#pragma unroll
+                for (int u = 0; u < FLAT; ++u) {
+                    const int q = 4 * (threadIdx.x + u * SMALL_NT);
+                    if (4 * u * SMALL_NT < n) w[u] = load_four(a.out, first + q, TENSOR_F32, n - q, true);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < FLAT; ++u) {
+                const int q = 4 * (threadIdx.x + u * SMALL_NT);
+                if (q >= n) continue;
+                Places at_x(a, q);
+                v4f o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int p = at_x.next();
+                    o[e] = q + e < n ? kept(lds, p) : 0.f;
+                    if (l.muon) o[e] = __builtin_fmaf(-a.scale, o[e], __builtin_fmaf(-l.decay, w[u][e], w[u][e]));
+                }
+                if (bf16) {
+                    __bf16 *const to = static_cast<__bf16 *>(a.out) + first + q;
+                    if (q + 4 <= n) {
+                        v4b b;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) b[e] = (__bf16)o[e];
+                        *reinterpret_cast<v4b *>(to) = b;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 3; ++e)
+                            if (q + e < n) to[e] = (__bf16)o[e];
+                    }
+                } else {
+                    store_four(static_cast<float *>(a.out) + first + q, o, n - q, true);
+                }
+            }
+            return;
+        }
+        rows_of(a, j0, columns, [&](int r, int c, int step, int rows) {
+            constexpr int U = ROWS_AT_ONCE;
+            float w[U];
+            if (l.muon) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) w[u] = static_cast<const float *>(a.out)[first + min(r + u * step, rows - 1) * a.ldo + c];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (r + u * step >= rows) continue;
+                const float o = kept(lds, a.flip ? at(r + u * step, c) : at(c, r + u * step));
+                const long long q = first + (r + u * step) * a.ldo + c;
+                if (bf16) static_cast<__bf16 *>(a.out)[q] = (__bf16)o;
+                else static_cast<float *>(a.out)[q] = l.muon ? __builtin_fmaf(-a.scale, o, __builtin_fmaf(-l.decay, w[u], w[u])) : o;
+            }
+        });
     }
 };
 
@@ -958,30 +1107,89 @@ __device__ __forceinline__ int find_small(const SmallArgs &l, int block, F first
     return k;
 }
 
+// The arguments of a launch are in the host's memory, and every line of them that is read is a trip there of more than a microsecond: what is needed of them comes
+// at once, in front of everything else, and is not read again where it is used
+template <typename T>
+__device__ __forceinline__ void here(T &x)
+{
+    asm volatile("" : "+s"(x));
+}
+__device__ __forceinline__ void args_here(How &l, SmallMat &a)
+{
+    int flip = a.flip, muon = l.muon, nesterov = l.nesterov;
+    here(flip);
+    here(muon);
+    here(nesterov);
+    here(a.rows);
+    here(a.cols);
+    here(a.scale);
+    here(a.g);
+    here(a.out);
+    here(a.mom);
+    here(a.ldg);
+    here(a.ldo);
+    here(a.ldm);
+    here(a.n);
+    here(l.g_tensor);
+    here(l.out_tensor);
+    here(l.momentum);
+    here(l.eps);
+    here(l.decay);
+    a.flip = flip != 0;
+    l.muon = muon != 0;
+    l.nesterov = nesterov != 0;
+}
+__device__ __forceinline__ void copy_steps(const SmallArgs &l, SmallStep *steps)
+{
+    const unsigned *const from = reinterpret_cast<const unsigned *>(l.step);
+    for (unsigned i = threadIdx.x; i < sizeof(l.step) / 4; i += SMALL_NT) reinterpret_cast<unsigned *>(steps)[i] = from[i];
+}
+
+// over a workgroup, in a fixed order
+__device__ __forceinline__ double sum_of_all(double s, double *red, int lane, int wave)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (lane == 0) red[wave] = s;
+    __syncthreads();
+    s = red[0];
+#pragma unroll
+    for (int i = 1; i < SMALL_WAVES; ++i) s += red[i];
+    __syncthreads();
+    return s;
+}
+
 // A matrix a workgroup, everything in one launch
 template <int MP, int NB>
 __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallArgs l)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    __shared__ SmallStep steps[ORTHO_STEPS];
+    __shared__ double red[SMALL_WAVES];
     typedef Small<MP, NB> M;
-    const SmallMat &a = l.mat[blockIdx.x];
+    copy_steps(l, steps);
+    SmallMat a = l.mat[blockIdx.x];
+    How how = l;
+    int count = l.steps;
+    args_here(how, a);
+    here(count);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), strip = wave % M::S, part = wave / M::S;
-    const double sum = sum_of_block<SMALL_NT>(l, a, 0, 1, reinterpret_cast<double *>(lds));
-    __syncthreads();  // the momenta are there, and the sums have been read
     const int columns = (a.n + 31) / 32 * 32;
-    M::load_g(lds, l, a, 0, columns, factor_of(sum, l.eps));
+    const double sum = sum_of_all(M::load_g(lds, how, a, 0, columns, true), red, lane, wave);
+    M::scale_g(lds, a, 0, columns, factor_of(sum, how.eps));
     __syncthreads();
     typename M::Strip m;
 #pragma unroll 1
-    for (int k = 0; k < l.steps;) {
+    for (int k = 0; k < count;) {
         M::gram(lds, columns, m, strip, part, lane);
         M::add_parts(lds + M::SHARED, m, strip, part, lane);
 #pragma unroll
         for (int i = 0; i < M::S; ++i) m.v[i] *= 1.f / (SX * SX);
-        k = M::run(l, lds + M::SHARED, m, k, strip, part, lane);
-        M::apply(lds, l, a, 0, columns, 1.f / l.step[k - 1].sq, k == l.steps, wave, lane);
+        k = M::run(steps, lds + M::SHARED, m, k, strip, part, lane);
+        M::apply(lds, columns, 1.f / steps[k - 1].sq, k == count, wave, lane);
         __syncthreads();
     }
+    M::put_out(lds, how, a, 0, columns);
 }
 
 __global__ __launch_bounds__(SUM_NT) void small_sum_kernel(SmallArgs l, double *partial)
@@ -998,24 +1206,21 @@ template <int MP, int NB>
 __global__ __launch_bounds__(SMALL_NT) void small_part_kernel(SmallArgs l, unsigned char *ws, const double *partial, int from, int turn)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    __shared__ SmallStep steps[ORTHO_STEPS];
+    __shared__ double red[SMALL_WAVES];
     typedef Small<MP, NB> M;
     const SmallMat &a = l.mat[find_small(l, blockIdx.x, [](const SmallMat &x) { return x.block0; })];
+    copy_steps(l, steps);
     const int block = blockIdx.x - a.block0, j0 = block * NB, columns = (min(a.n - j0, NB) + 31) / 32 * 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), strip = wave % M::S, part = wave / M::S;
+    __syncthreads();
     half_t *const kept = reinterpret_cast<half_t *>(ws + a.x) + (size_t)block * NB * MP * 2;  // the planes as they are in LDS
     if (from <= 0) {
-        double *const red = reinterpret_cast<double *>(lds);
+        M::load_g(lds, l, a, j0, columns, false);
         double s = 0.0;
         for (int i = threadIdx.x; i < a.sums; i += SMALL_NT) s += partial[a.sum0 + i];
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-        if (lane == 0) red[wave] = s;
-        __syncthreads();
-        s = red[0];
-#pragma unroll
-        for (int i = 1; i < SMALL_WAVES; ++i) s += red[i];
-        __syncthreads();
-        M::load_g(lds, l, a, j0, columns, factor_of(s, l.eps));
+        s = sum_of_all(s, red, lane, wave);
+        M::scale_g(lds, a, j0, columns, factor_of(s, l.eps));
     } else {
         const int n = columns * (2 * MP) / 16;
         for (int plane = 0; plane < 2; ++plane)
@@ -1035,9 +1240,13 @@ __global__ __launch_bounds__(SMALL_NT) void small_part_kernel(SmallArgs l, unsig
         M::add_parts(lds + M::SHARED, m, strip, part, lane);
 #pragma unroll
         for (int i = 0; i < M::S; ++i) m.v[i] *= 1.f / (SX * SX);
-        k = M::run(l, lds + M::SHARED, m, from, strip, part, lane);
-        M::apply(lds, l, a, j0, columns, 1.f / l.step[k - 1].sq, k == l.steps, wave, lane);
-        if (k == l.steps) return;
+        k = M::run(steps, lds + M::SHARED, m, from, strip, part, lane);
+        M::apply(lds, columns, 1.f / steps[k - 1].sq, k == l.steps, wave, lane);
+        if (k == l.steps) {
+            __syncthreads();
+            M::put_out(lds, l, a, j0, columns);
+            return;
+        }
     } else {
         k = 0;
     }
@@ -1392,7 +1601,14 @@ hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n
         for (int k0 = 0; k0 < n; k0 += ORTHO_GROUP) {
             const int count = n - k0 < ORTHO_GROUP ? n - k0 : ORTHO_GROUP;
             const SmallLayout y = lay_out_small(small, shapes + k0, count, rows);
-            for (int k = 0; k < count; ++k) describe(small.mat[k], list[k0 + k], shapes[k0 + k], how);
+            for (int k = 0; k < count; ++k) {
+                SmallMat &a = small.mat[k];
+                const OrthoMatrix &o = list[k0 + k];
+                describe(a, o, shapes[k0 + k], how);
+                a.whole_g = reinterpret_cast<uintptr_t>(o.g) % (how.g_tensor == TENSOR_BF16 ? 8 : 16) == 0;
+                a.whole_m = reinterpret_cast<uintptr_t>(o.momentum) % 16 == 0;
+                a.whole_out = reinterpret_cast<uintptr_t>(o.out) % (how.out_tensor == TENSOR_BF16 && !how.muon ? 8 : 16) == 0;
+            }
             unsigned char *const w = static_cast<unsigned char *>(ws);
             const hipError_t e = rows == 16   ? small_launches<16, 1024>(small, y, w, stream)
                                  : rows == 32 ? small_launches<32, 1024>(small, y, w, stream)
