@@ -216,11 +216,28 @@ int hb_batch_loss_csr_async(hb_model *m, const int32_t *d_row_ptr, const int32_t
 int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call);
 
 /*
+ * Orthogonalised updates: every later step of this handle (any loss; also those of the worker loops) updates the weights of layers
+ * first_layer .. last_layer (1 .. L) as hb_muon_async below does, with the step's lr, the batch gradient as G and the factor scale
+ * sqrt(max(d_l, d_(l-1))); the weights of other layers and all biases get W <- W - lr G as before, without decay.  how->lr is not
+ * looked at; how->ortho.coef is copied.  how NULL: off.  Each call sets the momenta to zero.  Gradients, losses and
+ * merges are what they were (a merge changes the replica only, the momenta stay).  The first call allocates 2 P floats and the
+ * workspace (the handle's device has to be current); steps enqueue kernels only and may be captured.  Networks then run layer by layer
+ * with the gradient in memory between the backward pass and the update.  HB_ERR_UNSUPPORTED for a sparse first layer.
+ *   hb_model_get_momenta, hb_model_set_momenta   the momenta in the flat layout (HOST pointers, P floats; biases and other layers have none
+ *                                                 and keep what is set), for checkpoints; synchronise the stream.  HB_ERR_STATE before hb_model_set_muon
+ */
+struct hb_muon;
+int hb_model_set_muon(hb_model *m, const struct hb_muon *how, int32_t first_layer, int32_t last_layer, float scale);
+int hb_model_get_momenta(hb_model *m, float *host_flat);
+int hb_model_set_momenta(hb_model *m, const float *host_flat);
+
+/*
  * Learning from rewards and comparisons instead of labels: the network is a policy over d_L classes, X the states of B rows
  * and y the class chosen in each (outside [0, d_L): no choice, padding).  The losses, their arguments (DEVICE pointers)
  * and what they return are those of hb_logprob_async, hb_policy_loss_async and hb_preference_loss_async below, on the last
  * layer's logits; rows outside of all sequences have no gradient.  Dense models with HB_LOSS_SOFTMAX_CE; pairs <= max_B.
  *   hb_batch_logprob_async    forward pass; the log-probabilities of the chosen classes (d_lse may be NULL)
+ *   hb_batch_scores_async     forward pass; the scores of hb_scores_async below on the last layer's logits (dy may be NULL without d_logp)
  *   hb_policy_step_async      one step W <- W - lr dloss/dW of the policy loss
  *   hb_policy_grad_async      its gradient instead (d_grad_flat: P floats, flat layout); the replica is left untouched
  *   hb_preference_step_async, hb_preference_grad_async   the same of the preference loss
@@ -231,6 +248,8 @@ int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call
 struct hb_policy;
 struct hb_preference;
 int hb_batch_logprob_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, float *d_logp, float *d_lse);
+int hb_batch_scores_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, int32_t top, float *d_logp, float *d_lse,
+                          float *d_entropy, int32_t *d_top_class, float *d_top_logp);
 int hb_policy_step_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, float lr, const struct hb_policy *policy,
                          float *d_stats, float *d_logp);
 int hb_policy_grad_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, const struct hb_policy *policy,
@@ -268,13 +287,14 @@ enum {
     HB_K_FWD_GEMM = 0,   /* Z_l = A_{l-1} W_l^T + b_l, activation          (Eq. (1)) */
     HB_K_DA_GEMM = 1,    /* delta_{l-1} = (delta_l W_l) * f'                (Eq. (2)) */
     HB_K_DW_GEMM = 2,    /* dW_l = delta_l^T A_{l-1}, db_l (split-K partials) (Eq. (2)) */
-    HB_K_LOSS = 3,       /* loss and output delta                           (Section 7.1); policy and preference losses and log-
-                            probabilities: `layer` 0 the pass over the logits, 1 sums over rows and pairs, 2 a second pass
+    HB_K_LOSS = 3,       /* loss and output delta                           (Section 7.1); policy and preference losses, log-
+                            probabilities and scores: `layer` 0 the pass over the logits, 1 sums over rows and pairs, 2 a second pass
                             over the logits for the gradient */
     HB_K_UPDATE = 4,     /* W <- W - lr * sum of partials, all tensors      (Eq. (3)) */
     HB_K_SPMM_FWD = 5,   /* CSR first layer, forward */
     HB_K_SPARSE_DW = 6,  /* CSR first layer, gradient + update of the touched columns */
-    HB_K_OTHER = 7,      /* helpers, numbered in `layer`; 6: a network that fits a workgroup, whole (M = rows); 7: dropout */
+    HB_K_OTHER = 7,      /* helpers, numbered in `layer`; 6: a network that fits a workgroup, whole (M = rows); 7: dropout; of
+                            orthogonalised updates 8: norms and layouts (small matrices: everything), 9: products */
     HB_K_OUT_LAYER = 8,  /* narrow output layer: forward + loss + delta + its gradients, fused */
     HB_K_BWD_PAIR = 9    /* two backward products in one launch, flops / bytes cover both.  fp32: backward-data and
                             weight gradient of `layer`, M, N, K those of the backward-data product.  bf16: the

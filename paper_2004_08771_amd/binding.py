@@ -133,6 +133,10 @@ class MuonMatrix(ctypes.Structure):
                 ("scale", _f32)]
 
 
+SIGNATURES["hb_model_set_muon"] = (_int, [_vp, ctypes.POINTER(Muon), _i32, _i32, _f32])
+SIGNATURES["hb_model_get_momenta"] = (_int, [_vp, _vp])
+SIGNATURES["hb_model_set_momenta"] = (_int, [_vp, _vp])
+SIGNATURES["hb_batch_scores_async"] = (_int, [_vp, _vp, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _vp])
 SIGNATURES["hb_scores_workspace_bytes"] = (_sz, [_i64, _i32, _i32])
 SIGNATURES["hb_scores_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp])
 SIGNATURES["hb_scores_grad_async"] = (_int, [_vp, _i64, _int, _vp, _i64, _i32, _vp, _vp, _vp, _i64, _vp, _sz, _vp])
@@ -276,6 +280,23 @@ class Model:
 
     def batch_logprob_async(self, dX, dy, B, d_logp, d_lse=None):
         _check(lib().hb_batch_logprob_async(self._h, _ptr(dX), _ptr(dy), int(B), _ptr(d_logp), _ptr(d_lse)))
+
+    def set_muon(self, how, first_layer=1, last_layer=None, scale=0.2):
+        """how: muon_args() (its lr is not looked at: the steps have it), or None to switch it off."""
+        _check(lib().hb_model_set_muon(self._h, None if how is None else ctypes.byref(how), int(first_layer),
+                                       len(self.layer_dims) - 1 if last_layer is None else int(last_layer), float(scale)))
+
+    def get_momenta(self, host_flat):
+        _check(lib().hb_model_get_momenta(self._h, _ptr(host_flat)))
+
+    def set_momenta(self, host_flat):
+        _check(lib().hb_model_set_momenta(self._h, _ptr(host_flat)))
+
+    def batch_scores_async(self, dX, dy, B, d_logp=None, d_lse=None, d_entropy=None, d_top_class=None, d_top_logp=None):
+        """As many alternatives as d_top_class (B x top int32) has columns."""
+        top = 0 if d_top_class is None else int(d_top_class.shape[1])
+        _check(lib().hb_batch_scores_async(self._h, _ptr(dX), _ptr(dy), int(B), top, _ptr(d_logp), _ptr(d_lse), _ptr(d_entropy),
+                                           _ptr(d_top_class), _ptr(d_top_logp)))
 
     def policy_step_async(self, dX, dy, B, lr, policy, d_stats, d_logp=None):
         """policy: policy_args()."""
@@ -665,7 +686,7 @@ def orthogonalize(G, out, steps=5, coef=ORTHO_COEF, eps=1e-7, products=None, ws=
     _check((_lib or lib()).hb_orthogonalize_async(mats, len(a), g_kind, o_kind, ctypes.byref(how), pw, nw, _stream(stream, ws)))
 
 
-def muon_args(lr, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5, coef=ORTHO_COEF, eps=1e-7, products=HB_TENSOR_F32) -> Muon:
+def muon_args(lr=0.0, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5, coef=ORTHO_COEF, eps=1e-7, products=HB_TENSOR_F32) -> Muon:
     """hb_muon."""
     return Muon(ortho_args(steps, coef, eps, products), lr, momentum, weight_decay, int(bool(nesterov)))
 

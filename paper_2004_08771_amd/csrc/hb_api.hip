@@ -169,6 +169,15 @@ struct hb_model {
     uint64_t drop_seed = 0, drop_call = 0;
     std::vector<void *> drop;            // [1..L-1] max_B x ld (fp32) or ld8 (bf16), allocated by the first hb_model_set_dropout
     std::vector<int> gemm_splits;        // [1..L] fp32: slices that the general weight gradient may use
+    // orthogonalised updates of the weights of layers muon_first .. muon_last (0: none) in steps; the first call allocates
+    int muon_first = 0, muon_last = 0;
+    hb_muon muon = {};
+    std::vector<float> muon_coef;
+    float muon_scale = 0.f;
+    float *d_muon_grad = nullptr, *d_momenta = nullptr;  // flat
+    void *muon_ws = nullptr;
+    size_t muon_ws_bytes = 0;
+    void *scores_ws = nullptr;           // workspace of the scores, allocated by the first call
     void *head_ws = nullptr;             // workspace of the policy and preference losses, allocated by the first call
     std::vector<void *> owned;           // every device allocation, for destroy
 
@@ -226,6 +235,10 @@ void release_device(hb_model *m)
     m->d_net_place = nullptr;
     m->drop.clear();
     m->head_ws = nullptr;
+    m->scores_ws = nullptr;
+    m->d_muon_grad = m->d_momenta = nullptr;
+    m->muon_ws = nullptr;
+    m->muon_first = m->muon_last = 0;
     if (m->h_loss) (void)hipHostFree(m->h_loss);
     m->h_loss = nullptr;
 }
@@ -276,11 +289,13 @@ struct Input {
     int64_t nnz = 0;
 };
 
-// A call whose loss is not the handle's own: one of the three
+// A call whose loss is not the handle's own: one of the four
 struct Head {
     const PolicyTerms *policy = nullptr;
     const PreferenceTerms *preference = nullptr;
     float *logp = nullptr, *lse = nullptr;  // log-probabilities only
+    const ScoreOut *scores = nullptr;
+    int top = 0;                            // of the scores
     const float *weight = nullptr;          // of the policy's rows
 };
 
@@ -307,6 +322,7 @@ int run_head(hb_model *m, const Head &head, const int32_t *y, int64_t B, void *d
                           }};
     if (head.policy) HB_HIP(launch_policy(r, *head.policy, d, m->head_ws, m->stream, ev));
     else if (head.preference) HB_HIP(launch_preference(r, *head.preference, d, m->head_ws, m->stream, ev));
+    else if (head.scores) HB_HIP(launch_scores(r, *head.scores, head.top, m->scores_ws, m->stream, ev));
     else HB_HIP(launch_logprob(r, head.logp, head.lse, m->head_ws, m->stream, ev));
     return HB_OK;
 }
@@ -433,9 +449,67 @@ int run_small_net(hb_model *m, const float *X, const int32_t *y, int64_t B, int 
 }
 
 // Issues the kernels of one step.
+int refresh_shadows(hb_model *m);
+
+// The update of a step from the gradient in d_muon_grad: orthogonalised for the layers that are to have it, plain SGD for the others and the biases
+int muon_update(hb_model *m, float lr)
+{
+    std::vector<OrthoMatrix> list;
+    std::vector<OrthoShape> shapes;
+    std::vector<UpdateArgs> plain;
+    try {
+        list.resize((size_t)(m->muon_last - m->muon_first + 1));
+        shapes.resize(list.size());
+        plain.resize((size_t)(2 * m->L + HB_MAX_SEGS - 1) / HB_MAX_SEGS);
+    } catch (const std::bad_alloc &) {
+        return fail(HB_ERR_ALLOC, "out of host memory");
+    }
+    int n = 0;
+    auto add = [&](int64_t off, long long count) {
+        UpdateArgs &ua = plain[(size_t)n / HB_MAX_SEGS];
+        UpdateSeg &s = ua.seg[n % HB_MAX_SEGS];
+        s.param = m->d_params + off;
+        s.partial = m->d_muon_grad + off;
+        s.count = s.stride = count;
+        s.splits = 1;
+        ua.lr = lr;
+        ua.n_seg = n % HB_MAX_SEGS + 1;
+        ++n;
+    };
+    for (int l = 1; l <= m->L; ++l) {
+        const int64_t w = m->w_off[l];
+        if (l < m->muon_first || l > m->muon_last) {
+            add(w, (long long)m->dims[l] * m->dims[l - 1]);
+        } else {
+            OrthoMatrix &o = list[(size_t)(l - m->muon_first)];
+            o.g = m->d_muon_grad + w;
+            o.out = m->d_params + w;
+            o.momentum = m->d_momenta + w;
+            o.ldg = o.ldo = o.ldm = m->dims[l - 1];
+            o.scale = m->muon_scale * std::sqrt((float)std::max(m->dims[l], m->dims[l - 1]));
+            shapes[(size_t)(l - m->muon_first)] = {m->dims[l], m->dims[l - 1]};
+        }
+        add(m->b_off[l], m->dims[l]);
+    }
+    for (int k = 0; k * HB_MAX_SEGS < n; ++k)
+        HB_HIP(launch_update(plain[(size_t)k], m->stream, prof_begin(m, HB_K_UPDATE, 0, 0, 0, 0, 0.0, 0.0)));
+    OrthoSteps steps = muon_steps(&m->muon, TENSOR_F32);
+    steps.lr = lr;
+    PassEvents ev;
+    if (m->prof_on) ev = {m, [](void *who, int pass, double bytes) {
+                              return prof_begin(static_cast<hb_model *>(who), HB_K_OTHER, 8 + pass, 0, 0, 0, 0.0, bytes);
+                          }};
+    HB_HIP(launch_ortho(list.data(), shapes.data(), (int)list.size(), steps, m->muon_ws, m->stream, ev));
+    return refresh_shadows(m);
+}
+
 int run_step(hb_model *m, const Input &in, const int32_t *y, int64_t B, float lr, StepMode mode,
              float *d_grad_flat, float *d_loss_user, const Head *head = nullptr)
 {
+    if (mode == MODE_STEP && m->muon_first > 0) {
+        const int rc = run_step(m, in, y, B, 0.f, MODE_GRAD, m->d_muon_grad, d_loss_user, head);
+        return rc != HB_OK ? rc : muon_update(m, lr);
+    }
     const int L = m->L;
     const int Bi = (int)B;
     hipStream_t st = m->stream;
@@ -775,6 +849,10 @@ int refresh_shadows(hb_model *m)
 int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float lr, StepMode mode,
                   float *d_grad_flat, float *d_loss_user, const Head *head = nullptr)
 {
+    if (mode == MODE_STEP && m->muon_first > 0) {
+        const int rc = run_step_bf16(m, X, y, B, 0.f, MODE_GRAD, m->d_muon_grad, d_loss_user, head);
+        return rc != HB_OK ? rc : muon_update(m, lr);
+    }
     const int L = m->L;
     const int Bi = (int)B;
     const long long ldB = round_up(Bi, 8);
@@ -1854,10 +1932,90 @@ int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call
     return HB_OK;
 }
 
-// What the calls with a loss of their own check, before their first device call but for the workspace of the handle's first one
-static int validate_head_call(hb_model *m, const void *dX, const int32_t *dy, int64_t B)
+int hb_model_set_muon(hb_model *m, const hb_muon *how, int32_t first_layer, int32_t last_layer, float scale)
 {
-    int rc = validate_batch_call(m, dX, dy, B, false, false);
+    int rc = check_handle(m, true);
+    if (rc != HB_OK) return rc;
+    if (!how) {
+        m->muon_first = m->muon_last = 0;
+        return HB_OK;
+    }
+    hb_muon h = *how;
+    h.lr = 0.f;  // the steps have it
+    rc = check_muon(&h);
+    if (rc != HB_OK) return rc;
+    if (m->sparse) return fail(HB_ERR_UNSUPPORTED, "orthogonalised updates need a dense model");
+    if (first_layer < 1 || last_layer > m->L || first_layer > last_layer)
+        return fail(HB_ERR_INVALID, "layers %d .. %d are not within 1 .. %d", first_layer, last_layer, m->L);
+    if (!std::isfinite(scale)) return fail(HB_ERR_INVALID, "scale is not finite");
+    for (int l = first_layer; l <= last_layer; ++l) {
+        rc = check_ortho_shape(m->dims[l], m->dims[l - 1], l);
+        if (rc != HB_OK) return rc;
+    }
+    rc = check_current_device(m);
+    if (rc != HB_OK) return rc;
+    std::vector<float> coef;
+    std::vector<OrthoShape> shapes;
+    try {
+        if (h.ortho.coef) coef.assign(h.ortho.coef, h.ortho.coef + 3 * h.ortho.n_coef);
+        for (int l = first_layer; l <= last_layer; ++l) shapes.push_back({m->dims[l], m->dims[l - 1]});
+    } catch (const std::bad_alloc &) {
+        return fail(HB_ERR_ALLOC, "out of host memory");
+    }
+    if (!m->d_muon_grad) rc = dev_alloc(m, &m->d_muon_grad, (size_t)m->P);
+    if (rc == HB_OK && !m->d_momenta) rc = dev_alloc(m, &m->d_momenta, (size_t)m->P);
+    const size_t need = ortho_workspace(shapes.data(), (int)shapes.size(), h.ortho.products);
+    if (rc == HB_OK && need > m->muon_ws_bytes) {  // (a smaller one goes with the handle)
+        unsigned char *ws = nullptr;
+        rc = dev_alloc(m, &ws, need);
+        if (rc == HB_OK) {
+            m->muon_ws = ws;
+            m->muon_ws_bytes = need;
+        }
+    }
+    if (rc != HB_OK) return rc;
+    HB_HIP(launch_fill_u32(reinterpret_cast<unsigned int *>(m->d_momenta), m->P, 0u, m->stream));
+    m->muon = h;
+    m->muon_coef.swap(coef);
+    m->muon.ortho.coef = m->muon_coef.empty() ? nullptr : m->muon_coef.data();
+    m->muon_scale = scale;
+    m->muon_first = first_layer;
+    m->muon_last = last_layer;
+    return HB_OK;
+}
+
+static int momenta_call(hb_model *m, const void *host)
+{
+    const int rc = check_handle(m, true);
+    if (rc != HB_OK) return rc;
+    if (!host) return fail(HB_ERR_INVALID, "host pointer is NULL");
+    if (!m->d_momenta) return fail(HB_ERR_STATE, "hb_model_set_muon has not been called on this model");
+    return HB_OK;
+}
+
+int hb_model_get_momenta(hb_model *m, float *host_flat)
+{
+    const int rc = momenta_call(m, host_flat);
+    if (rc != HB_OK) return rc;
+    HB_HIP(hipMemcpyAsync(host_flat, m->d_momenta, sizeof(float) * (size_t)m->P, hipMemcpyDeviceToHost, m->stream));
+    HB_HIP(hipStreamSynchronize(m->stream));
+    return HB_OK;
+}
+
+int hb_model_set_momenta(hb_model *m, const float *host_flat)
+{
+    const int rc = momenta_call(m, host_flat);
+    if (rc != HB_OK) return rc;
+    HB_HIP(hipMemcpyAsync(m->d_momenta, host_flat, sizeof(float) * (size_t)m->P, hipMemcpyHostToDevice, m->stream));
+    HB_HIP(hipStreamSynchronize(m->stream));
+    return HB_OK;
+}
+
+// What the calls with a loss of their own check, before their first device call but for the workspace of the handle's first one
+static int validate_head_call(hb_model *m, const void *dX, const int32_t *dy, int64_t B, bool needs_y = true)
+{
+    // (the classes are not looked at here: any pointer stands for none)
+    int rc = validate_batch_call(m, dX, needs_y || dy ? dy : static_cast<const int32_t *>(dX), B, false, false);
     if (rc != HB_OK) return rc;
     if (m->loss != HB_LOSS_SOFTMAX_CE) return fail(HB_ERR_INVALID, "this call needs a model with HB_LOSS_SOFTMAX_CE");
     return check_current_device(m);
@@ -1898,6 +2056,35 @@ int hb_batch_logprob_async(hb_model *m, const void *dX, const int32_t *dy, int64
     Head head;
     head.logp = d_logp;
     head.lse = d_lse;
+    return run_head_call(m, dX, dy, B, 0.f, MODE_LOSS, nullptr, head);
+}
+
+int hb_batch_scores_async(hb_model *m, const void *dX, const int32_t *dy, int64_t B, int32_t top, float *d_logp, float *d_lse,
+                          float *d_entropy, int32_t *d_top_class, float *d_top_logp)
+{
+    int rc = validate_head_call(m, dX, dy, B, d_logp != nullptr);
+    if (rc == HB_OK) rc = check_top(top);
+    if (rc != HB_OK) return rc;
+    if (top > 0 && !d_top_class) return fail(HB_ERR_INVALID, "d_top_class is NULL");
+    if (top == 0) {
+        d_top_class = nullptr;
+        d_top_logp = nullptr;
+    }
+    const size_t n = sizeof(float) * (size_t)B, t = n * (size_t)top;
+    rc = check_apart<5, 2>({{d_logp, n, "d_logp"}, {d_lse, n, "d_lse"}, {d_entropy, n, "d_entropy"}, {d_top_class, t, "d_top_class"},
+                            {d_top_logp, t, "d_top_logp"}},
+                           {input_block(m, dX, B), {dy, n, "dy"}});
+    if (rc != HB_OK) return rc;
+    if (!m->scores_ws) {
+        unsigned char *ws = nullptr;
+        rc = dev_alloc(m, &ws, scores_workspace(m->max_B, m->dims[m->L], 64));
+        if (rc != HB_OK) return rc;
+        m->scores_ws = ws;
+    }
+    const ScoreOut out = {d_logp, d_lse, d_entropy, d_top_class, d_top_logp};
+    Head head;
+    head.scores = &out;
+    head.top = top;
     return run_head_call(m, dX, dy, B, 0.f, MODE_LOSS, nullptr, head);
 }
 

@@ -125,7 +125,8 @@ struct OrthoSteps {
     float lr, momentum, weight_decay;
 };
 size_t ortho_workspace(const OrthoShape *shapes, int n, int products);
-hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n, const OrthoSteps &how, void *ws, hipStream_t stream);
+hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n, const OrthoSteps &how, void *ws, hipStream_t stream,
+                        const PassEvents &ev = PassEvents());
 
 // rows x cols elements of `size` bytes from p on, `ld` apart; or n bytes.  A null pointer has none.
 struct Block {
@@ -173,6 +174,8 @@ int check_dropout_p(float p, unsigned *threshold);
 int check_policy(const hb_policy *p);
 int check_preference(const hb_preference *p);
 int check_ortho(const hb_ortho *o);
+int check_ortho_shape(int64_t rows, int64_t cols, int k);
+int check_top(int32_t top);
 int check_muon(const hb_muon *h);
 OrthoSteps ortho_steps(const hb_ortho *o);
 OrthoSteps muon_steps(const hb_muon *h, int g_tensor);

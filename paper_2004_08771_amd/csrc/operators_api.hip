@@ -162,14 +162,6 @@ constexpr int64_t MAX_ORTHO_DIM = 32768, MAX_ORTHO_SIZE = 1 << 30;
 constexpr int MAX_ORTHO_LIST = 4096, MAX_ORTHO_STEPS = ORTHO_STEPS;
 const float USUAL_COEF[3] = {3.4445f, -4.7750f, 2.0315f};
 
-int check_ortho_shape(int64_t rows, int64_t cols, int k)
-{
-    if (rows < 0 || rows > MAX_ORTHO_DIM || cols < 0 || cols > MAX_ORTHO_DIM || rows * cols > MAX_ORTHO_SIZE)
-        return set_error(HB_ERR_INVALID, "matrix %d is %lld x %lld: at most %lld rows and columns and %lld elements are supported", k, (long long)rows,
-                         (long long)cols, (long long)MAX_ORTHO_DIM, (long long)MAX_ORTHO_SIZE);
-    return HB_OK;
-}
-
 int check_ortho_operand(const void *p, int64_t ld, int64_t cols, size_t size, const char *name, int k)
 {
     if (!p) return set_error(HB_ERR_INVALID, "%s of matrix %d is NULL", name, k);
@@ -286,6 +278,20 @@ int check_preference(const hb_preference *p)
     if (!std::isfinite(p->beta) || !(p->beta > 0.f)) return set_error(HB_ERR_INVALID, "beta = %g is not positive and finite", (double)p->beta);
     if (!(p->smoothing >= 0.f && p->smoothing <= 0.5f))
         return set_error(HB_ERR_INVALID, "smoothing = %g is outside [0, 0.5]", (double)p->smoothing);
+    return HB_OK;
+}
+
+int check_ortho_shape(int64_t rows, int64_t cols, int k)
+{
+    if (rows < 0 || rows > MAX_ORTHO_DIM || cols < 0 || cols > MAX_ORTHO_DIM || rows * cols > MAX_ORTHO_SIZE)
+        return set_error(HB_ERR_INVALID, "matrix %d is %lld x %lld: at most %lld rows and columns and %lld elements are supported", k, (long long)rows,
+                         (long long)cols, (long long)MAX_ORTHO_DIM, (long long)MAX_ORTHO_SIZE);
+    return HB_OK;
+}
+
+int check_top(int32_t top)
+{
+    if (top < 0 || top > MAX_TOP) return set_error(HB_ERR_INVALID, "top = %d is outside [0, %d]", top, MAX_TOP);
     return HB_OK;
 }
 
@@ -494,7 +500,8 @@ int hb_scores_async(const void *d_Z, int64_t ldz, int tensor, const int32_t *d_y
 {
     int rc = check_rows(d_Z, ldz, tensor, d_y, B, K, d_logp != nullptr);
     if (rc != HB_OK) return rc;
-    if (top < 0 || top > MAX_TOP) return set_error(HB_ERR_INVALID, "top = %d is outside [0, %d]", top, MAX_TOP);
+    rc = check_top(top);
+    if (rc != HB_OK) return rc;
     rc = check_scores_workspace(d_ws, ws_bytes, B, K, top);
     if (rc != HB_OK) return rc;
     if (B == 0) return HB_OK;

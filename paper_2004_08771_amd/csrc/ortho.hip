@@ -1267,6 +1267,19 @@ __global__ __launch_bounds__(SMALL_NT) void small_part_kernel(SmallArgs l, unsig
 }
 
 // ---------------------------------------------------------------- launches
+// the passes of a call, for who asks for their times: norms and layouts (small matrices: everything), products
+enum { PASS_NORM = 0, PASS_PRODUCT = 1 };
+
+template <typename K, typename... Args>
+hipError_t go(K kernel, int blocks, int threads, size_t lds, hipStream_t stream, const LaunchEvents &ev, Args... args)
+{
+    if (ev.start != nullptr)
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3((unsigned)threads), (unsigned)lds, stream, ev.start, ev.stop, 0, args...);
+    else
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3((unsigned)threads), lds, stream, args...);
+    return hipGetLastError();
+}
+
 long long round_to(long long v, int t) { return (v + t - 1) / t * t; }
 size_t aligned(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -1420,34 +1433,35 @@ struct Form<256> {
 };
 
 template <int T, int KIND>
-hipError_t product(int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream)
+hipError_t product(int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream, const LaunchEvents &ev)
 {
     typedef Form<T> F;
     static LdsGrant grant;
     const hipError_t e = grant_lds(grant, F::P::LDS, F::template kernel<KIND>);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(F::template kernel<KIND>, dim3((unsigned)blocks), dim3(F::P::NT), F::P::LDS, stream, dl, ws, from, c[0], c[1], c[2]);
-    return hipGetLastError();
+    return go(F::template kernel<KIND>, blocks, F::P::NT, F::P::LDS, stream, ev, dl, ws, from, c[0], c[1], c[2]);
 }
 
 template <int KIND>
-hipError_t product(int tile, int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream)
+hipError_t product(int tile, int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream, const PassEvents &passes)
 {
-    if (tile == 256) return product<256, KIND>(blocks, dl, ws, from, c, stream);
-    if (tile == 128) return product<128, KIND>(blocks, dl, ws, from, c, stream);
-    return product<64, KIND>(blocks, dl, ws, from, c, stream);
+    const LaunchEvents ev = passes(PASS_PRODUCT, 0.0);
+    if (tile == 256) return product<256, KIND>(blocks, dl, ws, from, c, stream, ev);
+    if (tile == 128) return product<128, KIND>(blocks, dl, ws, from, c, stream, ev);
+    return product<64, KIND>(blocks, dl, ws, from, c, stream, ev);
 }
 
-hipError_t products(const List *dl, unsigned char *ws, const Layout &y, const OrthoSteps &how, hipStream_t stream)
+hipError_t products(const List *dl, unsigned char *ws, const Layout &y, const OrthoSteps &how, hipStream_t stream, const PassEvents &ev)
 {
     hipError_t e = hipSuccess;
     for (int i = 0; i < how.steps && e == hipSuccess; ++i) {
         const float *c = how.coef + 3 * (how.n_coef == 1 ? 0 : i);
         const int from = i & 1;
-        e = product<GRAM>(y.tiles.sym, y.syms, dl, ws, from, c, stream);
-        if (e == hipSuccess) e = product<SQUARE>(y.tiles.sym, y.syms, dl, ws, from, c, stream);
+        e = product<GRAM>(y.tiles.sym, y.syms, dl, ws, from, c, stream, ev);
+        if (e == hipSuccess) e = product<SQUARE>(y.tiles.sym, y.syms, dl, ws, from, c, stream, ev);
         if (e != hipSuccess) return e;
-        e = i + 1 < how.steps ? product<NEXT>(y.tiles.all, y.alls, dl, ws, from, c, stream) : product<LAST>(y.tiles.all, y.alls, dl, ws, from, c, stream);
+        e = i + 1 < how.steps ? product<NEXT>(y.tiles.all, y.alls, dl, ws, from, c, stream, ev)
+                              : product<LAST>(y.tiles.all, y.alls, dl, ws, from, c, stream, ev);
     }
     return e;
 }
@@ -1548,27 +1562,24 @@ SmallLayout lay_out_small(SmallArgs &l, const OrthoShape *s, int n, int rows)
 }
 
 template <int MP, int NB>
-hipError_t small_launches(const SmallArgs &l, const SmallLayout &y, unsigned char *ws, hipStream_t stream)
+hipError_t small_launches(const SmallArgs &l, const SmallLayout &y, unsigned char *ws, hipStream_t stream, const PassEvents &ev)
 {
     typedef Small<MP, NB> M;
     static LdsGrant grant;
     hipError_t e = grant_lds(grant, M::LDS, small_kernel<MP, NB>, small_part_kernel<MP, NB>);
     if (e != hipSuccess) return e;
-    if (y.one) {
-        hipLaunchKernelGGL((small_kernel<MP, NB>), dim3(l.count), dim3(SMALL_NT), M::LDS, stream, l);
-        return hipGetLastError();
-    }
+    if (y.one) return go(small_kernel<MP, NB>, l.count, SMALL_NT, M::LDS, stream, ev(PASS_NORM, 0.0), l);
     double *const partial = reinterpret_cast<double *>(ws + y.partial);
-    hipLaunchKernelGGL(small_sum_kernel, dim3(y.sums), dim3(SUM_NT), 0, stream, l, partial);
-    hipLaunchKernelGGL((small_part_kernel<MP, NB>), dim3(y.blocks), dim3(SMALL_NT), M::LDS, stream, l, ws, partial, -1, 0);
+    e = go(small_sum_kernel, y.sums, SUM_NT, 0, stream, ev(PASS_NORM, 0.0), l, partial);
+    if (e == hipSuccess) e = go(small_part_kernel<MP, NB>, y.blocks, SMALL_NT, M::LDS, stream, ev(PASS_PRODUCT, 0.0), l, ws, (const double *)partial, -1, 0);
     int turn = 0;
-    for (int k = 0; k < l.steps;) {
-        hipLaunchKernelGGL((small_part_kernel<MP, NB>), dim3(y.blocks), dim3(SMALL_NT), M::LDS, stream, l, ws, partial, k, turn);
+    for (int k = 0; k < l.steps && e == hipSuccess;) {
+        e = go(small_part_kernel<MP, NB>, y.blocks, SMALL_NT, M::LDS, stream, ev(PASS_PRODUCT, 0.0), l, ws, (const double *)partial, k, turn);
         while (!l.step[k].end) ++k;
         ++k;
         turn ^= 1;
     }
-    return hipGetLastError();
+    return e;
 }
 
 }  // namespace
@@ -1592,7 +1603,8 @@ size_t ortho_workspace(const OrthoShape *shapes, int n, int products)
 }
 
 // Groups of at most ORTHO_GROUP matrices, one after the other in the same workspace
-hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n, const OrthoSteps &how, void *ws, hipStream_t stream)
+hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n, const OrthoSteps &how, void *ws, hipStream_t stream,
+                        const PassEvents &ev)
 {
     const int rows = small_rows(shapes, n);
     SmallArgs small = {};
@@ -1610,10 +1622,10 @@ hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n
                 a.whole_out = reinterpret_cast<uintptr_t>(o.out) % (how.out_tensor == TENSOR_BF16 && !how.muon ? 8 : 16) == 0;
             }
             unsigned char *const w = static_cast<unsigned char *>(ws);
-            const hipError_t e = rows == 16   ? small_launches<16, 1024>(small, y, w, stream)
-                                 : rows == 32 ? small_launches<32, 1024>(small, y, w, stream)
-                                 : rows == 64 ? small_launches<64, 512>(small, y, w, stream)
-                                              : small_launches<128, 128>(small, y, w, stream);
+            const hipError_t e = rows == 16   ? small_launches<16, 1024>(small, y, w, stream, ev)
+                                 : rows == 32 ? small_launches<32, 1024>(small, y, w, stream, ev)
+                                 : rows == 64 ? small_launches<64, 512>(small, y, w, stream, ev)
+                                              : small_launches<128, 128>(small, y, w, stream, ev);
             if (e != hipSuccess) return e;
         }
         return hipSuccess;
@@ -1631,11 +1643,9 @@ hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n
         unsigned char *const w = static_cast<unsigned char *>(ws);
         List *const dl = reinterpret_cast<List *>(w);
         double *const partial = reinterpret_cast<double *>(w + y.partial);
-        hipLaunchKernelGGL(sum_kernel, dim3(y.sums), dim3(SUM_NT), 0, stream, l, dl, partial);
-        hipLaunchKernelGGL(prep_kernel, dim3(y.preps), dim3(256), 0, stream, dl, w, partial);
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        e = products(dl, w, y, how, stream);
+        hipError_t e = go(sum_kernel, y.sums, SUM_NT, 0, stream, ev(PASS_NORM, 0.0), l, dl, partial);
+        if (e == hipSuccess) e = go(prep_kernel, y.preps, 256, 0, stream, ev(PASS_NORM, 0.0), (const List *)dl, w, (const double *)partial);
+        if (e == hipSuccess) e = products(dl, w, y, how, stream, ev);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

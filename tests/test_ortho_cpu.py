@@ -102,3 +102,11 @@ def test_the_definition():
         got = ref.ortho_ref(G.T).T if flip else ref.ortho_ref(G)
         assert np.abs(got - want).max() < 1e-12
         assert np.abs(ref.ortho_rounded(G, planes=2) - want).max() < 1e-4
+
+
+def test_a_model_that_is_not_configured():
+    m = hb.Model((8, 4, 2))
+    buf = np.zeros(m.num_params, np.float32)
+    for call in (lambda: m.set_muon(hb.muon_args()), lambda: m.set_muon(None), lambda: m.get_momenta(buf), lambda: m.set_momenta(buf),
+                 lambda: m.batch_scores_async(1, 1, 4)):
+        refused(call, hb.HB_ERR_STATE)
