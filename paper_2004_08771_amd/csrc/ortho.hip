@@ -275,20 +275,23 @@ __device__ __forceinline__ void wait_loads_and_meet()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// T x T tile of rows times rows, WM x WN wavefronts, S stages of both operands in LDS.
-template <int T, int WM, int WN, int S>
+// T x T tile of rows times rows, WM x WN wavefronts, S stages of both operands in LDS.  Two planes of an operand are in a stage together, so that each is
+// loaded once for the three products (instead of one segment of k behind the other: 983 x 512 fp32 18.0 -> 13.7, 11.9 -> 9.6, 11.4 -> 8.9 us for the
+// three products of a step, 1024 x 1024 30 -> 18); with one plane, 64 x 64 tiles have two k-tiles in a stage.
+template <int T, int WM, int WN, int S, int PL>
 struct Product {
     static constexpr int NW = WM * WN, NT = 64 * NW;
     static constexpr int RM = T / WM, RN = T / WN, MB = RM / 16, NB = RN / 16;
     static constexpr int LOADS = T * 8 / NT;  // 16-byte loads a lane and operand tile
-    static constexpr int OPERAND = T * ROW_BYTES, STAGE = 2 * OPERAND;
+    static constexpr int KT = T == 64 && PL == 1 ? 2 : 1, SUB = PL * KT;  // k-tiles in a stage
+    static constexpr int OPERAND = T * ROW_BYTES, STAGE = 2 * SUB * OPERAND;
     static constexpr int HM = RM < 64 ? RM : 64, AHEAD = 2, REGION = RN * (HM + 4) * 4;  // of the results: rows at a time, loads before one is used
     static constexpr size_t LDS = (size_t)(S * STAGE > NW * REGION ? S * STAGE : NW * REGION);
     v4f acc[MB][NB];
 
-    // P, Q: first rows of the tile, of `pitch` bytes; segments of nk k-tiles with the offsets (bytes) of their operands
-    __device__ __forceinline__ void run(unsigned char *lds, const unsigned char *P, const unsigned char *Q, unsigned pitch, int nk, int segs,
-                                        size_t low_p, size_t low_q, int tid)
+    // P, Q: first rows of the tile, of `pitch` bytes; nk k-tiles; low_p, low_q: bytes to the low parts
+    __device__ __forceinline__ void run(unsigned char *lds, const unsigned char *P, const unsigned char *Q, unsigned pitch, int nk, size_t low_p,
+                                        size_t low_q, int tid)
     {
         const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int wm = wave % WM, wn = wave / WM;
@@ -302,43 +305,53 @@ struct Product {
             const int R = (wave + NW * v) * 8 + (lane >> 3);
             off[v] = (unsigned)R * pitch + (((lane & 7) ^ swz(R)) << 4);
         }
-        const int total = nk * segs;
-        // segment 0: high x high, 1: high x low, 2: low x high
+        const int steps = (nk + KT - 1) / KT;
         auto issue = [&](int t, int stage) {
-            const int seg = t >= 2 * nk ? 2 : t >= nk ? 1 : 0;
-            const size_t k = (size_t)(t - seg * nk) * ROW_BYTES;
-            const unsigned char *p = P + (seg == 2 ? low_p : 0) + k, *q = Q + (seg == 1 ? low_q : 0) + k;
+            const size_t k = (size_t)t * (KT * ROW_BYTES);
             unsigned char *to = lds + stage * STAGE;
 #pragma unroll
-            for (int v = 0; v < LOADS; ++v) {
-                __builtin_amdgcn_global_load_lds((gptr_t)(p + off[v]), (lptr_t)(to + (wave + NW * v) * 1024), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((gptr_t)(q + off[v]), (lptr_t)(to + OPERAND + (wave + NW * v) * 1024), 16, 0, 0);
+            for (int u = 0; u < SUB; ++u) {
+                if (KT == 2 && u == 1 && 2 * t + 1 >= nk) continue;  // (an odd number of k-tiles)
+                const size_t at_p = KT == 2 ? k + u * ROW_BYTES : k + (u ? low_p : 0), at_q = KT == 2 ? k + u * ROW_BYTES : k + (u ? low_q : 0);
+#pragma unroll
+                for (int v = 0; v < LOADS; ++v) {
+                    __builtin_amdgcn_global_load_lds((gptr_t)(P + at_p + off[v]), (lptr_t)(to + 2 * u * OPERAND + (wave + NW * v) * 1024), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)(Q + at_q + off[v]), (lptr_t)(to + (2 * u + 1) * OPERAND + (wave + NW * v) * 1024), 16, 0, 0);
+                }
             }
         };
+        static_assert(S == 2, "every wait is for all loads: the last step may have fewer");
 #pragma unroll
         for (int t = 0; t < S - 1; ++t)
-            if (t < total) issue(t, t);
+            if (t < steps) issue(t, t);
         const int c16 = lane & 15, g4 = lane >> 4;
         const int p_off = (wm * RM + c16) * ROW_BYTES + ((g4 ^ swz(c16)) << 4);
         const int q_off = OPERAND + (wn * RN + c16) * ROW_BYTES + ((g4 ^ swz(c16)) << 4);
         int stage = 0;
-        for (int t = 0; t < total; ++t) {
+        for (int t = 0; t < steps; ++t) {
             // tile t has landed, and everybody is done with tile t - 1
-            if (t + S - 2 < total) wait_loads_and_meet<2 * LOADS *(S - 2)>();
-            else wait_loads_and_meet<0>();
-            if (t + S - 1 < total) issue(t + S - 1, stage == 0 ? S - 1 : stage - 1);
+            wait_loads_and_meet<0>();
+            if (t + S - 1 < steps) issue(t + S - 1, stage == 0 ? S - 1 : stage - 1);
             const unsigned char *at = lds + stage * STAGE;
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                v8h fp[MB], fq[NB];
+            for (int kk = 0; kk < 2 * KT; ++kk) {
+                if (KT == 2 && kk == 2 && 2 * t + 1 >= nk) break;
+                v8h fp[PL][MB], fq[PL][NB];
 #pragma unroll
-                for (int i = 0; i < MB; ++i) fp[i] = *reinterpret_cast<const v8h *>(at + (p_off ^ (kk << 6)) + i * 16 * ROW_BYTES);
+                for (int pl = 0; pl < PL; ++pl) {
+                    const unsigned char *from = at + 2 * (KT == 2 ? kk / 2 : pl) * OPERAND;
 #pragma unroll
-                for (int j = 0; j < NB; ++j) fq[j] = *reinterpret_cast<const v8h *>(at + (q_off ^ (kk << 6)) + j * 16 * ROW_BYTES);
+                    for (int i = 0; i < MB; ++i) fp[pl][i] = *reinterpret_cast<const v8h *>(from + (p_off ^ ((kk & 1) << 6)) + i * 16 * ROW_BYTES);
 #pragma unroll
-                for (int i = 0; i < MB; ++i)
+                    for (int j = 0; j < NB; ++j) fq[pl][j] = *reinterpret_cast<const v8h *>(from + (q_off ^ ((kk & 1) << 6)) + j * 16 * ROW_BYTES);
+                }
 #pragma unroll
-                    for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[i], fq[j], acc[i][j], 0, 0, 0);
+                for (int s = 0; s < 2 * PL - 1; ++s)  // high x high, high x low, low x high
+#pragma unroll
+                    for (int i = 0; i < MB; ++i)
+#pragma unroll
+                        for (int j = 0; j < NB; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[s == 2 ? PL - 1 : 0][i], fq[s == 1 ? PL - 1 : 0][j], acc[i][j], 0, 0, 0);
             }
             stage = stage == S - 1 ? 0 : stage + 1;
         }
@@ -348,8 +361,8 @@ struct Product {
 // 256 x 256 tiles of eight wavefronts, as 2 x 4, of 128 x 64 each: two stages of the left operand and three of the right one (all 160 KB of LDS).
 // The sixteen products of a group (half of the rows at one k-step of 32) are issued with the requests of the next group's fragments and two
 // loads from memory between them, so that neither the LDS nor the address unit gets them all at once; loads have two groups or more to land.
-template <>
-struct Product<256, 2, 4, 2> {
+template <int PL>
+struct Product<256, 2, 4, 2, PL> {
     static constexpr int T = 256, WM = 2, NW = 8, NT = 512, RM = 128, RN = 64, MB = 8, NB = 4;
     static constexpr int OPERAND = T * ROW_BYTES, Q_BASE = 2 * OPERAND;
     static constexpr int HM = 64, AHEAD = 4, REGION = RN * (HM + 4) * 4;
@@ -357,9 +370,10 @@ struct Product<256, 2, 4, 2> {
     static_assert(NW * REGION <= (int)LDS, "LDS");
     v4f acc[MB][NB];
 
-    __device__ __forceinline__ void run(unsigned char *lds, const unsigned char *P, const unsigned char *Q, unsigned pitch, int nk, int segs,
-                                        size_t low_p, size_t low_q, int tid)
+    __device__ __forceinline__ void run(unsigned char *lds, const unsigned char *P, const unsigned char *Q, unsigned pitch, int nk, size_t low_p,
+                                        size_t low_q, int tid)
     {
+        constexpr int segs = 2 * PL - 1;  // high x high, high x low, low x high: one behind the other
         const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int wm = wave % WM, wn = wave / WM;
 #pragma unroll
@@ -521,11 +535,11 @@ __device__ __forceinline__ void put_result(const How &l, const Matrix &a, int r,
     }
 }
 
-template <int T, int WM, int WN, int S, int KIND>
+template <int T, int WM, int WN, int S, int PL, int KIND>
 __global__ __launch_bounds__(64 * WM *WN) void product_kernel(const List *lp, unsigned char *ws, int from, float ca, float cb, float cc)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    typedef Product<T, WM, WN, S> P;
+    typedef Product<T, WM, WN, S, PL> P;
     const List &l = *lp;
     constexpr bool SYM = KIND == GRAM || KIND == SQUARE;
     const int k = find(l, blockIdx.x, [](const Mat &a) { return SYM ? a.sym0 : a.all0; });
@@ -540,7 +554,7 @@ __global__ __launch_bounds__(64 * WM *WN) void product_kernel(const List *lp, un
         ti = t / per_row;
         tj = t - ti * per_row;
     }
-    const int i0 = ti * T, j0 = tj * T, planes = l.planes;
+    const int i0 = ti * T, j0 = tj * T;
     const size_t xlow = (size_t)a.mp * a.np, alow = (size_t)a.mp * a.mp;
     const int tid = threadIdx.x;
     P p;
@@ -549,8 +563,7 @@ __global__ __launch_bounds__(64 * WM *WN) void product_kernel(const List *lp, un
         const unsigned char *y = KIND == GRAM || KIND == SQUARE ? x : ws + a.xt[from];
         const unsigned pitch = 2u * (unsigned)(KIND == GRAM ? a.np : a.mp);
         const int nk = (KIND == GRAM ? a.n : a.m) / BK;
-        p.run(lds, x + (size_t)i0 * pitch, y + (size_t)j0 * pitch, pitch, nk, planes == 2 ? 3 : 1, 2 * (KIND == GRAM ? xlow : alow),
-              2 * (SYM ? (KIND == GRAM ? xlow : alow) : xlow), tid);
+        p.run(lds, x + (size_t)i0 * pitch, y + (size_t)j0 * pitch, pitch, nk, 2 * (KIND == GRAM ? xlow : alow), 2 * (SYM ? (KIND == GRAM ? xlow : alow) : xlow), tid);
     }
     // The results leave through LDS, HM rows of the wavefront's block at a time: lane 16 g + c of a 16 x 16 block has column c, rows 4 g .. 4 g + 3, in LDS
     // they lie a column after the other.  From there lanes take eight rows of a column each (whole lines of the transposed
@@ -563,7 +576,8 @@ __global__ __launch_bounds__(64 * WM *WN) void product_kernel(const List *lp, un
     half_t *const xt = reinterpret_cast<half_t *>(ws + a.xt[from]);
     half_t *const new_xt = reinterpret_cast<half_t *>(ws + a.xt[from ^ 1]), *const new_x = reinterpret_cast<half_t *>(ws + a.x[from ^ 1]);
     constexpr int HM = P::HM, PITCH = HM + 4, PER = HM / 8, ITEMS = P::RN * PER / 64;
-    const bool two = planes == 2, rows_too = SYM ? ti != tj : KIND == NEXT || !a.flip;
+    constexpr bool two = PL == 2;
+    const bool rows_too = SYM ? ti != tj : KIND == NEXT || !a.flip;
     __syncthreads();  // nobody reads the operands any more: their place is for the results
     float *const mine = reinterpret_cast<float *>(lds + wave * P::REGION);
 #pragma unroll
@@ -1288,12 +1302,14 @@ struct Tiles {
     int most() const { return sym > all ? sym : all; }
 };
 
-// Time of a product of `tiles` tiles of T x T over the longest k, in us, from what the kernels take: a k-tile of 64 with a workgroup or less a
-// compute unit 0.30 (T = 64), 0.68 (128), 1.40 us (256), with two 0.60, 1.20; first loads and results 4, 8, 18.
-double product_time(int T, double tiles, double k_tiles)
+// Time of a product of `tiles` tiles of T x T over the longest k, in us, from what the kernels take for a k-tile of 64 (all planes of it) where a compute unit has a
+// workgroup, and where it has two (T = 64: one plane 0.25 and 0.40, two 0.55 and 0.80 us; 128: 0.68, 1.20; 1.70; 256: 1.40; 4.20), and for first loads and
+// results: 4, 8, 18.
+double product_time(int T, int planes, double tiles, double k_tiles)
 {
-    const double one = T == 64 ? 0.30 : T == 128 ? 0.68 : 1.40, two = T == 64 ? 0.60 : T == 128 ? 1.20 : 1.40;
-    const double at_once = T == 256 ? 256 : 512, rounds = floor(tiles / at_once), rest = tiles - rounds * at_once;
+    const double one = planes == 1 ? (T == 64 ? 0.25 : T == 128 ? 0.68 : 1.40) : T == 64 ? 0.55 : T == 128 ? 1.70 : 4.20;
+    const double two = planes == 1 ? (T == 64 ? 0.40 : T == 128 ? 1.20 : 1.40) : T == 64 ? 0.80 : one;
+    const double at_once = T == 256 || (T == 128 && planes == 2) ? 256 : 512, rounds = floor(tiles / at_once), rest = tiles - rounds * at_once;
     return k_tiles * (rounds * two + (rest == 0.0 ? 0.0 : rest <= 256 ? one : two)) + (T == 64 ? 4.0 : T == 128 ? 8.0 : 18.0);
 }
 
@@ -1312,8 +1328,8 @@ Tiles tiles_for(const OrthoShape *s, int n, int planes)
             m_most = fmax(m_most, s[k].m());
             n_most = fmax(n_most, s[k].n());
         }
-        const double km = ceil(m_most / BK) * (planes == 2 ? 3 : 1), kn = ceil(n_most / BK) * (planes == 2 ? 3 : 1);
-        const double ts = product_time(T, sym, kn) + product_time(T, sym, km), ta = product_time(T, all, km);
+        const double km = ceil(m_most / BK), kn = ceil(n_most / BK);
+        const double ts = product_time(T, planes, sym, kn) + product_time(T, planes, sym, km), ta = product_time(T, planes, all, km);
         if (T == 64 || ts < sym_time) {
             sym_time = ts;
             best.sym = T;
@@ -1411,44 +1427,46 @@ void describe(Matrix &a, const OrthoMatrix &o, const OrthoShape &s, const OrthoS
                   (o.ldo % (how.out_tensor == TENSOR_BF16 && !how.muon ? 8 : 4) == 0 || a.rows == 1);
 }
 
-template <int T>
+template <int T, int PL>
 struct Form;
-template <>
-struct Form<64> {
-    typedef Product<64, 2, 2, 4> P;
-    template <int KIND>
-    static constexpr auto kernel = product_kernel<64, 2, 2, 4, KIND>;
+template <int PL>
+struct Form<64, PL> {
+    static constexpr int WM = 2, WN = 2, S = 2;
 };
-template <>
-struct Form<128> {
-    typedef Product<128, 2, 2, 2> P;
-    template <int KIND>
-    static constexpr auto kernel = product_kernel<128, 2, 2, 2, KIND>;
+template <int PL>
+struct Form<128, PL> {
+    static constexpr int WM = 2, WN = 2, S = 2;
 };
-template <>
-struct Form<256> {
-    typedef Product<256, 2, 4, 2> P;
-    template <int KIND>
-    static constexpr auto kernel = product_kernel<256, 2, 4, 2, KIND>;
+template <int PL>
+struct Form<256, PL> {
+    static constexpr int WM = 2, WN = 4, S = 2;
 };
 
-template <int T, int KIND>
+template <int T, int PL, int KIND>
 hipError_t product(int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream, const LaunchEvents &ev)
 {
-    typedef Form<T> F;
+    typedef Form<T, PL> F;
+    typedef Product<T, F::WM, F::WN, F::S, PL> P;
+    const auto kernel = product_kernel<T, F::WM, F::WN, F::S, PL, KIND>;
     static LdsGrant grant;
-    const hipError_t e = grant_lds(grant, F::P::LDS, F::template kernel<KIND>);
+    const hipError_t e = grant_lds(grant, P::LDS, kernel);
     if (e != hipSuccess) return e;
-    return go(F::template kernel<KIND>, blocks, F::P::NT, F::P::LDS, stream, ev, dl, ws, from, c[0], c[1], c[2]);
+    return go(kernel, blocks, P::NT, P::LDS, stream, ev, dl, ws, from, c[0], c[1], c[2]);
 }
 
 template <int KIND>
-hipError_t product(int tile, int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream, const PassEvents &passes)
+hipError_t product(int tile, int planes, int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream,
+                   const PassEvents &passes)
 {
     const LaunchEvents ev = passes(PASS_PRODUCT, 0.0);
-    if (tile == 256) return product<256, KIND>(blocks, dl, ws, from, c, stream, ev);
-    if (tile == 128) return product<128, KIND>(blocks, dl, ws, from, c, stream, ev);
-    return product<64, KIND>(blocks, dl, ws, from, c, stream, ev);
+    if (planes == 2) {
+        if (tile == 256) return product<256, 2, KIND>(blocks, dl, ws, from, c, stream, ev);
+        if (tile == 128) return product<128, 2, KIND>(blocks, dl, ws, from, c, stream, ev);
+        return product<64, 2, KIND>(blocks, dl, ws, from, c, stream, ev);
+    }
+    if (tile == 256) return product<256, 1, KIND>(blocks, dl, ws, from, c, stream, ev);
+    if (tile == 128) return product<128, 1, KIND>(blocks, dl, ws, from, c, stream, ev);
+    return product<64, 1, KIND>(blocks, dl, ws, from, c, stream, ev);
 }
 
 hipError_t products(const List *dl, unsigned char *ws, const Layout &y, const OrthoSteps &how, hipStream_t stream, const PassEvents &ev)
@@ -1456,12 +1474,12 @@ hipError_t products(const List *dl, unsigned char *ws, const Layout &y, const Or
     hipError_t e = hipSuccess;
     for (int i = 0; i < how.steps && e == hipSuccess; ++i) {
         const float *c = how.coef + 3 * (how.n_coef == 1 ? 0 : i);
-        const int from = i & 1;
-        e = product<GRAM>(y.tiles.sym, y.syms, dl, ws, from, c, stream, ev);
-        if (e == hipSuccess) e = product<SQUARE>(y.tiles.sym, y.syms, dl, ws, from, c, stream, ev);
+        const int from = i & 1, planes = how.products == TENSOR_F32 ? 2 : 1;
+        e = product<GRAM>(y.tiles.sym, planes, y.syms, dl, ws, from, c, stream, ev);
+        if (e == hipSuccess) e = product<SQUARE>(y.tiles.sym, planes, y.syms, dl, ws, from, c, stream, ev);
         if (e != hipSuccess) return e;
-        e = i + 1 < how.steps ? product<NEXT>(y.tiles.all, y.alls, dl, ws, from, c, stream, ev)
-                              : product<LAST>(y.tiles.all, y.alls, dl, ws, from, c, stream, ev);
+        e = i + 1 < how.steps ? product<NEXT>(y.tiles.all, planes, y.alls, dl, ws, from, c, stream, ev)
+                              : product<LAST>(y.tiles.all, planes, y.alls, dl, ws, from, c, stream, ev);
     }
     return e;
 }
