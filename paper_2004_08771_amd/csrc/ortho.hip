@@ -277,16 +277,17 @@ __device__ __forceinline__ void wait_loads_and_meet()
 
 // T x T tile of rows times rows, WM x WN wavefronts, S stages of both operands in LDS.  Two planes of an operand are in a stage together, so that each is
 // loaded once for the three products (instead of one segment of k behind the other: 983 x 512 fp32 18.0 -> 13.7, 11.9 -> 9.6, 11.4 -> 8.9 us for the
-// three products of a step, 1024 x 1024 30 -> 18); with one plane, 64 x 64 tiles have two k-tiles in a stage.
-template <int T, int WM, int WN, int S, int PL>
+// three products of a step, 1024 x 1024 30 -> 18); with one plane, 64 x 64 tiles have two k-tiles in a stage.  KG = 2, where there is no more
+// than a workgroup a compute unit: twice the wavefronts, each half with one of two k-tiles or k-steps of a stage, and four stages.
+template <int T, int WM, int WN, int S, int PL, int KG>
 struct Product {
-    static constexpr int NW = WM * WN, NT = 64 * NW;
+    static constexpr int NW = WM * WN * KG, NT = 64 * NW;
     static constexpr int RM = T / WM, RN = T / WN, MB = RM / 16, NB = RN / 16;
     static constexpr int LOADS = T * 8 / NT;  // 16-byte loads a lane and operand tile
     static constexpr int KT = T == 64 && PL == 1 ? 2 : 1, SUB = PL * KT;  // k-tiles in a stage
     static constexpr int OPERAND = T * ROW_BYTES, STAGE = 2 * SUB * OPERAND;
     static constexpr int HM = RM < 64 ? RM : 64, AHEAD = 2, REGION = RN * (HM + 4) * 4;  // of the results: rows at a time, loads before one is used
-    static constexpr size_t LDS = (size_t)(S * STAGE > NW * REGION ? S * STAGE : NW * REGION);
+    static constexpr size_t LDS = (size_t)(S * STAGE > WM * WN * REGION ? S * STAGE : WM * WN * REGION);
     v4f acc[MB][NB];
 
     // P, Q: first rows of the tile, of `pitch` bytes; nk k-tiles; low_p, low_q: bytes to the low parts
@@ -294,7 +295,7 @@ struct Product {
                                         size_t low_q, int tid)
     {
         const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const int wm = wave % WM, wn = wave / WM;
+        const int wm = wave % WM, wn = wave / WM % WN, group = wave / (WM * WN);
 #pragma unroll
         for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -310,17 +311,19 @@ struct Product {
             const size_t k = (size_t)t * (KT * ROW_BYTES);
             unsigned char *to = lds + stage * STAGE;
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                if (KT == 2 && u == 1 && 2 * t + 1 >= nk) continue;  // (an odd number of k-tiles)
-                const size_t at_p = KT == 2 ? k + u * ROW_BYTES : k + (u ? low_p : 0), at_q = KT == 2 ? k + u * ROW_BYTES : k + (u ? low_q : 0);
+            for (int kt = 0; kt < KT; ++kt) {
+                if (kt == 1 && 2 * t + 1 >= nk) continue;  // (an odd number of k-tiles)
 #pragma unroll
-                for (int v = 0; v < LOADS; ++v) {
-                    __builtin_amdgcn_global_load_lds((gptr_t)(P + at_p + off[v]), (lptr_t)(to + 2 * u * OPERAND + (wave + NW * v) * 1024), 16, 0, 0);
-                    __builtin_amdgcn_global_load_lds((gptr_t)(Q + at_q + off[v]), (lptr_t)(to + (2 * u + 1) * OPERAND + (wave + NW * v) * 1024), 16, 0, 0);
-                }
+                for (int pl = 0; pl < PL; ++pl)
+#pragma unroll
+                    for (int v = 0; v < LOADS; ++v) {
+                        unsigned char *const to_v = to + 2 * (kt * PL + pl) * OPERAND + (wave + NW * v) * 1024;
+                        __builtin_amdgcn_global_load_lds((gptr_t)(P + (pl ? low_p : 0) + k + kt * ROW_BYTES + off[v]), (lptr_t)to_v, 16, 0, 0);
+                        __builtin_amdgcn_global_load_lds((gptr_t)(Q + (pl ? low_q : 0) + k + kt * ROW_BYTES + off[v]), (lptr_t)(to_v + OPERAND), 16, 0, 0);
+                    }
             }
         };
-        static_assert(S == 2, "every wait is for all loads: the last step may have fewer");
+        const int full = nk / KT;  // (the last step may have fewer loads)
 #pragma unroll
         for (int t = 0; t < S - 1; ++t)
             if (t < steps) issue(t, t);
@@ -330,20 +333,22 @@ struct Product {
         int stage = 0;
         for (int t = 0; t < steps; ++t) {
             // tile t has landed, and everybody is done with tile t - 1
-            wait_loads_and_meet<0>();
+            if (S > 2 && t + S - 2 < full) wait_loads_and_meet<2 * SUB * LOADS *(S - 2)>();
+            else wait_loads_and_meet<0>();
             if (t + S - 1 < steps) issue(t + S - 1, stage == 0 ? S - 1 : stage - 1);
             const unsigned char *at = lds + stage * STAGE;
 #pragma unroll
-            for (int kk = 0; kk < 2 * KT; ++kk) {
-                if (KT == 2 && kk == 2 && 2 * t + 1 >= nk) break;
+            for (int ks = 0; ks < 2 * KT / KG; ++ks) {
+                const int kk = KG == 1 || KT == 2 ? ks & 1 : group, kt = KT == 1 ? 0 : KG == 2 ? group : ks / 2;
+                if (KT == 2 && (KG == 2 || ks == 2) && kt == 1 && 2 * t + 1 >= nk) break;
                 v8h fp[PL][MB], fq[PL][NB];
 #pragma unroll
                 for (int pl = 0; pl < PL; ++pl) {
-                    const unsigned char *from = at + 2 * (KT == 2 ? kk / 2 : pl) * OPERAND;
+                    const unsigned char *from = at + 2 * (kt * PL + pl) * OPERAND;
 #pragma unroll
-                    for (int i = 0; i < MB; ++i) fp[pl][i] = *reinterpret_cast<const v8h *>(from + (p_off ^ ((kk & 1) << 6)) + i * 16 * ROW_BYTES);
+                    for (int i = 0; i < MB; ++i) fp[pl][i] = *reinterpret_cast<const v8h *>(from + (p_off ^ (kk << 6)) + i * 16 * ROW_BYTES);
 #pragma unroll
-                    for (int j = 0; j < NB; ++j) fq[pl][j] = *reinterpret_cast<const v8h *>(from + (q_off ^ ((kk & 1) << 6)) + j * 16 * ROW_BYTES);
+                    for (int j = 0; j < NB; ++j) fq[pl][j] = *reinterpret_cast<const v8h *>(from + (q_off ^ (kk << 6)) + j * 16 * ROW_BYTES);
                 }
 #pragma unroll
                 for (int s = 0; s < 2 * PL - 1; ++s)  // high x high, high x low, low x high
@@ -355,6 +360,23 @@ struct Product {
             }
             stage = stage == S - 1 ? 0 : stage + 1;
         }
+        if (KG == 1) return;
+        // the second group's sums to the first
+        v4f *const sums = reinterpret_cast<v4f *>(lds) + (wave % (WM * WN)) * (MB * NB * 64) + lane;
+        __syncthreads();
+        if (group == 1) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j2 = 0; j2 < NB; ++j2) sums[(i * NB + j2) * 64] = acc[i][j2];
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j2 = 0; j2 < NB; ++j2) acc[i][j2] += sums[(i * NB + j2) * 64];
+        }
     }
 };
 
@@ -362,7 +384,7 @@ struct Product {
 // The sixteen products of a group (half of the rows at one k-step of 32) are issued with the requests of the next group's fragments and two
 // loads from memory between them, so that neither the LDS nor the address unit gets them all at once; loads have two groups or more to land.
 template <int PL>
-struct Product<256, 2, 4, 2, PL> {
+struct Product<256, 2, 4, 2, PL, 1> {
     static constexpr int T = 256, WM = 2, NW = 8, NT = 512, RM = 128, RN = 64, MB = 8, NB = 4;
     static constexpr int OPERAND = T * ROW_BYTES, Q_BASE = 2 * OPERAND;
     static constexpr int HM = 64, AHEAD = 4, REGION = RN * (HM + 4) * 4;
@@ -535,11 +557,11 @@ __device__ __forceinline__ void put_result(const How &l, const Matrix &a, int r,
     }
 }
 
-template <int T, int WM, int WN, int S, int PL, int KIND>
-__global__ __launch_bounds__(64 * WM *WN) void product_kernel(const List *lp, unsigned char *ws, int from, float ca, float cb, float cc)
+template <int T, int WM, int WN, int S, int PL, int KG, int KIND>
+__global__ __launch_bounds__(64 * WM *WN *KG) void product_kernel(const List *lp, unsigned char *ws, int from, float ca, float cb, float cc)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    typedef Product<T, WM, WN, S, PL> P;
+    typedef Product<T, WM, WN, S, PL, KG> P;
     const List &l = *lp;
     constexpr bool SYM = KIND == GRAM || KIND == SQUARE;
     const int k = find(l, blockIdx.x, [](const Mat &a) { return SYM ? a.sym0 : a.all0; });
@@ -579,6 +601,7 @@ __global__ __launch_bounds__(64 * WM *WN) void product_kernel(const List *lp, un
     constexpr bool two = PL == 2;
     const bool rows_too = SYM ? ti != tj : KIND == NEXT || !a.flip;
     __syncthreads();  // nobody reads the operands any more: their place is for the results
+    if (KG == 2 && wave >= WM * WN) return;  // (no wavefront waits for another from here on)
     float *const mine = reinterpret_cast<float *>(lds + wave * P::REGION);
 #pragma unroll
     for (int half = 0; half < P::RM / HM; ++half) {
@@ -1431,23 +1454,26 @@ template <int T, int PL>
 struct Form;
 template <int PL>
 struct Form<64, PL> {
-    static constexpr int WM = 2, WN = 2, S = 2;
+    static constexpr int WM = 2, WN = 2;
 };
 template <int PL>
 struct Form<128, PL> {
-    static constexpr int WM = 2, WN = 2, S = 2;
+    static constexpr int WM = 2, WN = 2;
 };
 template <int PL>
 struct Form<256, PL> {
-    static constexpr int WM = 2, WN = 4, S = 2;
+    static constexpr int WM = 2, WN = 4;
 };
 
-template <int T, int PL, int KIND>
+template <int T, int PL, int KIND, int KG = 1>
 hipError_t product(int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream, const LaunchEvents &ev)
 {
+    if constexpr (T == 64 && KG == 1)
+        if (blocks <= 256) return product<T, PL, KIND, 2>(blocks, dl, ws, from, c, stream, ev);
     typedef Form<T, PL> F;
-    typedef Product<T, F::WM, F::WN, F::S, PL> P;
-    const auto kernel = product_kernel<T, F::WM, F::WN, F::S, PL, KIND>;
+    constexpr int S = KG == 2 ? 4 : 2;
+    typedef Product<T, F::WM, F::WN, S, PL, KG> P;
+    const auto kernel = product_kernel<T, F::WM, F::WN, S, PL, KG, KIND>;
     static LdsGrant grant;
     const hipError_t e = grant_lds(grant, P::LDS, kernel);
     if (e != hipSuccess) return e;
