@@ -140,19 +140,76 @@ __device__ __forceinline__ void put_nothing(const ScoreArgs &a, long long row, i
     }
 }
 
+// The value of lane ^ J, without the trip through the LDS unit that a general shuffle is (100 cycles; what a row waits for between its passes is a few
+// dozen of these): permutations within sixteen lanes are part of an instruction, those between sixteens and halves are swaps of gfx950.
+template <int CTRL>
+__device__ __forceinline__ float within(float v)
+{
+    const int x = __float_as_int(v);
+    return __int_as_float(__builtin_amdgcn_update_dpp(x, x, CTRL, 0xf, 0xf, true));
+}
+template <int J>
+__device__ __forceinline__ float across(float v)
+{
+    if constexpr (J == 1) return within<0xb1>(v);                      // 1 0 3 2 of four
+    else if constexpr (J == 2) return within<0x4e>(v);                 // 2 3 0 1
+    else if constexpr (J == 4) return within<0x1b>(within<0x141>(v));  // eight lanes mirrored, then each four
+    else if constexpr (J == 8) return within<0x141>(within<0x140>(v)); // sixteen mirrored, then each eight
+    else {
+        typedef unsigned two __attribute__((ext_vector_type(2)));
+        const unsigned x = __float_as_uint(v);
+        two r;
+        if constexpr (J == 16) r = __builtin_bit_cast(two, __builtin_amdgcn_permlane16_swap(x, x, false, false));
+        else r = __builtin_bit_cast(two, __builtin_amdgcn_permlane32_swap(x, x, false, false));
+        return __uint_as_float((threadIdx.x & J) ? r[0] : r[1]);
+    }
+}
+template <typename F>
+__device__ __forceinline__ float over_wave(float v, F f)
+{
+    v = f(v, across<32>(v));
+    v = f(v, across<16>(v));
+    v = f(v, across<8>(v));
+    v = f(v, across<4>(v));
+    v = f(v, across<2>(v));
+    return f(v, across<1>(v));
+}
+__device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+
 // the values of a wavefront's lanes in descending order
-__device__ __forceinline__ float sorted(float v)
+template <int K, int J>
+__device__ __forceinline__ float exchanged(float v)
 {
     const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int k = 2; k <= 64; k <<= 1)
-#pragma unroll
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            const float w = __shfl_xor(v, j, 64);
-            const bool first = (lane & j) == 0, down = (lane & k) == 0;
-            v = first == down ? fmaxf(v, w) : fminf(v, w);
-        }
+    const float w = across<J>(v);
+    v = ((lane & J) == 0) == ((lane & K) == 0) ? fmaxf(v, w) : fminf(v, w);
+    if constexpr (J > 1) v = exchanged<K, J / 2>(v);
     return v;
+}
+__device__ __forceinline__ float sorted(float v)
+{
+    v = exchanged<2, 1>(v);
+    v = exchanged<4, 2>(v);
+    v = exchanged<8, 4>(v);
+    v = exchanged<16, 8>(v);
+    v = exchanged<32, 16>(v);
+    return exchanged<64, 32>(v);
+}
+
+// The maximum over the lanes of a row; red: a wavefront each
+template <int WAVES>
+__device__ __forceinline__ float max_of_lanes(float top, float *red)
+{
+    top = over_wave(top, max_of);
+    if (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+        __syncthreads();
+        top = red[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, red[w]);
+    }
+    return top;
 }
 
 __device__ __forceinline__ u64 max_of_wave(u64 v)
@@ -273,7 +330,7 @@ __device__ __forceinline__ void row_in_registers(const ScoreArgs &a, long long r
     }
     const int top_n = MODE == ROW_GRAD ? 0 : a.top;
     if (WAVES > 1 && top_n > 1) sh.lane_top[g] = lane_top;
-    const float top = max_of_row<G, WAVES>(lane_top, sh.top);
+    const float top = max_of_lanes<WAVES>(lane_top, sh.top);
 
     // ---- the class of the largest logit, which leaves the sums
     int w = NO_CLASS;
@@ -333,11 +390,8 @@ __device__ __forceinline__ void row_in_registers(const ScoreArgs &a, long long r
         __builtin_amdgcn_sched_barrier(0);
     }
     float o = (o4[0] + o4[1]) + (o4[2] + o4[3]), h = (h4[0] + h4[1]) + (h4[2] + h4[3]);
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) {
-        o += __shfl_xor(o, i, 64);
-        h += __shfl_xor(h, i, 64);
-    }
+    o = over_wave(o, sum_of);
+    h = over_wave(h, sum_of);
     if (WAVES > 1) {
         if (lane == 0) {
             sh.o[wave] = o;
@@ -431,6 +485,7 @@ __device__ __forceinline__ void row_in_registers(const ScoreArgs &a, long long r
         for (int t = g; t < n; t += G) {
             const u64 key = sh.list[t];
             int rank = 1;
+#pragma unroll 8
             for (int j = 0; j < n; ++j) rank += sh.list[j] > key ? 1 : 0;
             if (rank < top_n) place(rank, key);
         }
@@ -536,7 +591,7 @@ __device__ __forceinline__ Part merged(const Part *parts, int chunks, Part *red)
 
 __global__ __launch_bounds__(NT) void merge_scores_kernel(ScoreArgs a, const Part *parts, const u64 *keys, int chunks, int row0)
 {
-    constexpr int LIST = 1024;
+    constexpr int LIST = 1024, MINE = 4;
     __shared__ Part red[NT / 64];
     __shared__ u64 red_key[2][NT / 64], list[LIST];
     __shared__ int count;
@@ -548,16 +603,26 @@ __global__ __launch_bounds__(NT) void merge_scores_kernel(ScoreArgs a, const Par
         return;
     }
     if (threadIdx.x == 0) count = 0;
+    const u64 *const k0 = keys + (long long)blockIdx.x * chunks * a.top;
+    const int n = chunks * a.top;
+    u64 mine[MINE];  // asked for before the sums are waited for
+#pragma unroll
+    for (int u = 0; u < MINE; ++u) mine[u] = threadIdx.x + u * NT < n ? k0[threadIdx.x + u * NT] : 0;
     const Part m = merged(parts + (long long)blockIdx.x * chunks, chunks, red);
     const RowNumbers r(m.top, m.o, m.h);
     if (threadIdx.x == 0) put_numbers(a, row, y, y >= 0 ? logit(a, row, y) : 0.f, r);
     if (a.top == 0) return;
-    // every part's keys are in order, and the last of any is a lower bound
-    const u64 *const k0 = keys + (long long)blockIdx.x * chunks * a.top;
-    const int n = chunks * a.top;
+    // Two lower bounds of the last key that is looked for: the largest of the parts' last ones, and the top-th largest first one (of 64 groups of parts)
     u64 bound = 1;
     for (int c = threadIdx.x; c < chunks; c += NT) {
         const u64 k = k0[(long long)c * a.top + a.top - 1];
+        bound = k > bound ? k : bound;
+    }
+    if (wave == 0) {
+        float first = -INFINITY;
+        for (int c = lane; c < chunks; c += 64) first = fmaxf(first, parts[(long long)blockIdx.x * chunks + c].top);
+        first = __shfl(sorted(first), a.top - 1, 64);
+        const u64 k = first >= LOWEST ? key_of(first, -1) & ~0xffffffffull : 0;
         bound = k > bound ? k : bound;
     }
     bound = max_of_wave(bound);
@@ -565,19 +630,21 @@ __global__ __launch_bounds__(NT) void merge_scores_kernel(ScoreArgs a, const Par
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NT / 64; ++i) bound = red_key[0][i] > bound ? red_key[0][i] : bound;
-    for (int i = threadIdx.x; i < n; i += NT) {
-        const u64 k = k0[i];
-        if (k >= bound) {
-            const int at = atomicAdd(&count, 1);
-            if (at < LIST) list[at] = k;
-        }
-    }
+    auto see = [&](u64 k) {
+        if (k < bound) return;
+        const int at = atomicAdd(&count, 1);
+        if (at < LIST) list[at] = k;
+    };
+#pragma unroll
+    for (int u = 0; u < MINE; ++u) see(mine[u]);
+    for (int i = threadIdx.x + MINE * NT; i < n; i += NT) see(k0[i]);
     __syncthreads();
     const int found = count;
     if (found <= LIST) {
         for (int t = threadIdx.x; t < found; t += NT) {
             const u64 key = list[t];
             int rank = 0;
+#pragma unroll 8
             for (int j = 0; j < found; ++j) rank += list[j] > key ? 1 : 0;
             if (rank < a.top) put(a, row, rank, key, r);
         }
