@@ -68,6 +68,8 @@ struct Mat : Matrix {
 };
 struct List : How {
     int count, planes;
+    int syms, splits;          // tiles of the symmetric products, and parts of k in GRAM_PART
+    size_t part;               // byte offset of its sums
     Mat mat[ORTHO_GROUP];
 };
 
@@ -264,7 +266,8 @@ __global__ __launch_bounds__(256) void prep_kernel(const List *lp, unsigned char
 }
 
 // ---------------------------------------------------------------- products
-enum { GRAM = 0, SQUARE = 1, NEXT = 2, LAST = 3 };
+// GRAM_PART, GRAM_JOIN: the first product of few rows and many columns in two launches: sums over parts of k, and what is made of them
+enum { GRAM = 0, SQUARE = 1, NEXT = 2, LAST = 3, GRAM_PART = 4, GRAM_JOIN = 5 };
 
 // slot of 16-byte chunk c of tile row R: c ^ swz(R), so that the sixteen rows of a fragment read lie on different banks
 __device__ __forceinline__ int swz(int R) { return (R >> 1) & 7; }
@@ -289,6 +292,29 @@ struct Product {
     static constexpr int HM = RM < 64 ? RM : 64, AHEAD = 2, REGION = RN * (HM + 4) * 4;  // of the results: rows at a time, loads before one is used
     static constexpr size_t LDS = (size_t)(S * STAGE > WM * WN * REGION ? S * STAGE : WM * WN * REGION);
     v4f acc[MB][NB];
+
+    // the sums as they lie in the first WM x WN wavefronts, and from several such parts in their order
+    __device__ __forceinline__ void keep(v4f *to, int tid) const
+    {
+        if (tid >= 64 * WM * WN) return;
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) to[(i * NB + j) * (64 * WM * WN) + tid] = acc[i][j];
+    }
+    __device__ __forceinline__ void join(const v4f *from, size_t step, int parts, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = from[(i * NB + j) * (64 * WM * WN) + tid];
+#pragma unroll 4
+        for (int s = 1; s < parts; ++s)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] += from[s * step + (i * NB + j) * (64 * WM * WN) + tid];
+    }
 
     // P, Q: first rows of the tile, of `pitch` bytes; nk k-tiles; low_p, low_q: bytes to the low parts
     __device__ __forceinline__ void run(unsigned char *lds, const unsigned char *P, const unsigned char *Q, unsigned pitch, int nk, size_t low_p,
@@ -557,16 +583,18 @@ __device__ __forceinline__ void put_result(const How &l, const Matrix &a, int r,
     }
 }
 
-template <int T, int WM, int WN, int S, int PL, int KG, int KIND>
+template <int T, int WM, int WN, int S, int PL, int KG, int WHAT>
 __global__ __launch_bounds__(64 * WM *WN *KG) void product_kernel(const List *lp, unsigned char *ws, int from, float ca, float cb, float cc)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     typedef Product<T, WM, WN, S, PL, KG> P;
     const List &l = *lp;
+    constexpr int KIND = WHAT == GRAM_PART || WHAT == GRAM_JOIN ? (int)GRAM : WHAT;
     constexpr bool SYM = KIND == GRAM || KIND == SQUARE;
-    const int k = find(l, blockIdx.x, [](const Mat &a) { return SYM ? a.sym0 : a.all0; });
+    const int slice = WHAT == GRAM_PART ? (int)blockIdx.x / l.syms : 0, block = (int)blockIdx.x - slice * l.syms;
+    const int k = find(l, block, [](const Mat &a) { return SYM ? a.sym0 : a.all0; });
     const Mat &a = l.mat[k];
-    const int t = blockIdx.x - (SYM ? a.sym0 : a.all0);
+    const int t = block - (SYM ? a.sym0 : a.all0);
     int ti, tj;
     if (SYM) {
         ti = triangle_row(t);
@@ -580,12 +608,24 @@ __global__ __launch_bounds__(64 * WM *WN *KG) void product_kernel(const List *lp
     const size_t xlow = (size_t)a.mp * a.np, alow = (size_t)a.mp * a.mp;
     const int tid = threadIdx.x;
     P p;
-    {
+    if constexpr (WHAT == GRAM_JOIN) {
+        p.join(reinterpret_cast<const v4f *>(ws + l.part) + (size_t)block * (T * T / 4), (size_t)l.syms * (T * T / 4), l.splits, tid);
+    } else {
         const unsigned char *x = ws + (KIND == GRAM ? a.x[from] : KIND == SQUARE ? a.f : a.h);
         const unsigned char *y = KIND == GRAM || KIND == SQUARE ? x : ws + a.xt[from];
         const unsigned pitch = 2u * (unsigned)(KIND == GRAM ? a.np : a.mp);
-        const int nk = (KIND == GRAM ? a.n : a.m) / BK;
+        int nk = (KIND == GRAM ? a.n : a.m) / BK;
+        if (WHAT == GRAM_PART) {
+            const int chunk = (nk + l.splits - 1) / l.splits, k0 = min(slice * chunk, nk);
+            nk = min(chunk, nk - k0);
+            x += (size_t)k0 * ROW_BYTES;
+            y += (size_t)k0 * ROW_BYTES;
+        }
         p.run(lds, x + (size_t)i0 * pitch, y + (size_t)j0 * pitch, pitch, nk, 2 * (KIND == GRAM ? xlow : alow), 2 * (SYM ? (KIND == GRAM ? xlow : alow) : xlow), tid);
+    }
+    if constexpr (WHAT == GRAM_PART) {
+        p.keep(reinterpret_cast<v4f *>(ws + l.part) + (size_t)blockIdx.x * (T * T / 4), tid);
+        return;
     }
     // The results leave through LDS, HM rows of the wavefront's block at a time: lane 16 g + c of a 16 x 16 block has column c, rows 4 g .. 4 g + 3, in LDS
     // they lie a column after the other.  From there lanes take eight rows of a column each (whole lines of the transposed
@@ -1229,6 +1269,19 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallArgs l)
     M::put_out(lds, how, a, 0, columns);
 }
 
+// The sums of a matrix's blocks, added up in their order where the first one's lie, four of them a lane
+template <int MP>
+__global__ __launch_bounds__(MP < 32 ? 64 : 128) void small_join_kernel(SmallArgs l, unsigned char *ws, int turn)
+{
+    constexpr int N = MP * MP / 4, NT = MP < 32 ? 64 : 128;
+    const int k = blockIdx.x / (N / NT), e = (blockIdx.x - k * (N / NT)) * NT + threadIdx.x, blocks = l.mat[k].blocks;
+    v4f *const sums = reinterpret_cast<v4f *>(ws + l.mat[k].part[turn]);
+    v4f m = sums[e];
+#pragma unroll 8
+    for (int b = 1; b < blocks; ++b) m += sums[b * N + e];
+    sums[e] = m;
+}
+
 __global__ __launch_bounds__(SUM_NT) void small_sum_kernel(SmallArgs l, double *partial)
 {
     __shared__ double red[SUM_NT / 64];
@@ -1240,7 +1293,7 @@ __global__ __launch_bounds__(SUM_NT) void small_sum_kernel(SmallArgs l, double *
 // A workgroup a block of columns.  from = -1: X from G and the sums of its products; else the run of steps from `from` on (every workgroup makes its Q itself:
 // one more launch would take longer), X times Q, and for another run the sums of its products.  turn: which of the sums are read
 template <int MP, int NB>
-__global__ __launch_bounds__(SMALL_NT) void small_part_kernel(SmallArgs l, unsigned char *ws, const double *partial, int from, int turn)
+__global__ __launch_bounds__(SMALL_NT) void small_part_kernel(SmallArgs l, unsigned char *ws, const double *partial, int from, int turn, int joined)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     __shared__ SmallStep steps[ORTHO_STEPS];
@@ -1271,7 +1324,7 @@ __global__ __launch_bounds__(SMALL_NT) void small_part_kernel(SmallArgs l, unsig
         for (int i = 0; i < M::S; ++i) m.v[i] = v4f{0.f, 0.f, 0.f, 0.f};
         const v4f *const sums = reinterpret_cast<const v4f *>(ws + a.part[turn]);
 #pragma unroll 2
-        for (int b = part; b < a.blocks; b += M::PARTS)
+        for (int b = part; b < (joined ? 1 : a.blocks); b += M::PARTS)
 #pragma unroll
             for (int i = 0; i < M::S; ++i) m.v[i] += sums[((b * M::S + strip) * M::S + i) * 64 + lane];
         M::add_parts(lds + M::SHARED, m, strip, part, lane);
@@ -1367,7 +1420,7 @@ Tiles tiles_for(const OrthoShape *s, int n, int planes)
 
 struct Layout {
     size_t partial, end;
-    int sums, preps, syms, alls;
+    int sums, preps, syms, alls, splits;
     Tiles tiles;
 };
 
@@ -1416,6 +1469,21 @@ Layout lay_out(List &l, const OrthoShape *s, int n, int planes)
         y.syms += mt * (mt + 1) / 2;
         y.alls += ((a.m + tiles.all - 1) / tiles.all) * ((a.n + tiles.all - 1) / tiles.all);
     }
+    // Few tiles over a long k leave most compute units without one: parts of at least 8 k-tiles, where that takes away more than the second launch takes
+    // (5 us; 140 x 8192 fp32 358 us without it, 149 with; 300 x 8192 392, 202)
+    l.syms = y.syms;
+    l.splits = 1;
+    l.part = at;
+    if (tiles.sym == 64 && y.syms > 0) {
+        int nk = 0;
+        for (int k = 0; k < n; ++k) nk = l.mat[k].n / BK > nk ? l.mat[k].n / BK : nk;
+        const int most = 256 / y.syms < nk / 8 ? 256 / y.syms : nk / 8;
+        if (most > 1 && nk * (planes == 1 ? 0.25 : 0.55) * (1.0 - 1.0 / most) > 6.0) {
+            l.splits = most;
+            at = aligned(at + (size_t)most * y.syms * (64 * 64 * 4));
+        }
+    }
+    y.splits = l.splits;
     y.end = at;
     return y;
 }
@@ -1468,7 +1536,7 @@ struct Form<256, PL> {
 template <int T, int PL, int KIND, int KG = 1>
 hipError_t product(int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream, const LaunchEvents &ev)
 {
-    if constexpr (T == 64 && KG == 1)
+    if constexpr (T == 64 && KG == 1 && KIND != GRAM_JOIN)
         if (blocks <= 256) return product<T, PL, KIND, 2>(blocks, dl, ws, from, c, stream, ev);
     typedef Form<T, PL> F;
     constexpr int S = KG == 2 ? 4 : 2;
@@ -1495,13 +1563,25 @@ hipError_t product(int tile, int planes, int blocks, const List *dl, unsigned ch
     return product<64, 1, KIND>(blocks, dl, ws, from, c, stream, ev);
 }
 
+template <int KIND>
+hipError_t product64(int planes, int blocks, const List *dl, unsigned char *ws, int from, const float *c, hipStream_t stream, const PassEvents &passes)
+{
+    const LaunchEvents ev = passes(PASS_PRODUCT, 0.0);
+    return planes == 2 ? product<64, 2, KIND>(blocks, dl, ws, from, c, stream, ev) : product<64, 1, KIND>(blocks, dl, ws, from, c, stream, ev);
+}
+
 hipError_t products(const List *dl, unsigned char *ws, const Layout &y, const OrthoSteps &how, hipStream_t stream, const PassEvents &ev)
 {
     hipError_t e = hipSuccess;
     for (int i = 0; i < how.steps && e == hipSuccess; ++i) {
         const float *c = how.coef + 3 * (how.n_coef == 1 ? 0 : i);
         const int from = i & 1, planes = how.products == TENSOR_F32 ? 2 : 1;
-        e = product<GRAM>(y.tiles.sym, planes, y.syms, dl, ws, from, c, stream, ev);
+        if (y.splits == 1) {
+            e = product<GRAM>(y.tiles.sym, planes, y.syms, dl, ws, from, c, stream, ev);
+        } else {
+            e = product64<GRAM_PART>(planes, y.syms * y.splits, dl, ws, from, c, stream, ev);
+            if (e == hipSuccess) e = product64<GRAM_JOIN>(planes, y.syms, dl, ws, from, c, stream, ev);
+        }
         if (e == hipSuccess) e = product<SQUARE>(y.tiles.sym, planes, y.syms, dl, ws, from, c, stream, ev);
         if (e != hipSuccess) return e;
         e = i + 1 < how.steps ? product<NEXT>(y.tiles.all, planes, y.alls, dl, ws, from, c, stream, ev)
@@ -1615,13 +1695,24 @@ hipError_t small_launches(const SmallArgs &l, const SmallLayout &y, unsigned cha
     if (y.one) return go(small_kernel<MP, NB>, l.count, SMALL_NT, M::LDS, stream, ev(PASS_NORM, 0.0), l);
     double *const partial = reinterpret_cast<double *>(ws + y.partial);
     e = go(small_sum_kernel, y.sums, SUM_NT, 0, stream, ev(PASS_NORM, 0.0), l, partial);
-    if (e == hipSuccess) e = go(small_part_kernel<MP, NB>, y.blocks, SMALL_NT, M::LDS, stream, ev(PASS_PRODUCT, 0.0), l, ws, (const double *)partial, -1, 0);
+    // every workgroup adds up the blocks' sums itself (64 KB in about 1 us), but for many, which a launch joins (4 us; 100 x 8192 fp32 204 us without it,
+    // 127 with; 128 x 4096 157, 124)
+    int joined = 0;
+    for (int k = 0; k < l.count; ++k) joined = joined || (long long)l.mat[k].blocks * MP * MP * 4 > (512 << 10);
+    auto sums_are_there = [&](int turn) {
+        constexpr int THREADS = MP < 32 ? 64 : 128;
+        return joined ? go(small_join_kernel<MP>, l.count * (MP * MP / 4 / THREADS), THREADS, 0, stream, ev(PASS_PRODUCT, 0.0), l, ws, turn) : hipSuccess;
+    };
+    if (e == hipSuccess)
+        e = go(small_part_kernel<MP, NB>, y.blocks, SMALL_NT, M::LDS, stream, ev(PASS_PRODUCT, 0.0), l, ws, (const double *)partial, -1, 0, joined);
+    if (e == hipSuccess) e = sums_are_there(0);
     int turn = 0;
     for (int k = 0; k < l.steps && e == hipSuccess;) {
-        e = go(small_part_kernel<MP, NB>, y.blocks, SMALL_NT, M::LDS, stream, ev(PASS_PRODUCT, 0.0), l, ws, (const double *)partial, k, turn);
+        e = go(small_part_kernel<MP, NB>, y.blocks, SMALL_NT, M::LDS, stream, ev(PASS_PRODUCT, 0.0), l, ws, (const double *)partial, k, turn, joined);
         while (!l.step[k].end) ++k;
         ++k;
         turn ^= 1;
+        if (k < l.steps && e == hipSuccess) e = sums_are_there(turn);
     }
     return e;
 }

@@ -92,6 +92,23 @@ def test_orthogonalize_larger(rows, cols, products):
     check(out, *tolerance(G, products), (rows, cols))
 
 
+@pytest.mark.parametrize("products", ["f32", "bf16"])
+@pytest.mark.parametrize("shapes", [[(140, 9000)], [(5000, 200), (130, 131)], [(190, 3001), (150, 8192), (1, 1)], [(100, 20000)], [(12, 30000), (16, 5)],
+                                    [(64, 32768)], [(16384, 128)]])
+def test_few_rows_and_many_columns(shapes, products):
+    """A long axis is split: what is joined again gives the definition, the same every time."""
+    rng = np.random.default_rng(shapes[0][1])
+    tiles = max(min(s) for s in shapes) > 128
+    G = [gradient(*s, rng).astype(np.float32).astype(np.float64) for s in shapes]
+    dG = [torch.as_tensor(g).float().cuda() for g in G]
+    out, again = [torch.empty_like(g) for g in dG], [torch.empty_like(g) for g in dG]
+    for o in (out, again):
+        hb.orthogonalize(dG, o, products=KINDS[products], ws=work(shapes, products))
+    for g, o, p in zip(G, out, again):
+        check(o, *tolerance(g, products, tiles=tiles), g.shape)
+        assert torch.equal(o, p)
+
+
 def test_large_matrix_against_products_on_the_device():
     """Sizes of the largest tiles: the definition in 64-bit products on the device."""
     g = torch.Generator(device="cuda").manual_seed(1)
