@@ -720,9 +720,11 @@ __global__ __launch_bounds__(64 * WM *WN *KG) void product_kernel(const List *lp
 //     X_k+1 = P_k X_k,   A_k+1 = P_k A_k P_k,   X_k+l = Q X_k,   Q = P_k+l-1 ... P_k
 // so a run of steps is products of m x m matrices, which commute and are symmetric.  A value of A near 0 keeps an absolute error while A_k+1 gives it the factor
 // p(0)^2, so the error of a long run is as of a square root of the precision: runs end where the product of the largest factors
-// passes 12 (HB_TENSOR_F32: two of the usual steps; the errors are those of single steps), or 500 (HB_TENSOR_BF16: five, 5e-4 at most).
-// Everything is held in 22 bits.  A wavefront has a strip of 16 columns of the m x m matrices in its registers.  A result of the matrix core holds four rows of a column a
-// lane, so two blocks of a strip are its operand of 32 values of k (in an order of their own, the same for both operands); rows go through LDS.
+// passes 12 (HB_TENSOR_F32: two of the usual steps), or 500 (HB_TENSOR_BF16: five, 5e-4 at most); of HB_TENSOR_F32 with up to 16 rows every step is a run,
+// since roundings do not average out over few of them (2 x 5 6.0e-6 in runs of two, 0.9e-6; 16 x 8192 takes 67 us for 53).
+// Everything but diagonals is held in 22 bits.  A wavefront has a strip of 16 columns of the m x m matrices in its registers.  A result of the matrix core holds four
+// rows of a column a lane, so two blocks of a strip are its operand of 32 values of k (in an order of their own, the same for both operands); rows go through LDS.
+// What bounds it is latency: 512 x 54 fp32 takes 58 us in one workgroup, of which reading and writing 220 KB are 17, the products with X 18, the m x m ones 16.
 constexpr int SMALL_NT = 512, SMALL_WAVES = 8;
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
@@ -754,7 +756,8 @@ struct Small {
     static constexpr int CHUNKS = MP / 8;
     static constexpr int PLANE = NB * MP * 2, FILE = S * KS * 2 * 1024, RED = (PARTS - 1) * MP * MP * 4;
     static constexpr int X = 0, SHARED = 2 * PLANE;  // X^T, high and low; then rows of the m x m matrices, or sums to be added up
-    static constexpr size_t LDS = 2 * (size_t)PLANE + (FILE > RED ? FILE : RED);
+    static constexpr int DIAG = FILE > RED ? FILE : RED;  // behind the rows: their matrix's diagonal
+    static constexpr size_t LDS = 2 * (size_t)PLANE + DIAG + 4 * MP;
 
     // byte of element (column j, row i) in a plane of X^T: the 16-byte pieces of a row are exchanged so that 16 rows lie on different banks, and so do the four
     // rows of 32 bytes of a transposing read
@@ -788,26 +791,33 @@ struct Small {
     }
     // The strip's part of the rows, for everybody, in the order in which the lanes ask for it.  (The matrices are symmetric but for roundings: columns in place of
     // rows would save the exchange, but what is not symmetric grows from step to step then, 8e-4 of the result after five.)
+    // The diagonal goes beside them in 32 bits: it is as large as all the rest of a row, and its rounding to 22 bits would be the same for every
+    // column of a product (1 x 6 2.3e-6 then).
     static __device__ __forceinline__ void put_rows(unsigned char *file, const Strip &m, float scale, int strip, int lane)
     {
         const int g4 = lane >> 4, c16 = lane & 15, ks = strip >> 1;
+        float d = 0.f;
         unsigned char *const to = file + ks * 2048 + (16 * (c16 >> 2) + 4 * g4) * 16 + (4 * (strip & 1) + (c16 & 3)) * 2;
 #pragma unroll
         for (int i = 0; i < S; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
+                const bool on = i == strip && 4 * g4 + e == c16;
+                d = on ? m.v[i][e] : d;
                 half_t hi, lo;
-                split(m.v[i][e] * scale, hi, lo);
+                split(on ? 0.f : m.v[i][e] * scale, hi, lo);
                 *reinterpret_cast<half_t *>(to + i * KS * 2048 + 16 * e) = hi;
                 *reinterpret_cast<half_t *>(to + i * KS * 2048 + 16 * e + 1024) = lo;
             }
+        if (g4 == c16 >> 2) *reinterpret_cast<float *>(file + DIAG + 4 * (16 * strip + c16)) = d;
         if (S == 1) {  // there is no second block of 16 values of k
             *reinterpret_cast<v4h *>(file + 16 * lane + 8) = v4h{0, 0, 0, 0};
             *reinterpret_cast<v4h *>(file + 1024 + 16 * lane + 8) = v4h{0, 0, 0, 0};
         }
     }
-    // rows in LDS times columns
-    static __device__ __forceinline__ void times(const unsigned char *file, const Frag &f, float scale, Strip &out, int lane)
+    // scale (rows in LDS times columns) + d_scale (diagonal times the same columns in 32 bits, of(block, row))
+    template <typename Of>
+    static __device__ __forceinline__ void times(const unsigned char *file, const Frag &f, float scale, float d_scale, Of of, Strip &out, int lane)
     {
 #pragma unroll
         for (int i = 0; i < S; ++i) {
@@ -821,7 +831,8 @@ struct Small {
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, f.hi[ks], acc, 0, 0, 0);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out.v[i][e] = acc[e] * scale;
+            for (int e = 0; e < 4; ++e)
+                out.v[i][e] = __builtin_fmaf(d_scale * *reinterpret_cast<const float *>(file + DIAG + 4 * (16 * i + 4 * (lane >> 4) + e)), of(i, e), acc[e] * scale);
             if (S == 8) __builtin_amdgcn_sched_barrier(0);  // (requests for all rows at once leave no registers)
         }
     }
@@ -1016,6 +1027,7 @@ struct Small {
         Strip q, p;
         Frag f;
         const bool mine = part == 0;
+        auto of = [](const Strip &x) { return [&x](int i, int e) { return x.v[i][e]; }; };
         for (;; ++k) {
             const SmallStep s = steps[k];
             const bool first = k == 0 || steps[k - 1].end != 0, end = __builtin_amdgcn_readfirstlane(s.end) != 0;
@@ -1025,7 +1037,7 @@ struct Small {
             }
             __syncthreads();
             if (mine) {
-                times(file, f, s.c / (s.sa * s.sa), p, lane);
+                times(file, f, s.c / (s.sa * s.sa), s.c, of(m), p, lane);
 #pragma unroll
                 for (int i = 0; i < S; ++i)
 #pragma unroll
@@ -1043,14 +1055,14 @@ struct Small {
                 } else {
                     const float before = steps[k - 1].sq;
                     frag_of(q, before, f);
-                    times(file, f, 1.f / (s.sp * before), q, lane);
+                    times(file, f, 1.f / (s.sp * before), 1.f, of(q), q, lane);
                 }
                 if (!end) {
                     const float next = steps[k + 1].sa;
                     frag_of(m, s.sa, f);
-                    times(file, f, 1.f / (s.sp * s.sa), p, lane);  // P A
+                    times(file, f, 1.f / (s.sp * s.sa), 1.f, of(m), p, lane);  // P A
                     frag_of(p, next, f);
-                    times(file, f, 1.f / (s.sp * next), m, lane);
+                    times(file, f, 1.f / (s.sp * next), 1.f, of(p), m, lane);
                 }
             }
             __syncthreads();
@@ -1087,7 +1099,7 @@ struct Small {
                     }
                 }
             Strip x;
-            times(file, f, inv_sq, x, lane);
+            times(file, f, inv_sq, 1.f, [&f](int i, int e) { return (float)f.hi[i / 2][4 * (i % 2) + e] + (float)f.lo[i / 2][4 * (i % 2) + e]; }, x, lane);
 #pragma unroll
             for (int i = 0; i < S; ++i) {
                 v4s hi, lo;
@@ -1591,9 +1603,9 @@ hipError_t products(const List *dl, unsigned char *ws, const Layout &y, const Or
 }
 
 // Runs of steps, and the scales: singular values of X are at most 1 at the start; the largest factor and value of a step are looked for
-bool plan_steps(SmallArgs &l, const OrthoSteps &how)
+bool plan_steps(SmallArgs &l, const OrthoSteps &how, int rows)
 {
-    const double limit = how.products == TENSOR_F32 ? 12.0 : 500.0;
+    const double limit = how.products != TENSOR_F32 ? 500.0 : rows > 16 ? 12.0 : 1.0;
     auto scale = [](double most, double cap) {  // a power of two that leaves room to 2^14
         double s = cap;
         while (s > 1.0 && most * s > 16384.0) s *= 0.5;
@@ -1743,7 +1755,7 @@ hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n
 {
     const int rows = small_rows(shapes, n);
     SmallArgs small = {};
-    if (rows && plan_steps(small, how)) {
+    if (rows && plan_steps(small, how, rows)) {
         describe(small, how);
         for (int k0 = 0; k0 < n; k0 += ORTHO_GROUP) {
             const int count = n - k0 < ORTHO_GROUP ? n - k0 : ORTHO_GROUP;

@@ -109,6 +109,27 @@ def test_few_rows_and_many_columns(shapes, products):
         assert torch.equal(o, p)
 
 
+@pytest.mark.parametrize("n", [1, 2, 5, 6, 31, 82])
+def test_one_row_keeps_its_digits(n):
+    """One singular value of 1 with exact arithmetic: f(s) = s p(s) five times.  Errors of a step relative to X: its planes 2^-22; products 2^-24 each of the
+    scale and the result; p by what A is off (2^-22 of dropped terms, (n + 2) 2^-24 of sums) and three roundings of up to |p's terms|; each times what later steps make of it."""
+    rng = np.random.default_rng(n)
+    G = rng.standard_normal((1, n)).astype(np.float32).astype(np.float64)
+    out = torch.empty(1, n, device="cuda")
+    hb.orthogonalize(torch.as_tensor(G).float().cuda(), out, products=KINDS["f32"], ws=work([(1, n)], "f32"))
+    a, b, c = 3.4445, -4.7750, 2.0315
+    s, tol = 1.0, 2.0 ** -22
+    for _ in range(5):
+        p = a + b * s ** 2 + c * s ** 4
+        slope = abs(a + 3 * b * s ** 2 + 5 * c * s ** 4) / abs(p)
+        terms = (a + abs(b) * s ** 2 + c * s ** 4) / abs(p)
+        off_a = 2.0 ** -22 + (n + 2) * 2.0 ** -24
+        tol = tol * max(1.0, slope) + 2.0 ** -22 + 2 * 2.0 ** -24 + abs(b * s ** 2 + 2 * c * s ** 4) / abs(p) * off_a + 3 * 2.0 ** -24 * terms
+        s *= p
+    want = s * G / np.linalg.norm(G)
+    assert np.abs(out.cpu().double().numpy() - want).max() <= tol * np.abs(want).max()
+
+
 def test_large_matrix_against_products_on_the_device():
     """Sizes of the largest tiles: the definition in 64-bit products on the device."""
     g = torch.Generator(device="cuda").manual_seed(1)
