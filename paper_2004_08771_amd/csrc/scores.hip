@@ -711,10 +711,12 @@ constexpr int ROW_PIECES = 20 * 1024;   // the longest row that a block has room
 constexpr int CHUNK_PIECES = 4 * NT, LONG_CHUNK = 16 * NT;
 constexpr int MAX_PAIRS = 8192;         // (row, chunk) pairs at a time
 
-bool in_registers(const ChoiceRows &r)
+// Chunks are two launches: up to 64 rows they pay from 8192 pieces on (fp32 32768 classes, 64 rows, scores 11.0 us in chunks, 8.0 in registers; 65536
+// 12.0 in chunks, 12.2), for gradients in bf16 from 4096 on (40000 classes 11.6, 12.4).
+bool in_registers(const ChoiceRows &r, bool grad)
 {
     const int n = most_pieces(r);
-    return n <= (r.B <= 64 ? 4096 : ROW_PIECES);
+    return n <= (r.B > 64 ? ROW_PIECES : grad && r.tensor == TENSOR_BF16 ? 4096 : 8192);
 }
 
 struct Chunks {
@@ -732,6 +734,13 @@ Chunks chunks_for(long long B, int pieces)
     return c;
 }
 
+// Lanes and pieces a lane.  A row's phases follow one another, so more lanes with less each are faster until a compute unit has rows enough to fill the
+// waits of one with the work of others (us, scores with five alternatives / gradients):
+//     bf16 16384 classes, 64 rows     256 x 8  8.7 /  8.5, 512 x 4  6.7 / 6.4;   4096 rows 34.5 / 49.1, 36.4 / 47.8
+//     bf16 32768          64          256 x 16 13.9 / 14.7, 512 x 8 9.7 / 10.1;  4096      62.5 / 98.1, 57.3 / 93.9
+//     bf16 50257          64          512 x 13 13.5 / 14.8, 1024 x 8 11.1 / 13.6; 4096     96.2 / 165, 105 / 164
+//     bf16 65536        1024          512 x 16 41.3 / 51.7, 1024 x 8 36.3 / 50.2; 4096     139 / 205, 120 / 198
+//     fp32 32768         256          512 x 16 10.1 / 16.5, 1024 x 8 8.7 / 16.2;  4096     99.8 / 192, 149 / 191
 template <typename T, int MODE>
 hipError_t rows_of_type(const ScoreArgs &a, int n, hipStream_t s, const LaunchEvents &ev)
 {
@@ -743,10 +752,14 @@ hipError_t rows_of_type(const ScoreArgs &a, int n, hipStream_t s, const LaunchEv
     if (n <= 256) return one(scores_kernel<T, 64, 4, MODE>, 64);
     if (n <= 512) return one(scores_kernel<T, 128, 4, MODE>, 128);
     if (n <= 1024) return one(scores_kernel<T, 256, 4, MODE>, 256);
-    if (n <= 2048) return one(scores_kernel<T, 256, 8, MODE>, 256);
-    if (n <= 4096) return one(scores_kernel<T, 256, 16, MODE>, 256);
+    if constexpr (MODE == ROW_SCORES)
+        if (n <= 2048 && a.B > 1024) return one(scores_kernel<T, 256, 8, MODE>, 256);
+    if (n <= 2048) return one(scores_kernel<T, 512, 4, MODE>, 512);
+    if (n <= 4096) return one(scores_kernel<T, 512, 8, MODE>, 512);
+    if (n <= 8192 && (a.B <= 256 || (sizeof(T) == 2 && n > 6656))) return one(scores_kernel<T, 1024, 8, MODE>, 1024);
     if (n <= 6656) return one(scores_kernel<T, 512, 13, MODE>, 512);
-    if (n <= 8192) return one(scores_kernel<T, 512, 16, MODE>, 512);
+    if constexpr (sizeof(T) == 4)
+        if (n <= 8192) return one(scores_kernel<T, 512, 16, MODE>, 512);
     if constexpr (sizeof(T) == 2 || MODE == ROW_GRAD)  // (fp32 scores would leave registers)
         if (n <= 12288) return one(scores_kernel<T, 512, 24, MODE>, 512);
     if (n <= 16384) return one(scores_kernel<T, 1024, 16, MODE>, 1024);
@@ -816,7 +829,7 @@ hipError_t launch_scores(const ChoiceRows &r, const ScoreOut &out, int top, void
     a.s.entropy = out.entropy;
     a.s.top_class = out.top_class;
     a.s.top_logp = out.top_logp;
-    if (in_registers(r)) {
+    if (in_registers(r, false)) {
         const LaunchEvents pass = ev(PASS_LOGITS, (double)size * r.B * r.K);
         return r.tensor == TENSOR_BF16 ? rows_of_type<__bf16, ROW_SCORES>(a, most_pieces(r), stream, pass)
                                        : rows_of_type<float, ROW_SCORES>(a, most_pieces(r), stream, pass);
@@ -837,7 +850,7 @@ hipError_t launch_scores_grad(const ChoiceRows &r, const float *g_logp, const fl
     a.g.g_entropy = g_entropy;
     a.g.dZ = d.dZ;
     a.g.lddz = (int)d.ld;
-    if (in_registers(r)) {
+    if (in_registers(r, true)) {
         const LaunchEvents pass = ev(PASS_GRAD, 2.0 * size * r.B * r.K);
         return r.tensor == TENSOR_BF16 ? rows_of_type<__bf16, ROW_GRAD>(a, most_pieces(r), stream, pass)
                                        : rows_of_type<float, ROW_GRAD>(a, most_pieces(r), stream, pass);

@@ -175,6 +175,23 @@ def test_gradient(B, K, dtype):
             assert torch.equal(Z, dZ)
 
 
+@pytest.mark.parametrize("dtype,B,K", [("f32", 1030, 5001), ("f32", 1024, 8000), ("bf16", 1025, 9001), ("f32", 257, 30001), ("bf16", 256, 50257), ("bf16", 300, 50257),
+                                       ("bf16", 259, 65536), ("f32", 64, 32771), ("bf16", 64, 40001), ("bf16", 64, 65543)])
+def test_both_sides_of_what_rows_decide(dtype, B, K):
+    rng = np.random.default_rng(B + K)
+    z, y = logits(B, K, rng, dtype)
+    gl, gh = rng.standard_normal(B).astype(np.float32), rng.standard_normal(B).astype(np.float32)
+    Z, _ = matrix(z, dtype, K + 1, 1)
+    Y = vec(y, torch.int32)
+    want = ref.scores_ref(z, y, 5)
+    compare(run(Z, Y, 5), want, y, K, (dtype, B, K))
+    dZ, flat = matrix(np.zeros((B, K)), dtype, K + 1, 1)
+    hb.scores_grad(Z, dZ, Y, vec(gl), vec(gh), ws=work(B, K))
+    g = ref.scores_grad_ref(want, y, gl, gh)
+    check(dZ, g, grad_tol(g, want, z, y, gl, gh, K, dtype), (dtype, B, K))
+    assert outside_is_nan(flat, dZ)
+
+
 def test_gradient_against_differences():
     rng = np.random.default_rng(2)
     B, K = 4, 9
