@@ -73,6 +73,8 @@ struct List : How {
     Mat mat[ORTHO_GROUP];
 };
 
+static_assert(sizeof(List) < 4000, "arguments of a launch");
+
 typedef __bf16 v4b __attribute__((ext_vector_type(4)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
