@@ -649,7 +649,7 @@ size_t hb_scores_workspace_bytes(int64_t B, int32_t K, int32_t top);
  *   coef    HOST pointer, read before the call returns: a, b, c of all steps (n_coef = 1) or of each (n_coef = steps), finite and within
  *           [-32, 32]; NULL (n_coef = 0): (3.4445, -4.7750, 2.0315), five steps of which bring singular values between 1e-2 and 1 to 0.7 .. 1.2
  *   eps     >= 0, finite; a matrix of zeros has a result of zeros if it is not 0 (NaN, 0 / 0, if it is)
- *   products  HB_TENSOR_F32: errors as of fp32 products (about 1e-6 of the result's norm for five of the usual steps), or HB_TENSOR_BF16: operands of 11 bits, the
+ *   products  HB_TENSOR_F32: errors as of fp32 products (about 1e-6 of the result's norm for five of the usual steps, more where G is nearly singular), or HB_TENSOR_BF16: operands of 11 bits, the
  *           linear term a X in 22: about 1e-3, a third of the work
  * What a rounding adds to a singular value near 0 is multiplied by up to a^steps, as the value itself.  Coefficients that let a singular value s grow
  * beyond 16, or b s^2 + c s^4 beyond 64, overflow (inf or NaN); so does a G with inf or NaN anywhere, whose whole result is NaN.  Entries of X below 2^-36 count as 0.
