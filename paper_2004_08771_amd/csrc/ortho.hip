@@ -44,8 +44,10 @@ constexpr int PREP = 64;  // tiles of the kernel that lays X out
 struct Matrix {
     int rows, cols;
     bool flip;                // X is its transpose
-    bool whole_g, whole_m;    // four elements at a time lie at boundaries of their size
-    bool whole_out;           // and of the result: four of four bytes, eight of two
+    // every row begins at a boundary of four elements (of a result in two bytes eight), so that these can be moved at once
+    bool whole_g : 1, whole_m : 1, whole_out : 1;
+    // ... of four elements, the first row does: what counts where rows follow one another without gaps
+    bool begins_g : 1, begins_m : 1, begins_out : 1;
     float scale;              // lr times the matrix's factor
     const void *g;
     void *out;                // the result, or the weights
@@ -78,7 +80,7 @@ static_assert(sizeof(List) < 4000, "arguments of a launch");
 typedef __bf16 v4b __attribute__((ext_vector_type(4)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
-// elements at .. at + 3 of a row of which `left` are there (0 for the others); whole: 4 elements lie at a boundary of their size
+// elements at .. at + 3 of a row of which `left` are there (0 for the others); whole: the four lie at a boundary of their size
 __device__ __forceinline__ v4f load_four(const void *p, long long at, int tensor, int left, bool whole)
 {
     v4f x = {0.f, 0.f, 0.f, 0.f};
@@ -143,6 +145,7 @@ __device__ __forceinline__ double sum_of_block(const How &l, const Matrix &a, in
 {
     const bool gaps = a.ldg != a.cols || (l.muon && a.ldm != a.cols);
     const int rows = gaps ? a.rows : 1, cols = gaps ? a.cols : a.rows * a.cols;
+    const bool whole_g = gaps ? a.whole_g : a.begins_g, whole_m = gaps ? a.whole_m : a.begins_m;
     int lanes = NT;
     while (lanes > 1 && 2 * lanes >= cols) lanes >>= 1;
     const int per_block = NT / lanes, step = 4 * lanes;
@@ -159,8 +162,8 @@ __device__ __forceinline__ double sum_of_block(const How &l, const Matrix &a, in
             for (int u = 0; u < 4; ++u) {
                 const long long at = c + (long long)u * stride;
                 left[u] = at < cols ? (int)min(4LL, cols - at) : 0;
-                x[u] = load_four(a.g, g + at, l.g_tensor, left[u], a.whole_g);
-                if (l.muon) y[u] = load_four(a.mom, m + at, TENSOR_F32, left[u], a.whole_m);
+                x[u] = load_four(a.g, g + at, l.g_tensor, left[u], whole_g);
+                if (l.muon) y[u] = load_four(a.mom, m + at, TENSOR_F32, left[u], whole_m);
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
@@ -170,7 +173,7 @@ __device__ __forceinline__ double sum_of_block(const How &l, const Matrix &a, in
                         y[u][e] = __builtin_fmaf(l.momentum, y[u][e], x[u][e]);
                         x[u][e] = updated(l, x[u][e], y[u][e]);
                     }
-                    store_four(a.mom + m + c + (long long)u * stride, y[u], left[u], a.whole_m);
+                    store_four(a.mom + m + c + (long long)u * stride, y[u], left[u], whole_m);
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s += (double)x[u][e] * (double)x[u][e];
@@ -741,7 +744,7 @@ struct SmallStep {
     int end;           // of a run
 };
 struct SmallMat : Matrix {
-    int m, n;            // (whole_g, whole_m, whole_out: the matrix begins at a 16-byte boundary, 8 for two bytes)
+    int m, n;
     int blocks, block0;  // of columns, and the first workgroup
     int sums, sum0;      // as in Mat
     size_t x;            // byte offset in the workspace: X^T, between launches
@@ -860,9 +863,9 @@ struct Small {
     // Rows without gaps between them, four elements at a time from a 16-byte boundary (8 for two bytes): f(first element, how many) for all of a thread's
     static constexpr int FLAT = NB * MP / (4 * SMALL_NT);
     static __device__ __forceinline__ int elements(const SmallMat &a, int j0, int columns) { return a.flip ? min(columns, a.rows - j0) * a.cols : a.rows * a.cols; }
-    static __device__ __forceinline__ bool flat(const SmallMat &a, long long ld, bool whole)
+    static __device__ __forceinline__ bool flat(const SmallMat &a, long long ld, bool begins)
     {
-        return ld == a.cols && whole && (a.flip || a.blocks == 1);  // (a block is then a run of rows that begins at a multiple of NB of them)
+        return ld == a.cols && begins && (a.flip || a.blocks == 1);  // (a block is then a run of rows that begins at a multiple of NB of them)
     }
     // the places in LDS of elements first .. first + 3
     struct Places {
@@ -899,7 +902,7 @@ struct Small {
         double sum = 0.0;
         const bool bf16 = l.g_tensor == TENSOR_BF16;
         const long long first_g = a.flip ? j0 * a.ldg : j0, first_m = a.flip ? j0 * a.ldm : j0;
-        if (flat(a, a.ldg, a.whole_g) && (!l.muon || flat(a, a.ldm, a.whole_m))) {
+        if (flat(a, a.ldg, a.begins_g) && (!l.muon || flat(a, a.ldm, a.begins_m))) {
             const int n = elements(a, j0, columns);
             v4f x[FLAT];
 #pragma unroll
@@ -1133,7 +1136,7 @@ struct Small {
     {
         const long long first = a.flip ? j0 * a.ldo : j0;
         const bool bf16 = l.out_tensor == TENSOR_BF16;
-        if (flat(a, a.ldo, a.whole_out)) {
+        if (flat(a, a.ldo, a.begins_out)) {
             const int n = elements(a, j0, columns);
             v4f w[FLAT];
             if (l.muon) {
@@ -1530,10 +1533,14 @@ void describe(Matrix &a, const OrthoMatrix &o, const OrthoShape &s, const OrthoS
     a.mom = o.momentum;
     a.ldm = o.ldm;
     a.scale = how.lr * o.scale;
-    a.whole_g = reinterpret_cast<uintptr_t>(o.g) % (4 * size) == 0 && (o.ldg % 4 == 0 || a.rows == 1);
-    a.whole_m = reinterpret_cast<uintptr_t>(o.momentum) % 16 == 0 && (o.ldm % 4 == 0 || a.rows == 1);
-    a.whole_out = reinterpret_cast<uintptr_t>(o.out) % 16 == 0 &&
-                  (o.ldo % (how.out_tensor == TENSOR_BF16 && !how.muon ? 8 : 4) == 0 || a.rows == 1);
+    auto begins = [](const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; };
+    const bool two = how.out_tensor == TENSOR_BF16 && !how.muon;
+    a.begins_g = begins(o.g, 4 * size);
+    a.begins_m = begins(o.momentum, 16);
+    a.begins_out = begins(o.out, two ? 8 : 16);
+    a.whole_g = a.begins_g && (o.ldg % 4 == 0 || a.rows == 1);
+    a.whole_m = a.begins_m && (o.ldm % 4 == 0 || a.rows == 1);
+    a.whole_out = begins(o.out, 16) && (o.ldo % (two ? 8 : 4) == 0 || a.rows == 1);
 }
 
 template <int T, int PL>
@@ -1766,14 +1773,7 @@ hipError_t launch_ortho(const OrthoMatrix *list, const OrthoShape *shapes, int n
         for (int k0 = 0; k0 < n; k0 += ORTHO_GROUP) {
             const int count = n - k0 < ORTHO_GROUP ? n - k0 : ORTHO_GROUP;
             const SmallLayout y = lay_out_small(small, shapes + k0, count, rows);
-            for (int k = 0; k < count; ++k) {
-                SmallMat &a = small.mat[k];
-                const OrthoMatrix &o = list[k0 + k];
-                describe(a, o, shapes[k0 + k], how);
-                a.whole_g = reinterpret_cast<uintptr_t>(o.g) % (how.g_tensor == TENSOR_BF16 ? 8 : 16) == 0;
-                a.whole_m = reinterpret_cast<uintptr_t>(o.momentum) % 16 == 0;
-                a.whole_out = reinterpret_cast<uintptr_t>(o.out) % (how.out_tensor == TENSOR_BF16 && !how.muon ? 8 : 16) == 0;
-            }
+            for (int k = 0; k < count; ++k) describe(small.mat[k], list[k0 + k], shapes[k0 + k], how);
             unsigned char *const w = static_cast<unsigned char *>(ws);
             const hipError_t e = rows == 16   ? small_launches<16, 1024>(small, y, w, stream, ev)
                                  : rows == 32 ? small_launches<32, 1024>(small, y, w, stream, ev)
