@@ -219,7 +219,8 @@ int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call
  * Orthogonalised updates: every later step of this handle (any loss; also those of the worker loops) updates the weights of layers
  * first_layer .. last_layer (1 .. L) as hb_muon_async below does, with the step's lr, the batch gradient as G and the factor scale
  * sqrt(max(d_l, d_(l-1))); the weights of other layers and all biases get W <- W - lr G as before, without decay.  how->lr is not
- * looked at; how->ortho.coef is copied.  how NULL: off.  Each call sets the momenta to zero.  Gradients, losses and
+ * looked at; how->ortho.coef is copied.  A step whose lr times such a factor or weight_decay is not finite is refused (HB_ERR_INVALID).
+ * how NULL: off.  Each call sets the momenta to zero.  Gradients, losses and
  * merges are what they were (a merge changes the replica only, the momenta stay).  The first call allocates 2 P floats and the
  * workspace (the handle's device has to be current); steps enqueue kernels only and may be captured.  Networks then run layer by layer
  * with the gradient in memory between the backward pass and the update.  HB_ERR_UNSUPPORTED for a sparse first layer.

@@ -448,8 +448,21 @@ int run_small_net(hb_model *m, const float *X, const int32_t *y, int64_t B, int 
     return HB_OK;
 }
 
-// Issues the kernels of one step.
 int refresh_shadows(hb_model *m);
+
+// What an update of layer l is multiplied by besides lr
+float muon_factor(const hb_model *m, int l) { return m->muon_scale * std::sqrt((float)std::max(m->dims[l], m->dims[l - 1])); }
+
+// What hb_muon_async refuses of a rate, before anything of the step is enqueued
+int check_muon_rate(const hb_model *m, float lr)
+{
+    if (!std::isfinite(lr * m->muon.weight_decay))
+        return fail(HB_ERR_INVALID, "lr = %g times weight_decay = %g is not finite", (double)lr, (double)m->muon.weight_decay);
+    for (int l = m->muon_first; l <= m->muon_last; ++l)
+        if (!std::isfinite(lr * muon_factor(m, l)))
+            return fail(HB_ERR_INVALID, "lr = %g times the factor %g of layer %d is not finite", (double)lr, (double)muon_factor(m, l), l);
+    return HB_OK;
+}
 
 // The update of a step from the gradient in d_muon_grad: orthogonalised for the layers that are to have it, plain SGD for the others and the biases
 int muon_update(hb_model *m, float lr)
@@ -486,7 +499,7 @@ int muon_update(hb_model *m, float lr)
             o.out = m->d_params + w;
             o.momentum = m->d_momenta + w;
             o.ldg = o.ldo = o.ldm = m->dims[l - 1];
-            o.scale = m->muon_scale * std::sqrt((float)std::max(m->dims[l], m->dims[l - 1]));
+            o.scale = muon_factor(m, l);
             shapes[(size_t)(l - m->muon_first)] = {m->dims[l], m->dims[l - 1]};
         }
         add(m->b_off[l], m->dims[l]);
@@ -503,11 +516,13 @@ int muon_update(hb_model *m, float lr)
     return refresh_shadows(m);
 }
 
+// Issues the kernels of one step.
 int run_step(hb_model *m, const Input &in, const int32_t *y, int64_t B, float lr, StepMode mode,
              float *d_grad_flat, float *d_loss_user, const Head *head = nullptr)
 {
     if (mode == MODE_STEP && m->muon_first > 0) {
-        const int rc = run_step(m, in, y, B, 0.f, MODE_GRAD, m->d_muon_grad, d_loss_user, head);
+        int rc = check_muon_rate(m, lr);
+        if (rc == HB_OK) rc = run_step(m, in, y, B, 0.f, MODE_GRAD, m->d_muon_grad, d_loss_user, head);
         return rc != HB_OK ? rc : muon_update(m, lr);
     }
     const int L = m->L;
@@ -850,7 +865,8 @@ int run_step_bf16(hb_model *m, const void *X, const int32_t *y, int64_t B, float
                   float *d_grad_flat, float *d_loss_user, const Head *head = nullptr)
 {
     if (mode == MODE_STEP && m->muon_first > 0) {
-        const int rc = run_step_bf16(m, X, y, B, 0.f, MODE_GRAD, m->d_muon_grad, d_loss_user, head);
+        int rc = check_muon_rate(m, lr);
+        if (rc == HB_OK) rc = run_step_bf16(m, X, y, B, 0.f, MODE_GRAD, m->d_muon_grad, d_loss_user, head);
         return rc != HB_OK ? rc : muon_update(m, lr);
     }
     const int L = m->L;
