@@ -57,3 +57,13 @@ def test_a_call_repeats_itself(rows, cols, products):
             ws.fill_(fill)
         hb.orthogonalize(G, out, products=KINDS[products], ws=ws)
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("low", [1e-2, 3e-3, 1e-4])
+@pytest.mark.parametrize("shape", r.SMALLER + [(64, 512), (100, 1000)])
+def test_singular_values_near_zero(shape, low):
+    """Three times the host's form: a step multiplies what a rounding leaves beside them, so a few roundings count more than the others."""
+    G = r.with_values(*shape, np.r_[1.0, np.full(min(shape) - 1, low)], np.random.default_rng(1))
+    for products, beside, form in [("f32", (), lambda: r.small(G, limit=12.0)), ("f32", [(130, 129)], lambda: r.tiled(G)),
+                                   ("bf16", (), lambda: r.small(G, limit=500.0)), ("bf16", [(130, 129)], lambda: r.tiled(G, planes=1))]:
+        assert r.off(result([G], products, beside)[0], G) < 3 * r.off(form(), G), (products, beside)
