@@ -33,3 +33,19 @@ def test_an_epoch_is_its_steps(dims, bf16):
     assert np.array_equal(params(a), params(b)) and np.array_equal(momenta(a), momenta(b)) and np.abs(momenta(a)).max() > 0
     assert of_epoch == float(each.double().sum())
     assert not np.array_equal(params(a), params(plain)) and not np.array_equal(params(a), flat)
+
+
+def test_momenta_stay_where_updates_are_switched_off():
+    dims, B = (30, 20, 5), 40
+    m, flat = model(dims)
+    rng = np.random.default_rng(1)
+    X, y = torch.as_tensor(rng.standard_normal((B, dims[0]))).float().cuda(), vec(rng.integers(0, 5, B), torch.int32)
+    m.set_muon(hb.muon_args())
+    m.batch_step_async(X, y, B, 0.01)
+    kept = momenta(m)
+    assert kept.any()
+    m.set_muon(None)
+    m.batch_step_async(X, y, B, 0.01)
+    assert np.array_equal(momenta(m), kept)
+    m.set_muon(hb.muon_args())
+    assert not momenta(m).any()
