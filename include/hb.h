@@ -220,10 +220,10 @@ int hb_model_set_dropout(hb_model *m, float p, uint64_t seed, uint64_t next_call
  * first_layer .. last_layer (1 .. L) as hb_muon_async below does, with the step's lr, the batch gradient as G and the factor scale
  * sqrt(max(d_l, d_(l-1))); the weights of other layers and all biases get W <- W - lr G as before, without decay.  how->lr is not
  * looked at; how->ortho.coef is copied.  A step whose lr times such a factor or weight_decay is not finite is refused (HB_ERR_INVALID).
- * how NULL: off.  Each call sets the momenta to zero.  Gradients, losses and
- * merges are what they were (a merge changes the replica only, the momenta stay).  The first call allocates 2 P floats and the
- * workspace (the handle's device has to be current); steps enqueue kernels only and may be captured.  Networks then run layer by layer
- * with the gradient in memory between the backward pass and the update.  HB_ERR_UNSUPPORTED for a sparse first layer.
+ * how NULL: off; the momenta stay.  Each other call sets them to zero.  Gradients, losses and merges are what they were (a merge changes
+ * the replica only, the momenta stay).  The first call allocates 2 P floats and the workspace (the handle's device has to be current); steps
+ * enqueue kernels only and may be captured.  The step's gradient is then made as hb_batch_grad makes it (in one launch by a network that fits a workgroup,
+ * otherwise layer by layer) and is in memory before the update.  HB_ERR_UNSUPPORTED for a sparse first layer.
  *   hb_model_get_momenta, hb_model_set_momenta   the momenta in the flat layout (HOST pointers, P floats; biases and other layers have none
  *                                                 and keep what is set), for checkpoints; synchronise the stream.  HB_ERR_STATE before hb_model_set_muon
  */
@@ -650,8 +650,10 @@ size_t hb_scores_workspace_bytes(int64_t B, int32_t K, int32_t top);
  *   coef    HOST pointer, read before the call returns: a, b, c of all steps (n_coef = 1) or of each (n_coef = steps), finite and within
  *           [-32, 32]; NULL (n_coef = 0): (3.4445, -4.7750, 2.0315), five steps of which bring singular values between 1e-2 and 1 to 0.7 .. 1.2
  *   eps     >= 0, finite; a matrix of zeros has a result of zeros if it is not 0 (NaN, 0 / 0, if it is)
- *   products  HB_TENSOR_F32: errors as of fp32 products (about 1e-6 of the result's norm for five of the usual steps, more where G is nearly singular), or HB_TENSOR_BF16: operands of 11 bits, the
- *           linear term a X in 22: about 1e-3, a third of the work
+ *   products  HB_TENSOR_F32: errors as of fp32 products (of the result's norm, for five of the usual steps: about 1e-6; where G is nearly singular, up to 1e-4), or
+ *           HB_TENSOR_BF16: operands of 11 bits, the linear term a X in 22, a third of the work: up to 1e-3 where singular values are spread over two decades;
+ *           where most of them are 1e-4 of the largest 2e-3 (134 x 176) to 4e-4 (520 x 513).  Matrices of up to 128 rows or columns have 1e-4 and 2e-3 in lists of
+ *           such matrices only (their steps are taken on X X^T), and beside a larger one 1e-3 and, nearly singular, 7e-3 (64 x 512) to 5e-2 (2 x 2)
  * What a rounding adds to a singular value near 0 is multiplied by up to a^steps, as the value itself.  Coefficients that let a singular value s grow
  * beyond 16, or b s^2 + c s^4 beyond 64, overflow (inf or NaN); so does a G with inf or NaN anywhere, whose whole result is NaN.  Entries of X below 2^-36 count as 0.
  * 1 <= rows, cols <= 32768, rows cols <= 2^30; ld < 2^31.

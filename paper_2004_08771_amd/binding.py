@@ -471,7 +471,7 @@ def _matrix(t, name):
         _invalid(f"{name} has {len(shape)} dimensions: a matrix is needed")
     rows, cols = shape
     step, along = t.stride()
-    if along != 1 and cols > 1 and rows > 0:
+    if along != 1 and cols > 1 and rows > 0:  # (no rows: nothing is read, any strides are taken)
         _invalid(f"{name}: the elements of a row must be next to each other")
     if rows < 2:
         step = cols if cols > 1 else 1
@@ -672,7 +672,7 @@ def _one_type(kinds, name):
 
 def orthogonalize(G, out, steps=5, coef=ORTHO_COEF, eps=1e-7, products=None, ws=None, stream=None):
     """hb_orthogonalize_async of a matrix or a list of them; out (may be G) has their shapes.  products: HB_TENSOR_F32 or HB_TENSOR_BF16, by
-    default the type of out."""
+    default the type of out (operands of 11 bits for a bfloat16 result, which has 8 itself)."""
     G = _list(G, "G")
     out = _list(out, "out", len(G))
     a, o = [_matrix(t, "G") for t in G], [_matrix(t, "out") for t in out]

@@ -13,9 +13,11 @@
 // roundings of X to 11 bits alone leave 1e-2 in the result of a gradient whose singular values are spread over two decades, to 8 bits
 // (bf16) 8e-2.  Two things take that away at no cost in products: the linear term a X is carried in 22 bits (two
 // fp16 numbers, x = high + low), and the diagonals of A and B, which hold most of their size, stay in fp32 outside of the products
-// (A = D + F:  A^2 = F^2 + D F + F D + D^2,  B X = E X + H X).  That leaves 1e-3 (HB_TENSOR_BF16, whose results are rounded to 2^-8 anyway).
-// HB_TENSOR_F32 takes the products of high and low parts, too (three products of the four; low times low is 2^-22): the errors are
-// those of fp32 products.
+// (A = D + F:  A^2 = F^2 + D F + F D + D^2,  B X = E X + H X).  That leaves (HB_TENSOR_BF16) 6e-4 to 9e-4 of the result's norm where
+// singular values are spread over two decades, and more the more of them are near 0: all but one at 1e-4 of the largest 4e-4 (520 x 513), 2.4e-3 (134 x 176), of small
+// matrices beside a larger one 7e-3 (64 x 512) to 5e-2 (2 x 2).  A result in bf16 is rounded (2^-8 at most, 1.7e-3 of its norm) besides; fp32 weights are not.
+// HB_TENSOR_F32 takes the products of high and low parts, too (three products of the four; low times low is 2^-22): the errors are those of fp32 products, about 1e-6,
+// and 4e-5 to 1e-4 with all but one singular value at 1e-4 of the largest, as plain fp32 has there.
 // Operands are scaled by powers of two so that neither what they hold nor its low part leaves fp16's range: X by 2^12 (entries are at most the largest
 // singular value s, 1.2 for the usual steps, and around (m n)^-1/2 at the start), A by 2^8 and B by 2^10 (entries beside the diagonal are at most half
 // the range of s^2, and of b s^2 + c s^4): s up to 16 and b s^2 + c s^4 up to 64 have room.
@@ -289,7 +291,7 @@ __device__ __forceinline__ void wait_loads_and_meet()
 // loaded once for the three products (instead of one segment of k behind the other: 983 x 512 fp32 18.0 -> 13.7, 11.9 -> 9.6, 11.4 -> 8.9 us for the
 // three products of a step, 1024 x 1024 30 -> 18); with one plane, 64 x 64 tiles have two k-tiles in a stage.  KG = 2, where there is no more
 // than a workgroup a compute unit: twice the wavefronts, each half with one of two k-tiles or k-steps of a stage, and four stages.
-// Bound by the loads into LDS where tiles are small (1000 x 4096: 1024 tiles of 64, 32.8 GFLOP in 21 us, 380 TFLOP/s a product of 8.2), by the
+// Bound by the loads into LDS where tiles are small (1000 x 4096: 1024 tiles of 64, the 8.2 GFLOP of a X + B X in 21.6 us, 380 TFLOP/s), by the
 // matrix cores and the units that have no tile where they are large.
 template <int T, int WM, int WN, int S, int PL, int KG>
 struct Product {
@@ -729,7 +731,8 @@ __global__ __launch_bounds__(64 * WM *WN *KG) void product_kernel(const List *lp
 //     X_k+1 = P_k X_k,   A_k+1 = P_k A_k P_k,   X_k+l = Q X_k,   Q = P_k+l-1 ... P_k
 // so a run of steps is products of m x m matrices, which commute and are symmetric.  A value of A near 0 keeps an absolute error while A_k+1 gives it the factor
 // p(0)^2, so the error of a long run is as of a square root of the precision: runs end where the product of the largest factors
-// passes 12 (HB_TENSOR_F32: two of the usual steps), or 500 (HB_TENSOR_BF16: five, 5e-4 at most); of HB_TENSOR_F32 with up to 16 rows every step is a run,
+// passes 12 (HB_TENSOR_F32: two of the usual steps), or 500 (HB_TENSOR_BF16: five; 2e-5 to 1e-4 of the result's norm where singular values are spread over two decades, 6e-4 to
+// 1.6e-3 at worst, where they are 3e-3 of the largest); of HB_TENSOR_F32 with up to 16 rows every step is a run,
 // since roundings do not average out over few of them (2 x 5 6.0e-6 in runs of two, 0.9e-6; 16 x 8192 takes 67 us for 53).
 // Everything but diagonals is held in 22 bits.  A wavefront has a strip of 16 columns of the m x m matrices in its registers.  A result of the matrix core holds four
 // rows of a column a lane, so two blocks of a strip are its operand of 32 values of k (in an order of their own, the same for both operands); rows go through LDS.
@@ -1411,7 +1414,7 @@ double product_time(int T, int planes, double tiles, double k_tiles)
 }
 
 // Large tiles read less for a product, small ones are more of them.  (4096 x 4096 bf16: sym 64 158, 128 120, 256 120 us, all 249, 165, 147;
-// 1000 x 4096: sym 23, 48, 105, all 22.6, 22.4, 43.)
+// 1000 x 4096: sym 19, 48, 105, all 22.6, 22.4, 43.)
 Tiles tiles_for(const OrthoShape *s, int n, int planes)
 {
     Tiles best = {64, 64};
@@ -1720,8 +1723,8 @@ hipError_t small_launches(const SmallArgs &l, const SmallLayout &y, unsigned cha
     if (y.one) return go(small_kernel<MP, NB>, l.count, SMALL_NT, M::LDS, stream, ev(PASS_NORM, 0.0), l);
     double *const partial = reinterpret_cast<double *>(ws + y.partial);
     e = go(small_sum_kernel, y.sums, SUM_NT, 0, stream, ev(PASS_NORM, 0.0), l, partial);
-    // every workgroup adds up the blocks' sums itself (64 KB in about 1 us), but for many, which a launch joins (4 us; 100 x 8192 fp32 204 us without it,
-    // 127 with; 128 x 4096 157, 124)
+    // every workgroup adds up the blocks' sums itself (64 KB in about 1 us), but for many, which a launch joins (6 us; 100 x 8192 fp32 227 us without it,
+    // 138 with; 128 x 4096 172, 131)
     int joined = 0;
     for (int k = 0; k < l.count; ++k) joined = joined || (long long)l.mat[k].blocks * MP * MP * 4 > (512 << 10);
     auto sums_are_there = [&](int turn) {
